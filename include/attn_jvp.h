@@ -256,6 +256,75 @@ int attn_jvp_qknorm_fwd(const void* x, const void* tx, const float* w, void* y, 
                         long long rows, int D, float eps, void* cuda_stream);
 
 /*
+ * The step between two branches of a DiT block, for tokens x of a residual stream: the branch's output h is
+ * (optionally) normalised and scaled, gated and added to the stream, and the result is normalised and modulated for
+ * the next branch, in one pass.  Per token of batch b, with C channels:
+ *     u  = post_weight . post_norm(h),   x' = x + gate_b . u
+ *     y  = weight . norm(x') (1 + scale_b) + shift_b
+ * norm and post_norm are ATTN_JVP_NORM_LAYER ((v - mean v) / sqrt(var v + eps)), _RMS (v / sqrt(mean v^2 + eps)) or
+ * _NONE.  post_norm = NONE: u = post_weight . h.  norm = NONE: no y (the last step of a network).  The paper's JVP
+ * mode needs the step with tangents (Appendix C.2 restructures every layer that way), its student step the gradients.
+ *
+ *   x              device, [B][L][C] contiguous, bf16 or fp32 (x_dtype: ATTN_JVP_BF16 / ATTN_JVP_FP32)
+ *   h              device, bf16 [B][L][C] contiguous, or NULL: x' = x (gate, post_norm, post_weight are then not used)
+ *   gate, scale, shift   device, fp32, one row of C contiguous values per batch, `*_stride` elements apart (0: the
+ *                  same row for every batch); NULL: gate 1, scale 0, shift 0.  For a modulation per frame instead of
+ *                  per sample, pass the frames as B.
+ *   weight, post_weight  device, fp32 [C], or NULL: 1.
+ *   tx, th         tangents of x (type of x) and h (bf16), read by attn_jvp_adaln_fwd when its tx_new or ty is given
+ *   tgate, tscale, tshift   tangents of the modulation, with their own strides; NULL: 0.  The weights are constants.
+ *   C              a multiple of 8, at most 8192.  eps >= 0.
+ * Tensors of tokens are 16-byte aligned, fp32 rows 4-byte aligned.  Statistics, sums and products are fp32; x', y and
+ * their tangents are rounded once, when they are stored, and y is formed from the unrounded x'.
+ */
+#define ATTN_JVP_BF16 0
+#define ATTN_JVP_FP32 1
+#define ATTN_JVP_NORM_NONE 0
+#define ATTN_JVP_NORM_LAYER 1
+#define ATTN_JVP_NORM_RMS 2
+typedef struct attn_jvp_adaln {
+    const void* x;
+    const void* h;
+    const float* gate;
+    const float* scale;
+    const float* shift;
+    const float* weight;
+    const float* post_weight;
+    const void* tx;
+    const void* th;
+    const float* tgate;
+    const float* tscale;
+    const float* tshift;
+    long long gate_stride, scale_stride, shift_stride, tgate_stride, tscale_stride, tshift_stride;
+    int B, L, C;
+    int x_dtype, norm, post_norm;
+    float eps;
+} attn_jvp_adaln_t;
+
+/*
+ * attn_jvp_adaln_fwd -- x' and y, and with tangents tx' and ty.
+ *   x_new   output, type and shape of x; NULL exactly when h is NULL.     y   output, bf16; NULL exactly when norm is NONE.
+ *   tx_new, ty   tangents of x_new and y: both NULL (no tangents), or each given exactly where its primal is.
+ * Outputs must not overlap inputs.  Asynchronous on `cuda_stream`; returns 0 or an ATTN_JVP_ERR_* code.
+ */
+int attn_jvp_adaln_fwd(const attn_jvp_adaln_t* in, void* x_new, void* y, void* tx_new, void* ty, void* cuda_stream);
+
+/*
+ * attn_jvp_adaln_bwd -- gradients of attn_jvp_adaln_fwd (tangent fields of `in` are ignored).
+ *   dx_new  gradient of x', type of x, or NULL: 0.      dy   gradient of y, bf16, or NULL: 0 (NULL when norm is NONE).
+ *   dx      output, type of x.       dh   output, bf16; NULL exactly when h is NULL.
+ *   dgate, dscale, dshift   outputs, fp32 [B][C] contiguous (one row per batch also where the input's rows were
+ *           shared), each optional;  dweight, dpost_weight   outputs, fp32 [C], optional.
+ *   workspace  device, 16-byte aligned, attn_jvp_adaln_bwd_workspace_bytes(...) bytes (column sums of the CTAs; they
+ *           are joined in a fixed order, so results do not change from run to run).  Calls that share one must be
+ *           ordered on the GPU.
+ */
+size_t attn_jvp_adaln_bwd_workspace_bytes(int B, int L, int C);
+int attn_jvp_adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const void* dy, void* dx, void* dh,
+                       float* dgate, float* dscale, float* dshift, float* dweight, float* dpost_weight,
+                       void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Self-test of the failure path (no counterpart in the paper): enqueues a one-warp kernel that waits on a
  * barrier nothing ever signals.  The wait expires after its time limit (about 2 s), the kernel ends normally,
  * and attn_jvp_device_status() then reports ATTN_JVP_ERR_DEVICE_TIMEOUT, exactly as it would for a stalled

@@ -1,5 +1,8 @@
 """B200 (sm_100a) attention-JVP library: Python binding of the C ABI in include/attn_jvp.h."""
 from . import synth  # noqa: F401
+from .adaln import (  # noqa: F401
+    AdaLNArgs, AdaLNGrads, adaln_backward, adaln_jvp, attn_jvp_adaln_bwd, attn_jvp_adaln_bwd_workspace_bytes,
+    attn_jvp_adaln_fwd)
 from .layers import AttentionCoreJVP, TensorWithT  # noqa: F401
 from .ulysses import UlyssesAttentionJVP  # noqa: F401
 from .attn_jvp import (  # noqa: F401

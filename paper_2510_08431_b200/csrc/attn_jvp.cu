@@ -9,6 +9,7 @@
 #include <atomic>
 #include <mutex>
 
+#include "adaln_jvp.cuh"
 #include "attn_jvp_kernel.cuh"
 #include "qknorm_jvp.cuh"
 
@@ -41,6 +42,7 @@ struct DeviceState {
     std::atomic<bool> unwatched_launch{false};    // a kernel ran here before the status word existed
     std::atomic<int> dyn_smem[2][3][2][2];        // dynamic shared memory per kernel instantiation, 0 = not set up
     std::atomic<int> dyn_smem_pair[3][2];         // ... of the CTA-pair kernels
+    std::atomic<bool> adaln_ready[2][3][2];       // launch attribute of adaln_kernel<x fp32><mode><wide> is set
     std::atomic<void*> static_scratch{nullptr};   // device address of the built-in scratch array
 };
 DeviceState g_dev[kMaxDevices];
@@ -620,6 +622,185 @@ int run_host(const void* q, const void* k, const void* v, const void* tq, const 
     return 0;
 }
 
+// ---------------------------------------------------------------------------------------------
+// Gate + residual + norm + modulation (adaln_jvp.cuh)
+// ---------------------------------------------------------------------------------------------
+using attn_jvp::AdalnParams;
+
+constexpr int kSms = 148;            // grids and workspaces are laid out for a B200's SMs, whatever is current
+
+// Rows per CTA and CTAs per batch: `waves` times as many CTAs as fit at once (kWarps warps per SM; a CTA has
+// C / 256 of them), but no fewer than `unit` rows each.
+struct AdalnGrid { int threads, rows_per_cta, chunks; };
+AdalnGrid adaln_grid(long long B, int L, int C, int warps_per_sm, int waves, int unit) {
+    AdalnGrid g;
+    g.threads = (C + 255) / 256 * 32;
+    int per_sm = warps_per_sm / (g.threads / 32);
+    per_sm = per_sm < 1 ? 1 : (per_sm > 32 ? 32 : per_sm);
+    const long long slots = (long long)kSms * per_sm * waves;
+    long long rows = (B * L + slots - 1) / slots;
+    rows = (rows + unit - 1) / unit * unit;
+    g.rows_per_cta = rows < L ? (int)rows : L;
+    g.chunks = (L + g.rows_per_cta - 1) / g.rows_per_cta;
+    return g;
+}
+constexpr int kAdalnBwdWarps = 20;
+AdalnGrid adaln_bwd_grid(int B, int L, int C) { return adaln_grid(B, L, C, kAdalnBwdWarps, 1, 1); }
+
+bool adaln_shape_ok(int B, int L, int C) {
+    if (B < 1 || L < 1 || C < 8 || C > attn_jvp::kAdalnMaxC || C % 8 != 0) return false;
+    return (long double)B * L * C * 4 < 9.0e18L && (long double)B * L < 2.0e9L;
+}
+
+template <typename TX, int MODE, int ROWS, int STAGES, int THREADS>
+int adaln_launch(const AdalnParams& p, const AdalnGrid& g, int B, int row_bytes_per_thread, cudaStream_t stream, DeviceState& st) {
+    auto kern = attn_jvp::adaln_kernel<TX, MODE, ROWS, STAGES, THREADS>;
+    const int smem = STAGES * ROWS * row_bytes_per_thread * g.threads;
+    // once per kernel and device: the most this instantiation can ask for (threads that race here set the same value)
+    std::atomic<bool>& ready = st.adaln_ready[sizeof(TX) == 4][MODE][THREADS > 640];
+    if (!ready.load(std::memory_order_acquire)) {
+        constexpr int most = STAGES * ROWS * attn_jvp::adaln_slot_bytes(sizeof(TX) == 4, true, MODE) * THREADS;
+        static_assert(most <= 220 * 1024, "ring does not fit into shared memory");
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+        if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute(MaxDynamicSharedMemorySize)", e);
+        ready.store(true, std::memory_order_release);
+    }
+    kern<<<(unsigned)((long long)B * g.chunks), g.threads, smem, stream>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail("adaln kernel launch", e);
+    return 0;
+}
+// CTAs of up to 640 threads (C <= 5120) have 102 registers per thread and three ring stages, wider ones 64 and two.
+template <int MODE, int ROWS>
+int adaln_dispatch(const AdalnParams& p, const AdalnGrid& g, int B, bool x_fp32, cudaStream_t stream, DeviceState& st) {
+    const int row = attn_jvp::adaln_slot_bytes(x_fp32, p.h != nullptr, MODE);
+    if (g.threads <= 640)
+        return x_fp32 ? adaln_launch<float, MODE, ROWS, 3, 640>(p, g, B, row, stream, st)
+                      : adaln_launch<__nv_bfloat16, MODE, ROWS, 3, 640>(p, g, B, row, stream, st);
+    return x_fp32 ? adaln_launch<float, MODE, ROWS, 2, 1024>(p, g, B, row, stream, st)
+                  : adaln_launch<__nv_bfloat16, MODE, ROWS, 2, 1024>(p, g, B, row, stream, st);
+}
+
+struct Span { const void* p; size_t bytes; int align; };     // align: bytes the address must be a multiple of
+
+// Alignment of every span, and no output over an input or another output.
+int check_spans(const Span* in, int n_in, const Span* out, int n_out) {
+    for (int i = 0; i < n_in; ++i) if (in[i].p && (uintptr_t)in[i].p % in[i].align) return ATTN_JVP_ERR_ALIGN;
+    for (int i = 0; i < n_out; ++i) if (out[i].p && (uintptr_t)out[i].p % out[i].align) return ATTN_JVP_ERR_ALIGN;
+    for (int a = 0; a < n_out; ++a) {
+        for (int i = 0; i < n_in; ++i) if (overlaps(out[a].p, out[a].bytes, in[i].p, in[i].bytes)) return ATTN_JVP_ERR_ALIAS;
+        for (int c = a + 1; c < n_out; ++c) if (overlaps(out[a].p, out[a].bytes, out[c].p, out[c].bytes)) return ATTN_JVP_ERR_ALIAS;
+    }
+    return 0;
+}
+
+// What the two directions share: shapes, kinds, strides; fills the kernel's parameters.
+int adaln_common(const attn_jvp_adaln_t* in, AdalnParams& p) {
+    if (!in) return ATTN_JVP_ERR_NULL;
+    if (!adaln_shape_ok(in->B, in->L, in->C)) return ATTN_JVP_ERR_SHAPE;
+    if (in->x_dtype != ATTN_JVP_BF16 && in->x_dtype != ATTN_JVP_FP32) return ATTN_JVP_ERR_FLAGS;
+    if (in->norm < 0 || in->norm > ATTN_JVP_NORM_RMS || in->post_norm < 0 || in->post_norm > ATTN_JVP_NORM_RMS) return ATTN_JVP_ERR_FLAGS;
+    if (!std::isfinite(in->eps) || in->eps < 0.0f) return ATTN_JVP_ERR_SCALE;
+    if (!in->x) return ATTN_JVP_ERR_NULL;
+    if (!in->h && in->norm == ATTN_JVP_NORM_NONE) return ATTN_JVP_ERR_NULL;       // nothing to compute
+    const long long strides[6] = {in->gate_stride, in->scale_stride, in->shift_stride, in->tgate_stride, in->tscale_stride, in->tshift_stride};
+    for (long long s : strides) if (s < 0 || s > (1LL << 40)) return ATTN_JVP_ERR_SHAPE;
+    p = AdalnParams{};
+    p.x = in->x;
+    p.h = static_cast<const __nv_bfloat16*>(in->h);
+    p.gate = in->h ? in->gate : nullptr;
+    p.wp = in->h ? in->post_weight : nullptr;
+    const bool norm = in->norm != ATTN_JVP_NORM_NONE;
+    p.scale = norm ? in->scale : nullptr;
+    p.shift = norm ? in->shift : nullptr;
+    p.w = norm ? in->weight : nullptr;
+    p.ld_gate = in->gate_stride;
+    p.ld_scale = in->scale_stride;
+    p.ld_shift = in->shift_stride;
+    p.L = in->L;
+    p.C = in->C;
+    p.norm = in->norm;
+    p.post = in->h ? in->post_norm : ATTN_JVP_NORM_NONE;
+    p.eps = in->eps;
+    return 0;
+}
+size_t mod_bytes(int B, int C, long long stride) { return ((size_t)(B - 1) * (size_t)stride + (size_t)C) * 4; }
+
+int adaln_fwd(const attn_jvp_adaln_t* in, void* x_new, void* y, void* tx_new, void* ty, cudaStream_t stream) {
+    AdalnParams p;
+    if (int rc = adaln_common(in, p)) return rc;
+    const bool norm = p.norm != ATTN_JVP_NORM_NONE, jvp = tx_new || ty;
+    if ((x_new != nullptr) != (p.h != nullptr) || (y != nullptr) != norm) return ATTN_JVP_ERR_NULL;
+    if (jvp && ((tx_new != nullptr) != (x_new != nullptr) || (ty != nullptr) != (y != nullptr))) return ATTN_JVP_ERR_NULL;
+    if (jvp && (!in->tx || (p.h && !in->th))) return ATTN_JVP_ERR_NULL;
+    if (jvp) {
+        p.tx = in->tx;
+        p.th = p.h ? static_cast<const __nv_bfloat16*>(in->th) : nullptr;
+        p.tgate = p.h ? in->tgate : nullptr;
+        p.tscale = norm ? in->tscale : nullptr;
+        p.tshift = norm ? in->tshift : nullptr;
+        p.ld_tgate = in->tgate_stride;
+        p.ld_tscale = in->tscale_stride;
+        p.ld_tshift = in->tshift_stride;
+    }
+    p.xn = x_new;
+    p.y = static_cast<__nv_bfloat16*>(y);
+    p.txn = tx_new;
+    p.ty = static_cast<__nv_bfloat16*>(ty);
+    const bool x_fp32 = in->x_dtype == ATTN_JVP_FP32;
+    const size_t cells = (size_t)in->B * in->L * in->C, xb = cells * (x_fp32 ? 4 : 2), hb = cells * 2, wb = (size_t)in->C * 4;
+    const Span ins[] = {{p.x, xb, 16}, {p.h, hb, 16}, {p.tx, xb, 16}, {p.th, hb, 16}, {p.w, wb, 4}, {p.wp, wb, 4},
+                        {p.gate, mod_bytes(in->B, in->C, p.ld_gate), 4}, {p.scale, mod_bytes(in->B, in->C, p.ld_scale), 4},
+                        {p.shift, mod_bytes(in->B, in->C, p.ld_shift), 4}, {p.tgate, mod_bytes(in->B, in->C, p.ld_tgate), 4},
+                        {p.tscale, mod_bytes(in->B, in->C, p.ld_tscale), 4}, {p.tshift, mod_bytes(in->B, in->C, p.ld_tshift), 4}};
+    const Span outs[] = {{x_new, xb, 16}, {y, hb, 16}, {tx_new, xb, 16}, {ty, hb, 16}};
+    if (int rc = check_spans(ins, 12, outs, 4)) return rc;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    const AdalnGrid g = jvp ? adaln_grid(in->B, in->L, in->C, 20, 4, 1) : adaln_grid(in->B, in->L, in->C, 20, 4, 2);
+    p.rows_per_cta = g.rows_per_cta;
+    p.chunks = g.chunks;
+    return jvp ? adaln_dispatch<1, 1>(p, g, in->B, x_fp32, stream, *stp) : adaln_dispatch<0, 2>(p, g, in->B, x_fp32, stream, *stp);
+}
+
+int adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const void* dy, void* dx, void* dh, float* dgate, float* dscale,
+              float* dshift, float* dweight, float* dpost_weight, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+    AdalnParams p;
+    if (int rc = adaln_common(in, p)) return rc;
+    if (!dx || (dh != nullptr) != (p.h != nullptr) || !workspace) return ATTN_JVP_ERR_NULL;
+    if (dy && p.norm == ATTN_JVP_NORM_NONE) return ATTN_JVP_ERR_NULL;
+    p.dxn = dx_new;
+    p.dy = static_cast<const __nv_bfloat16*>(dy);
+    p.dx = dx;
+    p.dh = static_cast<__nv_bfloat16*>(dh);
+    const bool x_fp32 = in->x_dtype == ATTN_JVP_FP32;
+    const size_t cells = (size_t)in->B * in->L * in->C, xb = cells * (x_fp32 ? 4 : 2), hb = cells * 2, wb = (size_t)in->C * 4;
+    const size_t mb = wb * in->B, need = attn_jvp_adaln_bwd_workspace_bytes(in->B, in->L, in->C);
+    const Span ins[] = {{p.x, xb, 16}, {p.h, hb, 16}, {dx_new, xb, 16}, {dy, hb, 16}, {p.w, wb, 4}, {p.wp, wb, 4},
+                        {p.gate, mod_bytes(in->B, in->C, p.ld_gate), 4}, {p.scale, mod_bytes(in->B, in->C, p.ld_scale), 4},
+                        {p.shift, mod_bytes(in->B, in->C, p.ld_shift), 4}};
+    const Span outs[] = {{dx, xb, 16}, {dh, hb, 16}, {dgate, mb, 4}, {dscale, mb, 4}, {dshift, mb, 4}, {dweight, wb, 4},
+                         {dpost_weight, wb, 4}, {workspace, need, 16}};
+    if (int rc = check_spans(ins, 9, outs, 8)) return rc;
+    if (workspace_bytes < need) return ATTN_JVP_ERR_WORKSPACE;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    const AdalnGrid g = adaln_bwd_grid(in->B, in->L, in->C);
+    p.rows_per_cta = g.rows_per_cta;
+    p.chunks = g.chunks;
+    p.part = static_cast<float*>(workspace);
+    if (int rc = adaln_dispatch<2, 1>(p, g, in->B, x_fp32, stream, *stp)) return rc;
+    if (!dgate && !dscale && !dshift && !dweight && !dpost_weight) return 0;
+    attn_jvp::AdalnJoin j = {p.part, p.gate, p.scale, p.w, p.wp, p.ld_gate, p.ld_scale, dgate, dscale, dshift, dweight, dpost_weight,
+                             in->B, in->C, g.chunks};
+    attn_jvp::adaln_join_kernel<<<(unsigned)((in->C + 31) / 32), 32 * attn_jvp::kAdalnJoinRows, 0, stream>>>(j);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail("adaln join kernel launch", e);
+    return 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -766,6 +947,22 @@ int attn_jvp_qknorm_fwd(const void* x, const void* tx, const float* w, void* y, 
     e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail("qknorm kernel launch", e);
     return 0;
+}
+
+int attn_jvp_adaln_fwd(const attn_jvp_adaln_t* in, void* x_new, void* y, void* tx_new, void* ty, void* cuda_stream) {
+    return adaln_fwd(in, x_new, y, tx_new, ty, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t attn_jvp_adaln_bwd_workspace_bytes(int B, int L, int C) {
+    if (!adaln_shape_ok(B, L, C)) return 0;
+    return (size_t)B * adaln_bwd_grid(B, L, C).chunks * 3 * C * sizeof(float);
+}
+
+int attn_jvp_adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const void* dy, void* dx, void* dh, float* dgate,
+                       float* dscale, float* dshift, float* dweight, float* dpost_weight, void* workspace,
+                       size_t workspace_bytes, void* cuda_stream) {
+    return adaln_bwd(in, dx_new, dy, dx, dh, dgate, dscale, dshift, dweight, dpost_weight, workspace, workspace_bytes,
+                     static_cast<cudaStream_t>(cuda_stream));
 }
 
 int attn_jvp_selftest_bounded_wait(void* cuda_stream) {
