@@ -325,6 +325,57 @@ int attn_jvp_adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const voi
                        void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Attention over selected key blocks.  At video lengths (32760 tokens) most of a head's keys matter little to a given
+ * patch; here every block of ATTN_JVP_SELECT_BLOCK = 128 queries attends only to the blocks of 128 keys kept for it
+ * (per batch and head; the last blocks are as long as the sequences leave them).  The selection is a constant of the
+ * tangents and gradients.  A selection is three device arrays, n_q = ceil(Lq / 128), n_k = ceil(Lk / 128):
+ *   mask   uint8 [B][H][n_q][n_k], 0 or not 0: is the key block kept for the query block
+ *   index  int32 [B][H][n_q][n_k]: the kept key blocks of a row in ascending order, at its start (the rest is undefined)
+ *   tiles  int32 [B][H][n_q]: how many 64-key tiles those have (two per block; one for a last block of at most 64 keys)
+ * index and tiles are always written by one of the two calls below.  A query block may keep nothing: its O and tO are
+ * then 0, its LSE is -inf, its mu 0, and its gradients are 0; so are those of a key block that nobody kept.
+ * Sequences of at most 786432 tokens; D is 64 or 128; tensors as in attn_jvp_fwd.
+ *
+ * attn_jvp_block_select -- keeps, for every query block, the min(topk, n_k) key blocks with the largest
+ * mean(q over the block) . mean(k over the block), formed in 64 bits, ties going to the lower key block.
+ *   workspace  device, 16-byte aligned, attn_jvp_block_select_workspace_bytes(...) bytes.
+ * attn_jvp_block_lists -- index and tiles of a mask that the caller made.
+ */
+#define ATTN_JVP_SELECT_BLOCK 128
+size_t attn_jvp_block_select_workspace_bytes(int B, int H, int Lq, int Lk, int D);
+int attn_jvp_block_select(const void* q, const void* k, int B, int H, int Lq, int Lk, int D, int topk,
+                          unsigned char* mask, int* index, int* tiles,
+                          void* workspace, size_t workspace_bytes, void* cuda_stream);
+int attn_jvp_block_lists(const unsigned char* mask, int B, int H, int Lq, int Lk, int* index, int* tiles, void* cuda_stream);
+
+/*
+ * attn_jvp_sparse_fwd -- Algorithm 2 over the kept key blocks: arguments, modes and results as attn_jvp_fwd_mu (mu may be
+ * NULL), with the selection's lists.
+ */
+int attn_jvp_sparse_fwd(const void* q, const void* k, const void* v,
+                        const void* tq, const void* tk, const void* tv,
+                        const int* index, const int* tiles,
+                        void* o, void* to, float* lse, float* mu,
+                        int B, int H, int Lq, int Lk, int D,
+                        float scale, unsigned flags, void* cuda_stream);
+
+/*
+ * attn_jvp_sparse_bwd -- gradients of O = softmax(s Q K^T) V over the kept key blocks:
+ *     dS = P (dO V^T - rowsum(dO . O)),  dQ = s dS K,  dK = s dS^T Q,  dV = P^T dO.
+ *   d_o, o     bf16 [B][Lq][H][D]: the gradient of O and the forward's O;  lse: the forward's LSE.
+ *   dq, dk, dv outputs, bf16, shapes of q, k, v; every element is written.
+ *   workspace  device, 256-byte aligned, attn_jvp_sparse_bwd_workspace_bytes(...) bytes (the transposed lists and two
+ *              words per query).  Calls that share one must be ordered on the GPU.
+ * P and dS are rounded to bf16 as MMA operands, sums are fp32; no atomics: results do not change from run to run.
+ */
+size_t attn_jvp_sparse_bwd_workspace_bytes(int B, int H, int Lq, int Lk, int D);
+int attn_jvp_sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse,
+                        const unsigned char* mask, const int* index, const int* tiles,
+                        void* dq, void* dk, void* dv,
+                        int B, int H, int Lq, int Lk, int D, float scale,
+                        void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Self-test of the failure path (no counterpart in the paper): enqueues a one-warp kernel that waits on a
  * barrier nothing ever signals.  The wait expires after its time limit (about 2 s), the kernel ends normally,
  * and attn_jvp_device_status() then reports ATTN_JVP_ERR_DEVICE_TIMEOUT, exactly as it would for a stalled

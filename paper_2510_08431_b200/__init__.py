@@ -4,6 +4,10 @@ from .adaln import (  # noqa: F401
     AdaLNArgs, AdaLNGrads, adaln_backward, adaln_jvp, attn_jvp_adaln_bwd, attn_jvp_adaln_bwd_workspace_bytes,
     attn_jvp_adaln_fwd)
 from .layers import AttentionCoreJVP, TensorWithT  # noqa: F401
+from .sparse import (  # noqa: F401
+    SELECT_BLOCK, BlockSelection, attn_jvp_block_lists, attn_jvp_block_select, attn_jvp_block_select_workspace_bytes,
+    attn_jvp_sparse_bwd, attn_jvp_sparse_bwd_workspace_bytes, attn_jvp_sparse_fwd, block_select, block_selection,
+    sparse_attention_backward, sparse_attention_jvp)
 from .ulysses import UlyssesAttentionJVP  # noqa: F401
 from .attn_jvp import (  # noqa: F401
     FWD_ONLY, KV_TANGENT_FREE, AttnJvpError, attention_jvp, attention_jvp_host, attn_jvp_device_status,

@@ -24,7 +24,8 @@ STATIC_SCRATCH_BYTES = 32 * 1024 * 1024
 EXPORTS = ("attn_jvp_fwd", "attn_jvp_fwd_stream", "attn_jvp_fwd_mu", "attn_jvp_splitkv_workspace_bytes",
            "attn_jvp_suggest_splits", "attn_jvp_fwd_splitkv", "attn_jvp_fwd_splitkv_static", "attn_jvp_host_workspace_bytes",
            "attn_jvp_fwd_host", "attn_jvp_qknorm_fwd", "attn_jvp_adaln_fwd", "attn_jvp_adaln_bwd_workspace_bytes",
-           "attn_jvp_adaln_bwd", "attn_jvp_set_tuning", "attn_jvp_debug_timeout_info", "attn_jvp_selftest_bounded_wait", "attn_jvp_set_stream", "attn_jvp_device_status", "attn_jvp_strerror",
+           "attn_jvp_adaln_bwd", "attn_jvp_block_select_workspace_bytes", "attn_jvp_block_select", "attn_jvp_block_lists",
+           "attn_jvp_sparse_fwd", "attn_jvp_sparse_bwd_workspace_bytes", "attn_jvp_sparse_bwd", "attn_jvp_set_tuning", "attn_jvp_debug_timeout_info", "attn_jvp_selftest_bounded_wait", "attn_jvp_set_stream", "attn_jvp_device_status", "attn_jvp_strerror",
            "attn_jvp_version")
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libattn_jvp.so")
@@ -80,6 +81,18 @@ def load():
             lib.attn_jvp_adaln_bwd_workspace_bytes.restype = ctypes.c_size_t
             lib.attn_jvp_adaln_bwd.argtypes = [vp] * 11 + [ctypes.c_size_t, vp]
             lib.attn_jvp_adaln_bwd.restype = ci
+            lib.attn_jvp_block_select_workspace_bytes.argtypes = [ci] * 5
+            lib.attn_jvp_block_select_workspace_bytes.restype = ctypes.c_size_t
+            lib.attn_jvp_block_select.argtypes = [vp] * 2 + [ci] * 6 + [vp] * 4 + [ctypes.c_size_t, vp]
+            lib.attn_jvp_block_select.restype = ci
+            lib.attn_jvp_block_lists.argtypes = [vp] + [ci] * 4 + [vp] * 3
+            lib.attn_jvp_block_lists.restype = ci
+            lib.attn_jvp_sparse_fwd.argtypes = [vp] * 12 + [ci] * 5 + [cf, cu, vp]
+            lib.attn_jvp_sparse_fwd.restype = ci
+            lib.attn_jvp_sparse_bwd_workspace_bytes.argtypes = [ci] * 5
+            lib.attn_jvp_sparse_bwd_workspace_bytes.restype = ctypes.c_size_t
+            lib.attn_jvp_sparse_bwd.argtypes = [vp] * 12 + [ci] * 5 + [cf, vp, ctypes.c_size_t, vp]
+            lib.attn_jvp_sparse_bwd.restype = ci
             lib.attn_jvp_selftest_bounded_wait.argtypes = [vp]
             lib.attn_jvp_selftest_bounded_wait.restype = ci
             lib.attn_jvp_set_tuning.argtypes = [ci, ci]

@@ -11,7 +11,9 @@
 
 #include "adaln_jvp.cuh"
 #include "attn_jvp_kernel.cuh"
+#include "block_select.cuh"
 #include "qknorm_jvp.cuh"
+#include "sparse_bwd.cuh"
 
 namespace {
 
@@ -42,6 +44,9 @@ struct DeviceState {
     std::atomic<bool> unwatched_launch{false};    // a kernel ran here before the status word existed
     std::atomic<int> dyn_smem[2][3][2][2];        // dynamic shared memory per kernel instantiation, 0 = not set up
     std::atomic<int> dyn_smem_pair[3][2];         // ... of the CTA-pair kernels
+    std::atomic<int> dyn_smem_sparse[2][3];       // ... of the kernels that walk lists of key blocks
+    std::atomic<bool> sparse_bwd_ready[2][2];     // launch attribute of sparse_bwd_kernel<D><pass> is set
+    std::atomic<bool> topk_ready[2];              // ... of block_topk_kernel<16>, <4>
     std::atomic<bool> adaln_ready[2][3][2];       // launch attribute of adaln_kernel<x fp32><mode><wide> is set
     std::atomic<void*> static_scratch{nullptr};   // device address of the built-in scratch array
 };
@@ -179,11 +184,12 @@ bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
     return a0 < b0 + nb && b0 < a0 + na;
 }
 
-template <int D, int MODE, bool SPLIT, int GROUPS, bool PAIR = false>
+template <int D, int MODE, bool SPLIT, int GROUPS, bool PAIR = false, bool SPARSE = false>
 int launch(const CUtensorMap* maps, const KernelArgs& ka, dim3 grid, cudaStream_t stream, DeviceState& st) {
-    auto kern = attn_jvp::attn_jvp_fwd_kernel<D, MODE, SPLIT, GROUPS, PAIR>;
+    auto kern = attn_jvp::attn_jvp_fwd_kernel<D, MODE, SPLIT, GROUPS, PAIR, SPARSE>;
     using Plan = attn_jvp::SmemPlan<D, MODE, GROUPS, PAIR, SPLIT>;
-    std::atomic<int>& slot = PAIR ? st.dyn_smem_pair[MODE][GROUPS - 1] : st.dyn_smem[D == 128][MODE][SPLIT][GROUPS - 1];
+    std::atomic<int>& slot = SPARSE ? st.dyn_smem_sparse[D == 128][MODE]
+                             : PAIR ? st.dyn_smem_pair[MODE][GROUPS - 1] : st.dyn_smem[D == 128][MODE][SPLIT][GROUPS - 1];
     int smem = slot.load(std::memory_order_acquire);
     if (smem == 0) {
         // dynamic shared memory = the operand layout (declared 1024-byte aligned in the kernel) plus the exchange
@@ -353,6 +359,8 @@ int run(const void* q, const void* k, const void* v, const void* tq, const void*
     ka.splits = eff_splits;
     ka.tiles_per_split = tiles_per_split;
     ka.part_o = ka.part_to = ka.part_lse = ka.part_mu = nullptr;
+    ka.list = ka.tiles = nullptr;
+    ka.list_stride = 0;
     if (split) {
         char* w = static_cast<char*>(workspace);
         ka.part_o = reinterpret_cast<float*>(w);
@@ -801,6 +809,273 @@ int adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const void* dy, vo
     return 0;
 }
 
+// ---------------------------------------------------------------------------------------------
+// Attention over selected key blocks (block_select.cuh, sparse_bwd.cuh and the list-walking form of the forward kernel)
+// ---------------------------------------------------------------------------------------------
+constexpr int kSelBlock = attn_jvp::kSelBlock;
+static_assert(kSelBlock == attn_jvp::kBlockM && kSelBlock == attn_jvp::kBwdBlock, "a query block is one work item");
+constexpr int kSelMaxBlocks = 6144;       // key or query blocks per sequence (786432 tokens): a CTA's rows of scores fit into shared memory
+
+int n_blocks(int L) { return (L + kSelBlock - 1) / kSelBlock; }
+
+// Shapes every entry point of this family takes.
+int sparse_shape(int B, int H, int Lq, int Lk, int D) {
+    if (B < 1 || H < 1 || Lq < 1 || Lk < 1) return ATTN_JVP_ERR_SHAPE;
+    if (D != 64 && D != 128) return ATTN_JVP_ERR_UNSUPPORTED_D;
+    if (n_blocks(Lq) > kSelMaxBlocks || n_blocks(Lk) > kSelMaxBlocks || B > 65535) return ATTN_JVP_ERR_SHAPE;
+    // work items, and rows of lists, are counted in ints
+    const long long most = n_blocks(Lq) > n_blocks(Lk) ? n_blocks(Lq) : n_blocks(Lk);
+    if ((long double)B * H * most > 1.0e9L) return ATTN_JVP_ERR_SHAPE;
+    return 0;
+}
+
+struct SelSizes { size_t mask, index, tiles; };
+SelSizes sel_sizes(int B, int H, int Lq, int Lk) {
+    const size_t rows = (size_t)B * H * n_blocks(Lq);
+    return {rows * n_blocks(Lk), rows * n_blocks(Lk) * 4, rows * 4};
+}
+
+size_t select_workspace(int B, int H, int Lq, int Lk, int D) {       // block means, fp64
+    return (size_t)B * H * D * 8 * ((size_t)n_blocks(Lq) + n_blocks(Lk));
+}
+
+template <int ROWS>
+int launch_topk(const double* qm, const double* kmt, unsigned char* mask, int* index, int* tiles, int BH, int n_q, int n_k, int D,
+                int Lk, int topk, cudaStream_t stream, DeviceState& st) {
+    auto kern = attn_jvp::block_topk_kernel<ROWS>;
+    std::atomic<bool>& ready = st.topk_ready[ROWS == 4];
+    if (!ready.load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+        if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute(MaxDynamicSharedMemorySize)", e);
+        ready.store(true, std::memory_order_release);
+    }
+    const size_t smem = (size_t)ROWS * (n_k + D) * 8;
+    kern<<<(unsigned)((long long)BH * ((n_q + ROWS - 1) / ROWS)), 256, smem, stream>>>(qm, kmt, mask, index, tiles, n_q, n_k, D, Lk, topk);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? 0 : cuda_fail("block top-k kernel launch", e);
+}
+
+int block_select(const void* q, const void* k, int B, int H, int Lq, int Lk, int D, int topk, unsigned char* mask, int* index,
+                 int* tiles, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+    if (int rc = sparse_shape(B, H, Lq, Lk, D)) return rc;
+    if (topk < 1) return ATTN_JVP_ERR_SHAPE;
+    if (!q || !k || !mask || !index || !tiles || !workspace) return ATTN_JVP_ERR_NULL;
+    const SelSizes n = sel_sizes(B, H, Lq, Lk);
+    const size_t need = select_workspace(B, H, Lq, Lk, D), row = (size_t)B * H * D * 2;
+    const Span ins[] = {{q, row * Lq, 16}, {k, row * Lk, 16}};
+    const Span outs[] = {{mask, n.mask, 1}, {index, n.index, 4}, {tiles, n.tiles, 4}, {workspace, need, 16}};
+    if (int rc = check_spans(ins, 2, outs, 4)) return rc;
+    if (workspace_bytes < need) return ATTN_JVP_ERR_WORKSPACE;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    const int n_q = n_blocks(Lq), n_k = n_blocks(Lk);
+    double* qm = static_cast<double*>(workspace);
+    double* kmt = qm + (size_t)B * H * D * n_q;
+    const unsigned cols = (unsigned)((H * D + 255) / 256);
+    attn_jvp::block_mean_kernel<false><<<dim3(cols, n_q, B), 256, 0, stream>>>(static_cast<const uint4*>(q), qm, Lq, H, D, n_q);
+    attn_jvp::block_mean_kernel<true><<<dim3(cols, n_k, B), 256, 0, stream>>>(static_cast<const uint4*>(k), kmt, Lk, H, D, n_k);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail("block mean kernel launch", e);
+    // sixteen rows of scores per CTA where they fit into its shared memory, else four
+    return n_k <= 1536 ? launch_topk<16>(qm, kmt, mask, index, tiles, B * H, n_q, n_k, D, Lk, topk, stream, *stp)
+                       : launch_topk<4>(qm, kmt, mask, index, tiles, B * H, n_q, n_k, D, Lk, topk, stream, *stp);
+}
+
+int block_lists(const unsigned char* mask, int B, int H, int Lq, int Lk, int* index, int* tiles, cudaStream_t stream) {
+    if (int rc = sparse_shape(B, H, Lq, Lk, 64)) return rc;
+    if (!mask || !index || !tiles) return ATTN_JVP_ERR_NULL;
+    const SelSizes n = sel_sizes(B, H, Lq, Lk);
+    const Span ins[] = {{mask, n.mask, 1}};
+    const Span outs[] = {{index, n.index, 4}, {tiles, n.tiles, 4}};
+    if (int rc = check_spans(ins, 1, outs, 2)) return rc;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    const long long rows = (long long)B * H * n_blocks(Lq);
+    attn_jvp::block_lists_kernel<<<(unsigned)((rows + 7) / 8), 256, 0, stream>>>(mask, index, tiles, rows, n_blocks(Lk), Lk);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? 0 : cuda_fail("block list kernel launch", e);
+}
+
+int sparse_fwd(const void* q, const void* k, const void* v, const void* tq, const void* tk, const void* tv, const int* index,
+               const int* tiles, void* o, void* to, float* lse, float* mu, int B, int H, int Lq, int Lk, int D, float scale,
+               unsigned flags, cudaStream_t stream) {
+    if (flags & ~(ATTN_JVP_KV_TANGENT_FREE | ATTN_JVP_FWD_ONLY)) return ATTN_JVP_ERR_FLAGS;
+    const bool fwd_only = (flags & ATTN_JVP_FWD_ONLY) != 0;
+    const int mode = fwd_only ? attn_jvp::kModeFwdOnly
+                              : (flags & ATTN_JVP_KV_TANGENT_FREE) ? attn_jvp::kModeKvTangentFree : attn_jvp::kModeJvp;
+    const bool jvp_kv = mode == attn_jvp::kModeJvp;
+    if (int rc = sparse_shape(B, H, Lq, Lk, D)) return rc;
+    if (!q || !k || !v || !index || !tiles || !o || !lse) return ATTN_JVP_ERR_NULL;
+    if (!fwd_only && (!tq || !to)) return ATTN_JVP_ERR_NULL;
+    if (jvp_kv && (!tk || !tv)) return ATTN_JVP_ERR_NULL;
+    if (!std::isfinite(scale)) return ATTN_JVP_ERR_SCALE;
+    const size_t row = (size_t)B * H * D * 2, nq = row * Lq, nk = row * Lk, nl = (size_t)B * H * Lq * 4;
+    const SelSizes n = sel_sizes(B, H, Lq, Lk);
+    const Span ins[] = {{q, nq, 16}, {k, nk, 16}, {v, nk, 16}, {fwd_only ? nullptr : tq, nq, 16}, {jvp_kv ? tk : nullptr, nk, 16},
+                        {jvp_kv ? tv : nullptr, nk, 16}, {index, n.index, 4}, {tiles, n.tiles, 4}};
+    const Span outs[] = {{o, nq, 16}, {fwd_only ? nullptr : to, nq, 16}, {lse, nl, 16}, {mu, nl, 16}};
+    if (int rc = check_spans(ins, 8, outs, 4)) return rc;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    DeviceState& st = *stp;
+    if (int rc = get_encode_fn()) return rc;
+    if (int rc = ensure_status_word(st)) return rc;
+
+    const int key_tile = attn_jvp::key_tile(D, mode, false, false);
+    CUtensorMap maps[9];
+    if (int rc = make_map(&maps[0], q, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
+    if (int rc = make_map(&maps[1], k, B, Lk, H, D, key_tile)) return rc;
+    if (int rc = make_map(&maps[2], v, B, Lk, H, D, key_tile)) return rc;
+    if (int rc = make_map(&maps[3], fwd_only ? q : tq, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
+    if (int rc = make_map(&maps[4], jvp_kv ? tk : k, B, Lk, H, D, key_tile)) return rc;
+    if (int rc = make_map(&maps[5], jvp_kv ? tv : v, B, Lk, H, D, key_tile)) return rc;
+    if (int rc = make_map(&maps[6], o, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
+    if (int rc = make_map(&maps[7], fwd_only ? o : to, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
+    maps[8] = maps[1];                                   // (only the CTA-pair kernel reads it)
+    KernelArgs ka = {};
+    ka.o = static_cast<__nv_bfloat16*>(o);
+    ka.to = static_cast<__nv_bfloat16*>(to);
+    ka.lse = lse;
+    ka.mu = mu;
+    ka.host_status = st.host_status_dev.load(std::memory_order_acquire);
+    ka.B = B;
+    ka.H = H;
+    ka.Lq = Lq;
+    ka.Lk = Lk;
+    ka.n_kv_tiles = (Lk + key_tile - 1) / key_tile;
+    ka.scale = scale;
+    ka.scale_log2 = (scale == 0.0f) ? 0x1p-100f : scale * 1.4426950408889634f;     // (see run())
+    ka.splits = 1;
+    ka.n_q_tiles = n_blocks(Lq);
+    ka.n_items = ka.n_q_tiles * H * B;
+    ka.list = index;
+    ka.tiles = tiles;
+    ka.list_stride = n_blocks(Lk);
+    const dim3 grid((unsigned)(ka.n_items < st.sm_count ? ka.n_items : st.sm_count), 1, 1);
+    // softmax groups as softmax_groups_for() chooses them for long items
+    if (D == 64) {
+        switch (mode) {
+            case attn_jvp::kModeJvp: return launch<64, attn_jvp::kModeJvp, false, 2, false, true>(maps, ka, grid, stream, st);
+            case attn_jvp::kModeKvTangentFree: return launch<64, attn_jvp::kModeKvTangentFree, false, 2, false, true>(maps, ka, grid, stream, st);
+            default: return launch<64, attn_jvp::kModeFwdOnly, false, 2, false, true>(maps, ka, grid, stream, st);
+        }
+    }
+    switch (mode) {
+        case attn_jvp::kModeJvp: return launch<128, attn_jvp::kModeJvp, false, 1, false, true>(maps, ka, grid, stream, st);
+        case attn_jvp::kModeKvTangentFree: return launch<128, attn_jvp::kModeKvTangentFree, false, 1, false, true>(maps, ka, grid, stream, st);
+        default: return launch<128, attn_jvp::kModeFwdOnly, false, 2, false, true>(maps, ka, grid, stream, st);
+    }
+}
+
+// Workspace of the backward pass: the transposed lists, then {LSE, delta} per padded query row.
+struct SparseBwdLayout { size_t index, tiles, rows, total; };
+SparseBwdLayout sparse_bwd_layout(int B, int H, int Lq, int Lk) {
+    auto pad = [](size_t n) { return (n + 255) & ~(size_t)255; };
+    const size_t bh = (size_t)B * H, n_q = n_blocks(Lq), n_k = n_blocks(Lk);
+    SparseBwdLayout l;
+    l.index = 0;
+    l.tiles = pad(bh * n_k * n_q * 4);
+    l.rows = l.tiles + pad(bh * n_k * 4);
+    l.total = l.rows + bh * n_q * kSelBlock * sizeof(float2);
+    return l;
+}
+
+template <int D, bool DKV>
+int launch_sparse_bwd(const CUtensorMap& x1, const CUtensorMap& x2, const CUtensorMap& y1, const CUtensorMap& y2,
+                      const attn_jvp::SparseBwdArgs& a, int n_items, cudaStream_t stream, DeviceState& st) {
+    auto kern = attn_jvp::sparse_bwd_kernel<D, DKV>;
+    constexpr int smem = attn_jvp::SparseBwdPlan<D>::kDynBytes;
+    std::atomic<bool>& ready = st.sparse_bwd_ready[D == 128][DKV];
+    if (!ready.load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute(MaxDynamicSharedMemorySize)", e);
+        ready.store(true, std::memory_order_release);
+    }
+    kern<<<(unsigned)n_items, attn_jvp::kBwdThreads, smem, stream>>>(x1, x2, y1, y2, a);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? 0 : cuda_fail("sparse backward kernel launch", e);
+}
+
+template <int D>
+int sparse_bwd_run(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo, const void* o,
+                   const void* d_o, const float* lse, float2* rows, attn_jvp::SparseBwdArgs dkv, attn_jvp::SparseBwdArgs dq, int B,
+                   int H, int Lq, int Lk, cudaStream_t stream, DeviceState& st) {
+    const int padded = n_blocks(Lq) * kSelBlock;
+    const long long threads = (long long)B * padded * H * (D / 8);
+    attn_jvp::sparse_bwd_rows_kernel<D><<<(unsigned)((threads + 255) / 256), 256, 0, stream>>>(
+        static_cast<const uint4*>(o), static_cast<const uint4*>(d_o), lse, rows, B, H, Lq, padded);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail("sparse backward row kernel launch", e);
+    if (int rc = launch_sparse_bwd<D, true>(mk, mv, mq, mdo, dkv, B * H * n_blocks(Lk), stream, st)) return rc;
+    return launch_sparse_bwd<D, false>(mq, mdo, mk, mv, dq, B * H * n_blocks(Lq), stream, st);
+}
+
+int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse,
+               const unsigned char* mask, const int* index, const int* tiles, void* dq, void* dk, void* dv, int B, int H, int Lq,
+               int Lk, int D, float scale, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+    if (int rc = sparse_shape(B, H, Lq, Lk, D)) return rc;
+    if (!d_o || !q || !k || !v || !o || !lse || !mask || !index || !tiles || !dq || !dk || !dv || !workspace) return ATTN_JVP_ERR_NULL;
+    if (!std::isfinite(scale)) return ATTN_JVP_ERR_SCALE;
+    const size_t row = (size_t)B * H * D * 2, nq = row * Lq, nk = row * Lk;
+    const SelSizes n = sel_sizes(B, H, Lq, Lk);
+    const SparseBwdLayout lay = sparse_bwd_layout(B, H, Lq, Lk);
+    const Span ins[] = {{d_o, nq, 16}, {q, nq, 16}, {k, nk, 16}, {v, nk, 16}, {o, nq, 16}, {lse, (size_t)B * H * Lq * 4, 4},
+                        {mask, n.mask, 1}, {index, n.index, 4}, {tiles, n.tiles, 4}};
+    const Span outs[] = {{dq, nq, 16}, {dk, nk, 16}, {dv, nk, 16}, {workspace, lay.total, 256}};
+    if (int rc = check_spans(ins, 9, outs, 4)) return rc;
+    if (workspace_bytes < lay.total) return ATTN_JVP_ERR_WORKSPACE;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    DeviceState& st = *stp;
+    if (int rc = get_encode_fn()) return rc;
+    if (int rc = ensure_status_word(st)) return rc;
+    CUtensorMap mq, mk, mv, mdo;
+    if (int rc = make_map(&mq, q, B, Lq, H, D, kSelBlock)) return rc;
+    if (int rc = make_map(&mk, k, B, Lk, H, D, kSelBlock)) return rc;
+    if (int rc = make_map(&mv, v, B, Lk, H, D, kSelBlock)) return rc;
+    if (int rc = make_map(&mdo, d_o, B, Lq, H, D, kSelBlock)) return rc;
+
+    char* w = static_cast<char*>(workspace);
+    int* t_index = reinterpret_cast<int*>(w + lay.index);
+    int* t_tiles = reinterpret_cast<int*>(w + lay.tiles);
+    float2* rows = reinterpret_cast<float2*>(w + lay.rows);
+    const int n_q = n_blocks(Lq), n_k = n_blocks(Lk);
+    attn_jvp::block_transpose_kernel<<<(unsigned)((long long)B * H * ((n_k + 31) / 32)), 256, (size_t)n_q * 4, stream>>>(
+        mask, t_index, t_tiles, n_q, n_k, Lq);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail("block transpose kernel launch", e);
+
+    attn_jvp::SparseBwdArgs a = {};
+    a.rows = rows;
+    a.host_status = st.host_status_dev.load(std::memory_order_acquire);
+    a.H = H;
+    a.n_q = n_q;
+    a.scale = scale;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    attn_jvp::SparseBwdArgs dkv = a, dqa = a;
+    dkv.list = t_index;
+    dkv.tiles = t_tiles;
+    dkv.list_stride = n_q;
+    dkv.n_items_per_head = n_k;
+    dkv.L_own = Lk;
+    dkv.L_other = Lq;
+    dkv.out1 = static_cast<__nv_bfloat16*>(dv);
+    dkv.out2 = static_cast<__nv_bfloat16*>(dk);
+    dqa.list = index;
+    dqa.tiles = tiles;
+    dqa.list_stride = n_k;
+    dqa.n_items_per_head = n_q;
+    dqa.L_own = Lq;
+    dqa.L_other = Lk;
+    dqa.out1 = static_cast<__nv_bfloat16*>(dq);
+    return D == 128 ? sparse_bwd_run<128>(mq, mk, mv, mdo, o, d_o, lse, rows, dkv, dqa, B, H, Lq, Lk, stream, st)
+                    : sparse_bwd_run<64>(mq, mk, mv, mdo, o, d_o, lse, rows, dkv, dqa, B, H, Lq, Lk, stream, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -963,6 +1238,36 @@ int attn_jvp_adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const voi
                        size_t workspace_bytes, void* cuda_stream) {
     return adaln_bwd(in, dx_new, dy, dx, dh, dgate, dscale, dshift, dweight, dpost_weight, workspace, workspace_bytes,
                      static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t attn_jvp_block_select_workspace_bytes(int B, int H, int Lq, int Lk, int D) {
+    return sparse_shape(B, H, Lq, Lk, D) ? 0 : select_workspace(B, H, Lq, Lk, D);
+}
+
+int attn_jvp_block_select(const void* q, const void* k, int B, int H, int Lq, int Lk, int D, int topk, unsigned char* mask,
+                          int* index, int* tiles, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return block_select(q, k, B, H, Lq, Lk, D, topk, mask, index, tiles, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int attn_jvp_block_lists(const unsigned char* mask, int B, int H, int Lq, int Lk, int* index, int* tiles, void* cuda_stream) {
+    return block_lists(mask, B, H, Lq, Lk, index, tiles, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int attn_jvp_sparse_fwd(const void* q, const void* k, const void* v, const void* tq, const void* tk, const void* tv,
+                        const int* index, const int* tiles, void* o, void* to, float* lse, float* mu, int B, int H, int Lq, int Lk,
+                        int D, float scale, unsigned flags, void* cuda_stream) {
+    return sparse_fwd(q, k, v, tq, tk, tv, index, tiles, o, to, lse, mu, B, H, Lq, Lk, D, scale, flags, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t attn_jvp_sparse_bwd_workspace_bytes(int B, int H, int Lq, int Lk, int D) {
+    return sparse_shape(B, H, Lq, Lk, D) ? 0 : sparse_bwd_layout(B, H, Lq, Lk).total;
+}
+
+int attn_jvp_sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse,
+                        const unsigned char* mask, const int* index, const int* tiles, void* dq, void* dk, void* dv, int B, int H,
+                        int Lq, int Lk, int D, float scale, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return sparse_bwd(d_o, q, k, v, o, lse, mask, index, tiles, dq, dk, dv, B, H, Lq, Lk, D, scale, workspace, workspace_bytes,
+                      static_cast<cudaStream_t>(cuda_stream));
 }
 
 int attn_jvp_selftest_bounded_wait(void* cuda_stream) {

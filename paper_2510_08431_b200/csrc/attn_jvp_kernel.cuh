@@ -122,6 +122,11 @@ struct KernelArgs {
     int B;
     int n_q_tiles;      // 128-row query tiles per (batch, head)
     int n_items;        // work items = n_q_tiles * H * B * splits; the grid's CTAs share them round-robin
+    // attention over selected key blocks (kSparse): per work item the ascending list of its 128-key blocks and its length
+    // in 64-key tiles (a last block of at most 64 keys is one tile)
+    const int* list;    // [B][H][n_q_tiles][list_stride]
+    const int* tiles;   // [B][H][n_q_tiles]
+    int list_stride;
 };
 
 // Shared-memory plan of a kernel variant.
@@ -543,7 +548,11 @@ __host__ __device__ constexpr int score_buffers(int D, int mode) {
 // tiles) are split between the two CTAs' shared memories, each CTA loading its part through its own TMA
 // requests (no multicast), and one instruction stream feeds two tensor pipes.  tm_k32 (32-row boxes of K) is
 // only used by that variant.
-template <int D, int MODE, bool kSplit, int kGroups, bool kPair>
+//
+// kSparse: an item's key tiles are those of the 128-key blocks on its list instead of all of them, in the list's order.
+// Every item then has its own number of tiles (an empty list counts as one tile without a valid key: its row maximum is
+// taken as 0, all of its P~ are 0, and the epilogue's 1 / l as 0), so items are not streamed into each other.
+template <int D, int MODE, bool kSplit, int kGroups, bool kPair, bool kSparse = false>
 __global__ void __launch_bounds__(num_threads(kGroups), 1)
 attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_tq,
@@ -551,6 +560,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ CUtensorMap tm_to,
                     const __grid_constant__ CUtensorMap tm_k32, const KernelArgs args) {
     static_assert(!kPair || (D == 128 && !kSplit), "the CTA-pair variant exists at D = 128, without key chunks");
+    static_assert(!kSparse || (!kPair && !kSplit), "key block lists: one CTA per query tile, no key chunks");
     using Plan = SmemPlan<D, MODE, kGroups, kPair, kSplit>;
     constexpr int kBN = Plan::kBN;                           // keys per tile
     constexpr bool kDoubleQ = Plan::kDoubleQ;
@@ -605,7 +615,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const bool lead_cta = cta_rank == 0u;
     const int first_item = kPair ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
     const int item_stride = kPair ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
-    struct Item { int q0, h, b, split, tile0, n_kv; };
+    struct Item { int q0, h, b, split, tile0, n_kv; const int* list; };
     // Work item number -> (query tile, head, batch [, chunk]).  The roles walk their items with a fixed stride, so
     // after the first item the three indices are advanced by the stride's own decomposition (carry by compare and
     // subtract) instead of being divided out again: the divisions would sit on the critical path of every item
@@ -635,14 +645,27 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         w.split = kSplit ? k.z % args.splits : 0;
         w.tile0 = kSplit ? w.split * args.tiles_per_split : 0;       // first key tile of this item
         w.n_kv = kSplit ? min(args.tiles_per_split, args.n_kv_tiles - w.tile0) : args.n_kv_tiles;
+        w.list = nullptr;
+        if (kSparse) {
+            const int row = (k.z * args.H + k.h) * args.n_q_tiles + k.qt;
+            const int tiles64 = min(__ldg(args.tiles + row), 2 * args.list_stride);
+            w.list = tiles64 > 0 ? args.list + static_cast<size_t>(row) * args.list_stride : nullptr;
+            w.n_kv = max(1, kBN == kBlockN ? tiles64 : (tiles64 + 1) / 2);
+        }
         return w;
+    };
+    // first key of tile j of an item (an empty list: behind the last key, where TMA fills in zeros)
+    auto key_of = [&](const Item& w, int j) -> int {
+        if (!kSparse) return (w.tile0 + j) * kBN;
+        if (w.list == nullptr) return args.list_stride * kBlockM;
+        return kBN == kBlockN ? __ldg(w.list + (j >> 1)) * kBlockM + (j & 1) * kBlockN : __ldg(w.list + j) * kBlockM;
     };
     const int n_items = args.n_items;
     // Two Q/tQ buffers, no key chunks (every item then has the same number of key tiles): the key tiles of all of a
     // CTA's items form one stream.  The score MMAs of an item's leading tiles are issued in the last bursts of the
     // item before (its Q, tQ are resident by then), and the ring carries their K tiles in that order, so that an
     // item boundary costs the MMA warp and the producer nothing.
-    const bool stream_items = kDoubleQ && !kSplit && args.n_kv_tiles >= kBufs;
+    const bool stream_items = kDoubleQ && !kSplit && !kSparse && args.n_kv_tiles >= kBufs;
     // Score buffer and barrier phase of a key tile, g % kBufs and (g / kBufs) & 1, carried along tile by tile (a
     // division by three per use would sit on the MMA warp's critical chain of dependent instructions).
     struct BufPos { int buf; uint32_t phase; };
@@ -832,12 +855,13 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     return true;
                 }
                 mbar_arrive_expect_tx(bar, kKTx);
+                const int row0 = key_of(w, j);
                 // per 64-column half: [K_half (8 KB)][tK_half (8 KB)] so that [K ; tK] is one N = 128 operand
 #pragma unroll
                 for (int hf = 0; hf < kHalves; ++hf) {
-                    tma_load_4d(dst + hf * kKHalfStride, &tm_k, bar, hf * 64, w.h, (w.tile0 + j) * kBN, w.b);
+                    tma_load_4d(dst + hf * kKHalfStride, &tm_k, bar, hf * 64, w.h, row0, w.b);
                     if (kHasTKV)
-                        tma_load_4d(dst + hf * kKHalfStride + Plan::kKvHalfBytes, &tm_tk, bar, hf * 64, w.h, (w.tile0 + j) * kBN, w.b);
+                        tma_load_4d(dst + hf * kKHalfStride + Plan::kKvHalfBytes, &tm_tk, bar, hf * 64, w.h, row0, w.b);
                 }
                 return true;
             };
@@ -862,12 +886,13 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     return true;
                 }
                 mbar_arrive_expect_tx(bar, kVTx);
+                const int row0 = key_of(w, j);
                 // [V_half0][V_half1][tV_half0][tV_half1]: consecutive 64-wide N atoms of [V | tV]
 #pragma unroll
                 for (int hf = 0; hf < kHalves; ++hf) {
-                    tma_load_4d(dst + hf * Plan::kKvHalfBytes, &tm_v, bar, hf * 64, w.h, (w.tile0 + j) * kBN, w.b);
+                    tma_load_4d(dst + hf * Plan::kKvHalfBytes, &tm_v, bar, hf * 64, w.h, row0, w.b);
                     if (kHasTKV)
-                        tma_load_4d(dst + (kHalves + hf) * Plan::kKvHalfBytes, &tm_tv, bar, hf * 64, w.h, (w.tile0 + j) * kBN, w.b);
+                        tma_load_4d(dst + (kHalves + hf) * Plan::kKvHalfBytes, &tm_tv, bar, hf * 64, w.h, row0, w.b);
                 }
                 return true;
             };
@@ -1359,6 +1384,8 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             float r_run = 0.0f;        // r (of the centred tS, see below; two groups: this group's share)
             float ts_shift = 0.0f;     // per-row constant subtracted from tS
             float m_other = -INFINITY; // two groups: the reference the other group's sums were last known to use
+            // (kSparse: only the last tile of an ascending list can reach past the last key)
+            const int last_valid = kSparse ? max(0, args.Lk - key_of(w, n_kv - 1)) : 0;
             // two groups: the group of the item's last tile finishes the item
             const bool finisher = (kGroups == 1) || (((g0 + n_kv - 1) & 1) == grp);
 
@@ -1395,7 +1422,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #endif
 
                 // keys past Lk (zero-filled by TMA) must not enter the softmax
-                const int valid = args.Lk - (w.tile0 + j) * kBN;
+                const int valid = !kSparse ? args.Lk - (w.tile0 + j) * kBN : (j + 1 < n_kv ? kBN : last_valid);
                 if (valid < kBN) {
                     const uint32_t masked = neg_scale ? 0x7F800000u : 0xFF800000u;   // -inf after scaling
 #pragma unroll
@@ -1416,6 +1443,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 float mx = neg_scale ? fminf(fminf(mx4[0], mx4[1]), fminf(mx4[2], mx4[3]))
                                      : fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
                 mx *= c1;
+                if (kSparse && valid <= 0) mx = 0.0f;       // (a finite reference for rows without any key)
 
                 if (kGroups == 2) {
                     // The decision of tile g - 1 (the other group's) comes first, also across items: the exchange
@@ -1446,7 +1474,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     float sm4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int c = 0; c < kBN; ++c) sm4[c & 3] += __uint_as_float(tv[c]);
-                    const int n_valid = valid < kBN ? valid : kBN;
+                    const int n_valid = valid < kBN ? (kSparse ? max(1, valid) : valid) : kBN;
                     return sc * ((sm4[0] + sm4[1]) + (sm4[2] + sm4[3])) / static_cast<float>(n_valid);
                 };
                 if (kHasTQ && kGroups == 1) tc_wait_ld();      // tS is in registers
@@ -1569,7 +1597,13 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (kRingStage > 0) {
                 const bool has_next = n_items - item > item_stride;
                 const int next_start = (ring_slot + 2 * (n_kv % kSlots) + (it > 0 ? kRingStage : 0)) % kSlots;
-                stage_slot_o = has_next ? (next_start + min(kBufs, n_kv)) % kSlots : next_start;
+                int lead = n_kv;                                  // key tiles of the next item
+                if (kSparse && has_next) {
+                    Walk wk_next = wk;
+                    walk_step(wk_next);
+                    lead = item_of(wk_next).n_kv;
+                }
+                stage_slot_o = has_next ? (next_start + min(kBufs, lead)) % kSlots : next_start;
                 ring_slot = next_start;
             }
 
@@ -1640,7 +1674,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const float l_tot = l_run, r_tot = r_run;
             const int qi = w.q0 + row;
             const bool in_range = qi < args.Lq;
-            const float inv_l = 1.0f / l_tot;
+            const float inv_l = (kSparse && l_tot == 0.0f) ? 0.0f : 1.0f / l_tot;
             const float mu = r_tot * inv_l;
             const int b = w.b, h = w.h, split = w.split;
             const size_t row_off = ((static_cast<size_t>(b) * args.Lq + (in_range ? qi : 0)) * args.H + h) * D;

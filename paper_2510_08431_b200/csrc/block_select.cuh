@@ -1,0 +1,204 @@
+// Which key blocks each query block attends to.  Queries and keys are cut into blocks of 128 tokens (the last one
+// ragged); a selection is a truth value per (batch, head, query block, key block), and beside it the lists that the
+// attention kernels walk: for every query block its key blocks in ascending order, and the transpose for the gradient
+// of the keys.
+//
+// The score of a pair is the dot product of the blocks' mean query and mean key, and the topk largest are kept, ties
+// going to the lower key block.  One wrong comparison exchanges 128 keys of 128 queries, so the order has to be that of
+// the scores themselves: means and dot products are formed in 64 bits, where the sum of 128 bf16 values is exact unless
+// their exponents lie more than 38 apart.  (In 32 bits neighbours around the topk-th place, about a hundredth of a
+// deviation apart, would change places a few times per call of a long video.)  The arithmetic is cheap all the same:
+// tokens / 128 means per head, 0.17 G multiply-adds for 12 heads of 32760 tokens, while reading q and k once bounds the
+// whole selection (201 MB there, 31 us).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace attn_jvp {
+
+constexpr int kSelBlock = 128;       // tokens of a block
+constexpr int kPoolRows = 8;         // row groups of a pooling CTA: 8 x 16 tokens
+constexpr int kPoolCols = 32;        // 16-byte pieces (8 channels) of a row it takes
+
+// Block means of q or k.  x: [B][L][H * D] bf16.  out: [B * H][n][D] fp64, or with kTransposed [B * H][D][n].
+// grid (ceil(H D / 256), n, B), 256 threads: thread (piece, row group) sums 16 tokens of 8 channels.
+template <bool kTransposed>
+__global__ void __launch_bounds__(kPoolRows* kPoolCols)
+block_mean_kernel(const uint4* __restrict__ x, double* __restrict__ out, int L, int H, int D, int n) {
+    __shared__ double part[kPoolRows][kPoolCols * 8];
+    const int piece = threadIdx.x % kPoolCols, group = threadIdx.x / kPoolCols;
+    const int pieces = H * D / 8, col = blockIdx.x * kPoolCols + piece;
+    const int block = blockIdx.y, b = blockIdx.z;
+    const int rows = min(kSelBlock, L - block * kSelBlock);
+    double s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = 0.0;
+    if (col < pieces) {
+        const uint4* row = x + (static_cast<long long>(b) * L + block * kSelBlock) * pieces + col;
+        constexpr int kEach = kSelBlock / kPoolRows;
+        uint4 v[kEach];
+#pragma unroll
+        for (int r = 0; r < kEach; ++r) {
+            const int at = r * kPoolRows + group;
+            v[r] = at < rows ? __ldg(row + static_cast<long long>(at) * pieces) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int r = 0; r < kEach; ++r) {
+            const uint32_t u[4] = {v[r].x, v[r].y, v[r].z, v[r].w};
+            // Two neighbouring tokens' values could be added in fp32 only if their exponents were close; a conversion to
+            // fp64 (a quarter-rate instruction) is avoided instead by placing the bf16 bits in the upper word of a
+            // double: sign, exponent and mantissa land in place with the exponent field taken as it is, which scales
+            // every finite value, subnormal ones included, by exactly 2^-896.
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t lo = u[i] << 16, hi = u[i] & 0xFFFF0000u;
+                s[2 * i] += __hiloint2double(static_cast<int>((lo & 0x80000000u) | ((lo & 0x7FFFFFFFu) >> 3)), 0);
+                s[2 * i + 1] += __hiloint2double(static_cast<int>((hi & 0x80000000u) | ((hi & 0x7FFFFFFFu) >> 3)), 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[group][i * kPoolCols + piece] = s[i];
+    __syncthreads();
+    const int c = threadIdx.x;                                   // one of the CTA's 256 channels
+    const int channel = blockIdx.x * kPoolCols * 8 + c;
+    if (channel < H * D) {
+        const int at = (c & 7) * kPoolCols + (c >> 3);
+        double sum = 0.0;
+#pragma unroll
+        for (int g = 0; g < kPoolRows; ++g) sum += part[g][at];
+        // (every term is a multiple of 2^-1029, far above the last place of a subnormal double: nothing is lost down there)
+        const double mean = sum * 0x1p896 / static_cast<double>(rows);
+        const int h = channel / D, d = channel - h * D;
+        const long long bh = static_cast<long long>(b) * H + h;
+        out[kTransposed ? (bh * D + d) * n + block : (bh * n + block) * D + d] = mean;
+    }
+}
+
+// 64-bit keys whose unsigned order is the order of the doubles.
+__device__ __forceinline__ unsigned long long ordered_key(double v) {
+    const long long b = __double_as_longlong(v + 0.0);           // (-0 becomes +0: equal scores have equal keys)
+    return b < 0 ? ~static_cast<unsigned long long>(b) : static_cast<unsigned long long>(b) | 0x8000000000000000ull;
+}
+
+// Writes one row of a selection: mask bytes (optional), the ascending list and its length in 64-token tiles (a last
+// block of at most 64 tokens is one tile, every other block two).  `keep(j)` for j = lane, lane + 32, ...; whole warp.
+template <typename Keep>
+__device__ __forceinline__ void write_row(const Keep& keep, int n, int tokens, unsigned char* mask, int* list, int* tiles) {
+    const int lane = threadIdx.x & 31;
+    int count = 0;
+    bool last_kept = false;
+    for (int j0 = 0; j0 < n; j0 += 32) {
+        const int j = j0 + lane;
+        const bool k = j < n && keep(j);
+        const unsigned votes = __ballot_sync(0xffffffffu, k);
+        if (mask != nullptr && j < n) mask[j] = k ? 1 : 0;
+        if (k) list[count + __popc(votes & ((1u << lane) - 1u))] = j;
+        count += __popc(votes);
+        if (j0 + 32 >= n) last_kept = (votes >> (n - 1 - j0)) & 1u;
+    }
+    if (lane == 0) *tiles = 2 * count - ((last_kept && tokens - (n - 1) * kSelBlock <= 64) ? 1 : 0);
+}
+
+// Scores and top-k.  A CTA takes kRows query blocks of one (batch, head): thread j forms the scores of key block j (and
+// j + 256, ...) with all of them (the means of k are stored channel by channel, so a warp reads 256 contiguous bytes per
+// channel and every value feeds kRows multiply-adds), then a warp per row finds the topk-th largest key bit by bit,
+// from the top, by counting (64 rounds at most; it stops when exactly topk keys are left), and among keys equal to it
+// keeps the first ones.
+template <int kRows>
+__global__ void __launch_bounds__(256)
+block_topk_kernel(const double* __restrict__ qm, const double* __restrict__ kmt, unsigned char* __restrict__ mask,
+                  int* __restrict__ index, int* __restrict__ tiles, int n_q, int n_k, int D, int Lk, int topk) {
+    extern __shared__ unsigned long long sel_keys[];             // [kRows][n_k], then the queries' means [D][kRows]
+    double* qs = reinterpret_cast<double*>(sel_keys + static_cast<size_t>(kRows) * n_k);
+    const int groups = (n_q + kRows - 1) / kRows;
+    const long long bh = blockIdx.x / groups;
+    const int i0 = static_cast<int>(blockIdx.x - bh * groups) * kRows;
+    for (int e = threadIdx.x; e < kRows * D; e += 256) {
+        const int r = e / D, d = e - r * D;
+        qs[d * kRows + r] = i0 + r < n_q ? qm[(bh * n_q + i0 + r) * D + d] : 0.0;
+    }
+    __syncthreads();
+    for (int j = threadIdx.x; j < n_k; j += 256) {
+        double acc[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) acc[r] = 0.0;
+        const double* kp = kmt + bh * D * n_k + j;
+#pragma unroll 4
+        for (int d = 0; d < D; ++d) {
+            const double kv = __ldg(kp + static_cast<long long>(d) * n_k);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) acc[r] = fma(qs[d * kRows + r], kv, acc[r]);
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) sel_keys[static_cast<size_t>(r) * n_k + j] = ordered_key(acc[r]);
+    }
+    __syncthreads();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int r = warp; r < kRows && i0 + r < n_q; r += 8) {
+        const unsigned long long* keys = sel_keys + static_cast<size_t>(r) * n_k;
+        const int want = min(topk, n_k);
+        // the largest `bound` with at least `want` keys >= bound
+        unsigned long long bound = 0;
+        int at_bound = n_k;                                      // keys >= bound
+        for (int bit = 63; bit >= 0 && at_bound != want; --bit) {
+            const unsigned long long trial = bound | (1ull << bit);
+            int c = 0;
+            for (int j = lane; j < n_k; j += 32) c += keys[j] >= trial ? 1 : 0;
+            c = __reduce_add_sync(0xffffffffu, c);
+            if (c >= want) { bound = trial; at_bound = c; }
+        }
+        // keys equal to the bound: only where more than `want` reach it, the last ones are dropped
+        int spare = at_bound - want;
+        int equal = 0;
+        if (spare > 0) {
+            for (int j = lane; j < n_k; j += 32) equal += keys[j] == bound ? 1 : 0;
+            equal = __reduce_add_sync(0xffffffffu, equal);
+        }
+        int keep_equal = equal - spare;                          // of the equal ones, how many are kept (spare > 0)
+        auto keep = [&](int j) {
+            const unsigned long long key = keys[j];
+            if (key != bound || spare == 0) return key >= bound;
+            int before = 0;                                      // (rare: exact ties around the last place)
+            for (int i = 0; i < j; ++i) before += keys[i] == bound ? 1 : 0;
+            return before < keep_equal;
+        };
+        const long long row = bh * n_q + i0 + r;
+        write_row(keep, n_k, Lk, mask + row * n_k, index + row * n_k, tiles + row);
+    }
+}
+
+// Lists of a given mask: a warp per row.
+__global__ void __launch_bounds__(256)
+block_lists_kernel(const unsigned char* __restrict__ mask, int* __restrict__ index, int* __restrict__ tiles, long long rows,
+                   int n_k, int Lk) {
+    const long long row = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const unsigned char* m = mask + row * n_k;
+    write_row([&](int j) { return m[j] != 0; }, n_k, Lk, nullptr, index + row * n_k, tiles + row);
+}
+
+// The transposed lists: for every key block the query blocks that kept it.  A CTA takes 32 key blocks of one (batch,
+// head): one word per query block holds their truth values, and a warp then walks the words for each of them.
+__global__ void __launch_bounds__(256)
+block_transpose_kernel(const unsigned char* __restrict__ mask, int* __restrict__ index, int* __restrict__ tiles, int n_q,
+                       int n_k, int Lq) {
+    extern __shared__ unsigned sel_words[];                      // [n_q]
+    const int groups = (n_k + 31) / 32;
+    const long long bh = blockIdx.x / groups;
+    const int j0 = static_cast<int>(blockIdx.x - bh * groups) * 32;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = warp; i < n_q; i += 8) {
+        const bool k = j0 + lane < n_k && mask[(bh * n_q + i) * n_k + j0 + lane] != 0;
+        const unsigned votes = __ballot_sync(0xffffffffu, k);
+        if (lane == 0) sel_words[i] = votes;
+    }
+    __syncthreads();
+    for (int c = warp; c < 32 && j0 + c < n_k; c += 8) {
+        const long long row = bh * n_k + j0 + c;
+        write_row([&](int i) { return (sel_words[i] >> c & 1u) != 0; }, n_q, Lq, nullptr, index + row * n_q, tiles + row);
+    }
+}
+
+}  // namespace attn_jvp
