@@ -9,14 +9,20 @@
 //     dx = dx' + r (dn - [mean dn] - n mean(n dn)),   dn = dy . w (1 + scale)
 // and per batch and channel dshift = sum_l dy, dscale = w sum_l dy n, dgate = wp sum_l dx hn.
 //
-// Bound by HBM: a few dozen operations per element against 8 to 24 bytes.  One CTA works on one row at a time (the
-// forward on two), thread t owns channels 8 t .. 8 t + 7 (16-byte accesses) and keeps that batch's modulation of its
-// channels in registers while the CTA walks down its rows, so HBM sees each row once and the modulation about never.
-// Rows come in through cp.async into a slot of shared memory that only the issuing thread reads back: the ring needs
-// no barrier, and it keeps several rows per CTA in flight whatever the registers allow.
-// All sums a row needs (of x', of x'^2, of t, of x' t) go through ONE block-wide reduction: each warp takes them
-// about its own mean and the warps' results are shifted to the row's mean when they are joined, so that a row whose
-// mean is large against its deviation loses nothing and no second pass over the block is needed.
+// Bound by HBM, if the instructions and the waits are kept few: a row of 5120 channels has 1700 cycles of an SM's share of
+// the bandwidth in the forward pass, 2600 in the backward pass, and a row's sums are a chain of shuffles and a barrier.
+// Hence two fp32 values per instruction (packed fp32x2 arithmetic), kRows rows at a time where one row's chain would not
+// be covered by other CTAs (their shuffles interleave and share the barrier), and only what a sum needs is held across it:
+// everything else is read from shared memory again.
+// One CTA works down a range of rows, thread t owns channels 8 t .. 8 t + 7 (16-byte accesses) and keeps that batch's
+// modulation of its channels in registers, so HBM sees each row once and the modulation about never.  Rows come in
+// through cp.async into a slot of shared memory that only the issuing warp reads back: the ring needs no block-wide
+// barrier, and it keeps several rows per CTA in flight whatever the registers allow.
+// All sums a row needs (of x', of x'^2, of t, of x' t) go through ONE block-wide reduction of 5 + 5 shuffle levels.  They
+// are taken about a pivot instead of zero, so that a row whose mean is large against its deviation loses nothing: a warp's
+// pivot is the mean p of 8 of its n <= 256 channels, and since 8 (p - mean)^2 is part of the n var that the sum of squares
+// holds, (p - mean)^2 <= 32 var: taking n (p - mean)^2 off again costs 5 bits at the very worst, on one outlier among the
+// 8, and usually none.  The warps' results are joined the same way about the first warp's mean.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -40,6 +46,7 @@ struct AdalnParams {
     float* part;                            // backward: [gridDim.x][3][C] column sums of each CTA
     int L, C, norm, post;
     int rows_per_cta, chunks;               // CTAs per batch
+    bool wide;                              // fp32 outputs are 32-byte aligned
     float eps;
 };
 
@@ -55,377 +62,477 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
 }
-__device__ __forceinline__ void bf16x8_to_f32(const uint4& r, float (&v)[8]) {
-    const uint32_t u[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(u[i] << 16);
-        v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
-    }
+// Pairs of fp32 values (f32x2) hold two neighbouring channels.
+using pair_t = uint64_t;
+__device__ __forceinline__ pair_t pair_of(float lo, float hi) {
+    pair_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
 }
-__device__ __forceinline__ uint4 f32_to_bf16x8(const float (&v)[8]) {
+__device__ __forceinline__ pair_t twice(float v) { return pair_of(v, v); }
+__device__ __forceinline__ void halves(pair_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ pair_t fma2(pair_t a, pair_t b, pair_t c) {
+    pair_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ pair_t mul2(pair_t a, pair_t b) {
+    pair_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ pair_t add2(pair_t a, pair_t b) {
+    pair_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float sum2(pair_t v) {
+    float a, b;
+    halves(v, a, b);
+    return a + b;
+}
+// 8 channels to and from memory
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const pair_t* v) {
     uint32_t u[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        u[i] = *reinterpret_cast<const uint32_t*>(&p);
+        float lo, hi;
+        halves(v[i], lo, hi);
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        u[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
-    return make_uint4(u[0], u[1], u[2], u[3]);
+    __stcs(reinterpret_cast<uint4*>(p), make_uint4(u[0], u[1], u[2], u[3]));      // (not read again by this kernel)
 }
-// outputs are not read again by this kernel: streaming stores
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
-    __stcs(reinterpret_cast<uint4*>(p), f32_to_bf16x8(v));
+__device__ __forceinline__ void store8(float* p, const pair_t* v) {
+    __stcs(reinterpret_cast<ulonglong2*>(p), make_ulonglong2(v[0], v[1]));
+    __stcs(reinterpret_cast<ulonglong2*>(p) + 1, make_ulonglong2(v[2], v[3]));
 }
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-    __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
-    __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+// `wide`: p is 32-byte aligned, and a thread's 32 bytes leave in one access (as two of 16, each would fill only half of
+// every 32-byte sector it touches)
+__device__ __forceinline__ void store8(float* p, const pair_t* v, bool wide) {
+    if (wide) asm volatile("st.global.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(p), "l"(v[0]), "l"(v[1]), "l"(v[2]), "l"(v[3]) : "memory");
+    else store8(p, v);
 }
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const pair_t* v, bool) { store8(p, v); }
+// A warp's 256 channels of an operand in the ring.  bf16: lane l's 16 bytes at 16 l.  fp32: 1024 bytes in their order in
+// memory; lane l copies pieces l and l + 32 (whole sectors per access) and reads back the 32 bytes at 32 l, which other
+// lanes of the warp have copied.
 template <typename T>
-__device__ __forceinline__ void load_slot(uint32_t a, float (&v)[8]);
-template <>
-__device__ __forceinline__ void load_slot<__nv_bfloat16>(uint32_t a, float (&v)[8]) { bf16x8_to_f32(lds128(a), v); }
-template <>
-__device__ __forceinline__ void load_slot<float>(uint32_t a, float (&v)[8]) {
-    // (the two halves of all threads' 32 bytes lie apart so that 16-byte accesses of a warp are contiguous)
-    const uint4 lo = lds128(a), hi = lds128(a + blockDim.x * 16);
-    const uint32_t u[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+__device__ __forceinline__ void load_slot(uint32_t a, int lane, pair_t* v) {
+    if (sizeof(T) == 2) {
+        const uint4 r = lds128(a + lane * 16);
+        const uint32_t u[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+        for (int i = 0; i < 4; ++i) v[i] = pair_of(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xFFFF0000u));
+    } else {
+        const uint4 lo = lds128(a + lane * 32), hi = lds128(a + lane * 32 + 16);
+        const uint32_t u[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pair_of(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+    }
 }
+// `src`: channel 0 of the warp in this row; `left`: channels from there to the row's end
 template <typename T>
-__device__ __forceinline__ void fetch_slot(uint32_t a, const T* src) {
-    cp_async16(a, src);
-    if (sizeof(T) == 4) cp_async16(a + blockDim.x * 16, src + 4);
+__device__ __forceinline__ void fetch_slot(uint32_t a, int lane, const T* src, int left) {
+    constexpr int kPer = 16 / sizeof(T);                         // channels of a 16-byte piece
+#pragma unroll
+    for (int k = 0; k < 8 / kPer; ++k) {
+        const int e = lane + 32 * k;
+        if (e * kPer < left) cp_async16(a + e * 16, src + e * kPer);
+    }
+}
+__device__ __forceinline__ void zero4(pair_t* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = 0ull;
 }
 // 8 values of a modulation row, `none` where there is none
-__device__ __forceinline__ void load_mod(const float* p, long long off, float none, float (&v)[8]) {
+__device__ __forceinline__ void load_mod(const float* p, long long off, float none, pair_t* v) {
+    float f[8];
     if (p == nullptr) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = none;
+        for (int i = 0; i < 8; ++i) f[i] = none;
     } else {
         p += off;
         if ((reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
             const float4 lo = __ldg(reinterpret_cast<const float4*>(p)), hi = __ldg(reinterpret_cast<const float4*>(p) + 1);
-            v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w;
-            v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+            f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w;
+            f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
         } else {        // (a row of any stride is 4-byte aligned at least)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __ldg(p + i);
+            for (int i = 0; i < 8; ++i) f[i] = __ldg(p + i);
         }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pair_of(f[2 * i], f[2 * i + 1]);
 }
 
 // What a row's normalisation needs, the same in every thread: n = (x - mean) r, and for a companion row t the two
 // constants of r (t - tbar - n q).
 struct RowNorm { float mean, r, tbar, q; };
 
-// One block-wide reduction for kRows rows at a time.  `red`: 2 x kRows x 32 float4 of shared memory used in turn
-// (`turn` flips per call: one barrier per call suffices, since a buffer is written again only after the next call's
-// barrier, which every thread reaches after its reads).
+// What a thread needs of the row's geometry, worked out once.
+struct RowShape {
+    float inv_c;          // 1 / C
+    float inv_mine;       // 1 / channels of this warp
+    float n_theirs;       // channels of the warp whose sums this lane joins (0: none)
+    int warps2;           // warps of the CTA, rounded up to a power of two: lane reads the sums of warp lane % warps2
+    bool active;          // this thread has channels (below C)
+};
+
+// One block-wide reduction for kRows rows.  `red`: 2 x kRows x 32 float4 of shared memory used in turn (`turn` flips per
+// call: one barrier per call suffices, since a buffer is written again only after the next call's barrier, which every
+// thread reaches after its reads).  Channels that a thread does not have (behind C) hold zeros.
 template <int kRows, bool kCompanion>
-__device__ __forceinline__ void row_norms(const float (&x)[kRows][8], const float (&t)[kRows][8], bool active, int C, int kind,
+__device__ __forceinline__ void row_norms(const pair_t (&x)[kRows][4], const pair_t (&t)[kRows][4], const RowShape& shape, int kind,
                                           float eps, float4* red, int& turn, RowNorm (&out)[kRows]) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_warps = blockDim.x >> 5;
-    const int n_mine = min(256, C - warp * 256);                 // channels of this warp
-    float s[kRows], T[kRows], m2[kRows], q[kRows];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float s[kRows], m2[kRows], T[kRows], q[kRows], mean[kRows];
 #pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-        s[k] = ((x[k][0] + x[k][1]) + (x[k][2] + x[k][3])) + ((x[k][4] + x[k][5]) + (x[k][6] + x[k][7]));
-        T[k] = kCompanion ? ((t[k][0] + t[k][1]) + (t[k][2] + t[k][3])) + ((t[k][4] + t[k][5]) + (t[k][6] + t[k][7])) : 0.0f;
+    for (int r = 0; r < kRows; ++r) {
+        // sums about a pivot near the warp's mean: the mean of the first 8 channels it has
+        mean[r] = __shfl_sync(0xffffffffu, sum2(add2(add2(x[r][0], x[r][1]), add2(x[r][2], x[r][3]))), 0) * 0.125f;
+        const pair_t minus = twice(shape.active ? -mean[r] : 0.0f);
+        pair_t d[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = add2(x[r][i], minus);
+        s[r] = sum2(add2(add2(d[0], d[1]), add2(d[2], d[3])));
+        m2[r] = sum2(add2(fma2(d[1], d[1], mul2(d[0], d[0])), fma2(d[3], d[3], mul2(d[2], d[2]))));
+        T[r] = kCompanion ? sum2(add2(add2(t[r][0], t[r][1]), add2(t[r][2], t[r][3]))) : 0.0f;
+        q[r] = kCompanion ? sum2(add2(fma2(d[1], t[r][1], mul2(d[0], t[r][0])), fma2(d[3], t[r][3], mul2(d[2], t[r][2])))) : 0.0f;
     }
 #pragma unroll
     for (int m = 16; m >= 1; m >>= 1)
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            s[k] += __shfl_xor_sync(0xffffffffu, s[k], m);
-            if (kCompanion) T[k] += __shfl_xor_sync(0xffffffffu, T[k], m);
+        for (int r = 0; r < kRows; ++r) {
+            s[r] += __shfl_xor_sync(0xffffffffu, s[r], m);
+            m2[r] += __shfl_xor_sync(0xffffffffu, m2[r], m);
+            if (kCompanion) T[r] += __shfl_xor_sync(0xffffffffu, T[r], m);
+            if (kCompanion) q[r] += __shfl_xor_sync(0xffffffffu, q[r], m);
         }
-    const float inv_mine = 1.0f / static_cast<float>(n_mine);
 #pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-        const float mean = s[k] * inv_mine;
-        m2[k] = q[k] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float d = active ? x[k][i] - mean : 0.0f;      // (threads past C hold zeros that are not channels)
-            m2[k] = fmaf(d, d, m2[k]);
-            if (kCompanion) q[k] = fmaf(d, t[k][i], q[k]);
-        }
+    for (int r = 0; r < kRows; ++r) {       // about the warp's mean
+        const float d = s[r] * shape.inv_mine;
+        mean[r] += d;
+        m2[r] = fmaf(-d, s[r], m2[r]);
+        if (kCompanion) q[r] = fmaf(-d, T[r], q[r]);
     }
-#pragma unroll
-    for (int m = 16; m >= 1; m >>= 1)
-#pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            m2[k] += __shfl_xor_sync(0xffffffffu, m2[k], m);
-            if (kCompanion) q[k] += __shfl_xor_sync(0xffffffffu, q[k], m);
-        }
-    const float inv_c = 1.0f / static_cast<float>(C);
-    if (n_warps > 1) {
+    if (shape.warps2 > 1) {
         float4* buf = red + turn * (kRows * 32);
         turn ^= 1;
         if (lane == 0) {
 #pragma unroll
-            for (int k = 0; k < kRows; ++k) buf[k * 32 + warp] = make_float4(s[k], m2[k], T[k], q[k]);
+            for (int r = 0; r < kRows; ++r) buf[r * 32 + warp] = make_float4(mean[r], m2[r], T[r], q[r]);
         }
         __syncthreads();
-        float4 v[kRows];
+        // the same again with the first warp's mean as the pivot
+        // (the entries of warps that do not exist are zero from the start and are never written)
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            v[k] = lane < n_warps ? buf[k * 32 + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
-            s[k] = v[k].x;
-            T[k] = v[k].z;
+        for (int r = 0; r < kRows; ++r) {
+            const float4 v = buf[r * 32 + (lane & (shape.warps2 - 1))];
+            mean[r] = buf[r * 32].x;
+            const float d = v.x - mean[r];
+            s[r] = shape.n_theirs * d;
+            m2[r] = fmaf(s[r], d, v.y);
+            T[r] = v.z;
+            if (kCompanion) q[r] = fmaf(d, v.z, v.w);
         }
 #pragma unroll
         for (int m = 16; m >= 1; m >>= 1)
+            if (m < shape.warps2) {
 #pragma unroll
-            for (int k = 0; k < kRows; ++k) {
-                s[k] += __shfl_xor_sync(0xffffffffu, s[k], m);
-                if (kCompanion) T[k] += __shfl_xor_sync(0xffffffffu, T[k], m);
+                for (int r = 0; r < kRows; ++r) {
+                    s[r] += __shfl_xor_sync(0xffffffffu, s[r], m);
+                    m2[r] += __shfl_xor_sync(0xffffffffu, m2[r], m);
+                    if (kCompanion) T[r] += __shfl_xor_sync(0xffffffffu, T[r], m);
+                    if (kCompanion) q[r] += __shfl_xor_sync(0xffffffffu, q[r], m);
+                }
             }
-        const float n_theirs = static_cast<float>(max(1, min(256, C - lane * 256)));
 #pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            const float d = lane < n_warps ? v[k].x / n_theirs - s[k] * inv_c : 0.0f;
-            m2[k] = fmaf(n_theirs * d, d, v[k].y);
-            if (kCompanion) q[k] = fmaf(d, v[k].z, v[k].w);
+        for (int r = 0; r < kRows; ++r) {
+            const float d = s[r] * shape.inv_c;
+            mean[r] += d;
+            m2[r] = fmaf(-d, s[r], m2[r]);
+            if (kCompanion) q[r] = fmaf(-d, T[r], q[r]);
         }
-#pragma unroll
-        for (int m = 16; m >= 1; m >>= 1)
-#pragma unroll
-            for (int k = 0; k < kRows; ++k) {
-                m2[k] += __shfl_xor_sync(0xffffffffu, m2[k], m);
-                if (kCompanion) q[k] += __shfl_xor_sync(0xffffffffu, q[k], m);
-            }
     }
+    const bool layer = kind == kAdalnLayer;
 #pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-        const float mean = s[k] * inv_c;
-        const bool layer = kind == kAdalnLayer;
+    for (int r = 0; r < kRows; ++r) {
+        m2[r] = fmaxf(m2[r], 0.0f);         // (a row of equal values may leave a rounding below zero)
         // rms: sum x^2 = M2 + C mean^2, sum x t = Q + mean sum t
-        const float var = layer ? m2[k] * inv_c : fmaf(mean, mean, m2[k] * inv_c);
-        out[k].mean = layer ? mean : 0.0f;
-        out[k].r = 1.0f / sqrtf(var + eps);
-        out[k].tbar = kCompanion && kind != kAdalnRms ? T[k] * inv_c : 0.0f;
-        out[k].q = kCompanion ? inv_c * (layer ? q[k] : fmaf(mean, T[k], q[k])) : 0.0f;      // mean(x t), for layer of the centred x
-        if (kind != kAdalnMeans) out[k].q *= out[k].r;
+        const float var = layer ? m2[r] * shape.inv_c : fmaf(mean[r], mean[r], m2[r] * shape.inv_c);
+        out[r].mean = layer ? mean[r] : 0.0f;
+        out[r].r = rsqrtf(var + eps);
+        out[r].tbar = kCompanion && kind != kAdalnRms ? T[r] * shape.inv_c : 0.0f;
+        out[r].q = kCompanion ? shape.inv_c * (layer ? q[r] : fmaf(mean[r], T[r], q[r])) : 0.0f;   // mean(x t), layer: of the centred x
+        if (kind != kAdalnMeans) out[r].q *= out[r].r;
     }
 }
 
-// Shared memory per thread and ring stage: one 16-byte slot per bf16 operand, two per fp32 operand.
+// Shared memory per thread and row of the ring: 16 bytes per bf16 operand, 32 per fp32 operand.
 __host__ __device__ constexpr int adaln_slot_bytes(bool x_fp32, bool has_h, int companions) {
-    // companions: rows that come beside x and h (forward 0; JVP: tx, th; backward: dx', dy)
+    // companions: rows that come beside x and h (forward 0; JVP 1: tx, th; backward 2: dx', dy)
     const int xs = x_fp32 ? 32 : 16;
     return (companions ? 2 : 1) * xs + (has_h ? 16 : 0) + (companions == 1 ? (has_h ? 16 : 0) : companions == 2 ? 16 : 0);
 }
 
-// kMode: 0 forward, 1 forward with tangents, 2 backward.  kThreads: the most threads a CTA is launched with.
-template <typename TX, int kMode, int kRows, int kStages, int kThreads>
-__global__ void __launch_bounds__(kThreads) adaln_kernel(const AdalnParams p) {
+// kMode: 0 forward, 1 forward with tangents, 2 backward.  kThreads: the most threads a CTA is launched with; kCtas: how
+// many of those an SM should hold.
+template <typename TX, int kMode, int kRows, int kStages, int kThreads, int kCtas>
+__global__ void __launch_bounds__(kThreads, kCtas) adaln_kernel(const AdalnParams p) {
     extern __shared__ __align__(16) uint8_t adaln_smem[];
-    __shared__ float4 red[2 * kRows * 32];
+    constexpr int kRed = 2 * kRows * 32;
+    __shared__ float4 red[kRed];
     constexpr bool kJvp = kMode == 1, kBwd = kMode == 2;
-    const int t = threadIdx.x, c = 8 * t;
-    const bool active = c < p.C;
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5, n_warps = blockDim.x >> 5;
+    const int c = 8 * t, left = p.C - 256 * warp;                // first channel of the thread; channels from the warp's first on
+    RowShape shape;
+    shape.active = c < p.C;
+    shape.warps2 = n_warps > 1 ? 1 << (32 - __clz(n_warps - 1)) : 1;
+    {
+        const int w = lane & (shape.warps2 - 1);
+        shape.inv_c = 1.0f / static_cast<float>(p.C);
+        shape.inv_mine = 1.0f / static_cast<float>(min(256, left));
+        shape.n_theirs = w < n_warps ? static_cast<float>(min(256, p.C - w * 256)) : 0.0f;
+        for (int i = t; i < kRed; i += blockDim.x) red[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    const bool active = shape.active;
     const int b = blockIdx.x / p.chunks;                         // a CTA's rows are of one batch
     const int row0 = (blockIdx.x - b * p.chunks) * p.rows_per_cta, row1 = min(p.L, row0 + p.rows_per_cta);
-    const long long base = (static_cast<long long>(b) * p.L) * p.C + c;       // channel c of the batch's first token
+    const long long first = (static_cast<long long>(b) * p.L + row0) * p.C;      // element 0 of the CTA's first row
     const bool has_h = p.h != nullptr, has_norm = p.norm != kAdalnNone, has_dxn = kBwd && p.dxn != nullptr, has_dy = kBwd && p.dy != nullptr;
 
-    float gate[8], mul[8], shift[8], wp[8];
-    float tgate[8], tmul[8], tshift[8];
+    // ring of kStages x kRows rows: per row the operands x [, h] [, companion of x] [, companion of h / dy], each with
+    // the warps' slots one after the other
+    const uint32_t plane = blockDim.x * 16;
+    constexpr uint32_t kXPlanes = sizeof(TX) / 2;
+    const uint32_t smem = static_cast<uint32_t>(__cvta_generic_to_shared(adaln_smem));
+    const uint32_t at_x = warp * 512 * kXPlanes, at_h = kXPlanes * plane + warp * 512;
+    const uint32_t end_h = kXPlanes * plane + (has_h ? plane : 0);
+    const uint32_t at_x2 = end_h + warp * 512 * kXPlanes, at_h2 = end_h + kXPlanes * plane + warp * 512;
+    const uint32_t row_bytes = kMode == 0 ? end_h : end_h + kXPlanes * plane + ((kBwd || has_h) ? plane : 0);
+    const uint32_t ring_end = smem + kStages * kRows * row_bytes;
+    // channels behind C: their slots are read like the others and have to hold zeros
+    if (left < 256) {
+        for (uint32_t a = smem; a < ring_end; a += row_bytes)
+            for (uint32_t o = lane * 16; o < 512 * kXPlanes; o += 512) {
+                auto zero = [](uint32_t d) { asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(d), "r"(0) : "memory"); };
+                zero(a + at_x + o);
+                if (kMode != 0) zero(a + at_x2 + o);
+                if (o < 512) {
+                    if (has_h) zero(a + at_h + o);
+                    if (kBwd || (kJvp && has_h)) zero(a + at_h2 + o);
+                }
+            }
+        __syncwarp();
+    }
+    long long ahead = first + 256 * warp;                        // the row that is fetched next, at this warp's first channel
+    int row_ahead = row0;
+    uint32_t slot_ahead = smem;
+    auto fetch = [&]() {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) gate[i] = mul[i] = shift[i] = wp[i] = tgate[i] = tmul[i] = tshift[i] = 0.0f;
+        for (int r = 0; r < kRows; ++r) {
+            if (row_ahead + r < row1) {
+                const long long e = ahead + static_cast<long long>(r) * p.C;
+                const uint32_t s = slot_ahead + r * row_bytes;
+                fetch_slot(s + at_x, lane, static_cast<const TX*>(p.x) + e, left);
+                if (has_h) fetch_slot(s + at_h, lane, p.h + e, left);
+                if (kJvp) {
+                    fetch_slot(s + at_x2, lane, static_cast<const TX*>(p.tx) + e, left);
+                    if (has_h) fetch_slot(s + at_h2, lane, p.th + e, left);
+                }
+                if (has_dxn) fetch_slot(s + at_x2, lane, static_cast<const TX*>(p.dxn) + e, left);
+                if (has_dy) fetch_slot(s + at_h2, lane, p.dy + e, left);
+            }
+        }
+        cp_async_commit();
+        ahead += static_cast<long long>(kRows) * p.C;
+        row_ahead += kRows;
+        slot_ahead += kRows * row_bytes;
+        if (slot_ahead == ring_end) slot_ahead = smem;
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) fetch();
+
+    pair_t gate[4], mul[4], shift[4], tgate[4], tmul[4], tshift[4];
+    zero4(gate); zero4(mul); zero4(shift); zero4(tgate); zero4(tmul); zero4(tshift);
     if (active) {
-        // u = wp hn enters only as gate u: both factors in one
+        // u = wp hn enters only as gate u: both factors in one; likewise w (1 + scale)
+        pair_t w[4], wp[4];
         load_mod(p.wp, c, 1.0f, wp);
         load_mod(p.gate, b * p.ld_gate + c, 1.0f, gate);
         load_mod(p.scale, b * p.ld_scale + c, 0.0f, mul);
-        load_mod(p.shift, b * p.ld_shift + c, 0.0f, shift);
-        float w[8];
+        if (!kBwd) load_mod(p.shift, b * p.ld_shift + c, 0.0f, shift);
         load_mod(p.w, c, 1.0f, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            gate[i] *= wp[i];
-            mul[i] = w[i] * (1.0f + mul[i]);
-        }
         if (kJvp) {
             load_mod(p.tgate, b * p.ld_tgate + c, 0.0f, tgate);
             load_mod(p.tscale, b * p.ld_tscale + c, 0.0f, tmul);
             load_mod(p.tshift, b * p.ld_tshift + c, 0.0f, tshift);
+        }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                tgate[i] *= wp[i];
-                tmul[i] *= w[i];
+        for (int i = 0; i < 4; ++i) {
+            gate[i] = mul2(gate[i], wp[i]);
+            mul[i] = fma2(mul[i], w[i], w[i]);
+            if (kJvp) {
+                tgate[i] = mul2(tgate[i], wp[i]);
+                tmul[i] = mul2(tmul[i], w[i]);
             }
         }
     }
 
-    // ring: stage s holds kRows rows; per row the slots x [, h] [, companion of x] [, companion of h / dy]
-    const uint32_t smem = static_cast<uint32_t>(__cvta_generic_to_shared(adaln_smem)) + t * 16;
-    const uint32_t plane = blockDim.x * 16;
-    constexpr uint32_t kXPlanes = sizeof(TX) / 2;
-    const uint32_t off_h = kXPlanes * plane, off_x2 = off_h + (has_h ? plane : 0);
-    const uint32_t off_h2 = off_x2 + kXPlanes * plane;
-    const uint32_t row_bytes = kMode == 0 ? off_x2 : off_h2 + ((kBwd || has_h) ? plane : 0);
-    auto fetch = [&](int i, int stage) {          // kRows rows from row i on
-#pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-            if (active && i + k < row1) {
-                const long long at = base + static_cast<long long>(i + k) * p.C;
-                const uint32_t s = smem + (stage * kRows + k) * row_bytes;
-                fetch_slot(s, static_cast<const TX*>(p.x) + at);
-                if (has_h) fetch_slot(s + off_h, p.h + at);
-                if (kJvp) {
-                    fetch_slot(s + off_x2, static_cast<const TX*>(p.tx) + at);
-                    if (has_h) fetch_slot(s + off_h2, p.th + at);
-                }
-                if (has_dxn) fetch_slot(s + off_x2, static_cast<const TX*>(p.dxn) + at);
-                if (has_dy) fetch_slot(s + off_h2, p.dy + at);
-            }
-        }
-        cp_async_commit();
-    };
-#pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) fetch(row0 + s * kRows, s);
-
-    float sum_dy[8], sum_dyn[8], sum_dhn[8];
-    if (kBwd) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum_dy[i] = sum_dyn[i] = sum_dhn[i] = 0.0f;
-    }
-    int turn = 0, stage = 0;
-    for (int row = row0; row < row1; row += kRows) {
-        {
-            int ahead = stage + kStages - 1;
-            if (ahead >= kStages) ahead -= kStages;
-            fetch(row + (kStages - 1) * kRows, ahead);       // (the slot read back an iteration ago, by this thread)
-        }
+    pair_t sum_dy[4], sum_dyn[4], sum_dhn[4];
+    zero4(sum_dy); zero4(sum_dyn); zero4(sum_dhn);
+    int turn = 0;
+    uint32_t slot = smem;
+    long long at = first + c;
+    __syncthreads();                                             // (the zeros in `red`)
+    for (int row = row0; row < row1; row += kRows, at += static_cast<long long>(kRows) * p.C) {
+        __syncwarp();                                            // (the slot that is filled now was read by the whole warp)
+        fetch();
         cp_async_wait<kStages - 1>();
-        float x[kRows][8], h[kRows][8], x2[kRows][8], h2[kRows][8];     // x2, h2: tangents, or dx' and dy
-#pragma unroll
-        for (int k = 0; k < kRows; ++k) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[k][i] = h[k][i] = x2[k][i] = h2[k][i] = 0.0f;
-            if (active && row + k < row1) {
-                const uint32_t s = smem + (stage * kRows + k) * row_bytes;
-                load_slot<TX>(s, x[k]);
-                if (has_h) load_slot<__nv_bfloat16>(s + off_h, h[k]);
-                if (kJvp || has_dxn) load_slot<TX>(s + off_x2, x2[k]);
-                if ((kJvp && has_h) || has_dy) load_slot<__nv_bfloat16>(s + off_h2, h2[k]);
-            }
-        }
-        if (++stage == kStages) stage = 0;
-
-        RowNorm hs[kRows], xs[kRows];
-        if (has_h) {
+        __syncwarp();                                            // (the lanes read what other lanes have copied)
+        // the branch's output, normalised if there is a post norm (hn)
+        pair_t x[kRows][4], x2[kRows][4];                        // x', and tx' / the gradient of x'
+        pair_t h[kRows][4], h2[kRows][4];                        // h, and th / dy
+        RowNorm hs[kRows] = {}, xs[kRows] = {};
+        // hn of row r again, from the ring
+        auto reload_hn = [&](int r) {
+            load_slot<__nv_bfloat16>(slot + r * row_bytes + at_h, lane, h[r]);
             if (p.post != kAdalnNone) {
-                row_norms<kRows, kJvp>(h, h2, active, p.C, p.post, p.eps, red, turn, hs);
+                const pair_t minus_mean = twice(active ? -hs[r].mean : 0.0f), rr = twice(hs[r].r);
 #pragma unroll
-                for (int k = 0; k < kRows; ++k)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        h[k][i] = active ? (h[k][i] - hs[k].mean) * hs[k].r : 0.0f;
-                        if (kJvp) h2[k][i] = active ? hs[k].r * (h2[k][i] - hs[k].tbar - h[k][i] * hs[k].q) : 0.0f;
-                    }
+                for (int i = 0; i < 4; ++i) h[r][i] = mul2(add2(h[r][i], minus_mean), rr);
             }
+        };
+        if (has_h && p.post != kAdalnNone) {
 #pragma unroll
-            for (int k = 0; k < kRows; ++k)
+            for (int r = 0; r < kRows; ++r) {
+                load_slot<__nv_bfloat16>(slot + r * row_bytes + at_h, lane, h[r]);
+                if (kJvp) load_slot<__nv_bfloat16>(slot + r * row_bytes + at_h2, lane, h2[r]);
+            }
+            row_norms<kRows, kJvp>(h, h2, shape, p.post, p.eps, red, turn, hs);
+        }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x[k][i] = fmaf(gate[i], h[k][i], x[k][i]);
-                    if (kJvp) x2[k][i] = fmaf(gate[i], h2[k][i], fmaf(tgate[i], h[k][i], x2[k][i]));
-                }
-            if (!kBwd) {
+        for (int r = 0; r < kRows; ++r) {
+            const uint32_t s = slot + r * row_bytes;
+            load_slot<TX>(s + at_x, lane, x[r]);
+            if (kJvp) load_slot<TX>(s + at_x2, lane, x2[r]);
+            if (has_h) {
+                reload_hn(r);
+                if (kJvp) {
+                    load_slot<__nv_bfloat16>(s + at_h2, lane, h2[r]);
+                    if (p.post != kAdalnNone) {
+                        // (channels behind C stay zero: sums run over them)
+                        const pair_t rr = twice(hs[r].r), minus_q = twice(-hs[r].q), minus_tbar = twice(active ? -hs[r].tbar : 0.0f);
 #pragma unroll
-                for (int k = 0; k < kRows; ++k) {
-                    if (active && row + k < row1) {
-                        const long long at = base + static_cast<long long>(row + k) * p.C;
-                        store8(static_cast<TX*>(p.xn) + at, x[k]);
-                        if (kJvp) store8(static_cast<TX*>(p.txn) + at, x2[k]);
+                        for (int i = 0; i < 4; ++i) h2[r][i] = mul2(rr, fma2(h[r][i], minus_q, add2(h2[r][i], minus_tbar)));
                     }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[r][i] = fma2(gate[i], h[r][i], x[r][i]);
+                    if (kJvp) x2[r][i] = fma2(gate[i], h2[r][i], fma2(tgate[i], h[r][i], x2[r][i]));
+                }
+                if (!kBwd && active && row + r < row1) {
+                    store8(static_cast<TX*>(p.xn) + at + r * p.C, x[r], p.wide);
+                    if (kJvp) store8(static_cast<TX*>(p.txn) + at + r * p.C, x2[r], p.wide);
                 }
             }
         }
         if (!kBwd) {
             if (has_norm) {
-                row_norms<kRows, kJvp>(x, x2, active, p.C, p.norm, p.eps, red, turn, xs);
+                row_norms<kRows, kJvp>(x, x2, shape, p.norm, p.eps, red, turn, xs);
 #pragma unroll
-                for (int k = 0; k < kRows; ++k) {
-                    float y[8], ty[8];
+                for (int r = 0; r < kRows; ++r) {
+                    const pair_t rr = twice(xs[r].r), minus_q = twice(-xs[r].q);
+                    const pair_t minus_mean = twice(-xs[r].mean), minus_tbar = twice(-xs[r].tbar);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float n = (x[k][i] - xs[k].mean) * xs[k].r;
-                        y[i] = fmaf(n, mul[i], shift[i]);
-                        if (kJvp) ty[i] = fmaf(xs[k].r * (x2[k][i] - xs[k].tbar - n * xs[k].q), mul[i], fmaf(n, tmul[i], tshift[i]));
+                    for (int i = 0; i < 4; ++i) {
+                        const pair_t n = mul2(add2(x[r][i], minus_mean), rr);
+                        x[r][i] = fma2(n, mul[i], shift[i]);
+                        if (kJvp) {
+                            const pair_t tn = mul2(rr, fma2(n, minus_q, add2(x2[r][i], minus_tbar)));
+                            x2[r][i] = fma2(tn, mul[i], fma2(n, tmul[i], tshift[i]));
+                        }
                     }
-                    if (active && row + k < row1) {
-                        const long long at = base + static_cast<long long>(row + k) * p.C;
-                        store8(p.y + at, y);
-                        if (kJvp) store8(p.ty + at, ty);
+                    if (active && row + r < row1) {
+                        store8(p.y + at + r * p.C, x[r]);
+                        if (kJvp) store8(p.ty + at + r * p.C, x2[r]);
                     }
                 }
             }
         } else {
-            float dn[kRows][8];
             if (has_norm) {
+                pair_t dn[kRows][4];
 #pragma unroll
-                for (int k = 0; k < kRows; ++k)
+                for (int r = 0; r < kRows; ++r) {
+                    if (has_dy) load_slot<__nv_bfloat16>(slot + r * row_bytes + at_h2, lane, dn[r]); else zero4(dn[r]);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) dn[k][i] = h2[k][i] * mul[i];
-                row_norms<kRows, true>(x, dn, active, p.C, p.norm, p.eps, red, turn, xs);
-#pragma unroll
-                for (int k = 0; k < kRows; ++k)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float n = active ? (x[k][i] - xs[k].mean) * xs[k].r : 0.0f;
-                        sum_dy[i] += h2[k][i];
-                        sum_dyn[i] = fmaf(h2[k][i], n, sum_dyn[i]);
-                        x2[k][i] += active ? xs[k].r * (dn[k][i] - xs[k].tbar - n * xs[k].q) : 0.0f;
-                    }
-            }
-#pragma unroll
-            for (int k = 0; k < kRows; ++k) {       // x2 is the whole gradient of x' now, which is that of x
-                if (active && row + k < row1)
-                    store8(static_cast<TX*>(p.dx) + base + static_cast<long long>(row + k) * p.C, x2[k]);
-            }
-            if (has_h) {
-#pragma unroll
-                for (int k = 0; k < kRows; ++k)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        sum_dhn[i] = fmaf(x2[k][i], h[k][i], sum_dhn[i]);
-                        x2[k][i] *= gate[i];
-                    }
-                if (p.post != kAdalnNone) {
-                    RowNorm es[kRows];       // h holds hn here: tbar = mean e, q = mean(e hn)
-                    row_norms<kRows, true>(h, x2, active, p.C, kAdalnMeans, 0.0f, red, turn, es);
-#pragma unroll
-                    for (int k = 0; k < kRows; ++k)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            x2[k][i] = hs[k].r * (x2[k][i] - (p.post == kAdalnLayer ? es[k].tbar : 0.0f) - h[k][i] * es[k].q);
+                    for (int i = 0; i < 4; ++i) dn[r][i] = mul2(dn[r][i], mul[i]);
                 }
+                row_norms<kRows, true>(x, dn, shape, p.norm, p.eps, red, turn, xs);
+            }
 #pragma unroll
-                for (int k = 0; k < kRows; ++k)
-                    if (active && row + k < row1) store8(p.dh + base + static_cast<long long>(row + k) * p.C, x2[k]);
+            for (int r = 0; r < kRows; ++r) {
+                if (row + r < row1) {                            // (uniform)
+                    const uint32_t s = slot + r * row_bytes;
+                    if (has_dxn) load_slot<TX>(s + at_x2, lane, x2[r]); else zero4(x2[r]);
+                    if (has_norm) {
+                        if (has_dy) load_slot<__nv_bfloat16>(s + at_h2, lane, h2[r]); else zero4(h2[r]);
+                        const pair_t rr = twice(xs[r].r), minus_q = twice(-xs[r].q);
+                        const pair_t minus_mean = twice(active ? -xs[r].mean : 0.0f), minus_tbar = twice(active ? -xs[r].tbar : 0.0f);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const pair_t n = mul2(add2(x[r][i], minus_mean), rr);
+                            sum_dy[i] = add2(sum_dy[i], h2[r][i]);
+                            sum_dyn[i] = fma2(h2[r][i], n, sum_dyn[i]);
+                            x2[r][i] = fma2(rr, fma2(n, minus_q, fma2(h2[r][i], mul[i], minus_tbar)), x2[r][i]);
+                        }
+                    }
+                    // x2 is the whole gradient of x' now, which is that of x
+                    if (active) store8(static_cast<TX*>(p.dx) + at + r * p.C, x2[r], p.wide);
+                    if (has_h) {
+                        reload_hn(r);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            sum_dhn[i] = fma2(x2[r][i], h[r][i], sum_dhn[i]);
+                            x2[r][i] = mul2(x2[r][i], gate[i]);
+                        }
+                        if (p.post == kAdalnNone && active) store8(p.dh + at + r * p.C, x2[r]);
+                    }
+                } else {
+                    zero4(x2[r]);
+                    zero4(h[r]);
+                }
+            }
+            if (has_h && p.post != kAdalnNone) {
+                RowNorm es[kRows];                               // of hn and e = dx gate wp: tbar = mean e, q = mean(e hn)
+                row_norms<kRows, true>(h, x2, shape, kAdalnMeans, 0.0f, red, turn, es);
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    const pair_t rr = twice(hs[r].r), minus_tbar = twice(p.post == kAdalnLayer ? -es[r].tbar : 0.0f), minus_q = twice(-es[r].q);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x2[r][i] = mul2(rr, fma2(h[r][i], minus_q, add2(x2[r][i], minus_tbar)));
+                    if (active && row + r < row1) store8(p.dh + at + r * p.C, x2[r]);
+                }
             }
         }
+        slot += kRows * row_bytes;
+        if (slot == ring_end) slot = smem;
     }
     if (kBwd && active) {
         float* out = p.part + static_cast<long long>(blockIdx.x) * 3 * p.C + c;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            out[i] = sum_dy[i];
-            out[p.C + i] = sum_dyn[i];
-            out[2 * p.C + i] = sum_dhn[i];
-        }
+        store8(out, sum_dy);
+        store8(out + p.C, sum_dyn);
+        store8(out + 2 * p.C, sum_dhn);
     }
 }
 
 // Joins the CTAs' column sums, always in the same order (no atomics: a gradient is the same from run to run):
 //     dshift = S0,  dscale = w S1,  dgate = wp S2,  dw = sum_b (1 + scale) S1,  dwp = sum_b gate S2.
-// A block owns 32 channels; its 8 warps share the CTAs' rows.
-constexpr int kAdalnJoinRows = 8;
+// A block owns 32 channels; its 32 warps share the CTAs' rows (its time is the latency of the loads one warp has to make
+// one after the other).
+constexpr int kAdalnJoinRows = 32;
 struct AdalnJoin {
     const float* part;
     const float *gate, *scale, *w, *wp;

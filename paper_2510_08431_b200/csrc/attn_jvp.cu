@@ -47,7 +47,7 @@ struct DeviceState {
     std::atomic<int> dyn_smem_sparse[2][3];       // ... of the kernels that walk lists of key blocks
     std::atomic<bool> sparse_bwd_ready[2][2];     // launch attribute of sparse_bwd_kernel<D><pass> is set
     std::atomic<bool> topk_ready[2];              // ... of block_topk_kernel<16>, <4>
-    std::atomic<bool> adaln_ready[2][3][2];       // launch attribute of adaln_kernel<x fp32><mode><wide> is set
+    std::atomic<bool> adaln_ready[2][3][3];       // launch attribute of adaln_kernel<x fp32><mode><wide> is set
     std::atomic<void*> static_scratch{nullptr};   // device address of the built-in scratch array
 };
 DeviceState g_dev[kMaxDevices];
@@ -637,38 +637,53 @@ using attn_jvp::AdalnParams;
 
 constexpr int kSms = 148;            // grids and workspaces are laid out for a B200's SMs, whatever is current
 
-// Rows per CTA and CTAs per batch: `waves` times as many CTAs as fit at once (kWarps warps per SM; a CTA has
-// C / 256 of them), but no fewer than `unit` rows each.
+// How a CTA is laid out, by mode (forward, with tangents, backward), type of x and row width (CLASS 0: C <= 2048, 1: C <=
+// 5120, 2: C <= 8192): rows at a time, ring stages, and the threads (C / 8) and CTAs per SM that the registers are
+// budgeted for.  Two rows at a time pay where a row's chain of shuffles is long (tangents: two norms and their companions)
+// and the registers allow (147 against 160 us on 3 x 10007 rows of 1536 with a post norm, gradients 25 against 27 us on
+// 514 rows); at 5120 channels the second row of the backward pass spills (585 against 408 us).
+template <int MODE, bool FP32, int CLASS> struct AdalnPlan;
+template <bool F> struct AdalnPlan<0, F, 0> { static constexpr int rows = 1, stages = 4, threads = 256, ctas = 3; };
+template <bool F> struct AdalnPlan<0, F, 1> { static constexpr int rows = 1, stages = 4, threads = 640, ctas = 1; };
+template <bool F> struct AdalnPlan<1, F, 0> { static constexpr int rows = 2, stages = F ? 2 : 3, threads = 256, ctas = 2; };
+template <bool F> struct AdalnPlan<1, F, 1> { static constexpr int rows = 1, stages = 3, threads = 640, ctas = 1; };
+template <bool F> struct AdalnPlan<2, F, 0> { static constexpr int rows = 2, stages = 2, threads = 256, ctas = 2; };
+template <bool F> struct AdalnPlan<2, F, 1> { static constexpr int rows = 1, stages = 3, threads = 640, ctas = 1; };
+template <int M, bool F> struct AdalnPlan<M, F, 2> { static constexpr int rows = 1, stages = 2, threads = 1024, ctas = 1; };
+
+// Rows per CTA and CTAs per batch: as many CTAs as fit at once, each with the same number of rows (but for the last of
+// a batch).  More, shorter CTAs spread better, but each pays for its modulation rows and for filling its ring (measured:
+// twice as many cost 6-12 % at 2048 channels).
 struct AdalnGrid { int threads, rows_per_cta, chunks; };
-AdalnGrid adaln_grid(long long B, int L, int C, int warps_per_sm, int waves, int unit) {
+AdalnGrid adaln_grid(int mode, long long B, int L, int C) {
     AdalnGrid g;
     g.threads = (C + 255) / 256 * 32;
-    int per_sm = warps_per_sm / (g.threads / 32);
-    per_sm = per_sm < 1 ? 1 : (per_sm > 32 ? 32 : per_sm);
-    const long long slots = (long long)kSms * per_sm * waves;
-    long long rows = (B * L + slots - 1) / slots;
-    rows = (rows + unit - 1) / unit * unit;
+    const int ctas = mode == 0 ? AdalnPlan<0, false, 0>::ctas : mode == 1 ? AdalnPlan<1, false, 0>::ctas : AdalnPlan<2, false, 0>::ctas;
+    int per_sm = g.threads <= 256 ? 256 * ctas / g.threads : 1;
+    per_sm = per_sm > 32 ? 32 : per_sm;
+    const long long slots = (long long)kSms * per_sm;
+    const long long rows = (B * L + slots - 1) / slots;
     g.rows_per_cta = rows < L ? (int)rows : L;
     g.chunks = (L + g.rows_per_cta - 1) / g.rows_per_cta;
     return g;
 }
-constexpr int kAdalnBwdWarps = 20;
-AdalnGrid adaln_bwd_grid(int B, int L, int C) { return adaln_grid(B, L, C, kAdalnBwdWarps, 1, 1); }
 
 bool adaln_shape_ok(int B, int L, int C) {
     if (B < 1 || L < 1 || C < 8 || C > attn_jvp::kAdalnMaxC || C % 8 != 0) return false;
     return (long double)B * L * C * 4 < 9.0e18L && (long double)B * L < 2.0e9L;
 }
 
-template <typename TX, int MODE, int ROWS, int STAGES, int THREADS>
-int adaln_launch(const AdalnParams& p, const AdalnGrid& g, int B, int row_bytes_per_thread, cudaStream_t stream, DeviceState& st) {
-    auto kern = attn_jvp::adaln_kernel<TX, MODE, ROWS, STAGES, THREADS>;
-    const int smem = STAGES * ROWS * row_bytes_per_thread * g.threads;
+template <typename TX, int MODE, int CLASS>
+int adaln_launch(const AdalnParams& p, const AdalnGrid& g, int B, cudaStream_t stream, DeviceState& st) {
+    constexpr bool fp32 = sizeof(TX) == 4;
+    using Plan = AdalnPlan<MODE, fp32, CLASS>;
+    auto kern = attn_jvp::adaln_kernel<TX, MODE, Plan::rows, Plan::stages, Plan::threads, Plan::ctas>;
+    const int smem = Plan::stages * Plan::rows * attn_jvp::adaln_slot_bytes(fp32, p.h != nullptr, MODE) * g.threads;
     // once per kernel and device: the most this instantiation can ask for (threads that race here set the same value)
-    std::atomic<bool>& ready = st.adaln_ready[sizeof(TX) == 4][MODE][THREADS > 640];
+    std::atomic<bool>& ready = st.adaln_ready[fp32][MODE][CLASS];
     if (!ready.load(std::memory_order_acquire)) {
-        constexpr int most = STAGES * ROWS * attn_jvp::adaln_slot_bytes(sizeof(TX) == 4, true, MODE) * THREADS;
-        static_assert(most <= 220 * 1024, "ring does not fit into shared memory");
+        constexpr int most = Plan::stages * Plan::rows * attn_jvp::adaln_slot_bytes(fp32, true, MODE) * Plan::threads;
+        static_assert(most * Plan::ctas <= 220 * 1024, "ring does not fit into shared memory");
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
         if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute(MaxDynamicSharedMemorySize)", e);
         ready.store(true, std::memory_order_release);
@@ -678,15 +693,14 @@ int adaln_launch(const AdalnParams& p, const AdalnGrid& g, int B, int row_bytes_
     if (e != cudaSuccess) return cuda_fail("adaln kernel launch", e);
     return 0;
 }
-// CTAs of up to 640 threads (C <= 5120) have 102 registers per thread and three ring stages, wider ones 64 and two.
-template <int MODE, int ROWS>
+template <int MODE>
 int adaln_dispatch(const AdalnParams& p, const AdalnGrid& g, int B, bool x_fp32, cudaStream_t stream, DeviceState& st) {
-    const int row = attn_jvp::adaln_slot_bytes(x_fp32, p.h != nullptr, MODE);
-    if (g.threads <= 640)
-        return x_fp32 ? adaln_launch<float, MODE, ROWS, 3, 640>(p, g, B, row, stream, st)
-                      : adaln_launch<__nv_bfloat16, MODE, ROWS, 3, 640>(p, g, B, row, stream, st);
-    return x_fp32 ? adaln_launch<float, MODE, ROWS, 2, 1024>(p, g, B, row, stream, st)
-                  : adaln_launch<__nv_bfloat16, MODE, ROWS, 2, 1024>(p, g, B, row, stream, st);
+    const int cls = g.threads <= 256 ? 0 : g.threads <= 640 ? 1 : 2;
+    if (x_fp32)
+        return cls == 0 ? adaln_launch<float, MODE, 0>(p, g, B, stream, st) : cls == 1 ? adaln_launch<float, MODE, 1>(p, g, B, stream, st)
+                                                                          : adaln_launch<float, MODE, 2>(p, g, B, stream, st);
+    return cls == 0 ? adaln_launch<__nv_bfloat16, MODE, 0>(p, g, B, stream, st) : cls == 1 ? adaln_launch<__nv_bfloat16, MODE, 1>(p, g, B, stream, st)
+                                                                              : adaln_launch<__nv_bfloat16, MODE, 2>(p, g, B, stream, st);
 }
 
 struct Span { const void* p; size_t bytes; int align; };     // align: bytes the address must be a multiple of
@@ -766,10 +780,11 @@ int adaln_fwd(const attn_jvp_adaln_t* in, void* x_new, void* y, void* tx_new, vo
     int dev = 0;
     DeviceState* stp = nullptr;
     if (int rc = current_device(&dev, &stp)) return rc;
-    const AdalnGrid g = jvp ? adaln_grid(in->B, in->L, in->C, 20, 4, 1) : adaln_grid(in->B, in->L, in->C, 20, 4, 2);
+    p.wide = (((uintptr_t)x_new | (uintptr_t)tx_new) & 31u) == 0;
+    const AdalnGrid g = adaln_grid(jvp ? 1 : 0, in->B, in->L, in->C);
     p.rows_per_cta = g.rows_per_cta;
     p.chunks = g.chunks;
-    return jvp ? adaln_dispatch<1, 1>(p, g, in->B, x_fp32, stream, *stp) : adaln_dispatch<0, 2>(p, g, in->B, x_fp32, stream, *stp);
+    return jvp ? adaln_dispatch<1>(p, g, in->B, x_fp32, stream, *stp) : adaln_dispatch<0>(p, g, in->B, x_fp32, stream, *stp);
 }
 
 int adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const void* dy, void* dx, void* dh, float* dgate, float* dscale,
@@ -795,11 +810,12 @@ int adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const void* dy, vo
     int dev = 0;
     DeviceState* stp = nullptr;
     if (int rc = current_device(&dev, &stp)) return rc;
-    const AdalnGrid g = adaln_bwd_grid(in->B, in->L, in->C);
+    p.wide = ((uintptr_t)dx & 31u) == 0;
+    const AdalnGrid g = adaln_grid(2, in->B, in->L, in->C);
     p.rows_per_cta = g.rows_per_cta;
     p.chunks = g.chunks;
     p.part = static_cast<float*>(workspace);
-    if (int rc = adaln_dispatch<2, 1>(p, g, in->B, x_fp32, stream, *stp)) return rc;
+    if (int rc = adaln_dispatch<2>(p, g, in->B, x_fp32, stream, *stp)) return rc;
     if (!dgate && !dscale && !dshift && !dweight && !dpost_weight) return 0;
     attn_jvp::AdalnJoin j = {p.part, p.gate, p.scale, p.w, p.wp, p.ld_gate, p.ld_scale, dgate, dscale, dshift, dweight, dpost_weight,
                              in->B, in->C, g.chunks};
@@ -1230,7 +1246,7 @@ int attn_jvp_adaln_fwd(const attn_jvp_adaln_t* in, void* x_new, void* y, void* t
 
 size_t attn_jvp_adaln_bwd_workspace_bytes(int B, int L, int C) {
     if (!adaln_shape_ok(B, L, C)) return 0;
-    return (size_t)B * adaln_bwd_grid(B, L, C).chunks * 3 * C * sizeof(float);
+    return (size_t)B * adaln_grid(2, B, L, C).chunks * 3 * C * sizeof(float);
 }
 
 int attn_jvp_adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const void* dy, void* dx, void* dh, float* dgate,
