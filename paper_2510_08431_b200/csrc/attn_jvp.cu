@@ -46,7 +46,7 @@ struct DeviceState {
     std::atomic<int> dyn_smem_pair[3][2];         // ... of the CTA-pair kernels
     std::atomic<int> dyn_smem_sparse[2][3];       // ... of the kernels that walk lists of key blocks
     std::atomic<bool> sparse_bwd_ready[2][2];     // launch attribute of sparse_bwd_kernel<D><pass> is set
-    std::atomic<bool> topk_ready[2];              // ... of block_topk_kernel<16>, <4>
+    std::atomic<bool> topk_ready[2];              // ... of block_topk_kernel<8>, <4>
     std::atomic<bool> adaln_ready[2][3][3];       // launch attribute of adaln_kernel<x fp32><mode><wide> is set
     std::atomic<void*> static_scratch{nullptr};   // device address of the built-in scratch array
 };
@@ -865,8 +865,11 @@ int launch_topk(const double* qm, const double* kmt, unsigned char* mask, int* i
         if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute(MaxDynamicSharedMemorySize)", e);
         ready.store(true, std::memory_order_release);
     }
-    const size_t smem = (size_t)ROWS * (n_k + D) * 8;
-    kern<<<(unsigned)((long long)BH * ((n_q + ROWS - 1) / ROWS)), 256, smem, stream>>>(qm, kmt, mask, index, tiles, n_q, n_k, D, Lk, topk);
+    // a key's channels are shared by the threads that a short row of keys leaves free (16 channels each at least)
+    int slices = 1;
+    while (slices < 16 && slices < D / 16 && 2 * slices * n_k <= attn_jvp::kTopkThreads) slices *= 2;
+    const size_t smem = ((size_t)ROWS * (n_k + D) + (slices > 1 ? ROWS * attn_jvp::kTopkThreads : 0)) * 8;
+    kern<<<(unsigned)((long long)BH * ((n_q + ROWS - 1) / ROWS)), attn_jvp::kTopkThreads, smem, stream>>>(qm, kmt, mask, index, tiles, n_q, n_k, D, Lk, topk, slices);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? 0 : cuda_fail("block top-k kernel launch", e);
 }
@@ -889,12 +892,12 @@ int block_select(const void* q, const void* k, int B, int H, int Lq, int Lk, int
     double* qm = static_cast<double*>(workspace);
     double* kmt = qm + (size_t)B * H * D * n_q;
     const unsigned cols = (unsigned)((H * D + 255) / 256);
-    attn_jvp::block_mean_kernel<false><<<dim3(cols, n_q, B), 256, 0, stream>>>(static_cast<const uint4*>(q), qm, Lq, H, D, n_q);
-    attn_jvp::block_mean_kernel<true><<<dim3(cols, n_k, B), 256, 0, stream>>>(static_cast<const uint4*>(k), kmt, Lk, H, D, n_k);
+    attn_jvp::block_mean_kernel<<<dim3(cols, n_q + n_k, B), 256, 0, stream>>>(static_cast<const uint4*>(q), static_cast<const uint4*>(k), qm, kmt,
+                                                                             Lq, Lk, H, D, n_q, n_k);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail("block mean kernel launch", e);
-    // sixteen rows of scores per CTA where they fit into its shared memory, else four
-    return n_k <= 1536 ? launch_topk<16>(qm, kmt, mask, index, tiles, B * H, n_q, n_k, D, Lk, topk, stream, *stp)
+    // eight rows of scores per CTA where they fit into its shared memory, else four
+    return n_k <= 3200 ? launch_topk<8>(qm, kmt, mask, index, tiles, B * H, n_q, n_k, D, Lk, topk, stream, *stp)
                        : launch_topk<4>(qm, kmt, mask, index, tiles, B * H, n_q, n_k, D, Lk, topk, stream, *stp);
 }
 

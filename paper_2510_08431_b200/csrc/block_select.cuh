@@ -21,21 +21,24 @@ constexpr int kSelBlock = 128;       // tokens of a block
 constexpr int kPoolRows = 8;         // row groups of a pooling CTA: 8 x 16 tokens
 constexpr int kPoolCols = 32;        // 16-byte pieces (8 channels) of a row it takes
 
-// Block means of q or k.  x: [B][L][H * D] bf16.  out: [B * H][n][D] fp64, or with kTransposed [B * H][D][n].
-// grid (ceil(H D / 256), n, B), 256 threads: thread (piece, row group) sums 16 tokens of 8 channels.
-template <bool kTransposed>
+// Block means of q and k in one launch.  q, k: [B][L][H * D] bf16.  qm: [B * H][n_q][D] fp64, kmt: [B * H][D][n_k] fp64 (a
+// channel's values of all key blocks side by side, as the scores read them).
+// grid (ceil(H D / 256), n_q + n_k, B), 256 threads: thread (piece, row group) sums 16 tokens of 8 channels.
 __global__ void __launch_bounds__(kPoolRows* kPoolCols)
-block_mean_kernel(const uint4* __restrict__ x, double* __restrict__ out, int L, int H, int D, int n) {
+block_mean_kernel(const uint4* __restrict__ q, const uint4* __restrict__ k, double* __restrict__ qm, double* __restrict__ kmt, int Lq,
+                  int Lk, int H, int D, int n_q, int n_k) {
     __shared__ double part[kPoolRows][kPoolCols * 8];
     const int piece = threadIdx.x % kPoolCols, group = threadIdx.x / kPoolCols;
     const int pieces = H * D / 8, col = blockIdx.x * kPoolCols + piece;
-    const int block = blockIdx.y, b = blockIdx.z;
+    const bool keys = blockIdx.y >= n_q;
+    const int block = keys ? blockIdx.y - n_q : blockIdx.y, b = blockIdx.z;
+    const int L = keys ? Lk : Lq;
     const int rows = min(kSelBlock, L - block * kSelBlock);
     double s[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) s[i] = 0.0;
     if (col < pieces) {
-        const uint4* row = x + (static_cast<long long>(b) * L + block * kSelBlock) * pieces + col;
+        const uint4* row = (keys ? k : q) + (static_cast<long long>(b) * L + block * kSelBlock) * pieces + col;
         constexpr int kEach = kSelBlock / kPoolRows;
         uint4 v[kEach];
 #pragma unroll
@@ -46,8 +49,7 @@ block_mean_kernel(const uint4* __restrict__ x, double* __restrict__ out, int L, 
 #pragma unroll
         for (int r = 0; r < kEach; ++r) {
             const uint32_t u[4] = {v[r].x, v[r].y, v[r].z, v[r].w};
-            // Two neighbouring tokens' values could be added in fp32 only if their exponents were close; a conversion to
-            // fp64 (a quarter-rate instruction) is avoided instead by placing the bf16 bits in the upper word of a
+            // A conversion to fp64 (a quarter-rate instruction) is avoided by placing the bf16 bits in the upper word of a
             // double: sign, exponent and mantissa land in place with the exponent field taken as it is, which scales
             // every finite value, subnormal ones included, by exactly 2^-896.
 #pragma unroll
@@ -72,7 +74,8 @@ block_mean_kernel(const uint4* __restrict__ x, double* __restrict__ out, int L, 
         const double mean = sum * 0x1p896 / static_cast<double>(rows);
         const int h = channel / D, d = channel - h * D;
         const long long bh = static_cast<long long>(b) * H + h;
-        out[kTransposed ? (bh * D + d) * n + block : (bh * n + block) * D + d] = mean;
+        if (keys) kmt[(bh * D + d) * n_k + block] = mean;
+        else qm[(bh * n_q + block) * D + d] = mean;
     }
 }
 
@@ -101,67 +104,131 @@ __device__ __forceinline__ void write_row(const Keep& keep, int n, int tokens, u
     if (lane == 0) *tiles = 2 * count - ((last_kept && tokens - (n - 1) * kSelBlock <= 64) ? 1 : 0);
 }
 
-// Scores and top-k.  A CTA takes kRows query blocks of one (batch, head): thread j forms the scores of key block j (and
-// j + 256, ...) with all of them (the means of k are stored channel by channel, so a warp reads 256 contiguous bytes per
-// channel and every value feeds kRows multiply-adds), then a warp per row finds the topk-th largest key bit by bit,
-// from the top, by counting (64 rounds at most; it stops when exactly topk keys are left), and among keys equal to it
-// keeps the first ones.
+// The topk-th largest of a row's keys, bit by bit from the first bit in which the keys differ: `count(trial)` says how many
+// keys reach a trial value; the search ends when exactly `want` do.  Whole warp; returns the bound and how many reach it.
+template <typename Count>
+__device__ __forceinline__ unsigned long long find_bound(const Count& count, unsigned long long all_or, unsigned long long all_and,
+                                                         int n, int want, int& reached) {
+    const unsigned long long differ = all_or ^ all_and;
+    reached = n;
+    if (differ == 0) return all_and;
+    const int top = 63 - __clzll(static_cast<long long>(differ));
+    unsigned long long bound = top == 63 ? 0ull : all_and & ~((1ull << (top + 1)) - 1ull);     // the common leading bits
+    for (int bit = top; bit >= 0 && reached != want; --bit) {
+        const unsigned long long trial = bound | (1ull << bit);
+        const int c = __reduce_add_sync(0xffffffffu, count(trial));
+        if (c >= want) { bound = trial; reached = c; }
+    }
+    return bound;
+}
+
+// Scores and top-k.  A CTA of 256 threads takes kRows query blocks of one (batch, head).  Thread (slice, j): key block j,
+// j + keys, ... and a slice of the channels, with all rows (the means of k are stored channel by channel, so a warp reads
+// contiguous bytes, and every value feeds kRows multiply-adds); few key blocks leave several slices per key, whose
+// sums are joined in a fixed order, so that equal key blocks have equal scores.  Then a warp per row finds the topk-th
+// largest key by counting (find_bound) and keeps the keys above it and, of those equal to it, the first ones.  Up to 256
+// key blocks a lane holds its share of the row in registers.
+// What bounds it is latency: with 12 heads of 256 x 256 blocks 201 M multiply-adds in fp64 are 12 us of the fp64 pipes.
+constexpr int kTopkThreads = 256;
 template <int kRows>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(kTopkThreads)
 block_topk_kernel(const double* __restrict__ qm, const double* __restrict__ kmt, unsigned char* __restrict__ mask,
-                  int* __restrict__ index, int* __restrict__ tiles, int n_q, int n_k, int D, int Lk, int topk) {
-    extern __shared__ unsigned long long sel_keys[];             // [kRows][n_k], then the queries' means [D][kRows]
+                  int* __restrict__ index, int* __restrict__ tiles, int n_q, int n_k, int D, int Lk, int topk, int slices) {
+    // keys [kRows][n_k], the queries' means [D][kRows], and with slices their sums [slices][kRows][256 / slices]
+    extern __shared__ unsigned long long sel_keys[];
     double* qs = reinterpret_cast<double*>(sel_keys + static_cast<size_t>(kRows) * n_k);
+    double* part = qs + D * kRows;
     const int groups = (n_q + kRows - 1) / kRows;
     const long long bh = blockIdx.x / groups;
     const int i0 = static_cast<int>(blockIdx.x - bh * groups) * kRows;
-    for (int e = threadIdx.x; e < kRows * D; e += 256) {
+    for (int e = threadIdx.x; e < kRows * D; e += kTopkThreads) {
         const int r = e / D, d = e - r * D;
         qs[d * kRows + r] = i0 + r < n_q ? qm[(bh * n_q + i0 + r) * D + d] : 0.0;
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < n_k; j += 256) {
+    const int keys = kTopkThreads / slices, slice = threadIdx.x / keys, j_own = threadIdx.x - slice * keys;
+    const int each = D / slices, d0 = slice * each;
+    for (int j0 = 0; j0 < n_k; j0 += keys) {                     // (once where there are slices)
+        const int j = j0 + j_own;
         double acc[kRows];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) acc[r] = 0.0;
-        const double* kp = kmt + bh * D * n_k + j;
-#pragma unroll 4
-        for (int d = 0; d < D; ++d) {
-            const double kv = __ldg(kp + static_cast<long long>(d) * n_k);
+        if (j < n_k) {
+            const double* kp = kmt + (bh * D + d0) * n_k + j;
+#pragma unroll 16
+            for (int d = 0; d < each; ++d) {
+                const double kv = __ldg(kp + static_cast<long long>(d) * n_k);
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) acc[r] = fma(qs[d * kRows + r], kv, acc[r]);
+                for (int r = 0; r < kRows; ++r) acc[r] = fma(qs[(d0 + d) * kRows + r], kv, acc[r]);
+            }
         }
+        if (slices == 1) {
+            if (j < n_k) {
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) sel_keys[static_cast<size_t>(r) * n_k + j] = ordered_key(acc[r]);
+                for (int r = 0; r < kRows; ++r) sel_keys[static_cast<size_t>(r) * n_k + j] = ordered_key(acc[r]);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) part[(slice * kRows + r) * keys + j_own] = acc[r];
+            __syncthreads();
+            for (int e = threadIdx.x; e < kRows * keys; e += kTopkThreads) {
+                const int r = e / keys, jj = e - r * keys;
+                double sum = 0.0;
+                for (int s = 0; s < slices; ++s) sum += part[(s * kRows + r) * keys + jj];
+                if (jj < n_k) sel_keys[static_cast<size_t>(r) * n_k + jj] = ordered_key(sum);
+            }
+        }
     }
     __syncthreads();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int r = warp; r < kRows && i0 + r < n_q; r += 8) {
-        const unsigned long long* keys = sel_keys + static_cast<size_t>(r) * n_k;
+    for (int r = warp; r < kRows && i0 + r < n_q; r += kTopkThreads / 32) {
+        const unsigned long long* row_keys = sel_keys + static_cast<size_t>(r) * n_k;
         const int want = min(topk, n_k);
-        // the largest `bound` with at least `want` keys >= bound
-        unsigned long long bound = 0;
-        int at_bound = n_k;                                      // keys >= bound
-        for (int bit = 63; bit >= 0 && at_bound != want; --bit) {
-            const unsigned long long trial = bound | (1ull << bit);
-            int c = 0;
-            for (int j = lane; j < n_k; j += 32) c += keys[j] >= trial ? 1 : 0;
-            c = __reduce_add_sync(0xffffffffu, c);
-            if (c >= want) { bound = trial; at_bound = c; }
+        unsigned long long all_or = 0, all_and = ~0ull, bound;
+        int reached;
+        if (n_k <= 256) {
+            unsigned long long own[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int j = lane + 32 * u;
+                own[u] = j < n_k ? row_keys[j] : 0ull;           // (0 is below every key of a finite score)
+                if (j < n_k) { all_or |= own[u]; all_and &= own[u]; }
+            }
+            for (int m = 16; m >= 1; m >>= 1) {
+                all_or |= __shfl_xor_sync(0xffffffffu, all_or, m);
+                all_and &= __shfl_xor_sync(0xffffffffu, all_and, m);
+            }
+            bound = find_bound([&](unsigned long long trial) {
+                int c = 0;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) c += own[u] >= trial ? 1 : 0;
+                return c;
+            }, all_or, all_and, n_k, want, reached);
+        } else {
+            for (int j = lane; j < n_k; j += 32) { all_or |= row_keys[j]; all_and &= row_keys[j]; }
+            for (int m = 16; m >= 1; m >>= 1) {
+                all_or |= __shfl_xor_sync(0xffffffffu, all_or, m);
+                all_and &= __shfl_xor_sync(0xffffffffu, all_and, m);
+            }
+            bound = find_bound([&](unsigned long long trial) {
+                int c = 0;
+                for (int j = lane; j < n_k; j += 32) c += row_keys[j] >= trial ? 1 : 0;
+                return c;
+            }, all_or, all_and, n_k, want, reached);
         }
-        // keys equal to the bound: only where more than `want` reach it, the last ones are dropped
-        int spare = at_bound - want;
+        // more than `want` keys reach the bound: of those equal to it only the first ones are kept
+        const int spare = reached - want;
         int equal = 0;
         if (spare > 0) {
-            for (int j = lane; j < n_k; j += 32) equal += keys[j] == bound ? 1 : 0;
+            for (int j = lane; j < n_k; j += 32) equal += row_keys[j] == bound ? 1 : 0;
             equal = __reduce_add_sync(0xffffffffu, equal);
         }
-        int keep_equal = equal - spare;                          // of the equal ones, how many are kept (spare > 0)
+        const int keep_equal = equal - spare;
         auto keep = [&](int j) {
-            const unsigned long long key = keys[j];
+            const unsigned long long key = row_keys[j];
             if (key != bound || spare == 0) return key >= bound;
             int before = 0;                                      // (rare: exact ties around the last place)
-            for (int i = 0; i < j; ++i) before += keys[i] == bound ? 1 : 0;
+            for (int i = 0; i < j; ++i) before += row_keys[i] == bound ? 1 : 0;
             return before < keep_equal;
         };
         const long long row = bh * n_q + i0 + r;
@@ -189,10 +256,17 @@ block_transpose_kernel(const unsigned char* __restrict__ mask, int* __restrict__
     const long long bh = blockIdx.x / groups;
     const int j0 = static_cast<int>(blockIdx.x - bh * groups) * 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = warp; i < n_q; i += 8) {
-        const bool k = j0 + lane < n_k && mask[(bh * n_q + i) * n_k + j0 + lane] != 0;
-        const unsigned votes = __ballot_sync(0xffffffffu, k);
-        if (lane == 0) sel_words[i] = votes;
+    const unsigned char* column = mask + bh * n_q * n_k + j0 + lane;
+    const bool inside = j0 + lane < n_k;
+    for (int i0 = warp * 8; i0 < n_q; i0 += 64) {                // (eight rows' loads in flight per warp)
+        unsigned char v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = inside && i0 + u < n_q ? __ldg(column + static_cast<long long>(i0 + u) * n_k) : 0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const unsigned votes = __ballot_sync(0xffffffffu, v[u] != 0);
+            if (lane == u && i0 + u < n_q) sel_words[i0 + u] = votes;
+        }
     }
     __syncthreads();
     for (int c = warp; c < 32 && j0 + c < n_k; c += 8) {

@@ -171,10 +171,11 @@ def test_ties_go_to_the_lower_block(aj):
     assert (sel.mask[..., :3]).all() and not sel.mask[..., 3:].any()
 
 
-def test_selection_of_many_key_blocks(aj):
-    """More key blocks than the sixteen-row kernel has room for."""
+@pytest.mark.parametrize("n_k", [300, 3300])
+def test_selection_of_many_key_blocks(aj, n_k):
+    """More key blocks than a lane holds in registers, and more than eight rows have room for."""
     q = torch.randn(1, 300, 1, 64, device="cuda").bfloat16()
-    k = torch.randn(1, 1600 * 128 - 37, 1, 64, device="cuda").bfloat16()
+    k = torch.randn(1, n_k * 128 - 37, 1, 64, device="cuda").bfloat16()
     sel = aj.block_select(q, k, 100)
     assert torch.equal(sel.mask, R.top_mask(q, k, 100))
     lists(sel)
