@@ -839,9 +839,9 @@ int sparse_shape(int B, int H, int Lq, int Lk, int D) {
     if (B < 1 || H < 1 || Lq < 1 || Lk < 1) return ATTN_JVP_ERR_SHAPE;
     if (D != 64 && D != 128) return ATTN_JVP_ERR_UNSUPPORTED_D;
     if (n_blocks(Lq) > kSelMaxBlocks || n_blocks(Lk) > kSelMaxBlocks || B > 65535) return ATTN_JVP_ERR_SHAPE;
-    // work items, and rows of lists, are counted in ints
+    // work items and rows of lists are counted in ints, 2048 blocks of 256 threads read an item's rows at the most
     const long long most = n_blocks(Lq) > n_blocks(Lk) ? n_blocks(Lq) : n_blocks(Lk);
-    if ((long double)B * H * most > 1.0e9L) return ATTN_JVP_ERR_SHAPE;
+    if ((long double)B * H * most > 1.0e7L) return ATTN_JVP_ERR_SHAPE;
     return 0;
 }
 
@@ -989,22 +989,23 @@ int sparse_fwd(const void* q, const void* k, const void* v, const void* tq, cons
     }
 }
 
-// Workspace of the backward pass: the transposed lists, then {LSE, delta} per padded query row.
-struct SparseBwdLayout { size_t index, tiles, rows, total; };
+// Workspace of the backward pass: the transposed lists, the two passes' item counters, LSE and delta per padded query row.
+struct SparseBwdLayout { size_t index, tiles, counters, rows, total; };
 SparseBwdLayout sparse_bwd_layout(int B, int H, int Lq, int Lk) {
     auto pad = [](size_t n) { return (n + 255) & ~(size_t)255; };
     const size_t bh = (size_t)B * H, n_q = n_blocks(Lq), n_k = n_blocks(Lk);
     SparseBwdLayout l;
     l.index = 0;
     l.tiles = pad(bh * n_k * n_q * 4);
-    l.rows = l.tiles + pad(bh * n_k * 4);
-    l.total = l.rows + bh * n_q * kSelBlock * sizeof(float2);
+    l.counters = l.tiles + pad(bh * n_k * 4);
+    l.rows = l.counters + 256;
+    l.total = l.rows + bh * n_q * kSelBlock * 2 * sizeof(float);
     return l;
 }
 
 template <int D, bool DKV>
 int launch_sparse_bwd(const CUtensorMap& x1, const CUtensorMap& x2, const CUtensorMap& y1, const CUtensorMap& y2,
-                      const attn_jvp::SparseBwdArgs& a, int n_items, cudaStream_t stream, DeviceState& st) {
+                      const attn_jvp::SparseBwdArgs& a, cudaStream_t stream, DeviceState& st) {
     auto kern = attn_jvp::sparse_bwd_kernel<D, DKV>;
     constexpr int smem = attn_jvp::SparseBwdPlan<D>::kDynBytes;
     std::atomic<bool>& ready = st.sparse_bwd_ready[D == 128][DKV];
@@ -1013,23 +1014,23 @@ int launch_sparse_bwd(const CUtensorMap& x1, const CUtensorMap& x2, const CUtens
         if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute(MaxDynamicSharedMemorySize)", e);
         ready.store(true, std::memory_order_release);
     }
-    kern<<<(unsigned)n_items, attn_jvp::kBwdThreads, smem, stream>>>(x1, x2, y1, y2, a);
+    kern<<<(unsigned)(a.n_items < st.sm_count ? a.n_items : st.sm_count), attn_jvp::kBwdThreads, smem, stream>>>(x1, x2, y1, y2, a);
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? 0 : cuda_fail("sparse backward kernel launch", e);
 }
 
 template <int D>
-int sparse_bwd_run(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo, const void* o,
-                   const void* d_o, const float* lse, float2* rows, attn_jvp::SparseBwdArgs dkv, attn_jvp::SparseBwdArgs dq, int B,
-                   int H, int Lq, int Lk, cudaStream_t stream, DeviceState& st) {
-    const int padded = n_blocks(Lq) * kSelBlock;
-    const long long threads = (long long)B * padded * H * (D / 8);
-    attn_jvp::sparse_bwd_rows_kernel<D><<<(unsigned)((threads + 255) / 256), 256, 0, stream>>>(
-        static_cast<const uint4*>(o), static_cast<const uint4*>(d_o), lse, rows, B, H, Lq, padded);
+int sparse_bwd_run(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo,
+                   attn_jvp::SparseBwdPrep prep, const attn_jvp::SparseBwdArgs& dkv, const attn_jvp::SparseBwdArgs& dq, cudaStream_t stream,
+                   DeviceState& st) {
+    const long long threads = (long long)prep.B * prep.n_q * kSelBlock * prep.H * (D / 8);
+    prep.row_blocks = (int)((threads + 255) / 256);
+    const int zero_blocks = (dkv.n_items + dq.n_items + 7) / 8;
+    attn_jvp::sparse_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + zero_blocks), 256, 0, stream>>>(prep);
     const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return cuda_fail("sparse backward row kernel launch", e);
-    if (int rc = launch_sparse_bwd<D, true>(mk, mv, mq, mdo, dkv, B * H * n_blocks(Lk), stream, st)) return rc;
-    return launch_sparse_bwd<D, false>(mq, mdo, mk, mv, dq, B * H * n_blocks(Lq), stream, st);
+    if (e != cudaSuccess) return cuda_fail("sparse backward preparation launch", e);
+    if (int rc = launch_sparse_bwd<D, true>(mk, mv, mq, mdo, dkv, stream, st)) return rc;
+    return launch_sparse_bwd<D, false>(mq, mdo, mk, mv, dq, stream, st);
 }
 
 int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse,
@@ -1061,7 +1062,7 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
     char* w = static_cast<char*>(workspace);
     int* t_index = reinterpret_cast<int*>(w + lay.index);
     int* t_tiles = reinterpret_cast<int*>(w + lay.tiles);
-    float2* rows = reinterpret_cast<float2*>(w + lay.rows);
+    float* rows = reinterpret_cast<float*>(w + lay.rows);
     const int n_q = n_blocks(Lq), n_k = n_blocks(Lk);
     attn_jvp::block_transpose_kernel<<<(unsigned)((long long)B * H * ((n_k + 31) / 32)), 256, (size_t)n_q * 4, stream>>>(
         mask, t_index, t_tiles, n_q, n_k, Lq);
@@ -1075,11 +1076,14 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
     a.n_q = n_q;
     a.scale = scale;
     a.scale_log2 = scale * 1.4426950408889634f;
+    a.wide_out = (((uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv) & 31u) == 0;
     attn_jvp::SparseBwdArgs dkv = a, dqa = a;
     dkv.list = t_index;
     dkv.tiles = t_tiles;
     dkv.list_stride = n_q;
     dkv.n_items_per_head = n_k;
+    dkv.n_items = B * H * n_k;
+    dkv.counter = reinterpret_cast<int*>(w + lay.counters);
     dkv.L_own = Lk;
     dkv.L_other = Lq;
     dkv.out1 = static_cast<__nv_bfloat16*>(dv);
@@ -1088,11 +1092,15 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
     dqa.tiles = tiles;
     dqa.list_stride = n_k;
     dqa.n_items_per_head = n_q;
+    dqa.n_items = B * H * n_q;
+    dqa.counter = dkv.counter + 1;
     dqa.L_own = Lq;
     dqa.L_other = Lk;
     dqa.out1 = static_cast<__nv_bfloat16*>(dq);
-    return D == 128 ? sparse_bwd_run<128>(mq, mk, mv, mdo, o, d_o, lse, rows, dkv, dqa, B, H, Lq, Lk, stream, st)
-                    : sparse_bwd_run<64>(mq, mk, mv, mdo, o, d_o, lse, rows, dkv, dqa, B, H, Lq, Lk, stream, st);
+    attn_jvp::SparseBwdPrep prep = {static_cast<const uint4*>(o), static_cast<const uint4*>(d_o), lse, rows, tiles, t_tiles, dqa.out1,
+                                    dkv.out2, dkv.out1, dkv.counter, B, H, Lq, Lk, n_q, n_k, 0};
+    return D == 128 ? sparse_bwd_run<128>(mq, mk, mv, mdo, prep, dkv, dqa, stream, st)
+                    : sparse_bwd_run<64>(mq, mk, mv, mdo, prep, dkv, dqa, stream, st);
 }
 
 }  // namespace

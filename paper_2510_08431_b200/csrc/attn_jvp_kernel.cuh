@@ -529,6 +529,27 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+// 2^x of two values on the FMA pipe, for kernels whose pace the special-function unit sets (8 cycles per warp instruction):
+// x = n + f with n the nearest integer (added and taken off again as 1.5 * 2^23 + n), 2^f by a polynomial on [-1/2, 1/2]
+// whose coefficients minimise the largest relative error with p(0) = 1 (2.9e-6 in fp32; P is rounded to bf16 for the value
+// products, an error of 3.9e-3, and sums of P take the error on average), and n added to the exponent field.  x below
+// -127 is taken as -127, where p(0) = 1 makes the result exactly +0; x must not exceed 127.
+__device__ __forceinline__ void exp2_poly_pair(uint64_t x, float& p0, float& p1) {
+    float x0, x1;
+    unpack_f32x2(x, x0, x1);
+    x = pack_f32x2(fmaxf(x0, -127.0f), fmaxf(x1, -127.0f));
+    const uint64_t t = add_f32x2(x, pack_f32x2(12582912.0f, 12582912.0f));
+    const uint64_t f = add_f32x2(x, fma_f32x2(t, pack_f32x2(-1.0f, -1.0f), pack_f32x2(12582912.0f, 12582912.0f)));
+    uint64_t y = fma_f32x2(f, pack_f32x2(0x1.3a02ccp-7f, 0x1.3a02ccp-7f), pack_f32x2(0x1.c9fc46p-5f, 0x1.c9fc46p-5f));
+    y = fma_f32x2(f, y, pack_f32x2(0x1.ec037ap-3f, 0x1.ec037ap-3f));
+    y = fma_f32x2(f, y, pack_f32x2(0x1.62e12cp-1f, 0x1.62e12cp-1f));
+    y = fma_f32x2(f, y, pack_f32x2(1.0f, 1.0f));
+    float t0, t1, y0, y1;
+    unpack_f32x2(t, t0, t1);
+    unpack_f32x2(y, y0, y1);
+    p0 = __int_as_float(__float_as_int(y0) + (__float_as_int(t0) << 23));
+    p1 = __int_as_float(__float_as_int(y1) + (__float_as_int(t1) << 23));
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t*>(&h);
@@ -550,8 +571,10 @@ __host__ __device__ constexpr int score_buffers(int D, int mode) {
 // only used by that variant.
 //
 // kSparse: an item's key tiles are those of the 128-key blocks on its list instead of all of them, in the list's order.
-// Every item then has its own number of tiles (an empty list counts as one tile without a valid key: its row maximum is
-// taken as 0, all of its P~ are 0, and the epilogue's 1 / l as 0), so items are not streamed into each other.
+// Every item then has its own number of tiles, filled up to the least number the kernel needs (one, or with streamed items
+// one per score buffer) with tiles that lie behind the last key: all of their P~ are 0; where even the first tile is one,
+// its row maximum is taken as 0 and the epilogue's 1 / l as 0.  Each role reads the length and the first entry of its next
+// item's list while it works on the current one (the loads would cost some 800 cycles each at every hand-over).
 template <int D, int MODE, bool kSplit, int kGroups, bool kPair, bool kSparse = false>
 __global__ void __launch_bounds__(num_threads(kGroups), 1)
 attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -576,8 +599,15 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     constexpr int kRingStage = kDoubleQ ? 0 : kStageSlots;           // ... of which in ring slots (else in the item's Q/tQ buffer)
     // P~ and H~ of a tile are handed to the MMA warp together (one barrier): the softmax warps form both in one
     // pass over the columns, so an earlier hand-over of P~ alone would gain nothing.
+    // of 8 pairs of exponentials, how many take the FMA pipe: the forward-only pass over key block lists, whose pace the
+    // special-function unit would set (1024 of its cycles per 128 x 128 scores, as many as the MMAs take at D = 128)
+#ifndef POLY_F
+#define POLY_F 2
+#endif
+    constexpr int kPolyPairs = (kSparse && MODE == kModeFwdOnly) ? POLY_F : 0;
     constexpr int kBufs = score_buffers(D, MODE);            // score buffers = how many tiles the score MMAs run ahead
     constexpr int kScoreCol0 = (kBufs == 3) ? 128 : 256;     // first column of score buffer 0
+    constexpr int kMinTiles = kDoubleQ ? kBufs : 1;          // kSparse: least number of key tiles of an item
     static_assert(kScoreCol0 + kBufs * kScoreBufStride <= kTmemCols, "score buffers must fit into tensor memory");
     static_assert((kHasTQ ? 2 * D : D) <= kScoreCol0, "accumulators and score buffers overlap");
     static_assert(kDoubleQ || Plan::kSlotBytes == Plan::kQBytes, "an output tile must fill one ring slot");
@@ -615,14 +645,22 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const bool lead_cta = cta_rank == 0u;
     const int first_item = kPair ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
     const int item_stride = kPair ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
-    struct Item { int q0, h, b, split, tile0, n_kv; const int* list; };
+    struct Item { int q0, h, b, split, tile0, n_kv; int n_real, first; const int* list; };
     // Work item number -> (query tile, head, batch [, chunk]).  The roles walk their items with a fixed stride, so
     // after the first item the three indices are advanced by the stride's own decomposition (carry by compare and
     // subtract) instead of being divided out again: the divisions would sit on the critical path of every item
     // hand-over, once per role.
-    struct Walk { int qt, h, z; };
+    struct Walk { int qt, h, z; int tiles64, first; };
+    // (kSparse: the length of item's list and its first entry; an item number is also the number of its list)
+    auto read_list = [&](Walk& k, int item) {
+        if (kSparse) {
+            const bool exists = item < args.n_items;
+            k.tiles64 = exists ? __ldg(args.tiles + item) : 0;
+            k.first = exists ? __ldg(args.list + static_cast<size_t>(item) * args.list_stride) : 0;
+        }
+    };
     auto walk_init = [&](int item) -> Walk {
-        Walk k;
+        Walk k{};
         k.qt = item % args.n_q_tiles;
         const int rest = item / args.n_q_tiles;
         k.h = rest % args.H;
@@ -630,12 +668,14 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         return k;
     };
     const Walk walk_stride = walk_init(item_stride);
-    auto walk_step = [&](Walk& k) {
+    // to item number `item`, item_stride items on
+    auto walk_step = [&](Walk& k, int item) {
         k.qt += walk_stride.qt;
         if (k.qt >= args.n_q_tiles) { k.qt -= args.n_q_tiles; ++k.h; }
         k.h += walk_stride.h;
         if (k.h >= args.H) { k.h -= args.H; ++k.z; }
         k.z += walk_stride.z;
+        read_list(k, item);
     };
     auto item_of = [&](const Walk& k) -> Item {
         Item w;
@@ -646,26 +686,31 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         w.tile0 = kSplit ? w.split * args.tiles_per_split : 0;       // first key tile of this item
         w.n_kv = kSplit ? min(args.tiles_per_split, args.n_kv_tiles - w.tile0) : args.n_kv_tiles;
         w.list = nullptr;
+        w.n_real = w.first = 0;
         if (kSparse) {
             const int row = (k.z * args.H + k.h) * args.n_q_tiles + k.qt;
-            const int tiles64 = min(__ldg(args.tiles + row), 2 * args.list_stride);
-            w.list = tiles64 > 0 ? args.list + static_cast<size_t>(row) * args.list_stride : nullptr;
-            w.n_kv = max(1, kBN == kBlockN ? tiles64 : (tiles64 + 1) / 2);
+            const int tiles64 = min(k.tiles64, 2 * args.list_stride);
+            w.list = args.list + static_cast<size_t>(row) * args.list_stride;
+            w.first = k.first;
+            w.n_real = kBN == kBlockN ? tiles64 : (tiles64 + 1) / 2;
+            w.n_kv = max(kMinTiles, w.n_real);
         }
         return w;
     };
-    // first key of tile j of an item (an empty list: behind the last key, where TMA fills in zeros)
+    // first key of tile j of an item (a tile that only fills up: behind the last key, where TMA fills in zeros)
     auto key_of = [&](const Item& w, int j) -> int {
         if (!kSparse) return (w.tile0 + j) * kBN;
-        if (w.list == nullptr) return args.list_stride * kBlockM;
-        return kBN == kBlockN ? __ldg(w.list + (j >> 1)) * kBlockM + (j & 1) * kBlockN : __ldg(w.list + j) * kBlockM;
+        if (j >= w.n_real) return args.list_stride * kBlockM;
+        const int e = kBN == kBlockN ? j >> 1 : j;
+        const int block = e == 0 ? w.first : __ldg(w.list + e);
+        return block * kBlockM + (kBN == kBlockN ? (j & 1) * kBlockN : 0);
     };
     const int n_items = args.n_items;
-    // Two Q/tQ buffers, no key chunks (every item then has the same number of key tiles): the key tiles of all of a
-    // CTA's items form one stream.  The score MMAs of an item's leading tiles are issued in the last bursts of the
+    // Two Q/tQ buffers, no key chunks (every item then has the same number of key tiles, or at least as many as there are
+    // score buffers): the key tiles of all of a CTA's items form one stream.  The score MMAs of an item's leading tiles are issued in the last bursts of the
     // item before (its Q, tQ are resident by then), and the ring carries their K tiles in that order, so that an
     // item boundary costs the MMA warp and the producer nothing.
-    const bool stream_items = kDoubleQ && !kSplit && !kSparse && args.n_kv_tiles >= kBufs;
+    const bool stream_items = kDoubleQ && !kSplit && (kSparse || args.n_kv_tiles >= kBufs);
     // Score buffer and barrier phase of a key tile, g % kBufs and (g / kBufs) & 1, carried along tile by tile (a
     // division by three per use would sit on the MMA warp's critical chain of dependent instructions).
     struct BufPos { int buf; uint32_t phase; };
@@ -975,12 +1020,13 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             };
             Item prev_w{};
             int it = 0;
-            Walk wk = walk_init(first_item);
-            for (int item = first_item; ok && item < n_items; item += item_stride, ++it, walk_step(wk)) {
+            Walk wk = walk_init(first_item), wk_next;
+            read_list(wk, first_item);
+            for (int item = first_item; ok && item < n_items; item += item_stride, ++it, wk = wk_next) {
                 w = item_of(wk);
                 const bool has_next = n_items - item > item_stride;
-                Walk wk_next = wk;
-                walk_step(wk_next);
+                wk_next = wk;
+                walk_step(wk_next, kSparse ? item + item_stride : 0);
                 if (!kDoubleQ) {
                     // one Q/tQ buffer: it is free once all score MMAs of the item before are complete
                     if (it > 0) ok = mbar_wait(smem_u32(&bar_q_free), (it - 1) & 1, abort_state);
@@ -1218,10 +1264,13 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             BufPos bp{0, 0u};    // score buffer / phase of the tile whose value MMAs come next
             int g0 = 0;          // global number of the item's first key tile
             int it = 0;
-            Walk wk = walk_init(first_item);
-            for (int item = first_item; ok && item < n_items; item += item_stride, ++it, walk_step(wk)) {
+            Walk wk = walk_init(first_item), wk_next;
+            read_list(wk, first_item);
+            for (int item = first_item; ok && item < n_items; item += item_stride, ++it, wk = wk_next) {
                 const Item w = item_of(wk);
                 const int n_kv = w.n_kv;
+                wk_next = wk;
+                walk_step(wk_next, kSparse ? item + item_stride : 0);
                 const bool has_next_item = n_items - item > item_stride;
                 // stream_items: this item's leading score MMAs went out with the last bursts of the item before
                 const bool leading_done = stream_items && it > 0;
@@ -1375,17 +1424,20 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         ACC_DECL(acc_sm_scores);   // blocked for a tile's scores
         ACC_DECL(acc_sm_values);   // blocked for the item's last value MMAs (epilogue)
         ACC_DECL(acc_sm_epi);      // epilogue after that wait
-        Walk wk = walk_init(first_item);
-        for (int item = first_item; ok && item < n_items; item += item_stride, ++it, walk_step(wk)) {
+        Walk wk = walk_init(first_item), wk_next;
+        read_list(wk, first_item);
+        for (int item = first_item; ok && item < n_items; item += item_stride, ++it, wk = wk_next) {
             const Item w = item_of(wk);
             const int n_kv = w.n_kv;
+            wk_next = wk;
+            walk_step(wk_next, kSparse ? item + item_stride : 0);
             float m_ref = -INFINITY;   // running reference max, log2 domain (m of Algorithm 2, lazily updated)
             float l_run = 0.0f;        // l (two groups: this group's share)
             float r_run = 0.0f;        // r (of the centred tS, see below; two groups: this group's share)
             float ts_shift = 0.0f;     // per-row constant subtracted from tS
             float m_other = -INFINITY; // two groups: the reference the other group's sums were last known to use
-            // (kSparse: only the last tile of an ascending list can reach past the last key)
-            const int last_valid = kSparse ? max(0, args.Lk - key_of(w, n_kv - 1)) : 0;
+            // (kSparse: of the list's tiles only the last one can reach past the last key)
+            const int last_valid = kSparse && w.n_real > 0 ? args.Lk - key_of(w, w.n_real - 1) : 0;
             // two groups: the group of the item's last tile finishes the item
             const bool finisher = (kGroups == 1) || (((g0 + n_kv - 1) & 1) == grp);
 
@@ -1422,7 +1474,8 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #endif
 
                 // keys past Lk (zero-filled by TMA) must not enter the softmax
-                const int valid = !kSparse ? args.Lk - (w.tile0 + j) * kBN : (j + 1 < n_kv ? kBN : last_valid);
+                const int valid = !kSparse ? args.Lk - (w.tile0 + j) * kBN
+                                           : (j + 1 < w.n_real ? kBN : (j + 1 == w.n_real ? last_valid : 0));
                 if (valid < kBN) {
                     const uint32_t masked = neg_scale ? 0x7F800000u : 0xFF800000u;   // -inf after scaling
 #pragma unroll
@@ -1443,7 +1496,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 float mx = neg_scale ? fminf(fminf(mx4[0], mx4[1]), fminf(mx4[2], mx4[3]))
                                      : fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
                 mx *= c1;
-                if (kSparse && valid <= 0) mx = 0.0f;       // (a finite reference for rows without any key)
+                if (kSparse && j == 0 && valid <= 0) mx = 0.0f;       // (a finite reference for rows without any key)
 
                 if (kGroups == 2) {
                     // The decision of tile g - 1 (the other group's) comes first, also across items: the exchange
@@ -1543,9 +1596,16 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     uint64_t rs2[2] = {0ull, 0ull};
 #pragma unroll
                     for (int c = 0; c < kBN; c += 2) {
-                        float x0, x1;
-                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), c1c1, negm), x0, x1);
-                        const float p0 = ex2f(x0), p1 = ex2f(x1);
+                        const uint64_t x2 = fma_f32x2(pack_f32x2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), c1c1, negm);
+                        float p0, p1;
+                        if ((c >> 1) % 8 < kPolyPairs) {
+                            exp2_poly_pair(x2, p0, p1);
+                        } else {
+                            float x0, x1;
+                            unpack_f32x2(x2, x0, x1);
+                            p0 = ex2f(x0);
+                            p1 = ex2f(x1);
+                        }
                         const uint64_t p2 = pack_f32x2(p0, p1);
                         ls2[(c >> 1) & 1] = add_f32x2(ls2[(c >> 1) & 1], p2);
                         pk_p[c >> 1] = pack_bf16(p0, p1);
@@ -1598,11 +1658,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 const bool has_next = n_items - item > item_stride;
                 const int next_start = (ring_slot + 2 * (n_kv % kSlots) + (it > 0 ? kRingStage : 0)) % kSlots;
                 int lead = n_kv;                                  // key tiles of the next item
-                if (kSparse && has_next) {
-                    Walk wk_next = wk;
-                    walk_step(wk_next);
-                    lead = item_of(wk_next).n_kv;
-                }
+                if (kSparse && has_next) lead = item_of(wk_next).n_kv;
                 stage_slot_o = has_next ? (next_start + min(kBufs, lead)) % kSlots : next_start;
                 ring_slot = next_start;
             }

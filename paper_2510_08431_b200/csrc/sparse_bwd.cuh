@@ -9,15 +9,20 @@
 // That is seven products per pair of blocks where a single pass with atomics on dQ needs five; with 128 x 128 blocks the
 // two passes take 7 x 512 tensor cycles per pair at D = 128.
 //
-// 384 threads: warp 0 issues the MMAs, warp 1 the TMA loads, warps 4..11 work on the scores: warp w owns the rows (lanes)
-// 32 (w % 4) .. + 31 and the columns 64 ((w - 4) / 4) .. + 63 of every 128 x 128 score tile.
+// 512 threads: warp 0 (kDq: and warp 2) issues the MMAs, warp 1 the TMA loads, warps 4..11 work on the scores, warps 12..15 write finished
+// accumulators out (a thread's row is 32 separate sectors away from its neighbour's: the stores keep the load/store unit
+// busy for some 2000 cycles, during which the others are in the next item).
 //
 // Order of work, kDkv (tensor memory: dV, dK, one buffer for S, one for dP, 512 columns at D = 128): P^T overwrites S and
 // dS^T overwrites dP, and the MMAs of tile j + 1 are queued behind those that read them,
 //     dV += P_j dO_j, S_(j+1) = K Q_(j+1)^T   |   dK += dS_j Q_j, dP_(j+1) = V dO_(j+1)^T
 // so the exponentials of tile j + 1 run beside dK_j and dP_(j+1), and its dS beside dV_(j+1) and S_(j+2).
-// kDq has no P operand and one accumulator: three score buffers in turn (matrix 2 j is S_j, 2 j + 1 is dP_j, matrix m is in
+// kDq has no P operand and one accumulator: three score buffers in turn (matrix 2 T is S_T, 2 T + 1 is dP_T, matrix m is in
 // buffer m % 3) let S run two tiles ahead.
+// CTAs are persistent, one per SM, and draw their items (stationary blocks) from a counter: lists differ in length.  Tiles
+// are numbered T = 0, 1, ... over all items of a CTA and run on without a break: the first score MMAs of an item go out
+// with the last value MMAs of the one before, and all that an item boundary costs is the hand-over of the accumulators
+// (with one CTA per item a boundary cost about 15 thousand cycles at D = 128, as much as six tiles).
 #pragma once
 
 #include "attn_jvp_kernel.cuh"
@@ -25,20 +30,29 @@
 namespace attn_jvp {
 
 constexpr int kBwdBlock = 128;
-constexpr int kBwdThreads = 384;
-constexpr int kBwdComputeWarps = 8;
+constexpr int kBwdThreads = 512;
+constexpr int kBwdComputeWarps = 8, kBwdEpilogueWarps = 4;
+constexpr int kBwdRegsLight = 64, kBwdRegsCompute = 200, kBwdRegsEpilogue = 48;      // 128 (64 + 200 + 200 + 48) = 65536
+constexpr int kItemRing = 4;                 // items known ahead: the score MMAs are at most two items ahead of the values
+constexpr int kMmaWarp2 = 2;
 constexpr int kBwdY1 = 3, kBwdY2 = 2;        // shared-memory buffers of the two streaming tensors
+#ifndef POLY_B
+#define POLY_B 2
+#endif
+constexpr int kBwdPoly = POLY_B;             // of 8 pairs of exponentials, how many take the FMA pipe
 
 struct SparseBwdArgs {
     const int* list;            // kDkv: [B][H][n_k][n_q] query blocks of a key block; kDq: [B][H][n_q][n_k]
     const int* tiles;           // their lengths in 64-token tiles
-    const float2* rows;         // [B][H][n_q * 128]: {LSE log2 e (+inf: the row has no probability), delta}
+    const float* rows;          // [B][H][n_q][2][128]: per block of queries LSE log2 e (+inf: no probability), then delta
     __nv_bfloat16* out1;        // kDkv: dV, kDq: dQ        [B][L][H][D]
     __nv_bfloat16* out2;        // kDkv: dK
     int* host_status;
-    int H, n_items_per_head, list_stride;
+    int* counter;               // items handed out beyond the first one of every CTA; starts at 0
+    int H, n_items, n_items_per_head, list_stride;
     int L_own, L_other;         // tokens on the stationary / streaming side
     int n_q;                    // query blocks
+    int wide_out;               // out1, out2 are 32-byte aligned
     float scale, scale_log2;
 };
 
@@ -49,29 +63,59 @@ struct SparseBwdPlan {
     static constexpr int kX = 0;
     static constexpr int kY1Off = 2 * kTile;
     static constexpr int kY2Off = kY1Off + kBwdY1 * kTile;
-    static constexpr int kRowsOff = kY2Off + kBwdY2 * kTile;     // kDkv: {LSE, delta} of two streaming tiles
+    static constexpr int kRowsOff = kY2Off + kBwdY2 * kTile;     // kDkv: LSE and delta of two streaming tiles
     static constexpr int kRowsBytes = kBwdBlock * 8;
     static constexpr int kDynBytes = kRowsOff + 2 * kRowsBytes;  // 226 KB at D = 128
 };
 
-// {LSE log2 e, delta} per query row, padded to whole blocks.  Rows behind the last query and rows without any key get
-// LSE = +inf, which makes their P exactly 0.  One group of D / 8 threads per row; reads dO and O once.
+// What the two passes need beforehand.  Blocks below `row_blocks`: LSE log2 e and delta per query row, padded to whole
+// blocks; rows behind the last query and rows without any key get LSE = +inf, which makes their P exactly 0; a group of
+// D / 8 threads per row reads dO and O once.  The blocks after them: a warp per stationary block of either pass, which
+// writes zero gradients where its list is empty (the passes never see those).  Both passes' counters start at 0.
+struct SparseBwdPrep {
+    const uint4 *o, *d_o;
+    const float* lse;
+    float* rows;
+    const int *q_tiles, *k_tiles;
+    __nv_bfloat16 *dq, *dk, *dv;
+    int* counters;
+    int B, H, Lq, Lk, n_q, n_k, row_blocks;
+};
 template <int D>
 __global__ void __launch_bounds__(256)
-sparse_bwd_rows_kernel(const uint4* __restrict__ o, const uint4* __restrict__ d_o, const float* __restrict__ lse,
-                       float2* __restrict__ rows, int B, int H, int Lq, int padded) {
+sparse_bwd_prep_kernel(const SparseBwdPrep p) {
     constexpr int kLanes = D / 8;
-    const long long n = static_cast<long long>(B) * padded * H;
+    if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
+        const int lane = threadIdx.x & 31;
+        int item = (blockIdx.x - p.row_blocks) * 8 + (threadIdx.x >> 5);
+        const int q_items = p.B * p.H * p.n_q;
+        const bool keys = item >= q_items;
+        if (keys) item -= q_items;
+        const int per_head = keys ? p.n_k : p.n_q, L = keys ? p.Lk : p.Lq;
+        if (item >= p.B * p.H * per_head || (keys ? p.k_tiles : p.q_tiles)[item] > 0) return;
+        const int bh = item / per_head, blk = item - bh * per_head, b = bh / p.H, h = bh - b * p.H;
+        for (int e = lane; e < kBwdBlock * kLanes; e += 32) {
+            const int r = blk * kBwdBlock + e / kLanes;
+            if (r >= L) break;
+            const long long at = ((static_cast<long long>(b) * L + r) * p.H + h) * D + (e % kLanes) * 8;
+            *reinterpret_cast<uint4*>((keys ? p.dk : p.dq) + at) = make_uint4(0u, 0u, 0u, 0u);
+            if (keys) *reinterpret_cast<uint4*>(p.dv + at) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        return;
+    }
+    if (blockIdx.x == 0 && threadIdx.x < 2) p.counters[threadIdx.x] = 0;
+    const int padded = p.n_q * kBwdBlock;
+    const long long n = static_cast<long long>(p.B) * padded * p.H;
     const long long r = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) / kLanes;
     const int sub = threadIdx.x % kLanes;
     // (row order [B][padded][H], that of the tensors)
-    const long long bl = min(r, n - 1) / H;
-    const int h = static_cast<int>(min(r, n - 1) - bl * H);
+    const long long bl = min(r, n - 1) / p.H;
+    const int h = static_cast<int>(min(r, n - 1) - bl * p.H);
     const int b = static_cast<int>(bl / padded), l = static_cast<int>(bl - static_cast<long long>(b) * padded);
     float sum = 0.0f;
-    if (l < Lq) {
-        const long long at = ((static_cast<long long>(b) * Lq + l) * H + h) * kLanes + sub;
-        const uint4 x = __ldg(o + at), y = __ldg(d_o + at);
+    if (l < p.Lq) {
+        const long long at = ((static_cast<long long>(b) * p.Lq + l) * p.H + h) * kLanes + sub;
+        const uint4 x = __ldg(p.o + at), y = __ldg(p.d_o + at);
         const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -82,13 +126,15 @@ sparse_bwd_rows_kernel(const uint4* __restrict__ o, const uint4* __restrict__ d_
 #pragma unroll
     for (int m = kLanes / 2; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
     if (sub == 0 && r < n) {
-        const long long bh = static_cast<long long>(b) * H + h;
+        const long long bh = static_cast<long long>(b) * p.H + h;
         float ls = INFINITY;
-        if (l < Lq) {
-            ls = lse[bh * Lq + l] * 1.4426950408889634f;
+        if (l < p.Lq) {
+            ls = p.lse[bh * p.Lq + l] * 1.4426950408889634f;
             if (ls == -INFINITY) ls = INFINITY;
         }
-        rows[bh * padded + l] = make_float2(ls, sum);
+        float* out = p.rows + 2 * bh * padded + (l / kBwdBlock) * (2 * kBwdBlock) + l % kBwdBlock;
+        out[0] = ls;
+        out[kBwdBlock] = sum;
     }
 }
 
@@ -102,6 +148,25 @@ __device__ __forceinline__ float4 ld_shared_f4(uint32_t a) {
     return v;
 }
 
+// mbar_wait_warp() of a warp that has time: it looks again every 64 ns or so.  A dozen warps that look all the time take issue
+// slots (and shared memory cycles, which the MMAs use in full) from the warp that feeds the tensor pipe: with a tight loop
+// here kDkv took 289 us where it takes 235.
+__device__ __forceinline__ bool mbar_wait_patient(uint32_t bar, uint32_t parity, const AbortState& st) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    const unsigned long long t0 = globaltimer_ns();
+    for (uint32_t it = 1;; ++it) {
+        __nanosleep(64);
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+        if ((it & 255u) == 0u) {
+            if (__any_sync(0xffffffffu, *st.cta_flag != 0)) return false;
+            if (__any_sync(0xffffffffu, globaltimer_ns() - t0 > kWaitLimitNs)) {
+                report_device_error(st, 10);                     // ATTN_JVP_ERR_DEVICE_TIMEOUT
+                return false;
+            }
+        }
+    }
+}
+
 template <int D, bool kDkv>
 __global__ void __launch_bounds__(kBwdThreads, 1)
 sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constant__ CUtensorMap tm_x2,
@@ -113,41 +178,30 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
     constexpr int kAcc2 = D;                                     // kDkv: first column of dK
     constexpr int kScore0 = kDkv ? 2 * D : D;                    // first column of score buffer 0
     constexpr int kBufs = kDkv ? 2 : 3;
+    constexpr int kTileWarps = kDkv ? kBwdComputeWarps : kBwdComputeWarps / 2;      // warps that work on one tile
     static_assert(kScore0 + kBufs * 128 <= kTmemCols, "tensor memory");
 
     extern __shared__ __align__(1024) uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bar_x, bar_y1_full[kBwdY1], bar_y1_empty[kBwdY1], bar_y2_full[kBwdY2], bar_y2_empty[kBwdY2];
-    __shared__ __align__(8) uint64_t bar_rows_full[2];           // kDkv: {LSE, delta} of the tile
-    // per tile, two barriers in turn (tile j: [j & 1], phase (j >> 1) & 1): kDq's S and dP run up to two tiles ahead of the
+    __shared__ __align__(8) uint64_t bar_x1_full, bar_x2_full;   // the item's stationary tiles are there, phase it & 1
+    __shared__ __align__(8) uint64_t bar_x1_free, bar_x2_free;   // ... and its last S / dP is complete: they may be replaced
+    __shared__ __align__(8) uint64_t bar_y1_full[kBwdY1], bar_y1_empty[kBwdY1], bar_y2_full[kBwdY2], bar_y2_empty[kBwdY2];
+    __shared__ __align__(8) uint64_t bar_rows_full[2];           // kDkv: LSE and delta of the tile
+    // per tile, two barriers in turn (tile T: [T & 1], phase (T >> 1) & 1): kDq's S and dP run up to two tiles ahead of the
     // warps that wait for them, which a single barrier's parity could not tell apart
-    __shared__ __align__(8) uint64_t bar_s_full[2], bar_dp_full[2];      // S_j / dP_j complete
-    __shared__ __align__(8) uint64_t bar_p_ready[2];             // kDkv: P_j is in tensor memory; kDq: S_j has been read
-    __shared__ __align__(8) uint64_t bar_ds_ready[2];            // dS_j is in tensor memory
-    __shared__ __align__(8) uint64_t bar_done, bar_drain;
+    __shared__ __align__(8) uint64_t bar_s_full[2], bar_dp_full[2];      // S_T / dP_T complete
+    __shared__ __align__(8) uint64_t bar_p_ready[2];             // kDkv: P_T is in tensor memory, all of it; kDq: S_T has been read
+    __shared__ __align__(8) uint64_t bar_p_half[2];              // kDkv: the first half of every thread's part of P_T is
+    __shared__ __align__(8) uint64_t bar_ds_ready[2];            // dS_T is in tensor memory
+    __shared__ __align__(8) uint64_t bar_done;                   // the item's accumulators are complete, phase it & 1 ...
+    __shared__ __align__(8) uint64_t bar_acc_free;               // ... and have been read: the next item may overwrite them
+    __shared__ __align__(8) uint64_t bar_item_full[kItemRing], bar_item_empty[kItemRing];
+    __shared__ __align__(8) uint64_t bar_drain, bar_drain2;
+    __shared__ int4 items[kItemRing];                            // {item (-1: no more), streaming blocks, the last of them, -}
     __shared__ uint32_t tmem_base_smem;
     __shared__ int cta_abort;
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int lane = threadIdx.x & 31;
-    const int item = blockIdx.x;
-    const int bh = item / args.n_items_per_head, blk = item - bh * args.n_items_per_head;
-    const int b = bh / args.H, h = bh - b * args.H;
-    const int own0 = blk * kBwdBlock;
-    const int* list = args.list + static_cast<long long>(item) * args.list_stride;
-    const int n = min((args.tiles[item] + 1) >> 1, args.list_stride);     // streaming blocks of this item
-
-    if (n <= 0) {
-        // nothing was kept: the gradients are zero
-        for (int e = threadIdx.x; e < kBwdBlock * (D / 8); e += kBwdThreads) {
-            const int r = own0 + e / (D / 8), c = (e % (D / 8)) * 8;
-            if (r < args.L_own) {
-                const long long at = ((static_cast<long long>(b) * args.L_own + r) * args.H + h) * D + c;
-                *reinterpret_cast<uint4*>(args.out1 + at) = make_uint4(0u, 0u, 0u, 0u);
-                if (kDkv) *reinterpret_cast<uint4*>(args.out2 + at) = make_uint4(0u, 0u, 0u, 0u);
-            }
-        }
-        return;
-    }
 
     if (threadIdx.x == 0) cta_abort = *reinterpret_cast<volatile int*>(&g_abort_flag);
     __syncthreads();
@@ -163,18 +217,28 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
         }
     }
     if (threadIdx.x == 0) {
-        mbar_init(smem_u32(&bar_x), 1);
+        mbar_init(smem_u32(&bar_x1_full), 1);
+        mbar_init(smem_u32(&bar_x2_full), 1);
+        mbar_init(smem_u32(&bar_x1_free), 1);
+        mbar_init(smem_u32(&bar_x2_free), 1);
         for (int i = 0; i < kBwdY1; ++i) { mbar_init(smem_u32(&bar_y1_full[i]), 1); mbar_init(smem_u32(&bar_y1_empty[i]), 1); }
         for (int i = 0; i < kBwdY2; ++i) { mbar_init(smem_u32(&bar_y2_full[i]), 1); mbar_init(smem_u32(&bar_y2_empty[i]), 1); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&bar_rows_full[i]), 1);
             mbar_init(smem_u32(&bar_s_full[i]), 1);
             mbar_init(smem_u32(&bar_dp_full[i]), 1);
-            mbar_init(smem_u32(&bar_p_ready[i]), kBwdComputeWarps);
-            mbar_init(smem_u32(&bar_ds_ready[i]), kBwdComputeWarps);
+            mbar_init(smem_u32(&bar_p_ready[i]), kTileWarps);
+            mbar_init(smem_u32(&bar_p_half[i]), kTileWarps);
+            mbar_init(smem_u32(&bar_ds_ready[i]), kTileWarps);
+        }
+        for (int i = 0; i < kItemRing; ++i) {
+            mbar_init(smem_u32(&bar_item_full[i]), 1);
+            mbar_init(smem_u32(&bar_item_empty[i]), (kDkv ? 1 : 2) + kBwdComputeWarps + kBwdEpilogueWarps);
         }
         mbar_init(smem_u32(&bar_done), 1);
+        mbar_init(smem_u32(&bar_acc_free), kBwdEpilogueWarps);
         mbar_init(smem_u32(&bar_drain), 1);
+        mbar_init(smem_u32(&bar_drain2), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == kMmaWarp) {
@@ -187,58 +251,98 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_base_smem);
 
+    // entry `it` of the CTA's sequence of items (it = 0, 1, ...); whole warp
+    auto item_at = [&](int it, int4& entry) -> bool {
+        if (!mbar_wait_warp(smem_u32(&bar_item_full[it % kItemRing]), static_cast<uint32_t>(it / kItemRing) & 1u, abort_state)) return false;
+        entry = *const_cast<const int4*>(&items[it % kItemRing]);
+        return true;
+    };
+
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLightWarps));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBwdRegsLight));
         if (warp == kProducerWarp && lane == 0) {
-            // ---- TMA producer: X once, then Y1_0, Y2_0, Y1_1, ... in the order the MMAs take them ----
+            // ---- TMA producer and scheduler: per item X1, Y1, X2, Y2 in the order the MMAs take them, then Y1_1, Y2_1, ... ----
             prefetch_tensormap(&tm_x1);
             prefetch_tensormap(&tm_x2);
             prefetch_tensormap(&tm_y1);
             prefetch_tensormap(&tm_y2);
-            auto load_tile = [&](uint32_t dst, const CUtensorMap* map, uint32_t bar, int row0) {
-#pragma unroll
-                for (int hf = 0; hf < kHalves; ++hf) tma_load_4d(dst + hf * Plan::kHalf, map, bar, hf * 64, h, row0, b);
-            };
-            mbar_arrive_expect_tx(smem_u32(&bar_x), 2 * Plan::kTile);
-            load_tile(smem + Plan::kX, &tm_x1, smem_u32(&bar_x), own0);
-            load_tile(smem + Plan::kX + Plan::kTile, &tm_x2, smem_u32(&bar_x), own0);
-            const float2* rows = args.rows + static_cast<long long>(bh) * args.n_q * kBwdBlock;
             bool ok = true;
-            int s1 = 0, s2 = 0;
-            uint32_t ph1 = 0, ph2 = 0;                           // parity of the buffers' current lap
-            for (int j = 0; j < n; ++j) {
-                const int other = __ldg(list + j);
-                const int row0 = other * kBwdBlock;
-                if (j >= kBwdY1) ok = mbar_wait(smem_u32(&bar_y1_empty[s1]), ph1 ^ 1u, abort_state);
-                if (!ok) break;
-                mbar_arrive_expect_tx(smem_u32(&bar_y1_full[s1]), Plan::kTile);
-                load_tile(smem + Plan::kY1Off + s1 * Plan::kTile, &tm_y1, smem_u32(&bar_y1_full[s1]), row0);
-                if (j >= kBwdY2) ok = mbar_wait(smem_u32(&bar_y2_empty[s2]), ph2 ^ 1u, abort_state);
-                if (!ok) break;
-                mbar_arrive_expect_tx(smem_u32(&bar_y2_full[s2]), Plan::kTile);
-                load_tile(smem + Plan::kY2Off + s2 * Plan::kTile, &tm_y2, smem_u32(&bar_y2_full[s2]), row0);
-                if (kDkv) {
-                    // Two sets of row constants: the one of tile j - 2 is free once that tile's dS has been formed, which
-                    // the release of its Q tile (after dK += dS Q) says
-                    if (j >= 2) {
-                        const int t = j - 2;
-                        ok = mbar_wait(smem_u32(&bar_y1_empty[t % kBwdY1]), static_cast<uint32_t>(t / kBwdY1) & 1u, abort_state);
-                        if (!ok) break;
-                    }
-                    const uint32_t rb = smem_u32(&bar_rows_full[j & 1]);
-                    mbar_arrive_expect_tx(rb, Plan::kRowsBytes);
-                    bulk_load(smem + Plan::kRowsOff + (j & 1) * Plan::kRowsBytes, rows + row0, Plan::kRowsBytes, rb);
+            int T = 0, s1 = 0, s2 = 0;
+            uint32_t ph1 = 0, ph2 = 0;                           // parity of the Y buffers' current lap
+            // the next item that keeps anything, from number `item` on; -1: none.  n: its streaming blocks
+            auto next_item = [&](int item, int& n) -> int {
+                for (;; item = static_cast<int>(gridDim.x) + atomicAdd(args.counter, 1)) {
+                    if (item >= args.n_items) return -1;
+                    n = min((__ldg(args.tiles + item) + 1) >> 1, args.list_stride);
+                    if (n > 0) return item;
                 }
-                if (++s1 == kBwdY1) { s1 = 0; ph1 ^= 1u; }
-                if (++s2 == kBwdY2) { s2 = 0; ph2 ^= 1u; }
+            };
+            int n = 0, n_next = 0;
+            int item = next_item(blockIdx.x, n);
+            for (int it = 0; ok; ++it) {
+                const int e = it % kItemRing;
+                if (it >= kItemRing) ok = mbar_wait(smem_u32(&bar_item_empty[e]), (static_cast<uint32_t>(it / kItemRing) & 1u) ^ 1u, abort_state);
+                if (!ok) break;
+                const int* list = args.list + static_cast<long long>(max(item, 0)) * args.list_stride;
+                items[e] = make_int4(item, n, item >= 0 ? __ldg(list + n - 1) : 0, 0);
+                mbar_arrive(smem_u32(&bar_item_full[e]));
+                if (item < 0) break;
+                const int bh = item / args.n_items_per_head, own0 = (item - bh * args.n_items_per_head) * kBwdBlock;
+                const int b = bh / args.H, h = bh - b * args.H;
+                auto load_tile = [&](uint32_t dst, const CUtensorMap* map, uint32_t bar, int row0) {
+                    mbar_arrive_expect_tx(bar, Plan::kTile);
+#pragma unroll
+                    for (int hf = 0; hf < kHalves; ++hf) tma_load_4d(dst + hf * Plan::kHalf, map, bar, hf * 64, h, row0, b);
+                };
+                const float* rows = args.rows + static_cast<long long>(bh) * args.n_q * (2 * kBwdBlock);
+                int next = -1;
+                for (int j = 0; j < n; ++j, ++T) {
+                    const int row0 = __ldg(list + j) * kBwdBlock;
+                    if (j == 0) {
+                        if (it > 0) ok = mbar_wait(smem_u32(&bar_x1_free), (it - 1) & 1, abort_state);
+                        if (!ok) break;
+                        load_tile(smem + Plan::kX, &tm_x1, smem_u32(&bar_x1_full), own0);
+                    }
+                    if (T >= kBwdY1) ok = mbar_wait(smem_u32(&bar_y1_empty[s1]), ph1 ^ 1u, abort_state);
+                    if (!ok) break;
+                    load_tile(smem + Plan::kY1Off + s1 * Plan::kTile, &tm_y1, smem_u32(&bar_y1_full[s1]), row0);
+                    if (j == 0) {
+                        if (it > 0) ok = mbar_wait(smem_u32(&bar_x2_free), (it - 1) & 1, abort_state);
+                        if (!ok) break;
+                        load_tile(smem + Plan::kX + Plan::kTile, &tm_x2, smem_u32(&bar_x2_full), own0);
+                    }
+                    if (T >= kBwdY2) ok = mbar_wait(smem_u32(&bar_y2_empty[s2]), ph2 ^ 1u, abort_state);
+                    if (!ok) break;
+                    load_tile(smem + Plan::kY2Off + s2 * Plan::kTile, &tm_y2, smem_u32(&bar_y2_full[s2]), row0);
+                    if (kDkv) {
+                        // Two sets of row constants: the one of tile T - 2 is free once that tile's dS has been formed, which
+                        // the release of its Q tile (after dK += dS Q) says
+                        if (T >= 2) {
+                            const int t = T - 2;
+                            ok = mbar_wait(smem_u32(&bar_y1_empty[t % kBwdY1]), static_cast<uint32_t>(t / kBwdY1) & 1u, abort_state);
+                            if (!ok) break;
+                        }
+                        const uint32_t rb = smem_u32(&bar_rows_full[T & 1]);
+                        mbar_arrive_expect_tx(rb, Plan::kRowsBytes);
+                        bulk_load(smem + Plan::kRowsOff + (T & 1) * Plan::kRowsBytes, rows + 2 * row0, Plan::kRowsBytes, rb);
+                    }
+                    if (++s1 == kBwdY1) { s1 = 0; ph1 ^= 1u; }
+                    if (++s2 == kBwdY2) { s2 = 0; ph2 ^= 1u; }
+                    if (j == min(n - 1, 2)) next = next_item(static_cast<int>(gridDim.x) + atomicAdd(args.counter, 1), n_next);
+                }
+                item = next;
+                n = n_next;
             }
             if (!ok) {
                 // give up: let the copies in flight land (bounded) before the CTA exits
                 const unsigned long long t0 = globaltimer_ns();
                 while (globaltimer_ns() - t0 < 100000000ull) {}
             }
-        } else if (warp == kMmaWarp) {
-            // ---- MMA issuer (whole warp in lock step, one elected lane's instructions take effect) ----
+        } else if (warp == kMmaWarp || (!kDkv && warp == kMmaWarp2)) {
+            // ---- MMA issuers (each warp in lock step, one elected lane's instructions take effect).  kDkv: one warp, so that
+            // dK and dP stand behind dV and S, for which the exponentials of the next tile wait (two warps, one for each half of
+            // the line above: 465 thousand cycles instead of 364 for 128 tiles).  kDq: the second warp issues dP (one warp:
+            // 10 % slower; it cannot issue fast enough beside the warps that work on scores). ----
             constexpr uint32_t kIdescS = make_idesc(kBwdBlock, false);
             constexpr uint32_t kIdescV = make_idesc(D, true);
             const uint32_t pred = elect_one() ? 1u : 0u;
@@ -253,201 +357,302 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
                     mma_ss_if<true, false>(pred, d, make_desc(x_lo + koff(k)), make_desc(y_lo + koff(k)), kIdescS);
             };
             // accumulator += (bf16 128 x 128 in a score buffer) y; columns 0..63 of it are at its start, 64..127 64 columns on
-            auto values = [&](uint32_t d, uint32_t a, uint32_t y, bool first) {
+            // (`part`: 0 = all of it, 1 / 2 = the first / second 32 columns of each 64)
+            auto values = [&](uint32_t d, uint32_t a, uint32_t y, bool first, int part) {
                 const uint32_t y_lo = make_desc_lo(y, Plan::kHalf);
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < 8; ++k) {
+                    if (part != 0 && (k % 4) / 2 != part - 1) continue;
                     mma_ts_if<false>(pred, d, a + (k / 4) * 64 + (k % 4) * 8, make_desc(y_lo + k * (2048 >> 4)), kIdescV,
                                      (first && k == 0) ? 0u : 1u);
+                }
             };
-            auto y1 = [&](int j) { return smem + Plan::kY1Off + (j % kBwdY1) * Plan::kTile; };
-            auto y2 = [&](int j) { return smem + Plan::kY2Off + (j % kBwdY2) * Plan::kTile; };
-            auto y1_full = [&](int j) { return mbar_wait_warp(smem_u32(&bar_y1_full[j % kBwdY1]), static_cast<uint32_t>(j / kBwdY1) & 1u, abort_state); };
-            auto y2_full = [&](int j) { return mbar_wait_warp(smem_u32(&bar_y2_full[j % kBwdY2]), static_cast<uint32_t>(j / kBwdY2) & 1u, abort_state); };
+            auto y1 = [&](int T) { return smem + Plan::kY1Off + (T % kBwdY1) * Plan::kTile; };
+            auto y2 = [&](int T) { return smem + Plan::kY2Off + (T % kBwdY2) * Plan::kTile; };
+            auto wait = [&](uint64_t& bar, uint32_t parity) { return mbar_wait_warp(smem_u32(&bar), parity & 1u, abort_state); };
             auto commit = [&](uint64_t& bar) { tc_commit_if<false>(pred, smem_u32(&bar)); };
             auto buf = [&](int m) { return tmem + kScore0 + (m % kBufs) * 128; };
-            bool ok = mbar_wait_warp(smem_u32(&bar_x), 0, abort_state) && y1_full(0);
-            if (ok) {
-                scores(buf(0), x1_lo, y1(0));
-                commit(bar_s_full[0]);
-                ok = y2_full(0);
-            }
-            if (ok) {
-                scores(buf(1), x2_lo, y2(0));
-                commit(bar_dp_full[0]);
-                if (!kDkv) commit(bar_y2_empty[0]);
-            }
-            if (kDkv) {
-                for (int j = 0; ok && j < n; ++j) {
-                    ok = mbar_wait_warp(smem_u32(&bar_p_ready[j & 1]), (j >> 1) & 1, abort_state);
-                    if (!ok) break;
+            // A place in the stream of tiles: tile T is number j of the n of item `it`; n = 0: the stream has ended.
+            struct Place { int it, n, j, T; };
+            bool ok = true;
+            auto next_place = [&](Place& c) {
+                ++c.T;
+                if (++c.j < c.n) return;
+                int4 entry;
+                ok = item_at(++c.it, entry);
+                // (through a reduction, whose result lies in a uniform register: with it everything that the loop below derives
+                // from it does, addresses and descriptors among them, and that is where the MMAs take them from)
+                c.n = static_cast<int>(__reduce_max_sync(0xffffffffu, ok && entry.x >= 0 ? entry.y : 0));
+                c.j = 0;
+            };
+            // S / dP of the tile at a place, and on to the next
+            auto issue_s = [&](Place& c) {
+                if (!ok || c.n == 0) return;
+                if (c.j == 0) ok = wait(bar_x1_full, c.it);
+                if (ok) ok = wait(bar_y1_full[c.T % kBwdY1], c.T / kBwdY1);
+                if (!ok) return;
+                scores(buf(kDkv ? 0 : 2 * c.T), x1_lo, y1(c.T));
+                commit(bar_s_full[c.T & 1]);
+                if (c.j + 1 == c.n) commit(bar_x1_free);
+                next_place(c);
+            };
+            auto issue_dp = [&](Place& c) {
+                if (!ok || c.n == 0) return;
+                if (c.j == 0) ok = wait(bar_x2_full, c.it);
+                if (ok) ok = wait(bar_y2_full[c.T % kBwdY2], c.T / kBwdY2);
+                if (ok && !kDkv && c.T > 0) {
+                    // goes where S of the tile before was, once that has been read
+                    ok = wait(bar_p_ready[(c.T - 1) & 1], (c.T - 1) >> 1);
                     tc_fence_after();
-                    values(tmem, buf(0), y2(j), j == 0);
-                    commit(bar_y2_empty[j % kBwdY2]);
-                    if (j + 1 < n) {
-                        ok = y1_full(j + 1);
-                        if (!ok) break;
-                        scores(buf(0), x1_lo, y1(j + 1));
-                        commit(bar_s_full[(j + 1) & 1]);
-                    }
-                    ok = mbar_wait_warp(smem_u32(&bar_ds_ready[j & 1]), (j >> 1) & 1, abort_state);
-                    if (!ok) break;
-                    tc_fence_after();
-                    values(tmem + kAcc2, buf(1), y1(j), j == 0);
-                    commit(bar_y1_empty[j % kBwdY1]);
-                    if (j + 1 < n) {
-                        ok = y2_full(j + 1);
-                        if (!ok) break;
-                        scores(buf(1), x2_lo, y2(j + 1));
-                        commit(bar_dp_full[(j + 1) & 1]);
-                    }
                 }
+                if (!ok) return;
+                scores(buf(kDkv ? 1 : 2 * c.T + 1), x2_lo, y2(c.T));
+                commit(bar_dp_full[c.T & 1]);
+                if (!kDkv) commit(bar_y2_empty[c.T % kBwdY2]);
+                if (c.j + 1 == c.n) commit(bar_x2_free);
+                next_place(c);
+            };
+            Place s{-1, 0, 0, -1};
+            next_place(s);
+            Place dp = s, v = s;
+            if (!kDkv && warp == kMmaWarp2) {
+                while (ok && dp.n > 0) {
+                    const int it = dp.it;
+                    issue_dp(dp);
+                    if (dp.it != it && lane == 0) mbar_arrive(smem_u32(&bar_item_empty[it % kItemRing]));
+                }
+                v.n = 0;
             } else {
-                if (ok && n > 1) {
-                    ok = y1_full(1);
-                    if (ok) {
-                        scores(buf(2), x1_lo, y1(1));
-                        commit(bar_s_full[1]);
-                    }
-                }
-                for (int j = 0; ok && j < n; ++j) {
-                    if (j + 1 < n) {
-                        // dP_(j+1) goes where S_j was, once that has been read
-                        ok = y2_full(j + 1) && mbar_wait_warp(smem_u32(&bar_p_ready[j & 1]), (j >> 1) & 1, abort_state);
-                        if (!ok) break;
-                        tc_fence_after();
-                        scores(buf(2 * j + 3), x2_lo, y2(j + 1));
-                        commit(bar_dp_full[(j + 1) & 1]);
-                        commit(bar_y2_empty[(j + 1) % kBwdY2]);
-                    }
-                    ok = mbar_wait_warp(smem_u32(&bar_ds_ready[j & 1]), (j >> 1) & 1, abort_state);
+                issue_s(s);
+                if (kDkv) issue_dp(dp);
+                else issue_s(s);
+            }
+            while (ok && v.n > 0) {
+                const bool first = v.j == 0, last = v.j + 1 == v.n;
+                // the first values of an item overwrite the accumulators: the epilogue of the one before must have read them
+                auto values_ready = [&](uint64_t& bar) {
+                    ok = wait(bar, v.T >> 1);
+                    if (ok && first && v.it > 0) ok = wait(bar_acc_free, v.it - 1);
+                    if (ok) tc_fence_after();
+                    return ok;
+                };
+                if (kDkv) {
+                    if (!values_ready(bar_p_half[v.T & 1])) break;
+                    values(tmem, buf(0), y2(v.T), first, 1);
+                    ok = wait(bar_p_ready[v.T & 1], v.T >> 1);
                     if (!ok) break;
                     tc_fence_after();
-                    values(tmem, buf(2 * j + 1), y1(j), j == 0);
-                    commit(bar_y1_empty[j % kBwdY1]);
-                    if (j + 2 < n) {
-                        ok = y1_full(j + 2);
-                        if (!ok) break;
-                        scores(buf(2 * j + 4), x1_lo, y1(j + 2));     // (the buffer that dS_j is read from by the MMAs before it)
-                        commit(bar_s_full[j & 1]);
-                    }
+                    values(tmem, buf(0), y2(v.T), false, 2);
+                    commit(bar_y2_empty[v.T % kBwdY2]);
+                    issue_s(s);                                  // (into the buffer that P has just been read from)
+                    if (!ok) break;
+                    ok = wait(bar_ds_ready[v.T & 1], v.T >> 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    values(tmem + kAcc2, buf(1), y1(v.T), first, 0);
+                    commit(bar_y1_empty[v.T % kBwdY1]);
+                    if (last) commit(bar_done);
+                    issue_dp(dp);
+                } else {
+                    if (!values_ready(bar_ds_ready[v.T & 1])) break;
+                    values(tmem, buf(2 * v.T + 1), y1(v.T), first, 0);
+                    commit(bar_y1_empty[v.T % kBwdY1]);
+                    if (last) commit(bar_done);
+                    issue_s(s);                                  // (into the buffer that dS has just been read from)
                 }
+                if (!ok) break;
+                if (last && lane == 0) mbar_arrive(smem_u32(&bar_item_empty[v.it % kItemRing]));
+                next_place(v);
             }
-            if (ok) commit(bar_done);
             if (!ok) {
                 // give up: wait (bounded) until the tensor core has drained what was issued
-                commit(bar_drain);
+                uint64_t& drain = warp == kMmaWarp ? bar_drain : bar_drain2;
+                commit(drain);
                 const unsigned long long t0 = globaltimer_ns();
-                while (!mbar_try_wait(smem_u32(&bar_drain), 0) && globaltimer_ns() - t0 < 100000000ull) {}
+                while (!mbar_try_wait(smem_u32(&drain), 0) && globaltimer_ns() - t0 < 100000000ull) {}
             }
             __syncwarp();
         }
-    } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmaxWarps));
-        // ---- scores: this thread's row and 64 of its columns ----
-        const int quarter = warp & 3, col0 = ((warp - 4) >> 2) * 64;
+    } else if (warp < 4 + kBwdComputeWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kBwdRegsCompute));
+        // ---- scores.  Warp w owns rows 32 (w % 4) + lane (its lanes of tensor memory).  kDkv: both groups of four warps take
+        // every tile, 64 columns each (the exponentials of a tile stand between its S and everything after).  kDq: the groups
+        // take alternate tiles, all columns, so that one group's waits are covered by the other's exponentials. ----
+        const int quarter = warp & 3, group = (warp - 4) >> 2;
         const int row = quarter * 32 + lane;
         const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
         const float c1 = args.scale_log2;
-        float2 own = make_float2(0.0f, 0.0f);                    // kDq: the row's {LSE, delta}
-        if (!kDkv) own = __ldg(args.rows + (static_cast<long long>(bh) * args.n_q + blk) * kBwdBlock + row);
-        const int last_valid = args.L_other - (kDkv ? 0 : __ldg(list + n - 1) * kBwdBlock);   // kDq: keys of the last block
-        bool ok = true;
-        for (int j = 0; j < n; ++j) {
-            const uint32_t tm_s = tmem + lane_base + kScore0 + (kDkv ? 0 : ((2 * j) % kBufs) * 128) + col0;
-            const uint32_t tm_dp = tmem + lane_base + kScore0 + (kDkv ? 128 : ((2 * j + 1) % kBufs) * 128) + col0;
-            const uint32_t rows_smem = smem + Plan::kRowsOff + (j & 1) * Plan::kRowsBytes + col0 * 8;
-            uint32_t sv[64];
-            if (kDkv) ok = mbar_wait_warp(smem_u32(&bar_rows_full[j & 1]), (j >> 1) & 1, abort_state);
-            if (ok) ok = mbar_wait_warp(smem_u32(&bar_s_full[j & 1]), (j >> 1) & 1, abort_state);
-            if (!ok) break;
-            tc_fence_after();
-            TMEM_LD32(tm_s, sv, 0);
-            TMEM_LD32(tm_s + 32, sv, 32);
-            tc_wait_ld();
-            if (!kDkv) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bar_p_ready[j & 1]));
-            }
-            // P = 2^(S c1 - LSE log2 e), kept in fp32 for dS
-            float p[64];
-            if (kDkv) {
-                uint32_t pk[32];
+        const uint64_t c1c1 = pack_f32x2(c1, c1);
+        float own_lse = 0.0f, own_delta = 0.0f;                  // kDq: of the row
+        auto read_own = [&](int item) {                          // (rows of a query block: [LSE 128][delta 128])
+            if (kDkv || item < 0) return;
+            const float* own = args.rows + static_cast<long long>(item) * (2 * kBwdBlock) + row;
+            own_lse = __ldg(own);
+            own_delta = __ldg(own + kBwdBlock);
+        };
+        // P = 2^(S c1 - LSE log2 e) of 32 columns, kept in fp32 for dS; part of the exponentials on the FMA pipe
+        auto exps = [&](const uint32_t* sv, float* p, uint32_t lse_smem) {
 #pragma unroll
-                for (int c = 0; c < 64; c += 2) {
-                    const float4 r = ld_shared_f4(rows_smem + c * 8);     // LSE, delta of two queries
-                    p[c] = ex2f(fmaf(__uint_as_float(sv[c]), c1, -r.x));
-                    p[c + 1] = ex2f(fmaf(__uint_as_float(sv[c + 1]), c1, -r.z));
-                    pk[c >> 1] = pack_bf16(p[c], p[c + 1]);
+            for (int c = 0; c < 32; c += 4) {
+                float4 l = make_float4(own_lse, own_lse, own_lse, own_lse);
+                if (kDkv) l = ld_shared_f4(lse_smem + c * 4);
+#pragma unroll
+                for (int u = 0; u < 4; u += 2) {
+                    const uint64_t x = fma_f32x2(pack_f32x2(__uint_as_float(sv[c + u]), __uint_as_float(sv[c + u + 1])), c1c1,
+                                                 u == 0 ? pack_f32x2(-l.x, -l.y) : pack_f32x2(-l.z, -l.w));
+                    if (((c + u) >> 1) % 8 < kBwdPoly) {
+                        exp2_poly_pair(x, p[c + u], p[c + u + 1]);
+                    } else {
+                        float x0, x1;
+                        unpack_f32x2(x, x0, x1);
+                        p[c + u] = ex2f(x0);
+                        p[c + u + 1] = ex2f(x1);
+                    }
                 }
-                TMEM_ST32(tm_s, pk, 0);
+            }
+        };
+        // dS = P (dP - delta) of 32 columns, rounded to bf16
+        auto ds_of = [&](const uint32_t* dp, const float* p, uint32_t delta_smem, uint32_t* ds) {
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+                float4 d = make_float4(own_delta, own_delta, own_delta, own_delta);
+                if (kDkv) d = ld_shared_f4(delta_smem + c * 4);
+#pragma unroll
+                for (int u = 0; u < 4; u += 2) {
+                    const uint64_t v = add_f32x2(pack_f32x2(__uint_as_float(dp[c + u]), __uint_as_float(dp[c + u + 1])),
+                                                 u == 0 ? pack_f32x2(-d.x, -d.y) : pack_f32x2(-d.z, -d.w));
+                    float v0, v1;
+                    unpack_f32x2(mul_f32x2(v, pack_f32x2(p[c + u], p[c + u + 1])), v0, v1);
+                    ds[(c + u) >> 1] = pack_bf16(v0, v1);
+                }
+            }
+        };
+        int T = 0;
+        int s_buf = 0;                                           // kDq: the score buffer of S_T, 2 T mod 3; dP_T is in the next one
+        int4 cur;
+        bool ok = item_at(0, cur);
+        if (ok) read_own(cur.x);
+        for (int it = 0; ok && cur.x >= 0; ++it) {
+            const int n = cur.y;
+            const int last_valid = kDkv ? kBwdBlock : args.L_other - cur.z * kBwdBlock;      // kDq: keys of the last block
+            for (int j = 0; j < n; ++j, ++T, s_buf = s_buf >= 1 ? s_buf - 1 : s_buf + 2) {
+                if (!kDkv && (T & 1) != group) continue;
+                const uint32_t buf_s = tmem + lane_base + kScore0 + (kDkv ? 0 : s_buf * 128);
+                const uint32_t buf_dp = tmem + lane_base + kScore0 + (kDkv ? 128 : (s_buf == 2 ? 0 : s_buf + 1) * 128);
+                const uint32_t rows_smem = smem + Plan::kRowsOff + (T & 1) * Plan::kRowsBytes;
+                const uint32_t phase = static_cast<uint32_t>(T >> 1) & 1u;
+                if (kDkv) ok = mbar_wait_patient(smem_u32(&bar_rows_full[T & 1]), phase, abort_state);
+                if (ok) ok = mbar_wait_patient(smem_u32(&bar_s_full[T & 1]), phase, abort_state);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int half = 0; half < (kDkv ? 1 : 2); ++half) {
+                    const int col0 = 64 * (kDkv ? group : half);
+                    uint32_t sv[64];
+                    float p[64];
+                    TMEM_LD32(buf_s + col0, sv, 0);
+                    TMEM_LD32(buf_s + col0 + 32, sv, 32);
+                    tc_wait_ld();
+                    if (!kDkv && half == 1) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&bar_p_ready[T & 1]));
+                    }
+#pragma unroll
+                    for (int c0 = 0; c0 < 64; c0 += 32) {
+                        exps(sv + c0, p + c0, rows_smem + (col0 + c0) * 4);
+                        if (kDkv) {
+                            // P^T in bf16 over the S that it came from; the MMAs take it in two halves
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int c = 0; c < 16; ++c) pk[c] = pack_bf16(p[c0 + 2 * c], p[c0 + 2 * c + 1]);
+                            TMEM_ST16(buf_s + col0 + c0 / 2, pk, 0);
+                            tc_wait_st();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(smem_u32(c0 == 0 ? &bar_p_half[T & 1] : &bar_p_ready[T & 1]));
+                        }
+                    }
+                    if (!kDkv && j + 1 == n && last_valid < kBwdBlock) {
+                        // keys behind the last one: their zero rows of K make any finite dS harmless, but 2^(-LSE) need not be finite
+#pragma unroll
+                        for (int c = 0; c < 64; ++c) if (col0 + c >= last_valid) p[c] = 0.0f;
+                    }
+                    if (half == 0) {
+                        ok = mbar_wait_patient(smem_u32(&bar_dp_full[T & 1]), phase, abort_state);
+                        if (!ok) break;
+                        tc_fence_after();
+                    }
+                    uint32_t ds[32];
+#pragma unroll
+                    for (int c0 = 0; c0 < 64; c0 += 32) {
+                        uint32_t dp[32];
+                        TMEM_LD32(buf_dp + col0 + c0, dp, 0);
+                        tc_wait_ld();
+                        ds_of(dp, p + c0, rows_smem + (kBwdBlock + col0 + c0) * 4, ds + c0 / 2);
+                    }
+                    TMEM_ST32(buf_dp + col0, ds, 0);
+                }
+                if (!ok) break;
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bar_p_ready[j & 1]));
-            } else {
-#pragma unroll
-                for (int c = 0; c < 64; ++c) p[c] = ex2f(fmaf(__uint_as_float(sv[c]), c1, -own.x));
-                if (j + 1 == n && last_valid < kBwdBlock) {
-                    // keys behind the last one: their zero rows of K make any finite dS harmless, but 2^(-LSE) need not be finite
-#pragma unroll
-                    for (int c = 0; c < 64; ++c) if (col0 + c >= last_valid) p[c] = 0.0f;
-                }
+                if (lane == 0) mbar_arrive(smem_u32(&bar_ds_ready[T & 1]));
             }
-            ok = mbar_wait_warp(smem_u32(&bar_dp_full[j & 1]), (j >> 1) & 1, abort_state);
+            if (!ok) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bar_item_empty[it % kItemRing]));
+            ok = item_at(it + 1, cur);
+            if (ok) read_own(cur.x);
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kBwdRegsEpilogue));
+        // ---- accumulators out: thread (warp, lane) owns row 32 (warp % 4) + lane of both ----
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t acc = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        int4 cur;
+        bool ok = item_at(0, cur);
+        for (int it = 0; ok && cur.x >= 0; ++it) {
+            const int item = cur.x;
+            const int bh = item / args.n_items_per_head, b = bh / args.H, h = bh - b * args.H;
+            const int r = (item - bh * args.n_items_per_head) * kBwdBlock + row;
+            const long long at = ((static_cast<long long>(b) * args.L_own + r) * args.H + h) * D;
+            ok = mbar_wait_patient(smem_u32(&bar_done), it & 1, abort_state);
             if (!ok) break;
             tc_fence_after();
-            uint32_t ds[32];
-#pragma unroll
-            for (int c0 = 0; c0 < 64; c0 += 32) {
-                uint32_t dp[32];
-                TMEM_LD32(tm_dp + c0, dp, 0);
-                tc_wait_ld();
-#pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    float d0 = own.y, d1 = own.y;
-                    if (kDkv) {
-                        const float4 r = ld_shared_f4(rows_smem + (c0 + c) * 8);
-                        d0 = r.y;
-                        d1 = r.w;
-                    }
-                    ds[(c0 + c) >> 1] = pack_bf16(p[c0 + c] * (__uint_as_float(dp[c]) - d0), p[c0 + c + 1] * (__uint_as_float(dp[c + 1]) - d1));
-                }
-            }
-            TMEM_ST32(tm_dp, ds, 0);
-            tc_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bar_ds_ready[j & 1]));
-        }
-        // ---- accumulators out: kDkv: the first four warps dV, the others dK; kDq: half of the columns each ----
-        if (ok) ok = mbar_wait_warp(smem_u32(&bar_done), 0, abort_state);
-        if (ok) {
-            tc_fence_after();
-            const bool second = col0 != 0;
-            constexpr int kCols = kDkv ? D : D / 2;
-            const uint32_t acc = tmem + lane_base + (second ? (kDkv ? kAcc2 : D / 2) : 0);
-            __nv_bfloat16* out = (kDkv && second) ? args.out2 : args.out1;
-            const float factor = (kDkv && !second) ? 1.0f : args.scale;
-            const int r = own0 + row;
-            const long long at = ((static_cast<long long>(b) * args.L_own + r) * args.H + h) * D + (kDkv ? 0 : (second ? D / 2 : 0));
-#pragma unroll
+            constexpr int kCols = kDkv ? 2 * D : D;
+#pragma unroll 1
             for (int c0 = 0; c0 < kCols; c0 += 32) {
                 uint32_t v[32];
                 TMEM_LD32(acc + c0, v, 0);
                 tc_wait_ld();
+                if (c0 + 32 == kCols) {
+                    // all in registers or stored: the next item's first values may overwrite them
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(smem_u32(&bar_acc_free));
+                        mbar_arrive(smem_u32(&bar_item_empty[it % kItemRing]));
+                    }
+                }
+                const bool second = kDkv && c0 >= D;
+                const float factor = (kDkv && !second) ? 1.0f : args.scale;
+#pragma unroll
+                for (int c = 0; c < 16; ++c) v[c] = pack_bf16(__uint_as_float(v[2 * c]) * factor, __uint_as_float(v[2 * c + 1]) * factor);
                 if (r < args.L_own) {
+                    __nv_bfloat16* out = (second ? args.out2 + (c0 - D) : args.out1 + c0) + at;
+                    if (args.wide_out) {                         // whole 32-byte sectors
 #pragma unroll
-                    for (int c = 0; c < 32; c += 8) {
-                        uint32_t u[4];
+                        for (int c = 0; c < 16; c += 8)
+                            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 2 * c), "r"(v[c]), "r"(v[c + 1]),
+                                         "r"(v[c + 2]), "r"(v[c + 3]), "r"(v[c + 4]), "r"(v[c + 5]), "r"(v[c + 6]), "r"(v[c + 7]) : "memory");
+                    } else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            u[i] = pack_bf16(__uint_as_float(v[c + 2 * i]) * factor, __uint_as_float(v[c + 2 * i + 1]) * factor);
-                        *reinterpret_cast<uint4*>(out + at + c0 + c) = make_uint4(u[0], u[1], u[2], u[3]);
+                        for (int c = 0; c < 16; c += 4) *reinterpret_cast<uint4*>(out + 2 * c) = make_uint4(v[c], v[c + 1], v[c + 2], v[c + 3]);
                     }
                 }
             }
+            ok = item_at(it + 1, cur);
         }
     }
 

@@ -96,9 +96,9 @@ def test_good_arguments_stop_at_the_device(aj):
 
 
 def test_workspace_sizes(aj):
-    # means of 3 query and 4 key blocks; lists of 4 key blocks over 3 query blocks, their lengths, 384 padded rows
+    # means of 3 query and 4 key blocks; lists of 4 key blocks over 3 query blocks, their lengths, counters, 384 padded rows
     assert aj.attn_jvp_block_select_workspace_bytes(**BASE) == 2 * 64 * 8 * (3 + 4)
-    assert aj.attn_jvp_sparse_bwd_workspace_bytes(**BASE) == 256 + 256 + 2 * 384 * 8
+    assert aj.attn_jvp_sparse_bwd_workspace_bytes(**BASE) == 256 + 256 + 256 + 2 * 384 * 8
 
 
 def test_python_layer_refuses_cpu_tensors(aj):
