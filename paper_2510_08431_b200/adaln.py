@@ -40,7 +40,7 @@ class AdaLNGrads(NamedTuple):
 
 def attn_jvp_adaln_fwd(args: AdaLNArgs, x_new, y, tx_new, ty, cuda_stream) -> int:
     p = _binding._ptr
-    return int(_binding.load().attn_jvp_adaln_fwd(ctypes.byref(args), p(x_new), p(y), p(tx_new), p(ty), p(cuda_stream)))
+    return _binding.load().attn_jvp_adaln_fwd(ctypes.byref(args), p(x_new), p(y), p(tx_new), p(ty), p(cuda_stream))
 
 
 def attn_jvp_adaln_bwd_workspace_bytes(B, L, C) -> int:
@@ -50,14 +50,25 @@ def attn_jvp_adaln_bwd_workspace_bytes(B, L, C) -> int:
 def attn_jvp_adaln_bwd(args: AdaLNArgs, dx_new, dy, dx, dh, dgate, dscale, dshift, dweight, dpost_weight, workspace,
                        workspace_bytes, cuda_stream) -> int:
     p = _binding._ptr
-    return int(_binding.load().attn_jvp_adaln_bwd(ctypes.byref(args), p(dx_new), p(dy), p(dx), p(dh), p(dgate), p(dscale),
-                                                  p(dshift), p(dweight), p(dpost_weight), p(workspace),
-                                                  int(workspace_bytes), p(cuda_stream)))
+    return _binding.load().attn_jvp_adaln_bwd(ctypes.byref(args), p(dx_new), p(dy), p(dx), p(dh), p(dgate), p(dscale),
+                                              p(dshift), p(dweight), p(dpost_weight), p(workspace), int(workspace_bytes),
+                                              p(cuda_stream))
 
 
-def _tokens(t, name, shape, dtypes, device):
-    if not t.is_cuda or t.device != device or t.dtype not in dtypes or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous tensor on {device} of shape {shape} and type {' or '.join(map(str, dtypes))}")
+def _tokens(t, name, shape, dtype, device):
+    """Address of a tensor of tokens (or of a norm weight), checked."""
+    if t.device != device or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device} of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _row(t, name, B, C, device):
+    """Address and row stride of a modulation row per batch."""
+    if t is None:
+        return None, 0
+    if t.device != device or t.dtype is not torch.float32 or t.shape != (B, C) or t.stride(1) != 1 and C > 1:
+        raise ValueError(f"{name} must be fp32 of shape {(B, C)} on {device} with contiguous rows")
+    return t.data_ptr(), t.stride(0) if B > 1 else 0
 
 
 def _marshal(x, h, gate, scale, shift, weight, post_weight, norm, post_norm, eps, tangents=None) -> AdaLNArgs:
@@ -65,47 +76,39 @@ def _marshal(x, h, gate, scale, shift, weight, post_weight, norm, post_norm, eps
         raise ValueError("x must be a CUDA tensor [B][L][C]")
     if norm not in NORMS or post_norm not in NORMS:
         raise ValueError(f"norm and post_norm are one of {list(NORMS)}")
-    dev, shape = x.device, tuple(x.shape)
+    dev, shape, xt = x.device, x.shape, x.dtype
     B, L, C = shape
-    _tokens(x, "x", shape, (torch.bfloat16, torch.float32), dev)
-    a = AdaLNArgs(B=B, L=L, C=C, x_dtype=int(x.dtype == torch.float32), norm=NORMS[norm], post_norm=NORMS[post_norm], eps=eps)
-    a.x = x.data_ptr()
-    if h is not None:
-        _tokens(h, "h", shape, (torch.bfloat16,), dev)
-        a.h = h.data_ptr()
-    elif gate is not None or post_weight is not None or post_norm is not None:
+    if xt is not torch.bfloat16 and xt is not torch.float32 or not x.is_contiguous():
+        raise ValueError("x must be contiguous, bf16 or fp32")
+    if h is None and (gate is not None or post_weight is not None or post_norm is not None):
         raise ValueError("gate, post_norm and post_weight act on h, which is None")
     if norm is None and (scale is not None or shift is not None or weight is not None):
         raise ValueError("scale, shift and weight act on the norm's result, and norm is None")
-    tx, th, tgate, tscale, tshift = tangents if tangents is not None else (None,) * 5
-    rows = dict(gate=gate, scale=scale, shift=shift, tgate=tgate, tscale=tscale, tshift=tshift)
-    for name, t in rows.items():
-        if t is None:
-            continue
-        if t.device != dev or t.dtype != torch.float32 or tuple(t.shape) != (B, C) or (C > 1 and t.stride(1) != 1):
-            raise ValueError(f"{name} must be fp32 of shape {(B, C)} on {dev} with contiguous rows")
-        setattr(a, name, t.data_ptr())
-        setattr(a, name + "_stride", t.stride(0) if B > 1 else 0)
-    for name, t in dict(weight=weight, post_weight=post_weight).items():
-        if t is not None:
-            _tokens(t, name, (C,), (torch.float32,), dev)
-            setattr(a, name, t.data_ptr())
+    g, ld_g = _row(gate, "gate", B, C, dev)
+    s, ld_s = _row(scale, "scale", B, C, dev)
+    b, ld_b = _row(shift, "shift", B, C, dev)
+    tx = th = tg = ts = tb = None
+    ld_tg = ld_ts = ld_tb = 0
     if tangents is not None:
+        tx, th, tg, ts, tb = tangents
         if tx is None or (th is None) != (h is None):
             raise ValueError("with tangents tx is required, and th exactly where h is given")
-        if h is None and tgate is not None or norm is None and (tscale is not None or tshift is not None):
+        if h is None and tg is not None or norm is None and (ts is not None or tb is not None):
             raise ValueError("a tangent of something that does not act")
-        _tokens(tx, "tx", shape, (x.dtype,), dev)
-        a.tx = tx.data_ptr()
-        if th is not None:
-            _tokens(th, "th", shape, (torch.bfloat16,), dev)
-            a.th = th.data_ptr()
-    return a
+        tx = _tokens(tx, "tx", shape, xt, dev)
+        th = None if th is None else _tokens(th, "th", shape, torch.bfloat16, dev)
+        tg, ld_tg = _row(tg, "tgate", B, C, dev)
+        ts, ld_ts = _row(ts, "tscale", B, C, dev)
+        tb, ld_tb = _row(tb, "tshift", B, C, dev)
+    return AdaLNArgs(x.data_ptr(), None if h is None else _tokens(h, "h", shape, torch.bfloat16, dev), g, s, b,
+                     None if weight is None else _tokens(weight, "weight", (C,), torch.float32, dev),
+                     None if post_weight is None else _tokens(post_weight, "post_weight", (C,), torch.float32, dev),
+                     tx, th, tg, ts, tb, ld_g, ld_s, ld_b, ld_tg, ld_ts, ld_tb, B, L, C, int(xt is torch.float32), NORMS[norm],
+                     NORMS[post_norm], eps)
 
 
-def _raise(rc):
-    if rc != 0:
-        raise _binding.AttnJvpError(rc, _binding.attn_jvp_strerror(rc))
+def _bf16_like(x, h):
+    return torch.empty_like(h) if h is not None else torch.empty_like(x, dtype=torch.bfloat16)
 
 
 def adaln_jvp(x, h=None, gate=None, scale=None, shift=None, weight=None, post_weight=None, norm="layer", post_norm=None,
@@ -123,13 +126,11 @@ def adaln_jvp(x, h=None, gate=None, scale=None, shift=None, weight=None, post_we
                  (tx, th, tgate, tscale, tshift) if jvp else None)
     if h is None and norm is None:
         raise ValueError("neither h nor norm: nothing to compute")
-    y_like = dict(dtype=torch.bfloat16, device=x.device)
     xn = None if h is None else torch.empty_like(x)
-    y = None if norm is None else torch.empty(x.shape, **y_like)
+    y = None if norm is None else _bf16_like(x, h)
     txn = torch.empty_like(x) if jvp and h is not None else None
-    ty = torch.empty(x.shape, **y_like) if jvp and norm is not None else None
-    with torch.cuda.device(x.device):
-        _raise(attn_jvp_adaln_fwd(a, xn, y, txn, ty, torch.cuda.current_stream().cuda_stream))
+    ty = _bf16_like(x, h) if jvp and norm is not None else None
+    _binding._call_on(x.device, attn_jvp_adaln_fwd, a, xn, y, txn, ty)
     return (x if h is None else xn), y, (tx if h is None else txn), ty
 
 
@@ -143,26 +144,26 @@ def adaln_backward(dx_new, dy, x, h=None, gate=None, scale=None, shift=None, wei
     """
     a = _marshal(x, h, gate, scale, shift, weight, post_weight, norm, post_norm, eps)
     if dx_new is not None:
-        _tokens(dx_new, "dx_new", tuple(x.shape), (x.dtype,), x.device)
+        _tokens(dx_new, "dx_new", x.shape, x.dtype, x.device)
     if dy is not None:
         if norm is None:
             raise ValueError("dy given, but norm is None")
-        _tokens(dy, "dy", tuple(x.shape), (torch.bfloat16,), x.device)
+        _tokens(dy, "dy", x.shape, torch.bfloat16, x.device)
     B, L, C = x.shape
     dx = torch.empty_like(x)
     dh = None if h is None else torch.empty_like(h)
 
-    def row(t, *shape):
-        return None if t is None else torch.empty(shape, dtype=torch.float32, device=x.device)
-
-    dgate, dscale, dshift = row(gate, B, C), row(scale, B, C), row(shift, B, C)
-    dw, dwp = row(weight, C), row(post_weight, C)
+    # the gradients of the modulation and of the weights, one allocation
+    rows = [C * B if t is not None and t.dim() == 2 else C if t is not None else 0 for t in (gate, scale, shift, weight, post_weight)]
+    flat = x.new_empty(sum(rows), dtype=torch.float32).split(rows) if any(rows) else (None,) * 5
+    dgate, dscale, dshift = (f.view(B, C) if n else None for f, n in zip(flat, rows[:3]))
+    dw, dwp = (f if n else None for f, n in zip(flat[3:], rows[3:]))
     need = attn_jvp_adaln_bwd_workspace_bytes(B, L, C)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        workspace, size = x.new_empty(need, dtype=torch.uint8), need
     elif workspace.device != x.device:
         raise ValueError(f"workspace must be on {x.device}")
-    with torch.cuda.device(x.device):
-        _raise(attn_jvp_adaln_bwd(a, dx_new, dy, dx, dh, dgate, dscale, dshift, dw, dwp, workspace,
-                                  workspace.numel() * workspace.element_size(), torch.cuda.current_stream().cuda_stream))
+    else:
+        size = workspace.numel() * workspace.element_size()
+    _binding._call_on(x.device, attn_jvp_adaln_bwd, a, dx_new, dy, dx, dh, dgate, dscale, dshift, dw, dwp, workspace, size)
     return AdaLNGrads(dx, dh, dgate, dscale, dshift, dw, dwp)

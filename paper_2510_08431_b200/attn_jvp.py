@@ -124,6 +124,28 @@ def _ptr(x):
     return int(x)
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _call_on(device, fn, *args):
+    """fn(*args, stream) with ``device`` current, on torch's current stream of it; raises on a return code.
+
+    Short calls are bound by the host: a device guard and a Stream object cost as much as the launch itself, so the guard
+    is only taken where another device is current, and the stream's handle is read directly where torch offers that."""
+    i = device.index
+
+    def call():
+        return fn(*args, _raw_stream(i) if _raw_stream is not None else torch.cuda.current_stream(i).cuda_stream)
+
+    if torch.cuda.current_device() == i:
+        rc = call()
+    else:
+        with torch.cuda.device(i):
+            rc = call()
+    if rc != 0:
+        raise AttnJvpError(rc, attn_jvp_strerror(rc))
+
+
 def attn_jvp_strerror(code: int) -> str:
     return load().attn_jvp_strerror(int(code)).decode()
 

@@ -944,16 +944,20 @@ int sparse_fwd(const void* q, const void* k, const void* v, const void* tq, cons
     if (int rc = ensure_status_word(st)) return rc;
 
     const int key_tile = attn_jvp::key_tile(D, mode, false, false);
-    CUtensorMap maps[9];
+    CUtensorMap maps[9];                                 // (maps that the mode does not read are copies: an encoding costs 0.4 us)
     if (int rc = make_map(&maps[0], q, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
     if (int rc = make_map(&maps[1], k, B, Lk, H, D, key_tile)) return rc;
     if (int rc = make_map(&maps[2], v, B, Lk, H, D, key_tile)) return rc;
-    if (int rc = make_map(&maps[3], fwd_only ? q : tq, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
-    if (int rc = make_map(&maps[4], jvp_kv ? tk : k, B, Lk, H, D, key_tile)) return rc;
-    if (int rc = make_map(&maps[5], jvp_kv ? tv : v, B, Lk, H, D, key_tile)) return rc;
+    maps[3] = maps[0];
+    maps[4] = maps[5] = maps[8] = maps[1];
+    if (!fwd_only) if (int rc = make_map(&maps[3], tq, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
+    if (jvp_kv) {
+        if (int rc = make_map(&maps[4], tk, B, Lk, H, D, key_tile)) return rc;
+        if (int rc = make_map(&maps[5], tv, B, Lk, H, D, key_tile)) return rc;
+    }
     if (int rc = make_map(&maps[6], o, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
-    if (int rc = make_map(&maps[7], fwd_only ? o : to, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
-    maps[8] = maps[1];                                   // (only the CTA-pair kernel reads it)
+    maps[7] = maps[6];
+    if (!fwd_only) if (int rc = make_map(&maps[7], to, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
     KernelArgs ka = {};
     ka.o = static_cast<__nv_bfloat16*>(o);
     ka.to = static_cast<__nv_bfloat16*>(to);

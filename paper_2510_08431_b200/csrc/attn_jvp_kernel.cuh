@@ -529,27 +529,6 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-// 2^x of two values on the FMA pipe, for kernels whose pace the special-function unit sets (8 cycles per warp instruction):
-// x = n + f with n the nearest integer (added and taken off again as 1.5 * 2^23 + n), 2^f by a polynomial on [-1/2, 1/2]
-// whose coefficients minimise the largest relative error with p(0) = 1 (2.9e-6 in fp32; P is rounded to bf16 for the value
-// products, an error of 3.9e-3, and sums of P take the error on average), and n added to the exponent field.  x below
-// -127 is taken as -127, where p(0) = 1 makes the result exactly +0; x must not exceed 127.
-__device__ __forceinline__ void exp2_poly_pair(uint64_t x, float& p0, float& p1) {
-    float x0, x1;
-    unpack_f32x2(x, x0, x1);
-    x = pack_f32x2(fmaxf(x0, -127.0f), fmaxf(x1, -127.0f));
-    const uint64_t t = add_f32x2(x, pack_f32x2(12582912.0f, 12582912.0f));
-    const uint64_t f = add_f32x2(x, fma_f32x2(t, pack_f32x2(-1.0f, -1.0f), pack_f32x2(12582912.0f, 12582912.0f)));
-    uint64_t y = fma_f32x2(f, pack_f32x2(0x1.3a02ccp-7f, 0x1.3a02ccp-7f), pack_f32x2(0x1.c9fc46p-5f, 0x1.c9fc46p-5f));
-    y = fma_f32x2(f, y, pack_f32x2(0x1.ec037ap-3f, 0x1.ec037ap-3f));
-    y = fma_f32x2(f, y, pack_f32x2(0x1.62e12cp-1f, 0x1.62e12cp-1f));
-    y = fma_f32x2(f, y, pack_f32x2(1.0f, 1.0f));
-    float t0, t1, y0, y1;
-    unpack_f32x2(t, t0, t1);
-    unpack_f32x2(y, y0, y1);
-    p0 = __int_as_float(__float_as_int(y0) + (__float_as_int(t0) << 23));
-    p1 = __int_as_float(__float_as_int(y1) + (__float_as_int(t1) << 23));
-}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<uint32_t*>(&h);
@@ -571,10 +550,10 @@ __host__ __device__ constexpr int score_buffers(int D, int mode) {
 // only used by that variant.
 //
 // kSparse: an item's key tiles are those of the 128-key blocks on its list instead of all of them, in the list's order.
-// Every item then has its own number of tiles, filled up to the least number the kernel needs (one, or with streamed items
-// one per score buffer) with tiles that lie behind the last key: all of their P~ are 0; where even the first tile is one,
-// its row maximum is taken as 0 and the epilogue's 1 / l as 0.  Each role reads the length and the first entry of its next
-// item's list while it works on the current one (the loads would cost some 800 cycles each at every hand-over).
+// Every item then has its own number of tiles.  An empty list counts as one tile behind the last key: its row maximum is
+// taken as 0, all of its P~ are 0, and the epilogue's 1 / l as 0.  Each role reads the length and the first entry of its next
+// item's list while it works on the current one (the loads would cost some 800 cycles each at every hand-over).  Items are
+// not streamed into each other: tried, with short lists filled up to one tile per score buffer, 2 to 10 % slower.
 template <int D, int MODE, bool kSplit, int kGroups, bool kPair, bool kSparse = false>
 __global__ void __launch_bounds__(num_threads(kGroups), 1)
 attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -599,15 +578,8 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     constexpr int kRingStage = kDoubleQ ? 0 : kStageSlots;           // ... of which in ring slots (else in the item's Q/tQ buffer)
     // P~ and H~ of a tile are handed to the MMA warp together (one barrier): the softmax warps form both in one
     // pass over the columns, so an earlier hand-over of P~ alone would gain nothing.
-    // of 8 pairs of exponentials, how many take the FMA pipe: the forward-only pass over key block lists, whose pace the
-    // special-function unit would set (1024 of its cycles per 128 x 128 scores, as many as the MMAs take at D = 128)
-#ifndef POLY_F
-#define POLY_F 2
-#endif
-    constexpr int kPolyPairs = (kSparse && MODE == kModeFwdOnly) ? POLY_F : 0;
     constexpr int kBufs = score_buffers(D, MODE);            // score buffers = how many tiles the score MMAs run ahead
     constexpr int kScoreCol0 = (kBufs == 3) ? 128 : 256;     // first column of score buffer 0
-    constexpr int kMinTiles = kDoubleQ ? kBufs : 1;          // kSparse: least number of key tiles of an item
     static_assert(kScoreCol0 + kBufs * kScoreBufStride <= kTmemCols, "score buffers must fit into tensor memory");
     static_assert((kHasTQ ? 2 * D : D) <= kScoreCol0, "accumulators and score buffers overlap");
     static_assert(kDoubleQ || Plan::kSlotBytes == Plan::kQBytes, "an output tile must fill one ring slot");
@@ -693,7 +665,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             w.list = args.list + static_cast<size_t>(row) * args.list_stride;
             w.first = k.first;
             w.n_real = kBN == kBlockN ? tiles64 : (tiles64 + 1) / 2;
-            w.n_kv = max(kMinTiles, w.n_real);
+            w.n_kv = max(1, w.n_real);
         }
         return w;
     };
@@ -706,11 +678,11 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         return block * kBlockM + (kBN == kBlockN ? (j & 1) * kBlockN : 0);
     };
     const int n_items = args.n_items;
-    // Two Q/tQ buffers, no key chunks (every item then has the same number of key tiles, or at least as many as there are
-    // score buffers): the key tiles of all of a CTA's items form one stream.  The score MMAs of an item's leading tiles are issued in the last bursts of the
+    // Two Q/tQ buffers, no key chunks (every item then has the same number of key tiles): the key tiles of all of a
+    // CTA's items form one stream.  The score MMAs of an item's leading tiles are issued in the last bursts of the
     // item before (its Q, tQ are resident by then), and the ring carries their K tiles in that order, so that an
     // item boundary costs the MMA warp and the producer nothing.
-    const bool stream_items = kDoubleQ && !kSplit && (kSparse || args.n_kv_tiles >= kBufs);
+    const bool stream_items = kDoubleQ && !kSplit && !kSparse && args.n_kv_tiles >= kBufs;
     // Score buffer and barrier phase of a key tile, g % kBufs and (g / kBufs) & 1, carried along tile by tile (a
     // division by three per use would sit on the MMA warp's critical chain of dependent instructions).
     struct BufPos { int buf; uint32_t phase; };
@@ -1596,16 +1568,9 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     uint64_t rs2[2] = {0ull, 0ull};
 #pragma unroll
                     for (int c = 0; c < kBN; c += 2) {
-                        const uint64_t x2 = fma_f32x2(pack_f32x2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), c1c1, negm);
-                        float p0, p1;
-                        if ((c >> 1) % 8 < kPolyPairs) {
-                            exp2_poly_pair(x2, p0, p1);
-                        } else {
-                            float x0, x1;
-                            unpack_f32x2(x2, x0, x1);
-                            p0 = ex2f(x0);
-                            p1 = ex2f(x1);
-                        }
+                        float x0, x1;
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(sv[c]), __uint_as_float(sv[c + 1])), c1c1, negm), x0, x1);
+                        const float p0 = ex2f(x0), p1 = ex2f(x1);
                         const uint64_t p2 = pack_f32x2(p0, p1);
                         ls2[(c >> 1) & 1] = add_f32x2(ls2[(c >> 1) & 1], p2);
                         pk_p[c >> 1] = pack_bf16(p0, p1);

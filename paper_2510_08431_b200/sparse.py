@@ -7,12 +7,12 @@ such a selection, ``sparse_attention_backward`` its gradients.
 from __future__ import annotations
 
 import math
-from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
 from . import attn_jvp as _binding
-from .attn_jvp import FWD_ONLY, KV_TANGENT_FREE, AttnJvpError, _check, _ptr, attn_jvp_strerror
+from .attn_jvp import FWD_ONLY, KV_TANGENT_FREE, _call_on, _ptr
 
 SELECT_BLOCK = 128
 
@@ -22,7 +22,7 @@ def attn_jvp_block_select_workspace_bytes(B, H, Lq, Lk, D) -> int:
 
 
 def attn_jvp_block_select(q, k, B, H, Lq, Lk, D, topk, mask, index, tiles, workspace, workspace_bytes, cuda_stream) -> int:
-    return int(_binding.load().attn_jvp_block_select(_ptr(q), _ptr(k), B, H, Lq, Lk, D, int(topk), _ptr(mask), _ptr(index),
+    return (_binding.load().attn_jvp_block_select(_ptr(q), _ptr(k), B, H, Lq, Lk, D, int(topk), _ptr(mask), _ptr(index),
                                                      _ptr(tiles), _ptr(workspace), int(workspace_bytes), _ptr(cuda_stream)))
 
 
@@ -31,7 +31,7 @@ def attn_jvp_block_lists(mask, B, H, Lq, Lk, index, tiles, cuda_stream) -> int:
 
 
 def attn_jvp_sparse_fwd(q, k, v, tq, tk, tv, index, tiles, o, to, lse, mu, B, H, Lq, Lk, D, scale, flags, cuda_stream) -> int:
-    return int(_binding.load().attn_jvp_sparse_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(tq), _ptr(tk), _ptr(tv), _ptr(index),
+    return (_binding.load().attn_jvp_sparse_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(tq), _ptr(tk), _ptr(tv), _ptr(index),
                                                    _ptr(tiles), _ptr(o), _ptr(to), _ptr(lse), _ptr(mu), B, H, Lq, Lk, D,
                                                    float(scale), int(flags), _ptr(cuda_stream)))
 
@@ -42,18 +42,30 @@ def attn_jvp_sparse_bwd_workspace_bytes(B, H, Lq, Lk, D) -> int:
 
 def attn_jvp_sparse_bwd(d_o, q, k, v, o, lse, mask, index, tiles, dq, dk, dv, B, H, Lq, Lk, D, scale, workspace,
                         workspace_bytes, cuda_stream) -> int:
-    return int(_binding.load().attn_jvp_sparse_bwd(_ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(mask),
+    return (_binding.load().attn_jvp_sparse_bwd(_ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(mask),
                                                    _ptr(index), _ptr(tiles), _ptr(dq), _ptr(dk), _ptr(dv), B, H, Lq, Lk, D,
                                                    float(scale), _ptr(workspace), int(workspace_bytes), _ptr(cuda_stream)))
 
 
-def _raise(rc):
-    if rc != 0:
-        raise AttnJvpError(rc, attn_jvp_strerror(rc))
+def _check(t, name, shape, device):
+    if t.dtype is not torch.bfloat16 or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous bf16 tensor of shape {tuple(shape)} on {device}")
 
 
-@dataclass(frozen=True)
-class BlockSelection:
+def _check_qkv(q, k, v):
+    """Sizes of the call; q, k, v (or None) checked."""
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must be CUDA tensors [B][L][H][D]")
+    B, Lq, H, D = q.shape
+    dev, kv = q.device, (B, k.shape[1], H, D)
+    _check(q, "q", q.shape, dev)
+    _check(k, "k", kv, dev)
+    if v is not None:
+        _check(v, "v", kv, dev)
+    return B, H, Lq, kv[1], D
+
+
+class BlockSelection(NamedTuple):
     """Which key blocks each query block attends to.  Made by ``block_select`` or ``block_selection``; immutable: the
     lists are those of the mask, and changing one by hand would leave the others behind."""
     mask: torch.Tensor       # bool [B][H][n_q][n_k]
@@ -67,10 +79,8 @@ def _blocks(L):
     return -(-L // SELECT_BLOCK)
 
 
-def _lists(B, H, Lq, Lk, device):
-    n_q, n_k = _blocks(Lq), _blocks(Lk)
-    return (torch.empty((B, H, n_q, n_k), dtype=torch.int32, device=device),
-            torch.empty((B, H, n_q), dtype=torch.int32, device=device))
+def _lists(t, B, H, n_q, n_k):
+    return t.new_empty((B, H, n_q, n_k), dtype=torch.int32), t.new_empty((B, H, n_q), dtype=torch.int32)
 
 
 def block_select(q, k, topk, workspace=None) -> BlockSelection:
@@ -79,19 +89,18 @@ def block_select(q, k, topk, workspace=None) -> BlockSelection:
 
     q: [B][Lq][H][D], k: [B][Lk][H][D], contiguous CUDA bf16, D = 64 or 128.  ``workspace``: a CUDA uint8 tensor of at least
     attn_jvp_block_select_workspace_bytes(B, H, Lq, Lk, D)."""
-    B, Lq, H, D = q.shape
-    Lk = k.shape[1]
-    _check(q, "q", (B, Lq, H, D)); _check(k, "k", (B, Lk, H, D))
-    if k.device != q.device:
-        raise ValueError("q and k must be on one device")
+    B, H, Lq, Lk, D = _check_qkv(q, k, None)
     need = attn_jvp_block_select_workspace_bytes(B, H, Lq, Lk, D)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    mask = torch.empty((B, H, _blocks(Lq), _blocks(Lk)), dtype=torch.bool, device=q.device)
-    index, tiles = _lists(B, H, Lq, Lk, q.device)
-    with torch.cuda.device(q.device):
-        _raise(attn_jvp_block_select(q, k, B, H, Lq, Lk, D, topk, mask, index, tiles, workspace,
-                                     workspace.numel() * workspace.element_size(), torch.cuda.current_stream().cuda_stream))
+        workspace, size = q.new_empty(need, dtype=torch.uint8), need
+    elif workspace.device != q.device:
+        raise ValueError(f"workspace must be on {q.device}")
+    else:
+        size = workspace.numel() * workspace.element_size()
+    n_q, n_k = _blocks(Lq), _blocks(Lk)
+    mask = q.new_empty((B, H, n_q, n_k), dtype=torch.bool)
+    index, tiles = _lists(q, B, H, n_q, n_k)
+    _call_on(q.device, attn_jvp_block_select, q, k, B, H, Lq, Lk, D, topk, mask, index, tiles, workspace, size)
     return BlockSelection(mask, index, tiles, Lq, Lk)
 
 
@@ -103,17 +112,15 @@ def block_selection(mask, Lq, Lk) -> BlockSelection:
     B, H = mask.shape[:2]
     if tuple(mask.shape[2:]) != (_blocks(Lq), _blocks(Lk)):
         raise ValueError(f"mask must have {_blocks(Lq)} x {_blocks(Lk)} blocks for {Lq} queries and {Lk} keys")
-    index, tiles = _lists(B, H, Lq, Lk, mask.device)
-    with torch.cuda.device(mask.device):
-        _raise(attn_jvp_block_lists(mask, B, H, Lq, Lk, index, tiles, torch.cuda.current_stream().cuda_stream))
+    index, tiles = _lists(mask, B, H, _blocks(Lq), _blocks(Lk))
+    _call_on(mask.device, attn_jvp_block_lists, mask, B, H, Lq, Lk, index, tiles)
     return BlockSelection(mask, index, tiles, Lq, Lk)
 
 
 def _check_selection(sel, B, H, Lq, Lk, device):
     if not isinstance(sel, BlockSelection):
         raise ValueError("the selection must come from block_select or block_selection")
-    shape = (B, H, _blocks(Lq), _blocks(Lk))
-    if (sel.Lq, sel.Lk) != (Lq, Lk) or tuple(sel.mask.shape) != shape or sel.mask.device != device:
+    if sel.Lq != Lq or sel.Lk != Lk or sel.mask.shape[:2] != (B, H) or sel.mask.device != device:
         raise ValueError(f"the selection is for other sizes or another device than q and k (B={B}, H={H}, Lq={Lq}, Lk={Lk})")
 
 
@@ -122,36 +129,35 @@ def sparse_attention_jvp(q, k, v, selection, tq=None, tk=None, tv=None, scale=No
 
     Arguments as ``attention_jvp``; ``selection``: a ``BlockSelection`` for these sizes.  Rows of a query block without any
     key: o = to = 0, lse = -inf.  The selection does not move with the tangents."""
-    B, Lq, H, D = q.shape
-    Lk = k.shape[1]
-    _check(q, "q", (B, Lq, H, D)); _check(k, "k", (B, Lk, H, D)); _check(v, "v", (B, Lk, H, D))
-    _check_selection(selection, B, H, Lq, Lk, q.device)
+    B, H, Lq, Lk, D = _check_qkv(q, k, v)
+    dev = q.device
+    _check_selection(selection, B, H, Lq, Lk, dev)
     flags = 0
     if fwd_only:
-        flags |= FWD_ONLY
+        flags = FWD_ONLY
         tq = tk = tv = None
     else:
         if tq is None:
             raise ValueError("tq is required unless fwd_only")
-        _check(tq, "tq", (B, Lq, H, D))
+        _check(tq, "tq", q.shape, dev)
         if tk is None and tv is None:
-            flags |= KV_TANGENT_FREE
+            flags = KV_TANGENT_FREE
         elif tk is None or tv is None:
             raise ValueError("tk and tv must both be given or both be None")
         else:
-            _check(tk, "tk", (B, Lk, H, D)); _check(tv, "tv", (B, Lk, H, D))
+            _check(tk, "tk", k.shape, dev)
+            _check(tv, "tv", k.shape, dev)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     if out is None:
         o = torch.empty_like(q)
         to = None if fwd_only else torch.empty_like(q)
-        lse = torch.empty((B, H, Lq), dtype=torch.float32, device=q.device)
+        lse = q.new_empty((B, H, Lq), dtype=torch.float32)
     else:
         o, to, lse = out
-    mu = torch.empty((B, H, Lq), dtype=torch.float32, device=q.device) if return_mu else None
-    with torch.cuda.device(q.device):
-        _raise(attn_jvp_sparse_fwd(q, k, v, tq, tk, tv, selection.index, selection.tiles, o, to, lse, mu, B, H, Lq, Lk, D, scale,
-                                   flags, torch.cuda.current_stream().cuda_stream))
+    mu = q.new_empty((B, H, Lq), dtype=torch.float32) if return_mu else None
+    _call_on(dev, attn_jvp_sparse_fwd, q, k, v, tq, tk, tv, selection.index, selection.tiles, o, to, lse, mu, B, H, Lq, Lk, D, scale,
+             flags)
     return (o, to, lse, mu) if return_mu else (o, to, lse)
 
 
@@ -160,21 +166,23 @@ def sparse_attention_backward(d_o, q, k, v, o, lse, selection, scale=None, works
 
     ``o``, ``lse``: what that call returned.  ``workspace``: a CUDA uint8 tensor of at least
     attn_jvp_sparse_bwd_workspace_bytes(B, H, Lq, Lk, D), 256-byte aligned."""
-    B, Lq, H, D = q.shape
-    Lk = k.shape[1]
-    _check(q, "q", (B, Lq, H, D)); _check(k, "k", (B, Lk, H, D)); _check(v, "v", (B, Lk, H, D))
-    _check(o, "o", (B, Lq, H, D)); _check(d_o, "d_o", (B, Lq, H, D))
-    if not lse.is_cuda or lse.dtype != torch.float32 or tuple(lse.shape) != (B, H, Lq) or not lse.is_contiguous():
-        raise ValueError(f"lse must be a contiguous CUDA fp32 tensor of shape {(B, H, Lq)}")
-    _check_selection(selection, B, H, Lq, Lk, q.device)
+    B, H, Lq, Lk, D = _check_qkv(q, k, v)
+    dev = q.device
+    _check(o, "o", q.shape, dev)
+    _check(d_o, "d_o", q.shape, dev)
+    if lse.dtype is not torch.float32 or lse.device != dev or lse.shape != (B, H, Lq) or not lse.is_contiguous():
+        raise ValueError(f"lse must be a contiguous fp32 tensor of shape {(B, H, Lq)} on {dev}")
+    _check_selection(selection, B, H, Lq, Lk, dev)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     need = attn_jvp_sparse_bwd_workspace_bytes(B, H, Lq, Lk, D)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace, size = q.new_empty(need, dtype=torch.uint8), need
+    elif workspace.device != dev:
+        raise ValueError(f"workspace must be on {dev}")
+    else:
+        size = workspace.numel() * workspace.element_size()
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
-    with torch.cuda.device(q.device):
-        _raise(attn_jvp_sparse_bwd(d_o, q, k, v, o, lse, selection.mask, selection.index, selection.tiles, dq, dk, dv, B, H, Lq,
-                                   Lk, D, scale, workspace, workspace.numel() * workspace.element_size(),
-                                   torch.cuda.current_stream().cuda_stream))
+    _call_on(dev, attn_jvp_sparse_bwd, d_o, q, k, v, o, lse, selection.mask, selection.index, selection.tiles, dq, dk, dv, B, H, Lq,
+             Lk, D, scale, workspace, size)
     return dq, dk, dv
