@@ -3,7 +3,7 @@ from . import synth  # noqa: F401
 from .adaln import (  # noqa: F401
     AdaLNArgs, AdaLNGrads, adaln_backward, adaln_jvp, attn_jvp_adaln_bwd, attn_jvp_adaln_bwd_workspace_bytes,
     attn_jvp_adaln_fwd)
-from .layers import AttentionCoreJVP, TensorWithT  # noqa: F401
+from .layers import AdaLNJVP, AttentionCoreJVP, SparseAttentionCoreJVP, TensorWithT  # noqa: F401
 from .sparse import (  # noqa: F401
     SELECT_BLOCK, BlockSelection, attn_jvp_block_lists, attn_jvp_block_select, attn_jvp_block_select_workspace_bytes,
     attn_jvp_sparse_bwd, attn_jvp_sparse_bwd_workspace_bytes, attn_jvp_sparse_fwd, block_select, block_selection,

@@ -1,10 +1,11 @@
-"""Layer-level front end: an attention core that runs either as a plain forward or in JVP mode.
+"""Layer-level front end: the attention core, dense or over selected key blocks, and the step between two branches of a
+DiT block, each of which runs either as a plain call or in JVP mode.
 
 The paper restructures every network layer so that one call can carry primals alone or (primal, tangent)
 pairs, selected by a ``withT`` keyword (Appendix C.2, "Network Restructuring"); all layers use PyTorch's
 forward-mode operator for the JVP branch except the attention core, which calls the fused kernel
-(Appendix C.1).  This module is that attention core for [B][L][H][D] bf16 tensors.  It holds no
-parameters and does no arithmetic itself: both branches are calls into the CUDA library.
+(Appendix C.1).  Here the attention core for [B][L][H][D] bf16 tensors and the norms around it run in the CUDA library
+in both modes; the plain calls of the layers below the dense core are differentiable.
 """
 from __future__ import annotations
 
@@ -12,7 +13,9 @@ from typing import Optional, Tuple, Union
 
 import torch
 
+from . import adaln as _adaln
 from . import attn_jvp as _binding
+from . import sparse as _sparse
 
 TensorWithT = Tuple[torch.Tensor, torch.Tensor]   # (primal, tangent)
 
@@ -57,6 +60,110 @@ class AttentionCoreJVP(torch.nn.Module):
         res = _binding.attention_jvp(qp, kp, vp, qt.detach(), None if kt is None else kt.detach(),
                                      None if vt is None else vt.detach(), scale=self.scale,
                                      return_mu=self.keep_mu)
+        self.last_lse = res[2]
+        self.last_mu = res[3] if self.keep_mu else None
+        return res[0], res[1]
+
+
+def _pair(v):
+    """(primal, tangent) of a value that may carry a tangent."""
+    return v if isinstance(v, (tuple, list)) else (v, None)
+
+
+class _AdaLN(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, h, gate, scale, shift, weight, post_weight, kinds):
+        ctx.set_materialize_grads(False)
+        ctx.kinds = kinds
+        ctx.save_for_backward(x, h, gate, scale, shift, weight, post_weight)
+        xn, y, _, _ = _adaln.adaln_jvp(x, h, gate, scale, shift, weight, post_weight, **kinds)
+        return (x.view_as(x) if h is None else xn), y
+
+    @staticmethod
+    def backward(ctx, dxn, dy):
+        x, h, gate, scale, shift, weight, post_weight = ctx.saved_tensors
+        if dxn is None and dy is None:
+            return (None,) * 8
+        g = _adaln.adaln_backward(None if dxn is None else dxn.contiguous(), None if dy is None else dy.contiguous(), x, h, gate,
+                                  scale, shift, weight, post_weight, **ctx.kinds)
+        return (*g, None)
+
+
+class AdaLNJVP(torch.nn.Module):
+    """Gate + residual + norm + modulation between two branches of a DiT block (``adaln_jvp``), with an optional tangent
+    channel and, without it, autograd.
+
+    ``forward(x, h, gate, scale, shift)`` returns (x', y); h and the modulation may be None.  ``forward(..., withT=True)``
+    takes x and h as (primal, tangent) pairs and gate, scale, shift as pairs or as plain tensors (constant), and returns the
+    pairs (x', tx') and (y, ty).  ``affine`` / ``post_affine`` give the norms learnt fp32 weights (constants of the tangents:
+    the JVP runs on the frozen network).
+    """
+
+    def __init__(self, dim: int, norm: Optional[str] = "layer", post_norm: Optional[str] = None, eps: float = 1e-6,
+                 affine: bool = False, post_affine: bool = False):
+        super().__init__()
+        self.kinds = dict(norm=norm, post_norm=post_norm, eps=eps)
+        self.weight = torch.nn.Parameter(torch.ones(dim)) if affine else None
+        self.post_weight = torch.nn.Parameter(torch.ones(dim)) if post_affine else None
+
+    def forward(self, x, h=None, gate=None, scale=None, shift=None, withT: bool = False):
+        # (a call without a branch has nothing for the post norm to act on)
+        kinds = self.kinds if (_pair(h)[0] if withT else h) is not None else dict(self.kinds, post_norm=None)
+        if not withT:
+            return _AdaLN.apply(x, h, gate, scale, shift, self.weight, None if h is None else self.post_weight, kinds)
+        (x, tx), (h, th) = _pair(x), _pair(h)
+        (gate, tgate), (scale, tscale), (shift, tshift) = _pair(gate), _pair(scale), _pair(shift)
+        if h is not None and th is None:
+            raise ValueError("withT: h must carry a tangent where x does")
+        w = None if self.weight is None else self.weight.detach()
+        wp = None if self.post_weight is None or h is None else self.post_weight.detach()
+        xn, y, txn, ty = _adaln.adaln_jvp(x, h, gate, scale, shift, w, wp, **kinds, tx=tx.detach(),
+                                          th=None if th is None else th.detach(), tgate=tgate, tscale=tscale, tshift=tshift)
+        return (xn, txn), (y, ty)
+
+
+class _SparseAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, selection, scale):
+        o, _, lse = _sparse.sparse_attention_jvp(q, k, v, selection, scale=scale, fwd_only=True)
+        ctx.selection, ctx.scale = selection, scale
+        ctx.save_for_backward(q, k, v, o, lse)
+        ctx.mark_non_differentiable(lse)
+        return o, lse
+
+    @staticmethod
+    def backward(ctx, d_o, _):
+        q, k, v, o, lse = ctx.saved_tensors
+        return (*_sparse.sparse_attention_backward(d_o.contiguous(), q, k, v, o, lse, ctx.selection, scale=ctx.scale), None, None)
+
+
+class SparseAttentionCoreJVP(torch.nn.Module):
+    """``AttentionCoreJVP`` over selected key blocks: every block of 128 queries attends to the ``topk`` blocks of 128 keys
+    whose mean key fits its mean query best, or to those of a ``selection`` that the caller passes.
+
+    Plain calls are differentiable (the selection is a constant); ``withT=True`` takes and returns pairs as
+    ``AttentionCoreJVP`` does.  The selection, log-sum-exp and (``keep_mu``) its tangent of the last call are kept in
+    ``last_selection``, ``last_lse`` and ``last_mu``.
+    """
+
+    def __init__(self, topk: int, scale: Optional[float] = None, keep_mu: bool = False):
+        super().__init__()
+        self.topk, self.scale, self.keep_mu = topk, scale, keep_mu
+        self.last_selection = self.last_lse = self.last_mu = None
+
+    def forward(self, q, k, v, withT: bool = False, selection=None):
+        if withT:
+            (q, tq), (k, tk), (v, tv) = _pair(q), _pair(k), _pair(v)
+            if (tk is None) != (tv is None):
+                raise ValueError("k and v must both carry tangents (self-attention) or both be constant (context)")
+        if selection is None:
+            selection = _sparse.block_select(q.detach(), k.detach(), self.topk)
+        self.last_selection, self.last_mu = selection, None
+        if not withT:
+            o, self.last_lse = _SparseAttention.apply(q, k, v, selection, self.scale)
+            return o
+        res = _sparse.sparse_attention_jvp(q, k, v, selection, tq.detach(), None if tk is None else tk.detach(),
+                                           None if tv is None else tv.detach(), scale=self.scale, return_mu=self.keep_mu)
         self.last_lse = res[2]
         self.last_mu = res[3] if self.keep_mu else None
         return res[0], res[1]
