@@ -124,26 +124,29 @@ def _ptr(x):
     return int(x)
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_host_module = None
 
 
-def _call_on(device, fn, *args):
-    """fn(*args, stream) with ``device`` current, on torch's current stream of it; raises on a return code.
+def host():
+    """The host binding (_host.so, built in-tree like the library): tensor checks, allocation and the call in one step, for
+    entry points whose kernels take microseconds.  Its functions return the library's code first."""
+    global _host_module
+    if _host_module is None:
+        lib = load()
+        try:
+            from . import _host
+        except ImportError as e:
+            raise RuntimeError("_host.so is missing or does not load: build it with `python -m paper_2510_08431_b200.build` "
+                               "(there is no fallback path)") from e
+        names = ("adaln_fwd", "adaln_bwd", "adaln_bwd_workspace_bytes", "block_select", "block_select_workspace_bytes",
+                 "block_lists", "sparse_fwd", "sparse_bwd", "sparse_bwd_workspace_bytes")
+        _host.bind(*(ctypes.cast(getattr(lib, "attn_jvp_" + n), ctypes.c_void_p).value for n in names))
+        _host_module = _host
+    return _host_module
 
-    Short calls are bound by the host: a device guard and a Stream object cost as much as the launch itself, so the guard
-    is only taken where another device is current, and the stream's handle is read directly where torch offers that."""
-    i = device.index
 
-    def call():
-        return fn(*args, _raw_stream(i) if _raw_stream is not None else torch.cuda.current_stream(i).cuda_stream)
-
-    if torch.cuda.current_device() == i:
-        rc = call()
-    else:
-        with torch.cuda.device(i):
-            rc = call()
-    if rc != 0:
-        raise AttnJvpError(rc, attn_jvp_strerror(rc))
+def _raise(rc):
+    raise AttnJvpError(rc, attn_jvp_strerror(rc))
 
 
 def attn_jvp_strerror(code: int) -> str:

@@ -1,4 +1,4 @@
-"""Builds libattn_jvp.so (sm_100a only) in-tree with nvcc.  Needs no GPU."""
+"""Builds libattn_jvp.so (sm_100a only) with nvcc and the host binding with g++, in-tree.  Needs no GPU."""
 from __future__ import annotations
 
 import os
@@ -13,6 +13,8 @@ DEPS = [SRC, os.path.join(PKG, "csrc", "attn_jvp_kernel.cuh"), os.path.join(PKG,
         os.path.join(PKG, "csrc", "sparse_bwd.cuh"),
         os.path.join(ROOT, "include", "attn_jvp.h")]
 LIB = os.path.join(PKG, "libattn_jvp.so")
+HOST_SRC = os.path.join(PKG, "csrc", "host_binding.cpp")
+HOST_LIB = os.path.join(PKG, "_host.so")
 
 
 def _nvcc() -> str:
@@ -22,15 +24,40 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found: the attention-JVP library is CUDA-only (sm_100a) and has no fallback")
 
 
+def _older(lib: str, deps) -> bool:
+    return not os.path.exists(lib) or any(os.path.getmtime(d) > os.path.getmtime(lib) for d in deps)
+
+
 def is_stale() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(d) > t for d in DEPS)
+    return _older(LIB, DEPS)
+
+
+def build_host(force: bool = False) -> str:
+    """Compiles the host binding (a CPython module against the installed torch) if it is missing or older than its sources."""
+    deps = [HOST_SRC, os.path.join(ROOT, "include", "attn_jvp.h")]
+    if not force and not _older(HOST_LIB, deps):
+        return HOST_LIB
+    import sysconfig
+
+    import torch
+    tdir = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(_nvcc())))
+    includes = [os.path.join(ROOT, "include"), os.path.join(tdir, "include"), os.path.join(tdir, "include", "torch", "csrc", "api", "include"),
+                sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    tmp = HOST_LIB + f".tmp{os.getpid()}"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *(f"-I{i}" for i in includes), "-o", tmp, HOST_SRC, f"-L{os.path.join(tdir, 'lib')}", "-ltorch_python", "-ltorch_cpu", "-lc10",
+           "-lc10_cuda"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + res.stdout + res.stderr)
+    os.replace(tmp, HOST_LIB)
+    return HOST_LIB
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compiles the library if it is missing or older than its sources; returns its path."""
+    """Compiles the library and the host binding where they are missing or older than their sources; returns the library's path."""
+    build_host(force)
     if not force and not is_stale():
         return LIB
     tmp = LIB + f".tmp{os.getpid()}"

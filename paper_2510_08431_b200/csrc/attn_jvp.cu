@@ -805,8 +805,8 @@ int adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const void* dy, vo
                         {p.shift, mod_bytes(in->B, in->C, p.ld_shift), 4}};
     const Span outs[] = {{dx, xb, 16}, {dh, hb, 16}, {dgate, mb, 4}, {dscale, mb, 4}, {dshift, mb, 4}, {dweight, wb, 4},
                          {dpost_weight, wb, 4}, {workspace, need, 16}};
-    if (int rc = check_spans(ins, 9, outs, 8)) return rc;
     if (workspace_bytes < need) return ATTN_JVP_ERR_WORKSPACE;
+    if (int rc = check_spans(ins, 9, outs, 8)) return rc;
     int dev = 0;
     DeviceState* stp = nullptr;
     if (int rc = current_device(&dev, &stp)) return rc;
@@ -883,8 +883,8 @@ int block_select(const void* q, const void* k, int B, int H, int Lq, int Lk, int
     const size_t need = select_workspace(B, H, Lq, Lk, D), row = (size_t)B * H * D * 2;
     const Span ins[] = {{q, row * Lq, 16}, {k, row * Lk, 16}};
     const Span outs[] = {{mask, n.mask, 1}, {index, n.index, 4}, {tiles, n.tiles, 4}, {workspace, need, 16}};
-    if (int rc = check_spans(ins, 2, outs, 4)) return rc;
     if (workspace_bytes < need) return ATTN_JVP_ERR_WORKSPACE;
+    if (int rc = check_spans(ins, 2, outs, 4)) return rc;
     int dev = 0;
     DeviceState* stp = nullptr;
     if (int rc = current_device(&dev, &stp)) return rc;
@@ -1049,8 +1049,8 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
     const Span ins[] = {{d_o, nq, 16}, {q, nq, 16}, {k, nk, 16}, {v, nk, 16}, {o, nq, 16}, {lse, (size_t)B * H * Lq * 4, 4},
                         {mask, n.mask, 1}, {index, n.index, 4}, {tiles, n.tiles, 4}};
     const Span outs[] = {{dq, nq, 16}, {dk, nk, 16}, {dv, nk, 16}, {workspace, lay.total, 256}};
-    if (int rc = check_spans(ins, 9, outs, 4)) return rc;
     if (workspace_bytes < lay.total) return ATTN_JVP_ERR_WORKSPACE;
+    if (int rc = check_spans(ins, 9, outs, 4)) return rc;
     int dev = 0;
     DeviceState* stp = nullptr;
     if (int rc = current_device(&dev, &stp)) return rc;

@@ -283,8 +283,10 @@ def test_rows_behind_the_last_are_left_alone(aj):
     a, t, d = make(1, 3, 264, torch.bfloat16, weights=False)
     n = 3 * 264
     buf = [torch.full((n + 512,), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(4)]
-    args = aj.adaln._marshal(a["x"], a["h"], a["gate"], a["scale"], a["shift"], None, None, "layer", None, 1e-6,
-                             (t["tx"], t["th"], t["tgate"], t["tscale"], t["tshift"]))
+    args = aj.AdaLNArgs(B=1, L=3, C=264, norm=1, eps=1e-6)
+    for k, v in {**a, **t}.items():
+        if v is not None:
+            setattr(args, k, v.data_ptr())
     assert aj.attn_jvp_adaln_fwd(args, *buf, torch.cuda.current_stream().cuda_stream) == 0
     torch.cuda.synchronize()
     for b in buf:
