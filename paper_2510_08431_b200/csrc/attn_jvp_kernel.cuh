@@ -1503,6 +1503,11 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     return sc * ((sm4[0] + sm4[1]) + (sm4[2] + sm4[3])) / static_cast<float>(n_valid);
                 };
                 if (kHasTQ && kGroups == 1) tc_wait_ld();      // tS is in registers
+                if (kSparse && kHasTQ && valid <= 0) {
+                    // (a row without any key has H~ = 0 whatever its query holds: NaN times the zero-filled keys is NaN)
+#pragma unroll
+                    for (int c = 0; c < kBN; ++c) tv[c] = 0u;
+                }
                 if (kHasTQ && j == 0) ts_shift = centre_of_first_tile();
 
                 // m_new = max(m, rowmax), applied lazily: the result does not depend on which

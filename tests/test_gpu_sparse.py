@@ -252,6 +252,39 @@ def test_rows_behind_the_last_are_left_alone(aj):
         assert (t[n:] == 3.0).all() and not (t[:n] == 3.0).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_nothing_is_read_where_nothing_is_kept(aj, D):
+    """NaN and infinities in a query block without keys and in a key block that nobody kept reach no result."""
+    B, H, Lq, Lk = 1, 2, 400, 500
+    mask = make_mask("all", B, H, 4, 4)
+    mask[:, :, 1] = False
+    mask[..., 2] = False
+    sel = aj.block_selection(mask, Lq, Lk)
+
+    def path(x):
+        o, to, lse, mu = aj.sparse_attention_jvp(x["q"], x["k"], x["v"], sel, x["tq"], x["tk"], x["tv"], return_mu=True)
+        free = aj.sparse_attention_jvp(x["q"], x["k"], x["v"], sel, x["tq"], return_mu=True)
+        f, _, fl = aj.sparse_attention_jvp(x["q"], x["k"], x["v"], sel, fwd_only=True)
+        res = dict(o=o, to=to, lse=lse, mu=mu, free_to=free[1], free_mu=free[3], f=f, fl=fl)
+        res.update(zip(("dq", "dk", "dv"), aj.sparse_attention_backward(x["d_o"], x["q"], x["k"], x["v"], f, fl, sel)))
+        no_timeout(aj)
+        return res
+
+    x = inputs(B, H, Lq, Lk, D)
+    want = path(x)
+    for n, bad in (("q", float("nan")), ("tq", float("inf")), ("d_o", float("nan"))):
+        x[n][:, 128:256] = bad
+    for n, bad in (("k", float("nan")), ("v", float("inf")), ("tk", float("-inf")), ("tv", float("nan"))):
+        x[n][:, 256:384] = bad
+    got = path(x)
+    for n in want:
+        assert torch.equal(got[n], want[n]), n
+    for n in ("o", "to", "free_to", "f", "dq"):
+        assert not got[n][:, 128:256].any(), n
+    assert not got["mu"][:, :, 128:256].any() and (got["lse"][:, :, 128:256] == -float("inf")).all()
+    assert not got["dk"][:, 256:384].any() and not got["dv"][:, 256:384].any()
+
+
 def test_captured_and_replayed_on_a_side_stream(aj):
     """The whole path in a CUDA graph: selection, forward and gradients follow the inputs of the replay."""
     B, H, Lq, Lk, D = 1, 2, 700, 900, 64
