@@ -86,7 +86,8 @@ __device__ __forceinline__ unsigned long long ordered_key(double v) {
 }
 
 // Writes one row of a selection: mask bytes (optional), the ascending list and its length in 64-token tiles (a last
-// block of at most 64 tokens is one tile, every other block two).  `keep(j)` for j = lane, lane + 32, ...; whole warp.
+// block of at most 64 tokens is one tile, every other block two).  Whole warp; `keep(j, inside)` is called by all lanes for
+// j = lane, lane + 32, ... in this order, also behind the row's end (inside = false, its result is not used there).
 template <typename Keep>
 __device__ __forceinline__ void write_row(const Keep& keep, int n, int tokens, unsigned char* mask, int* list, int* tiles) {
     const int lane = threadIdx.x & 31;
@@ -94,9 +95,9 @@ __device__ __forceinline__ void write_row(const Keep& keep, int n, int tokens, u
     bool last_kept = false;
     for (int j0 = 0; j0 < n; j0 += 32) {
         const int j = j0 + lane;
-        const bool k = j < n && keep(j);
+        const bool inside = j < n, k = keep(j, inside) && inside;
         const unsigned votes = __ballot_sync(0xffffffffu, k);
-        if (mask != nullptr && j < n) mask[j] = k ? 1 : 0;
+        if (mask != nullptr && inside) mask[j] = k ? 1 : 0;
         if (k) list[count + __popc(votes & ((1u << lane) - 1u))] = j;
         count += __popc(votes);
         if (j0 + 32 >= n) last_kept = (votes >> (n - 1 - j0)) & 1u;
@@ -224,12 +225,14 @@ block_topk_kernel(const double* __restrict__ qm, const double* __restrict__ kmt,
             equal = __reduce_add_sync(0xffffffffu, equal);
         }
         const int keep_equal = equal - spare;
-        auto keep = [&](int j) {
-            const unsigned long long key = row_keys[j];
-            if (key != bound || spare == 0) return key >= bound;
-            int before = 0;                                      // (rare: exact ties around the last place)
-            for (int i = 0; i < j; ++i) before += row_keys[i] == bound ? 1 : 0;
-            return before < keep_equal;
+        int seen = 0;                                            // keys equal to the bound among the columns so far
+        auto keep = [&](int j, bool inside) {
+            const unsigned long long key = inside ? row_keys[j] : 0ull;
+            if (spare == 0) return key >= bound;
+            const unsigned ties = __ballot_sync(0xffffffffu, inside && key == bound);
+            const int before = seen + __popc(ties & ((1u << lane) - 1u));
+            seen += __popc(ties);
+            return key > bound || (key == bound && before < keep_equal);
         };
         const long long row = bh * n_q + i0 + r;
         write_row(keep, n_k, Lk, mask + row * n_k, index + row * n_k, tiles + row);
@@ -243,7 +246,7 @@ block_lists_kernel(const unsigned char* __restrict__ mask, int* __restrict__ ind
     const long long row = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
     if (row >= rows) return;
     const unsigned char* m = mask + row * n_k;
-    write_row([&](int j) { return m[j] != 0; }, n_k, Lk, nullptr, index + row * n_k, tiles + row);
+    write_row([&](int j, bool inside) { return inside && m[j] != 0; }, n_k, Lk, nullptr, index + row * n_k, tiles + row);
 }
 
 // The transposed lists: for every key block the query blocks that kept it.  A CTA takes 32 key blocks of one (batch,
@@ -271,7 +274,7 @@ block_transpose_kernel(const unsigned char* __restrict__ mask, int* __restrict__
     __syncthreads();
     for (int c = warp; c < 32 && j0 + c < n_k; c += 8) {
         const long long row = bh * n_k + j0 + c;
-        write_row([&](int i) { return (sel_words[i] >> c & 1u) != 0; }, n_q, Lq, nullptr, index + row * n_q, tiles + row);
+        write_row([&](int i, bool inside) { return inside && (sel_words[i] >> c & 1u) != 0; }, n_q, Lq, nullptr, index + row * n_q, tiles + row);
     }
 }
 

@@ -170,6 +170,19 @@ def test_ties_go_to_the_lower_block(aj):
     assert (sel.mask[..., :3]).all() and not sel.mask[..., 3:].any()
 
 
+def test_ties_of_many_key_blocks(aj):
+    """A row of equal scores (padding) longer than a lane holds in registers: the first ones, in one pass over the row."""
+    q = torch.randn(1, 128 * 20, 1, 64, device="cuda").bfloat16()
+    k = torch.zeros(1, 128 * 6144, 1, 64, device="cuda", dtype=torch.bfloat16)
+    k[:, 128 * 6000 : 128 * 6002] = 1.0                                   # above zero or below it, by the sign of the query's sum
+    sel = aj.block_select(q, k, 700)
+    high = q.view(20, 128 * 64).double().sum(1) > 0
+    for i in range(20):
+        want = torch.cat([torch.arange(698), torch.tensor([6000, 6001])]) if high[i] else torch.arange(700)
+        assert torch.equal(sel.mask[0, 0, i].nonzero()[:, 0].cpu(), want)
+    lists(sel)
+
+
 @pytest.mark.parametrize("n_k", [300, 3300])
 def test_selection_of_many_key_blocks(aj, n_k):
     """More key blocks than a lane holds in registers, and more than eight rows have room for."""
