@@ -70,6 +70,25 @@ def _pair(v):
     return v if isinstance(v, (tuple, list)) else (v, None)
 
 
+class _FirstOrder(torch.autograd.Function):
+    """A gradient as a function of what it was computed from, whose own gradient does not exist."""
+
+    @staticmethod
+    def forward(ctx, grad, *inputs):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("second derivatives of this layer are not available")
+
+
+def _first_order(grads, *inputs):
+    """Under create_graph a gradient's own gradient must be an error: left as a constant, it would silently count as zero."""
+    if not torch.is_grad_enabled():
+        return grads
+    return tuple(None if g is None else _FirstOrder.apply(g, *inputs) for g in grads)
+
+
 class _AdaLN(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, h, gate, scale, shift, weight, post_weight, kinds):
@@ -86,7 +105,7 @@ class _AdaLN(torch.autograd.Function):
             return (None,) * 8
         g = _adaln.adaln_backward(None if dxn is None else dxn.contiguous(), None if dy is None else dy.contiguous(), x, h, gate,
                                   scale, shift, weight, post_weight, **ctx.kinds)
-        return (*g, None)
+        return (*_first_order(g, dxn, dy, *ctx.saved_tensors), None)
 
 
 class AdaLNJVP(torch.nn.Module):
@@ -113,8 +132,8 @@ class AdaLNJVP(torch.nn.Module):
             return _AdaLN.apply(x, h, gate, scale, shift, self.weight, None if h is None else self.post_weight, kinds)
         (x, tx), (h, th) = _pair(x), _pair(h)
         (gate, tgate), (scale, tscale), (shift, tshift) = _pair(gate), _pair(scale), _pair(shift)
-        if h is not None and th is None:
-            raise ValueError("withT: h must carry a tangent where x does")
+        if tx is None or (h is not None and th is None):
+            raise ValueError("withT: x and h must carry tangents")
         w = None if self.weight is None else self.weight.detach()
         wp = None if self.post_weight is None or h is None else self.post_weight.detach()
         xn, y, txn, ty = _adaln.adaln_jvp(x, h, gate, scale, shift, w, wp, **kinds, tx=tx.detach(),
@@ -126,15 +145,17 @@ class _SparseAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, selection, scale):
         o, _, lse = _sparse.sparse_attention_jvp(q, k, v, selection, scale=scale, fwd_only=True)
-        ctx.selection, ctx.scale = selection, scale
-        ctx.save_for_backward(q, k, v, o, lse)
+        ctx.lengths, ctx.scale = selection[3:], scale
+        ctx.save_for_backward(q, k, v, o, lse, *selection[:3])      # (a mask that is written to meanwhile is an error)
         ctx.mark_non_differentiable(lse)
         return o, lse
 
     @staticmethod
     def backward(ctx, d_o, _):
-        q, k, v, o, lse = ctx.saved_tensors
-        return (*_sparse.sparse_attention_backward(d_o.contiguous(), q, k, v, o, lse, ctx.selection, scale=ctx.scale), None, None)
+        q, k, v, o, lse, *lists = ctx.saved_tensors
+        selection = _sparse.BlockSelection(*lists, *ctx.lengths)
+        grads = _sparse.sparse_attention_backward(d_o.contiguous(), q, k, v, o, lse, selection, scale=ctx.scale)
+        return (*_first_order(grads, d_o, q, k, v), None, None)
 
 
 class SparseAttentionCoreJVP(torch.nn.Module):
@@ -156,6 +177,8 @@ class SparseAttentionCoreJVP(torch.nn.Module):
             (q, tq), (k, tk), (v, tv) = _pair(q), _pair(k), _pair(v)
             if (tk is None) != (tv is None):
                 raise ValueError("k and v must both carry tangents (self-attention) or both be constant (context)")
+            if tq is None:
+                raise ValueError("withT: q must carry a tangent")
         if selection is None:
             selection = _sparse.block_select(q.detach(), k.detach(), self.topk)
         self.last_selection, self.last_mu = selection, None

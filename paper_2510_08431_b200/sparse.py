@@ -70,7 +70,7 @@ def block_select(q, k, topk, workspace=None) -> BlockSelection:
 
 def block_selection(mask, Lq, Lk) -> BlockSelection:
     """The selection of a caller's mask: contiguous CUDA bool [B][H][ceil(Lq / 128)][ceil(Lk / 128)].  The mask is kept, not
-    copied: later writes to it do not reach the lists."""
+    copied: it must not be written to while the selection is in use, the gradients of keys and values read it again."""
     rc, index, tiles = _binding.host().block_lists(mask, Lq, Lk)
     if rc:
         _binding._raise(rc)

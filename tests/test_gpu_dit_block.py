@@ -129,3 +129,42 @@ def test_selection_passed_in(aj):
     assert all(t.grad is not None and torch.isfinite(t.grad).all() for t in (q, k, v))
     with pytest.raises(ValueError):
         core((q, q), (k, k), v, withT=True)
+
+
+@pytest.mark.parametrize("loss", [torch.sum, lambda t: t.square().sum()])
+def test_no_second_derivatives(aj, loss):
+    """A gradient of a gradient is an error, not a silent zero; the first gradients under create_graph are the usual ones."""
+    x, h = (torch.randn(1, 20, 64, device="cuda").bfloat16().requires_grad_() for _ in range(2))
+    _, y = aj.AdaLNJVP(64)(x, h)
+    (want,) = torch.autograd.grad(loss(y.float()), h, retain_graph=True)
+    (g,) = torch.autograd.grad(loss(y.float()), h, create_graph=True)
+    assert torch.equal(g, want)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        (g.float().sum() + x.float().sum()).backward()
+    q = torch.randn(1, 200, 2, 64, device="cuda").bfloat16().requires_grad_()
+    (g,) = torch.autograd.grad(loss(aj.SparseAttentionCoreJVP(1)(q, q, q).float()), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        (g.float().sum() + q.float().sum()).backward()
+
+
+def test_a_mask_changed_before_the_backward_pass_is_an_error(aj):
+    q = torch.randn(1, 300, 2, 64, device="cuda").bfloat16().requires_grad_()
+    mask = torch.ones(1, 2, 3, 3, dtype=torch.bool, device="cuda")
+    o = aj.SparseAttentionCoreJVP(1)(q, q, q, selection=aj.block_selection(mask, 300, 300))
+    mask[0, 0, 0, 0] = False
+    with pytest.raises(RuntimeError):
+        o.float().sum().backward()
+
+
+def test_frozen_inputs_get_no_gradient(aj):
+    """Gradients go where they are asked for: a frozen stream, a frozen key."""
+    p = params(4)
+    layer = aj.AdaLNJVP(C).cuda()
+    scale = p["mod"][:, 0].clone().requires_grad_()
+    _, y = layer(p["x"], p["dy"], scale=scale)
+    y.float().sum().backward()
+    assert scale.grad.shape == (B, C) and p["x"].grad is None
+    q, k, v = (torch.randn(1, 300, 2, 64, device="cuda").bfloat16() for _ in range(3))
+    v.requires_grad_()
+    aj.SparseAttentionCoreJVP(2)(q, k, v).float().sum().backward()
+    assert v.grad is not None and q.grad is None and k.grad is None

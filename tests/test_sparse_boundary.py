@@ -109,6 +109,18 @@ def test_python_layer_refuses_cpu_tensors(aj):
         aj.block_selection(torch.ones(1, 2, 2, 2, dtype=torch.bool), 200, 200)
 
 
+def test_layers_refuse_missing_tangents(aj):
+    x = torch.zeros(1, 200, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="tangent"):
+        aj.SparseAttentionCoreJVP(1)(x, x, x, withT=True)
+    with pytest.raises(ValueError, match="tangent"):
+        aj.SparseAttentionCoreJVP(1)((x, x), (x, x), x, withT=True)
+    y = torch.zeros(1, 20, 64, dtype=torch.bfloat16)
+    for a in ((y,), (y, (y, y)), ((y, y), y)):
+        with pytest.raises(ValueError, match="tangent"):
+            aj.AdaLNJVP(64)(*a, withT=True)
+
+
 # ---- the 64-bit statement ----
 def test_statement_with_every_block_is_attention(oracle):
     g = torch.Generator().manual_seed(0)
