@@ -293,6 +293,40 @@ def test_rows_behind_the_last_are_left_alone(aj):
         assert (b[n:] == 7.0).all() and (b[:n] != 7.0).any()
 
 
+def test_outputs_between_sectors(aj):
+    """fp32 tensors 16 bytes off a 32-byte boundary, as the boundary allows: the same bits as the aligned ones."""
+    a, t, d = make(2, 21, 1288, torch.float32)
+    n = a["x"].numel()
+    want = aj.adaln_jvp(**a, norm="rms", post_norm="layer", **t)
+    want_g = aj.adaln_backward(d["dx_new"], d["dy"], **a, norm="rms", post_norm="layer")
+
+    def off(v=None):
+        buf = torch.full((n + 8,), 7.0, device="cuda")
+        assert buf.data_ptr() % 32 == 0
+        if v is not None:
+            buf[4:n + 4] = v.reshape(-1)
+        return buf
+
+    ins = dict(x=off(a["x"]), tx=off(t["tx"]))
+    args = aj.AdaLNArgs(B=2, L=21, C=1288, norm=2, post_norm=1, eps=1e-6, x_dtype=1)
+    for k, v in {**a, **t}.items():
+        setattr(args, k, ins[k][4:].data_ptr() if k in ins else v.data_ptr())
+        if v.dim() == 2:
+            setattr(args, k + "_stride", v.stride(0))
+    xn, txn, dx, dxn = off(), off(), off(), off(d["dx_new"])
+    y, ty, dh = (torch.empty_like(a["h"]) for _ in range(3))
+    st = torch.cuda.current_stream().cuda_stream
+    assert aj.attn_jvp_adaln_fwd(args, xn[4:], y, txn[4:], ty, st) == 0
+    g = [torch.empty(2, 1288, device="cuda") for _ in range(3)] + [torch.empty(1288, device="cuda") for _ in range(2)]
+    ws = torch.empty(aj.attn_jvp_adaln_bwd_workspace_bytes(2, 21, 1288), dtype=torch.uint8, device="cuda")
+    assert aj.attn_jvp_adaln_bwd(args, dxn[4:], d["dy"], dx[4:], dh, *g, ws, ws.numel(), st) == 0
+    torch.cuda.synchronize()
+    for got, ref in zip((xn, txn, dx), (want[0], want[2], want_g.x)):
+        assert torch.equal(got[4:n + 4], ref.reshape(-1)) and (got[:4] == 7.0).all() and (got[n + 4:] == 7.0).all()
+    for got, ref in zip([y, ty, dh] + g, [want[1], want[3], want_g.h, want_g.gate, want_g.scale, want_g.shift, want_g.weight, want_g.post_weight]):
+        assert torch.equal(got, ref)
+
+
 def test_workspace_must_be_large_enough(aj):
     a, _, d = make(1, 40, 64, torch.bfloat16)
     need = aj.attn_jvp_adaln_bwd_workspace_bytes(1, 40, 64)

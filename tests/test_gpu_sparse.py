@@ -298,6 +298,40 @@ def test_nothing_is_read_where_nothing_is_kept(aj, D):
     assert not got["dk"][:, 256:384].any() and not got["dv"][:, 256:384].any()
 
 
+def test_outputs_between_sectors_and_given_buffers(aj):
+    """Gradients 16 bytes off a 32-byte boundary, outputs and workspaces of the caller: the same bits."""
+    B, H, Lq, Lk, D = 1, 3, 300, 450, 64
+    x = inputs(B, H, Lq, Lk, D)
+    sel = aj.block_select(x["q"], x["k"], 2)
+    ws = torch.empty(aj.attn_jvp_block_select_workspace_bytes(B, H, Lq, Lk, D), dtype=torch.uint8, device="cuda")
+    for u, v in zip(aj.block_select(x["q"], x["k"], 2, workspace=ws)[:1], sel[:1]):
+        assert torch.equal(u, v)
+    o, _, lse = aj.sparse_attention_jvp(x["q"], x["k"], x["v"], sel, fwd_only=True)
+    mine = (torch.empty_like(o), None, torch.empty_like(lse))
+    res = aj.sparse_attention_jvp(x["q"], x["k"], x["v"], sel, fwd_only=True, out=mine)
+    assert res[0].data_ptr() == mine[0].data_ptr() and torch.equal(res[0], o) and torch.equal(res[2], lse)
+    need = aj.attn_jvp_sparse_bwd_workspace_bytes(B, H, Lq, Lk, D)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    want = aj.sparse_attention_backward(x["d_o"], x["q"], x["k"], x["v"], o, lse, sel)
+    for u, v in zip(aj.sparse_attention_backward(x["d_o"], x["q"], x["k"], x["v"], o, lse, sel, workspace=ws), want):
+        assert torch.equal(u, v)
+    outs = [torch.full((w.numel() + 16,), 5.0, dtype=torch.bfloat16, device="cuda") for w in want]
+    assert all(t.data_ptr() % 32 == 0 for t in outs)
+    assert aj.attn_jvp_sparse_bwd(x["d_o"], x["q"], x["k"], x["v"], o, lse, sel.mask, sel.index, sel.tiles, *(t[8:] for t in outs),
+                                  B, H, Lq, Lk, D, D ** -0.5, ws, need, torch.cuda.current_stream().cuda_stream) == 0
+    no_timeout(aj)
+    for t, w in zip(outs, want):
+        assert torch.equal(t[8:w.numel() + 8], w.reshape(-1)) and (t[:8] == 5.0).all() and (t[w.numel() + 8:] == 5.0).all()
+
+
+def test_many_heads_and_batches_of_one_block(aj):
+    """More work items than an SM draws in a lap, all short, across batches."""
+    B, H, L, D = 40, 9, 70, 64
+    x = inputs(B, H, L, L, D)
+    sel = aj.block_select(x["q"], x["k"], 1)
+    run_all(aj, x, sel, D)
+
+
 def test_captured_and_replayed_on_a_side_stream(aj):
     """The whole path in a CUDA graph: selection, forward and gradients follow the inputs of the replay."""
     B, H, Lq, Lk, D = 1, 2, 700, 900, 64
