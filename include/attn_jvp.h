@@ -273,7 +273,7 @@ int attn_jvp_qknorm_fwd(const void* x, const void* tx, const float* w, void* y, 
  *   weight, post_weight  device, fp32 [C], or NULL: 1.
  *   tx, th         tangents of x (type of x) and h (bf16), read by attn_jvp_adaln_fwd when its tx_new or ty is given
  *   tgate, tscale, tshift   tangents of the modulation, with their own strides; NULL: 0.  The weights are constants.
- *   C              a multiple of 8, at most 8192.  eps >= 0.
+ *   C              a multiple of 8, at most 8192.  eps >= 0.  B * L below 2 * 10^9.
  * Tensors of tokens are 16-byte aligned, fp32 rows 4-byte aligned.  Statistics, sums and products are fp32; x', y and
  * their tangents are rounded once, when they are stored, and y is formed from the unrounded x'.
  */
@@ -334,7 +334,9 @@ int attn_jvp_adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const voi
  *   tiles  int32 [B][H][n_q]: how many 64-key tiles those have (two per block; one for a last block of at most 64 keys)
  * index and tiles are always written by one of the two calls below.  A query block may keep nothing: its O and tO are
  * then 0, its LSE is -inf, its mu 0, and its gradients are 0; so are those of a key block that nobody kept.
- * Sequences of at most 786432 tokens; D is 64 or 128; tensors as in attn_jvp_fwd.
+ * Sequences of at most 786432 tokens, at most 65535 batches, at most 10^7 blocks of queries or keys over all batches and
+ * heads; D is 64 or 128; tensors as in attn_jvp_fwd.  Whatever index and tiles hold, the calls read and write inside the
+ * tensors; results are defined for lists that one of the two calls wrote.
  *
  * attn_jvp_block_select -- keeps, for every query block, the min(topk, n_k) key blocks with the largest
  * mean(q over the block) . mean(k over the block), formed in 64 bits, ties going to the lower key block.

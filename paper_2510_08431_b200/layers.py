@@ -5,7 +5,9 @@ The paper restructures every network layer so that one call can carry primals al
 pairs, selected by a ``withT`` keyword (Appendix C.2, "Network Restructuring"); all layers use PyTorch's
 forward-mode operator for the JVP branch except the attention core, which calls the fused kernel
 (Appendix C.1).  Here the attention core for [B][L][H][D] bf16 tensors and the norms around it run in the CUDA library
-in both modes; the plain calls of the layers below the dense core are differentiable.
+in both modes; the plain calls of the layers below the dense core are differentiable (once).  Their forward and backward
+passes can be captured into a CUDA graph; as with any layer, no autograd graph made outside the capture may then be alive
+for the same leaf tensors (the layers themselves keep none).
 """
 from __future__ import annotations
 

@@ -168,3 +168,37 @@ def test_frozen_inputs_get_no_gradient(aj):
     v.requires_grad_()
     aj.SparseAttentionCoreJVP(2)(q, k, v).float().sum().backward()
     assert v.grad is not None and q.grad is None and k.grad is None
+
+
+def test_training_step_captured(aj):
+    """Forward and backward of both layers in a CUDA graph, on a side stream, replayed on other inputs."""
+    layer, core = aj.AdaLNJVP(C, norm="rms", affine=True).cuda(), aj.SparseAttentionCoreJVP(TOPK)
+
+    def step(x, scale, dx):
+        xn, y = layer(x, None, None, scale)
+        q = y.view(B, L, H, D)
+        o = core(q, q, q).reshape(B, L, C)
+        _, z = layer(xn, o, None, scale)
+        return (z.detach(), *torch.autograd.grad(z, (x, scale, layer.weight), dx))
+
+    def args(seed):
+        p = params(seed)
+        return p["x"].requires_grad_(), p["mod"][:, 0].clone().requires_grad_(), p["dy"]
+
+    a, b = args(1), args(2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        want = [t.clone() for t in step(*b)]
+        step(*a)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = step(*a)
+    with torch.no_grad():
+        for u, v in zip(a, b):
+            u.copy_(v)
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    for u, v in zip(got, want):
+        assert torch.equal(u, v)
