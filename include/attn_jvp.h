@@ -328,27 +328,30 @@ int attn_jvp_adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const voi
  * Attention over selected key blocks.  At video lengths (32760 tokens) most of a head's keys matter little to a given
  * patch; here every block of ATTN_JVP_SELECT_BLOCK = 128 queries attends only to the blocks of 128 keys kept for it
  * (per batch and head; the last blocks are as long as the sequences leave them).  The selection is a constant of the
- * tangents and gradients.  A selection is three device arrays, n_q = ceil(Lq / 128), n_k = ceil(Lk / 128):
+ * tangents and gradients.  A selection is three or four device arrays, n_q = ceil(Lq / 128), n_k = ceil(Lk / 128):
  *   mask   uint8 [B][H][n_q][n_k], 0 or not 0: is the key block kept for the query block
  *   index  int32 [B][H][n_q][n_k]: the kept key blocks of a row in ascending order, at its start (the rest is undefined)
  *   tiles  int32 [B][H][n_q]: how many 64-key tiles those have (two per block; one for a last block of at most 64 keys)
- * index and tiles are always written by one of the two calls below.  A query block may keep nothing: its O and tO are
+ *   order  int32 [B][H][n_q], or NULL: the numbers (b H + h) n_q + i of all rows in the order in which they are worked on,
+ *          long rows first within neighbouring heads; it decides about time, not about results
+ * index, tiles and order are always written by one of the two calls below.  A query block may keep nothing: its O and tO are
  * then 0, its LSE is -inf, its mu 0, and its gradients are 0; so are those of a key block that nobody kept.
  * Sequences of at most 786432 tokens, at most 65535 batches, at most 10^7 blocks of queries or keys over all batches and
- * heads; D is 64 or 128; tensors as in attn_jvp_fwd.  Whatever index and tiles hold, the calls read and write inside the
+ * heads; D is 64 or 128; tensors as in attn_jvp_fwd.  Whatever the lists hold, the calls read and write inside the
  * tensors; results are defined for lists that one of the two calls wrote.
  *
  * attn_jvp_block_select -- keeps, for every query block, the min(topk, n_k) key blocks with the largest
  * mean(q over the block) . mean(k over the block), formed in 64 bits, ties going to the lower key block.
  *   workspace  device, 16-byte aligned, attn_jvp_block_select_workspace_bytes(...) bytes.
- * attn_jvp_block_lists -- index and tiles of a mask that the caller made.
+ * attn_jvp_block_lists -- index, tiles and order (NULL: not wanted) of a mask that the caller made.  (Rows of
+ * attn_jvp_block_select are of one length and need no order.)
  */
 #define ATTN_JVP_SELECT_BLOCK 128
 size_t attn_jvp_block_select_workspace_bytes(int B, int H, int Lq, int Lk, int D);
 int attn_jvp_block_select(const void* q, const void* k, int B, int H, int Lq, int Lk, int D, int topk,
                           unsigned char* mask, int* index, int* tiles,
                           void* workspace, size_t workspace_bytes, void* cuda_stream);
-int attn_jvp_block_lists(const unsigned char* mask, int B, int H, int Lq, int Lk, int* index, int* tiles, void* cuda_stream);
+int attn_jvp_block_lists(const unsigned char* mask, int B, int H, int Lq, int Lk, int* index, int* tiles, int* order, void* cuda_stream);
 
 /*
  * attn_jvp_sparse_fwd -- Algorithm 2 over the kept key blocks: arguments, modes and results as attn_jvp_fwd_mu (mu may be
@@ -356,7 +359,7 @@ int attn_jvp_block_lists(const unsigned char* mask, int B, int H, int Lq, int Lk
  */
 int attn_jvp_sparse_fwd(const void* q, const void* k, const void* v,
                         const void* tq, const void* tk, const void* tv,
-                        const int* index, const int* tiles,
+                        const int* index, const int* tiles, const int* order,
                         void* o, void* to, float* lse, float* mu,
                         int B, int H, int Lq, int Lk, int D,
                         float scale, unsigned flags, void* cuda_stream);
@@ -372,7 +375,7 @@ int attn_jvp_sparse_fwd(const void* q, const void* k, const void* v,
  */
 size_t attn_jvp_sparse_bwd_workspace_bytes(int B, int H, int Lq, int Lk, int D);
 int attn_jvp_sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse,
-                        const unsigned char* mask, const int* index, const int* tiles,
+                        const unsigned char* mask, const int* index, const int* tiles, const int* order,
                         void* dq, void* dk, void* dv,
                         int B, int H, int Lq, int Lk, int D, float scale,
                         void* workspace, size_t workspace_bytes, void* cuda_stream);

@@ -85,13 +85,13 @@ def load():
             lib.attn_jvp_block_select_workspace_bytes.restype = ctypes.c_size_t
             lib.attn_jvp_block_select.argtypes = [vp] * 2 + [ci] * 6 + [vp] * 4 + [ctypes.c_size_t, vp]
             lib.attn_jvp_block_select.restype = ci
-            lib.attn_jvp_block_lists.argtypes = [vp] + [ci] * 4 + [vp] * 3
+            lib.attn_jvp_block_lists.argtypes = [vp] + [ci] * 4 + [vp] * 4
             lib.attn_jvp_block_lists.restype = ci
-            lib.attn_jvp_sparse_fwd.argtypes = [vp] * 12 + [ci] * 5 + [cf, cu, vp]
+            lib.attn_jvp_sparse_fwd.argtypes = [vp] * 13 + [ci] * 5 + [cf, cu, vp]
             lib.attn_jvp_sparse_fwd.restype = ci
             lib.attn_jvp_sparse_bwd_workspace_bytes.argtypes = [ci] * 5
             lib.attn_jvp_sparse_bwd_workspace_bytes.restype = ctypes.c_size_t
-            lib.attn_jvp_sparse_bwd.argtypes = [vp] * 12 + [ci] * 5 + [cf, vp, ctypes.c_size_t, vp]
+            lib.attn_jvp_sparse_bwd.argtypes = [vp] * 13 + [ci] * 5 + [cf, vp, ctypes.c_size_t, vp]
             lib.attn_jvp_sparse_bwd.restype = ci
             lib.attn_jvp_selftest_bounded_wait.argtypes = [vp]
             lib.attn_jvp_selftest_bounded_wait.restype = ci

@@ -851,6 +851,8 @@ SelSizes sel_sizes(int B, int H, int Lq, int Lk) {
     return {rows * n_blocks(Lk), rows * n_blocks(Lk) * 4, rows * 4};
 }
 
+unsigned order_windows(long long rows) { return (unsigned)((rows + attn_jvp::kOrderWindow - 1) / attn_jvp::kOrderWindow); }
+
 size_t select_workspace(int B, int H, int Lq, int Lk, int D) {       // block means, fp64
     return (size_t)B * H * D * 8 * ((size_t)n_blocks(Lq) + n_blocks(Lk));
 }
@@ -901,25 +903,29 @@ int block_select(const void* q, const void* k, int B, int H, int Lq, int Lk, int
                        : launch_topk<4>(qm, kmt, mask, index, tiles, B * H, n_q, n_k, D, Lk, topk, stream, *stp);
 }
 
-int block_lists(const unsigned char* mask, int B, int H, int Lq, int Lk, int* index, int* tiles, cudaStream_t stream) {
+int block_lists(const unsigned char* mask, int B, int H, int Lq, int Lk, int* index, int* tiles, int* order, cudaStream_t stream) {
     if (int rc = sparse_shape(B, H, Lq, Lk, 64)) return rc;
     if (!mask || !index || !tiles) return ATTN_JVP_ERR_NULL;
     const SelSizes n = sel_sizes(B, H, Lq, Lk);
     const Span ins[] = {{mask, n.mask, 1}};
-    const Span outs[] = {{index, n.index, 4}, {tiles, n.tiles, 4}};
-    if (int rc = check_spans(ins, 1, outs, 2)) return rc;
+    const Span outs[] = {{index, n.index, 4}, {tiles, n.tiles, 4}, {order, n.tiles, 4}};
+    if (int rc = check_spans(ins, 1, outs, 3)) return rc;
     int dev = 0;
     DeviceState* stp = nullptr;
     if (int rc = current_device(&dev, &stp)) return rc;
     const long long rows = (long long)B * H * n_blocks(Lq);
     attn_jvp::block_lists_kernel<<<(unsigned)((rows + 7) / 8), 256, 0, stream>>>(mask, index, tiles, rows, n_blocks(Lk), Lk);
-    const cudaError_t e = cudaGetLastError();
+    cudaError_t e = cudaGetLastError();
+    if (e == cudaSuccess && order) {
+        attn_jvp::block_order_kernel<<<order_windows(rows), attn_jvp::kOrderThreads, 0, stream>>>(tiles, order, (int)rows);
+        e = cudaGetLastError();
+    }
     return e == cudaSuccess ? 0 : cuda_fail("block list kernel launch", e);
 }
 
 int sparse_fwd(const void* q, const void* k, const void* v, const void* tq, const void* tk, const void* tv, const int* index,
-               const int* tiles, void* o, void* to, float* lse, float* mu, int B, int H, int Lq, int Lk, int D, float scale,
-               unsigned flags, cudaStream_t stream) {
+               const int* tiles, const int* order, void* o, void* to, float* lse, float* mu, int B, int H, int Lq, int Lk, int D,
+               float scale, unsigned flags, cudaStream_t stream) {
     if (flags & ~(ATTN_JVP_KV_TANGENT_FREE | ATTN_JVP_FWD_ONLY)) return ATTN_JVP_ERR_FLAGS;
     const bool fwd_only = (flags & ATTN_JVP_FWD_ONLY) != 0;
     const int mode = fwd_only ? attn_jvp::kModeFwdOnly
@@ -933,9 +939,9 @@ int sparse_fwd(const void* q, const void* k, const void* v, const void* tq, cons
     const size_t row = (size_t)B * H * D * 2, nq = row * Lq, nk = row * Lk, nl = (size_t)B * H * Lq * 4;
     const SelSizes n = sel_sizes(B, H, Lq, Lk);
     const Span ins[] = {{q, nq, 16}, {k, nk, 16}, {v, nk, 16}, {fwd_only ? nullptr : tq, nq, 16}, {jvp_kv ? tk : nullptr, nk, 16},
-                        {jvp_kv ? tv : nullptr, nk, 16}, {index, n.index, 4}, {tiles, n.tiles, 4}};
+                        {jvp_kv ? tv : nullptr, nk, 16}, {index, n.index, 4}, {tiles, n.tiles, 4}, {order, n.tiles, 4}};
     const Span outs[] = {{o, nq, 16}, {fwd_only ? nullptr : to, nq, 16}, {lse, nl, 16}, {mu, nl, 16}};
-    if (int rc = check_spans(ins, 8, outs, 4)) return rc;
+    if (int rc = check_spans(ins, 9, outs, 4)) return rc;
     int dev = 0;
     DeviceState* stp = nullptr;
     if (int rc = current_device(&dev, &stp)) return rc;
@@ -976,6 +982,7 @@ int sparse_fwd(const void* q, const void* k, const void* v, const void* tq, cons
     ka.n_items = ka.n_q_tiles * H * B;
     ka.list = index;
     ka.tiles = tiles;
+    ka.order = order;
     ka.list_stride = n_blocks(Lk);
     const dim3 grid((unsigned)(ka.n_items < st.sm_count ? ka.n_items : st.sm_count), 1, 1);
     // softmax groups as softmax_groups_for() chooses them for long items
@@ -993,15 +1000,16 @@ int sparse_fwd(const void* q, const void* k, const void* v, const void* tq, cons
     }
 }
 
-// Workspace of the backward pass: the transposed lists, the two passes' item counters, LSE and delta per padded query row.
-struct SparseBwdLayout { size_t index, tiles, counters, rows, total; };
+// Workspace of the backward pass: the transposed lists and their order, the two passes' item counters, LSE and delta per padded query row.
+struct SparseBwdLayout { size_t index, tiles, order, counters, rows, total; };
 SparseBwdLayout sparse_bwd_layout(int B, int H, int Lq, int Lk) {
     auto pad = [](size_t n) { return (n + 255) & ~(size_t)255; };
     const size_t bh = (size_t)B * H, n_q = n_blocks(Lq), n_k = n_blocks(Lk);
     SparseBwdLayout l;
     l.index = 0;
     l.tiles = pad(bh * n_k * n_q * 4);
-    l.counters = l.tiles + pad(bh * n_k * 4);
+    l.order = l.tiles + pad(bh * n_k * 4);
+    l.counters = l.order + pad(bh * n_k * 4);
     l.rows = l.counters + 256;
     l.total = l.rows + bh * n_q * kSelBlock * 2 * sizeof(float);
     return l;
@@ -1029,8 +1037,8 @@ int sparse_bwd_run(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorM
                    DeviceState& st) {
     const long long threads = (long long)prep.B * prep.n_q * kSelBlock * prep.H * (D / 8);
     prep.row_blocks = (int)((threads + 255) / 256);
-    const int zero_blocks = (dkv.n_items + dq.n_items + 7) / 8;
-    attn_jvp::sparse_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + zero_blocks), 256, 0, stream>>>(prep);
+    prep.zero_blocks = (dkv.n_items + dq.n_items + 7) / 8;
+    attn_jvp::sparse_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + prep.zero_blocks) + order_windows(dkv.n_items), 256, 0, stream>>>(prep);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail("sparse backward preparation launch", e);
     if (int rc = launch_sparse_bwd<D, true>(mk, mv, mq, mdo, dkv, stream, st)) return rc;
@@ -1038,8 +1046,8 @@ int sparse_bwd_run(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorM
 }
 
 int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse,
-               const unsigned char* mask, const int* index, const int* tiles, void* dq, void* dk, void* dv, int B, int H, int Lq,
-               int Lk, int D, float scale, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+               const unsigned char* mask, const int* index, const int* tiles, const int* order, void* dq, void* dk, void* dv, int B,
+               int H, int Lq, int Lk, int D, float scale, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
     if (int rc = sparse_shape(B, H, Lq, Lk, D)) return rc;
     if (!d_o || !q || !k || !v || !o || !lse || !mask || !index || !tiles || !dq || !dk || !dv || !workspace) return ATTN_JVP_ERR_NULL;
     if (!std::isfinite(scale)) return ATTN_JVP_ERR_SCALE;
@@ -1047,10 +1055,10 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
     const SelSizes n = sel_sizes(B, H, Lq, Lk);
     const SparseBwdLayout lay = sparse_bwd_layout(B, H, Lq, Lk);
     const Span ins[] = {{d_o, nq, 16}, {q, nq, 16}, {k, nk, 16}, {v, nk, 16}, {o, nq, 16}, {lse, (size_t)B * H * Lq * 4, 4},
-                        {mask, n.mask, 1}, {index, n.index, 4}, {tiles, n.tiles, 4}};
+                        {mask, n.mask, 1}, {index, n.index, 4}, {tiles, n.tiles, 4}, {order, n.tiles, 4}};
     const Span outs[] = {{dq, nq, 16}, {dk, nk, 16}, {dv, nk, 16}, {workspace, lay.total, 256}};
     if (workspace_bytes < lay.total) return ATTN_JVP_ERR_WORKSPACE;
-    if (int rc = check_spans(ins, 9, outs, 4)) return rc;
+    if (int rc = check_spans(ins, 10, outs, 4)) return rc;
     int dev = 0;
     DeviceState* stp = nullptr;
     if (int rc = current_device(&dev, &stp)) return rc;
@@ -1066,6 +1074,7 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
     char* w = static_cast<char*>(workspace);
     int* t_index = reinterpret_cast<int*>(w + lay.index);
     int* t_tiles = reinterpret_cast<int*>(w + lay.tiles);
+    int* t_order = reinterpret_cast<int*>(w + lay.order);
     float* rows = reinterpret_cast<float*>(w + lay.rows);
     const int n_q = n_blocks(Lq), n_k = n_blocks(Lk);
     attn_jvp::block_transpose_kernel<<<(unsigned)((long long)B * H * ((n_k + 31) / 32)), 256, (size_t)n_q * 4, stream>>>(
@@ -1084,6 +1093,7 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
     attn_jvp::SparseBwdArgs dkv = a, dqa = a;
     dkv.list = t_index;
     dkv.tiles = t_tiles;
+    dkv.order = t_order;
     dkv.list_stride = n_q;
     dkv.n_items_per_head = n_k;
     dkv.n_items = B * H * n_k;
@@ -1094,6 +1104,7 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
     dkv.out2 = static_cast<__nv_bfloat16*>(dk);
     dqa.list = index;
     dqa.tiles = tiles;
+    dqa.order = order;
     dqa.list_stride = n_k;
     dqa.n_items_per_head = n_q;
     dqa.n_items = B * H * n_q;
@@ -1101,8 +1112,8 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
     dqa.L_own = Lq;
     dqa.L_other = Lk;
     dqa.out1 = static_cast<__nv_bfloat16*>(dq);
-    attn_jvp::SparseBwdPrep prep = {static_cast<const uint4*>(o), static_cast<const uint4*>(d_o), lse, rows, tiles, t_tiles, dqa.out1,
-                                    dkv.out2, dkv.out1, dkv.counter, B, H, Lq, Lk, n_q, n_k, 0};
+    attn_jvp::SparseBwdPrep prep = {static_cast<const uint4*>(o), static_cast<const uint4*>(d_o), lse, rows, tiles, t_tiles, t_order, dqa.out1,
+                                    dkv.out2, dkv.out1, dkv.counter, B, H, Lq, Lk, n_q, n_k, 0, 0};
     return D == 128 ? sparse_bwd_run<128>(mq, mk, mv, mdo, prep, dkv, dqa, stream, st)
                     : sparse_bwd_run<64>(mq, mk, mv, mdo, prep, dkv, dqa, stream, st);
 }
@@ -1280,14 +1291,14 @@ int attn_jvp_block_select(const void* q, const void* k, int B, int H, int Lq, in
     return block_select(q, k, B, H, Lq, Lk, D, topk, mask, index, tiles, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
-int attn_jvp_block_lists(const unsigned char* mask, int B, int H, int Lq, int Lk, int* index, int* tiles, void* cuda_stream) {
-    return block_lists(mask, B, H, Lq, Lk, index, tiles, static_cast<cudaStream_t>(cuda_stream));
+int attn_jvp_block_lists(const unsigned char* mask, int B, int H, int Lq, int Lk, int* index, int* tiles, int* order, void* cuda_stream) {
+    return block_lists(mask, B, H, Lq, Lk, index, tiles, order, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int attn_jvp_sparse_fwd(const void* q, const void* k, const void* v, const void* tq, const void* tk, const void* tv,
-                        const int* index, const int* tiles, void* o, void* to, float* lse, float* mu, int B, int H, int Lq, int Lk,
-                        int D, float scale, unsigned flags, void* cuda_stream) {
-    return sparse_fwd(q, k, v, tq, tk, tv, index, tiles, o, to, lse, mu, B, H, Lq, Lk, D, scale, flags, static_cast<cudaStream_t>(cuda_stream));
+                        const int* index, const int* tiles, const int* order, void* o, void* to, float* lse, float* mu, int B, int H,
+                        int Lq, int Lk, int D, float scale, unsigned flags, void* cuda_stream) {
+    return sparse_fwd(q, k, v, tq, tk, tv, index, tiles, order, o, to, lse, mu, B, H, Lq, Lk, D, scale, flags, static_cast<cudaStream_t>(cuda_stream));
 }
 
 size_t attn_jvp_sparse_bwd_workspace_bytes(int B, int H, int Lq, int Lk, int D) {
@@ -1295,9 +1306,9 @@ size_t attn_jvp_sparse_bwd_workspace_bytes(int B, int H, int Lq, int Lk, int D) 
 }
 
 int attn_jvp_sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse,
-                        const unsigned char* mask, const int* index, const int* tiles, void* dq, void* dk, void* dv, int B, int H,
-                        int Lq, int Lk, int D, float scale, void* workspace, size_t workspace_bytes, void* cuda_stream) {
-    return sparse_bwd(d_o, q, k, v, o, lse, mask, index, tiles, dq, dk, dv, B, H, Lq, Lk, D, scale, workspace, workspace_bytes,
+                        const unsigned char* mask, const int* index, const int* tiles, const int* order, void* dq, void* dk, void* dv,
+                        int B, int H, int Lq, int Lk, int D, float scale, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return sparse_bwd(d_o, q, k, v, o, lse, mask, index, tiles, order, dq, dk, dv, B, H, Lq, Lk, D, scale, workspace, workspace_bytes,
                       static_cast<cudaStream_t>(cuda_stream));
 }
 

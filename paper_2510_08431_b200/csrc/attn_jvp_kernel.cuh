@@ -126,6 +126,7 @@ struct KernelArgs {
     // in 64-key tiles (a last block of at most 64 keys is one tile)
     const int* list;    // [B][H][n_q_tiles][list_stride]
     const int* tiles;   // [B][H][n_q_tiles]
+    const int* order;   // the lists in the order of their work (block_order()); null: as they lie
     int list_stride;
 };
 
@@ -622,14 +623,21 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     // after the first item the three indices are advanced by the stride's own decomposition (carry by compare and
     // subtract) instead of being divided out again: the divisions would sit on the critical path of every item
     // hand-over, once per role.
-    struct Walk { int qt, h, z; int tiles64, first; };
-    // (kSparse: the length of item's list and its first entry; an item number is also the number of its list)
-    auto read_list = [&](Walk& k, int item) {
-        if (kSparse) {
-            const bool exists = item < args.n_items;
-            k.tiles64 = exists ? __ldg(args.tiles + item) : 0;
-            k.first = exists ? __ldg(args.list + static_cast<size_t>(item) * args.list_stride) : 0;
-        }
+    // kSparse: item number i is list number i, or with an order its entry at place i, where every other round of the CTAs runs
+    // backwards through the sorted lists, so that each CTA gets its share of long and short ones.  `after`: the list of the
+    // item behind this one.
+    struct Walk { int qt, h, z; int tiles64, first, round, after; };
+    auto ordered_list = [&](int round) -> int {
+        const int item = first_item + round * item_stride;
+        if (item >= args.n_items) return args.n_items;
+        const bool back = (round & 1) != 0 && (round + 1) * item_stride <= args.n_items;
+        return min(max(__ldg(args.order + (back ? round * item_stride + item_stride - 1 - first_item : item)), 0), args.n_items - 1);
+    };
+    // the length of a list and its first entry
+    auto read_list = [&](Walk& k, int row) {
+        const bool exists = row < args.n_items;
+        k.tiles64 = exists ? __ldg(args.tiles + row) : 0;
+        k.first = exists ? __ldg(args.list + static_cast<size_t>(row) * args.list_stride) : 0;
     };
     auto walk_init = [&](int item) -> Walk {
         Walk k{};
@@ -640,14 +648,30 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         return k;
     };
     const Walk walk_stride = walk_init(item_stride);
+    auto walk_first = [&]() -> Walk {
+        const bool ordered = kSparse && args.order != nullptr;
+        const int row = ordered ? ordered_list(0) : first_item;
+        Walk k = walk_init(row);
+        if (kSparse) read_list(k, row);
+        if (ordered) k.after = ordered_list(1);
+        return k;
+    };
     // to item number `item`, item_stride items on
     auto walk_step = [&](Walk& k, int item) {
+        if (kSparse && args.order != nullptr) {
+            const int row = k.after, round = k.round + 1;
+            k = walk_init(min(row, args.n_items - 1));
+            read_list(k, row);
+            k.round = round;
+            k.after = ordered_list(round + 1);
+            return;
+        }
         k.qt += walk_stride.qt;
         if (k.qt >= args.n_q_tiles) { k.qt -= args.n_q_tiles; ++k.h; }
         k.h += walk_stride.h;
         if (k.h >= args.H) { k.h -= args.H; ++k.z; }
         k.z += walk_stride.z;
-        read_list(k, item);
+        if (kSparse) read_list(k, item);
     };
     auto item_of = [&](const Walk& k) -> Item {
         Item w;
@@ -992,8 +1016,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             };
             Item prev_w{};
             int it = 0;
-            Walk wk = walk_init(first_item), wk_next;
-            read_list(wk, first_item);
+            Walk wk = walk_first(), wk_next;
             for (int item = first_item; ok && item < n_items; item += item_stride, ++it, wk = wk_next) {
                 w = item_of(wk);
                 const bool has_next = n_items - item > item_stride;
@@ -1236,8 +1259,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             BufPos bp{0, 0u};    // score buffer / phase of the tile whose value MMAs come next
             int g0 = 0;          // global number of the item's first key tile
             int it = 0;
-            Walk wk = walk_init(first_item), wk_next;
-            read_list(wk, first_item);
+            Walk wk = walk_first(), wk_next;
             for (int item = first_item; ok && item < n_items; item += item_stride, ++it, wk = wk_next) {
                 const Item w = item_of(wk);
                 const int n_kv = w.n_kv;
@@ -1396,8 +1418,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         ACC_DECL(acc_sm_scores);   // blocked for a tile's scores
         ACC_DECL(acc_sm_values);   // blocked for the item's last value MMAs (epilogue)
         ACC_DECL(acc_sm_epi);      // epilogue after that wait
-        Walk wk = walk_init(first_item), wk_next;
-        read_list(wk, first_item);
+        Walk wk = walk_first(), wk_next;
         for (int item = first_item; ok && item < n_items; item += item_stride, ++it, wk = wk_next) {
             const Item w = item_of(wk);
             const int n_kv = w.n_kv;

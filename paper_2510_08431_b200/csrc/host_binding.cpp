@@ -250,17 +250,19 @@ struct Qkv {
     }
     int64_t n_q() const { return (q.size(1) + ATTN_JVP_SELECT_BLOCK - 1) / ATTN_JVP_SELECT_BLOCK; }
     int64_t n_k() const { return (k.size(1) + ATTN_JVP_SELECT_BLOCK - 1) / ATTN_JVP_SELECT_BLOCK; }
-    // a selection for these sizes: mask, index, tiles, Lq, Lk
-    void selection(PyObject* const* p, at::Tensor& mask, at::Tensor& index, at::Tensor& tiles) const {
+    // a selection for these sizes: mask, index, tiles, order (or None), Lq, Lk
+    void selection(PyObject* const* p, at::Tensor& mask, at::Tensor& index, at::Tensor& tiles, at::Tensor& order) const {
         mask = required(p[0], "selection");
         index = required(p[1], "selection");
         tiles = required(p[2], "selection");
+        order = tensor(p[3], "selection");
         const at::Device dev = q.device();
-        if (whole(p[3], "Lq") != Lq || whole(p[4], "Lk") != Lk || mask.dim() != 4 || mask.size(0) != B || mask.size(1) != H || mask.device() != dev)
+        if (whole(p[4], "Lq") != Lq || whole(p[5], "Lk") != Lk || mask.dim() != 4 || mask.size(0) != B || mask.size(1) != H || mask.device() != dev)
             refuse("the selection is for other sizes or another device than q and k (B=%d, H=%d, Lq=%d, Lk=%d)", B, H, Lq, Lk);
         expect(mask, "selection.mask", at::kBool, {q.size(0), q.size(2), n_q(), n_k()}, dev);
         expect(index, "selection.index", at::kInt, {q.size(0), q.size(2), n_q(), n_k()}, dev);
         expect(tiles, "selection.tiles", at::kInt, {q.size(0), q.size(2), n_q()}, dev);
+        if (order.defined()) expect(order, "selection.order", at::kInt, tiles.sizes(), dev);
     }
     cudaStream_t stream() const { return c10::cuda::getCurrentCUDAStream(q.device().index()).stream(); }
 };
@@ -281,7 +283,7 @@ PyObject* block_select(PyObject*, PyObject* const* p, Py_ssize_t n) {
     });
 }
 
-// mask, Lq, Lk -> (rc, index, tiles)
+// mask, Lq, Lk -> (rc, index, tiles, order)
 PyObject* block_lists(PyObject*, PyObject* const* p, Py_ssize_t n) {
     if (!count(n, 3, "block_lists")) return nullptr;
     return guarded([&]() -> PyObject* {
@@ -289,28 +291,30 @@ PyObject* block_lists(PyObject*, PyObject* const* p, Py_ssize_t n) {
         if (!mask.is_cuda() || mask.scalar_type() != at::kBool || mask.dim() != 4 || !mask.is_contiguous()) refuse("mask must be a contiguous CUDA bool tensor [B][H][n_q][n_k]");
         const int Lq = whole(p[1], "Lq"), Lk = whole(p[2], "Lk"), blk = ATTN_JVP_SELECT_BLOCK;
         if (mask.size(2) != (Lq + (int64_t)blk - 1) / blk || mask.size(3) != (Lk + (int64_t)blk - 1) / blk) refuse("mask must have a block for every 128 of %d queries and of %d keys", Lq, Lk);
-        at::Tensor index = like(mask, mask.sizes(), at::kInt), tiles = like(mask, {mask.size(0), mask.size(1), mask.size(2)}, at::kInt);
+        at::Tensor index = like(mask, mask.sizes(), at::kInt);
+        at::Tensor tiles = like(mask, {mask.size(0), mask.size(1), mask.size(2)}, at::kInt), order = like(mask, tiles.sizes(), at::kInt);
         const c10::cuda::CUDAGuard guard(mask.device());
         const int rc = unlocked([&] { return f_block_lists(ptr<unsigned char>(mask), size32(mask.size(0)), size32(mask.size(1)), Lq, Lk, ptr<int>(index), ptr<int>(tiles),
-                                     c10::cuda::getCurrentCUDAStream(mask.device().index()).stream()); });
-        return result(rc, {index, tiles});
+                                     ptr<int>(order), c10::cuda::getCurrentCUDAStream(mask.device().index()).stream()); });
+        return result(rc, {index, tiles, order});
     });
 }
 
-// q, k, v, mask, index, tiles, Lq, Lk, tq, tk, tv, scale (None: 1/sqrt D), fwd_only, return_mu, o, to, lse (outputs, or None)
+// q, k, v, mask, index, tiles, order, Lq, Lk, tq, tk, tv, scale (None: 1/sqrt D), fwd_only, return_mu, o, to, lse (outputs, or None)
 // -> (rc, o, to, lse, mu)
 PyObject* sparse_fwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
-    if (!count(n, 17, "sparse_fwd")) return nullptr;
+    if (!count(n, 18, "sparse_fwd")) return nullptr;
     return guarded([&]() -> PyObject* {
         Qkv c(p[0], p[1], p[2]);
-        at::Tensor mask, index, tiles, tq, tk, tv;
-        c.selection(p + 3, mask, index, tiles);
-        const bool fwd_only = p[12] == Py_True;
+        at::Tensor mask, index, tiles, order, tq, tk, tv;
+        c.selection(p + 3, mask, index, tiles, order);
+        p += 9;                                                  // (the arguments behind the selection)
+        const bool fwd_only = p[4] == Py_True;
         unsigned flags = ATTN_JVP_FWD_ONLY;
         if (!fwd_only) {
-            tq = tensor(p[8], "tq");
-            tk = tensor(p[9], "tk");
-            tv = tensor(p[10], "tv");
+            tq = tensor(p[0], "tq");
+            tk = tensor(p[1], "tk");
+            tv = tensor(p[2], "tv");
             if (!tq.defined()) refuse("tq is required unless fwd_only");
             expect(tq, "tq", at::kBFloat16, c.q.sizes(), c.q.device());
             if (tk.defined() != tv.defined()) refuse("tk and tv must both be given or both be None");
@@ -320,9 +324,9 @@ PyObject* sparse_fwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
                 expect(tv, "tv", at::kBFloat16, c.k.sizes(), c.q.device());
             }
         }
-        const float scale = p[11] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(c.D))) : static_cast<float>(number(p[11], "scale"));
+        const float scale = p[3] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(c.D))) : static_cast<float>(number(p[3], "scale"));
         const int64_t rows[3] = {c.q.size(0), c.q.size(2), c.q.size(1)};
-        at::Tensor o = tensor(p[14], "o"), to = tensor(p[15], "to"), lse = tensor(p[16], "lse"), mu;
+        at::Tensor o = tensor(p[6], "o"), to = tensor(p[7], "to"), lse = tensor(p[8], "lse"), mu;
         if (o.defined()) expect(o, "o", at::kBFloat16, c.q.sizes(), c.q.device()); else o = same(c.q);
         if (!fwd_only) {
             if (to.defined()) expect(to, "to", at::kBFloat16, c.q.sizes(), c.q.device()); else to = same(c.q);
@@ -330,30 +334,30 @@ PyObject* sparse_fwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
             to = at::Tensor();
         }
         if (lse.defined()) expect(lse, "lse", at::kFloat, rows, c.q.device()); else lse = like(c.q, rows, at::kFloat);
-        if (p[13] == Py_True) mu = like(c.q, rows, at::kFloat);
+        if (p[5] == Py_True) mu = like(c.q, rows, at::kFloat);
         const c10::cuda::CUDAGuard guard(c.q.device());
-        const int rc = unlocked([&] { return f_sparse_fwd(ptr(c.q), ptr(c.k), ptr(c.v), ptr(tq), ptr(tk), ptr(tv), ptr<int>(index), ptr<int>(tiles), ptr(o), ptr(to), ptr<float>(lse),
+        const int rc = unlocked([&] { return f_sparse_fwd(ptr(c.q), ptr(c.k), ptr(c.v), ptr(tq), ptr(tk), ptr(tv), ptr<int>(index), ptr<int>(tiles), ptr<int>(order), ptr(o), ptr(to), ptr<float>(lse),
                                     ptr<float>(mu), c.B, c.H, c.Lq, c.Lk, c.D, scale, flags, c.stream()); });
         return result(rc, {o, to, lse, mu});
     });
 }
 
-// d_o, q, k, v, o, lse, mask, index, tiles, Lq, Lk, scale, workspace -> (rc, dq, dk, dv)
+// d_o, q, k, v, o, lse, mask, index, tiles, order, Lq, Lk, scale, workspace -> (rc, dq, dk, dv)
 PyObject* sparse_bwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
-    if (!count(n, 13, "sparse_bwd")) return nullptr;
+    if (!count(n, 14, "sparse_bwd")) return nullptr;
     return guarded([&]() -> PyObject* {
         Qkv c(p[1], p[2], p[3]);
-        at::Tensor d_o = required(p[0], "d_o"), o = required(p[4], "o"), lse = required(p[5], "lse"), mask, index, tiles;
+        at::Tensor d_o = required(p[0], "d_o"), o = required(p[4], "o"), lse = required(p[5], "lse"), mask, index, tiles, order;
         const at::Device dev = c.q.device();
         expect(d_o, "d_o", at::kBFloat16, c.q.sizes(), dev);
         expect(o, "o", at::kBFloat16, c.q.sizes(), dev);
         expect(lse, "lse", at::kFloat, {c.q.size(0), c.q.size(2), c.q.size(1)}, dev);
-        c.selection(p + 6, mask, index, tiles);
-        const float scale = p[11] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(c.D))) : static_cast<float>(number(p[11], "scale"));
-        at::Tensor ws = scratch(p[12], c.q, f_sparse_bwd_bytes(c.B, c.H, c.Lq, c.Lk, c.D));
+        c.selection(p + 6, mask, index, tiles, order);
+        const float scale = p[12] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(c.D))) : static_cast<float>(number(p[12], "scale"));
+        at::Tensor ws = scratch(p[13], c.q, f_sparse_bwd_bytes(c.B, c.H, c.Lq, c.Lk, c.D));
         at::Tensor dq = same(c.q), dk = same(c.k), dv = same(c.k);
         const c10::cuda::CUDAGuard guard(dev);
-        const int rc = unlocked([&] { return f_sparse_bwd(ptr(d_o), ptr(c.q), ptr(c.k), ptr(c.v), ptr(o), ptr<float>(lse), ptr<unsigned char>(mask), ptr<int>(index), ptr<int>(tiles), ptr(dq),
+        const int rc = unlocked([&] { return f_sparse_bwd(ptr(d_o), ptr(c.q), ptr(c.k), ptr(c.v), ptr(o), ptr<float>(lse), ptr<unsigned char>(mask), ptr<int>(index), ptr<int>(tiles), ptr<int>(order), ptr(dq),
                                     ptr(dk), ptr(dv), c.B, c.H, c.Lq, c.Lk, c.D, scale, ptr(ws), ws.nbytes(), c.stream()); });
         return result(rc, {dq, dk, dv});
     });

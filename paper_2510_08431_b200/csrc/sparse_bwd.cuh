@@ -26,6 +26,7 @@
 #pragma once
 
 #include "attn_jvp_kernel.cuh"
+#include "block_select.cuh"
 
 namespace attn_jvp {
 
@@ -41,6 +42,7 @@ constexpr int kBwdPoly = 2;                  // of 8 pairs of exponentials, how 
 struct SparseBwdArgs {
     const int* list;            // kDkv: [B][H][n_k][n_q] query blocks of a key block; kDq: [B][H][n_q][n_k]
     const int* tiles;           // their lengths in 64-token tiles
+    const int* order;           // the order in which they are handed out (block_order()); null: as they lie
     const float* rows;          // [B][H][n_q][2][128]: per block of queries LSE log2 e (+inf: no probability), then delta
     __nv_bfloat16* out1;        // kDkv: dV, kDq: dQ        [B][L][H][D]
     __nv_bfloat16* out2;        // kDkv: dK
@@ -68,20 +70,28 @@ struct SparseBwdPlan {
 // What the two passes need beforehand.  Blocks below `row_blocks`: LSE log2 e and delta per query row, padded to whole
 // blocks; rows behind the last query and rows without any key get LSE = +inf, which makes their P exactly 0; a group of
 // D / 8 threads per row reads dO and O once.  The blocks after them: a warp per stationary block of either pass, which
-// writes zero gradients where its list is empty (the passes never see those).  Both passes' counters start at 0.
+// writes zero gradients where its list is empty (the passes never see those).  The last blocks sort the transposed lists,
+// which differ in length whatever selection there was.  Both passes' counters start at 0.
 struct SparseBwdPrep {
     const uint4 *o, *d_o;
     const float* lse;
     float* rows;
     const int *q_tiles, *k_tiles;
+    int* k_order;
     __nv_bfloat16 *dq, *dk, *dv;
     int* counters;
-    int B, H, Lq, Lk, n_q, n_k, row_blocks;
+    int B, H, Lq, Lk, n_q, n_k, row_blocks, zero_blocks;
 };
 template <int D>
 __global__ void __launch_bounds__(256)
 sparse_bwd_prep_kernel(const SparseBwdPrep p) {
     constexpr int kLanes = D / 8;
+    if (static_cast<int>(blockIdx.x) >= p.row_blocks + p.zero_blocks) {
+        __shared__ uint4 swap[kOrderThreads];
+        static_assert(kOrderThreads == 256, "the sort's CTA");
+        block_order(p.k_tiles, p.k_order, p.B * p.H * p.n_k, blockIdx.x - p.row_blocks - p.zero_blocks, swap);
+        return;
+    }
     if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
         const int lane = threadIdx.x & 31;
         int item = (blockIdx.x - p.row_blocks) * 8 + (threadIdx.x >> 5);
@@ -287,10 +297,11 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
             bool ok = true;
             int T = 0, s1 = 0, s2 = 0;
             uint32_t ph1 = 0, ph2 = 0;                           // parity of the Y buffers' current lap
-            // the next item that keeps anything, from number `item` on; -1: none.  n: its streaming blocks
-            auto next_item = [&](int item, int& n) -> int {
-                for (;; item = static_cast<int>(gridDim.x) + atomicAdd(args.counter, 1)) {
-                    if (item >= args.n_items) return -1;
+            // the next item that keeps anything, from place `at` of the order on; -1: none.  n: its streaming blocks
+            auto next_item = [&](int at, int& n) -> int {
+                for (;; at = static_cast<int>(gridDim.x) + atomicAdd(args.counter, 1)) {
+                    if (at >= args.n_items) return -1;
+                    const int item = args.order == nullptr ? at : min(max(__ldg(args.order + at), 0), args.n_items - 1);
                     n = min((__ldg(args.tiles + item) + 1) >> 1, args.list_stride);
                     if (n > 0) return item;
                 }

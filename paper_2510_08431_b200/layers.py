@@ -147,8 +147,8 @@ class _SparseAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, selection, scale):
         o, _, lse = _sparse.sparse_attention_jvp(q, k, v, selection, scale=scale, fwd_only=True)
-        ctx.lengths, ctx.scale = selection[3:], scale
-        ctx.save_for_backward(q, k, v, o, lse, *selection[:3])      # (a mask that is written to meanwhile is an error)
+        ctx.lengths, ctx.scale = selection[4:], scale
+        ctx.save_for_backward(q, k, v, o, lse, *selection[:4])      # (a mask that is written to meanwhile is an error)
         ctx.mark_non_differentiable(lse)
         return o, lse
 

@@ -6,7 +6,7 @@ such a selection, ``sparse_attention_backward`` its gradients.
 """
 from __future__ import annotations
 
-from typing import NamedTuple
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -21,29 +21,29 @@ def attn_jvp_block_select_workspace_bytes(B, H, Lq, Lk, D) -> int:
 
 
 def attn_jvp_block_select(q, k, B, H, Lq, Lk, D, topk, mask, index, tiles, workspace, workspace_bytes, cuda_stream) -> int:
-    return (_binding.load().attn_jvp_block_select(_ptr(q), _ptr(k), B, H, Lq, Lk, D, int(topk), _ptr(mask), _ptr(index),
-                                                     _ptr(tiles), _ptr(workspace), int(workspace_bytes), _ptr(cuda_stream)))
+    return _binding.load().attn_jvp_block_select(_ptr(q), _ptr(k), B, H, Lq, Lk, D, int(topk), _ptr(mask), _ptr(index),
+                                                 _ptr(tiles), _ptr(workspace), int(workspace_bytes), _ptr(cuda_stream))
 
 
-def attn_jvp_block_lists(mask, B, H, Lq, Lk, index, tiles, cuda_stream) -> int:
-    return int(_binding.load().attn_jvp_block_lists(_ptr(mask), B, H, Lq, Lk, _ptr(index), _ptr(tiles), _ptr(cuda_stream)))
+def attn_jvp_block_lists(mask, B, H, Lq, Lk, index, tiles, order, cuda_stream) -> int:
+    return _binding.load().attn_jvp_block_lists(_ptr(mask), B, H, Lq, Lk, _ptr(index), _ptr(tiles), _ptr(order), _ptr(cuda_stream))
 
 
-def attn_jvp_sparse_fwd(q, k, v, tq, tk, tv, index, tiles, o, to, lse, mu, B, H, Lq, Lk, D, scale, flags, cuda_stream) -> int:
-    return (_binding.load().attn_jvp_sparse_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(tq), _ptr(tk), _ptr(tv), _ptr(index),
-                                                   _ptr(tiles), _ptr(o), _ptr(to), _ptr(lse), _ptr(mu), B, H, Lq, Lk, D,
-                                                   float(scale), int(flags), _ptr(cuda_stream)))
+def attn_jvp_sparse_fwd(q, k, v, tq, tk, tv, index, tiles, order, o, to, lse, mu, B, H, Lq, Lk, D, scale, flags, cuda_stream) -> int:
+    return _binding.load().attn_jvp_sparse_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(tq), _ptr(tk), _ptr(tv), _ptr(index),
+                                                _ptr(tiles), _ptr(order), _ptr(o), _ptr(to), _ptr(lse), _ptr(mu), B, H, Lq, Lk, D,
+                                                float(scale), int(flags), _ptr(cuda_stream))
 
 
 def attn_jvp_sparse_bwd_workspace_bytes(B, H, Lq, Lk, D) -> int:
     return int(_binding.load().attn_jvp_sparse_bwd_workspace_bytes(B, H, Lq, Lk, D))
 
 
-def attn_jvp_sparse_bwd(d_o, q, k, v, o, lse, mask, index, tiles, dq, dk, dv, B, H, Lq, Lk, D, scale, workspace,
+def attn_jvp_sparse_bwd(d_o, q, k, v, o, lse, mask, index, tiles, order, dq, dk, dv, B, H, Lq, Lk, D, scale, workspace,
                         workspace_bytes, cuda_stream) -> int:
-    return (_binding.load().attn_jvp_sparse_bwd(_ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(mask),
-                                                   _ptr(index), _ptr(tiles), _ptr(dq), _ptr(dk), _ptr(dv), B, H, Lq, Lk, D,
-                                                   float(scale), _ptr(workspace), int(workspace_bytes), _ptr(cuda_stream)))
+    return _binding.load().attn_jvp_sparse_bwd(_ptr(d_o), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(mask),
+                                               _ptr(index), _ptr(tiles), _ptr(order), _ptr(dq), _ptr(dk), _ptr(dv), B, H, Lq, Lk, D,
+                                               float(scale), _ptr(workspace), int(workspace_bytes), _ptr(cuda_stream))
 
 
 class BlockSelection(NamedTuple):
@@ -52,6 +52,7 @@ class BlockSelection(NamedTuple):
     mask: torch.Tensor       # bool [B][H][n_q][n_k]
     index: torch.Tensor      # int32 [B][H][n_q][n_k], ascending, the first entries of a row count
     tiles: torch.Tensor      # int32 [B][H][n_q], 64-key tiles of a row's blocks
+    order: Optional[torch.Tensor]    # int32 [B][H][n_q], all rows in the order of their work; None: as they lie
     Lq: int
     Lk: int
 
@@ -65,16 +66,16 @@ def block_select(q, k, topk, workspace=None) -> BlockSelection:
     rc, mask, index, tiles = _binding.host().block_select(q, k, topk, workspace)
     if rc:
         _binding._raise(rc)
-    return BlockSelection(mask, index, tiles, q.shape[1], k.shape[1])
+    return BlockSelection(mask, index, tiles, None, q.shape[1], k.shape[1])
 
 
 def block_selection(mask, Lq, Lk) -> BlockSelection:
     """The selection of a caller's mask: contiguous CUDA bool [B][H][ceil(Lq / 128)][ceil(Lk / 128)].  The mask is kept, not
     copied: it must not be written to while the selection is in use, the gradients of keys and values read it again."""
-    rc, index, tiles = _binding.host().block_lists(mask, Lq, Lk)
+    rc, index, tiles, order = _binding.host().block_lists(mask, Lq, Lk)
     if rc:
         _binding._raise(rc)
-    return BlockSelection(mask, index, tiles, Lq, Lk)
+    return BlockSelection(mask, index, tiles, order, Lq, Lk)
 
 
 def _selection(sel) -> BlockSelection:

@@ -145,6 +145,11 @@ def lists(sel):
     want = torch.sort(sel.mask.to(torch.uint8), dim=-1, descending=True, stable=True).indices
     live = torch.arange(n, device="cuda") < count[..., None]
     assert torch.equal(sel.index[live].long(), want[live])
+    if sel.order is not None:
+        # windows of 888 consecutive rows, the longest lists first, equal ones as they lie
+        tiles = sel.tiles.flatten().long()
+        expected = [w + torch.sort(tiles[w:w + 888], descending=True, stable=True).indices for w in range(0, tiles.numel(), 888)]
+        assert torch.equal(sel.order.flatten().long(), torch.cat(expected))
 
 
 @pytest.mark.parametrize("n_k", [1, 31, 32, 33, 100])
@@ -153,6 +158,24 @@ def test_lists_of_a_mask(aj, n_k, tail):
     Lk = (n_k - 1) * 128 + tail
     for kind in ("mixed", "none", "all", "last"):
         lists(aj.block_selection(make_mask(kind, 2, 3, 5, n_k), 600, Lk))
+
+
+@pytest.mark.parametrize("B,H,Lq,Lk,D", [(1, 3, 12700, 900, 64), (2, 10, 6000, 700, 128), (3, 7, 5700, 5700, 64)])
+def test_order_of_work(aj, B, H, Lq, Lk, D):
+    """More rows than a window, and partial last rounds of either direction: the same bits in either order of work."""
+    x = inputs(B, H, Lq, Lk, D)
+    sel = aj.block_selection(make_mask("mixed", B, H, R.blocks(Lq), R.blocks(Lk)), Lq, Lk)
+    lists(sel)
+
+    def path(s):
+        o, to, lse, mu = aj.sparse_attention_jvp(x["q"], x["k"], x["v"], s, x["tq"], x["tk"], x["tv"], return_mu=True)
+        f, _, fl = aj.sparse_attention_jvp(x["q"], x["k"], x["v"], s, fwd_only=True)
+        res = (o, to, lse, mu, f, fl) + aj.sparse_attention_backward(x["d_o"], x["q"], x["k"], x["v"], f, fl, s)
+        no_timeout(aj)
+        return res
+
+    for u, v in zip(path(sel), path(sel._replace(order=None))):
+        assert torch.equal(u, v)
 
 
 def test_ties_go_to_the_lower_block(aj):
@@ -255,10 +278,10 @@ def test_rows_behind_the_last_are_left_alone(aj):
     dk, dv = (torch.full((nk + pad,), 3.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
     lse = torch.full((B * H * Lq + 256,), 3.0, device="cuda")
     st = torch.cuda.current_stream().cuda_stream
-    assert aj.attn_jvp_sparse_fwd(x["q"], x["k"], x["v"], x["tq"], x["tk"], x["tv"], sel.index, sel.tiles, o, to, lse, None, B, H,
+    assert aj.attn_jvp_sparse_fwd(x["q"], x["k"], x["v"], x["tq"], x["tk"], x["tv"], sel.index, sel.tiles, sel.order, o, to, lse, None, B, H,
                                   Lq, Lk, D, 0.1, 0, st) == 0
     ws = torch.empty(aj.attn_jvp_sparse_bwd_workspace_bytes(B, H, Lq, Lk, D), dtype=torch.uint8, device="cuda")
-    assert aj.attn_jvp_sparse_bwd(x["d_o"], x["q"], x["k"], x["v"], o, lse, sel.mask, sel.index, sel.tiles, dq, dk, dv, B, H, Lq,
+    assert aj.attn_jvp_sparse_bwd(x["d_o"], x["q"], x["k"], x["v"], o, lse, sel.mask, sel.index, sel.tiles, sel.order, dq, dk, dv, B, H, Lq,
                                   Lk, D, 0.1, ws, ws.numel(), st) == 0
     no_timeout(aj)
     for t, n in ((o, nq), (to, nq), (dq, nq), (dk, nk), (dv, nk), (lse, B * H * Lq)):
@@ -317,7 +340,7 @@ def test_outputs_between_sectors_and_given_buffers(aj):
         assert torch.equal(u, v)
     outs = [torch.full((w.numel() + 16,), 5.0, dtype=torch.bfloat16, device="cuda") for w in want]
     assert all(t.data_ptr() % 32 == 0 for t in outs)
-    assert aj.attn_jvp_sparse_bwd(x["d_o"], x["q"], x["k"], x["v"], o, lse, sel.mask, sel.index, sel.tiles, *(t[8:] for t in outs),
+    assert aj.attn_jvp_sparse_bwd(x["d_o"], x["q"], x["k"], x["v"], o, lse, sel.mask, sel.index, sel.tiles, sel.order, *(t[8:] for t in outs),
                                   B, H, Lq, Lk, D, D ** -0.5, ws, need, torch.cuda.current_stream().cuda_stream) == 0
     no_timeout(aj)
     for t, w in zip(outs, want):

@@ -29,14 +29,14 @@ def select(aj, topk=2, q=A, k=A + STEP, mask=A + 2 * STEP, index=A + 3 * STEP, t
 
 def fwd(aj, flags=0, scale=0.1, **kw):
     p = dict(q=A, k=A + STEP, v=A + 2 * STEP, tq=A + 3 * STEP, tk=A + 4 * STEP, tv=A + 5 * STEP, index=A + 6 * STEP,
-             tiles=A + 7 * STEP, o=A + 8 * STEP, to=A + 9 * STEP, lse=A + 10 * STEP, mu=None, **BASE)
+             tiles=A + 7 * STEP, order=None, o=A + 8 * STEP, to=A + 9 * STEP, lse=A + 10 * STEP, mu=None, **BASE)
     p.update(kw)
     return aj.attn_jvp_sparse_fwd(**p, scale=scale, flags=flags, cuda_stream=None)
 
 
 def bwd(aj, n=None, scale=0.1, **kw):
     p = dict(d_o=A, q=A + STEP, k=A + 2 * STEP, v=A + 3 * STEP, o=A + 4 * STEP, lse=A + 5 * STEP, mask=A + 6 * STEP,
-             index=A + 7 * STEP, tiles=A + 8 * STEP, dq=A + 9 * STEP, dk=A + 10 * STEP, dv=A + 11 * STEP, workspace=A + 12 * STEP,
+             index=A + 7 * STEP, tiles=A + 8 * STEP, order=None, dq=A + 9 * STEP, dk=A + 10 * STEP, dv=A + 11 * STEP, workspace=A + 12 * STEP,
              **BASE)
     p.update(kw)
     if n is None:
@@ -52,7 +52,7 @@ def test_shapes(aj, kw, code):
     s = {**BASE, **kw}
     assert aj.attn_jvp_block_select_workspace_bytes(**s) == aj.attn_jvp_sparse_bwd_workspace_bytes(**s) == 0
     if code == 2:
-        assert aj.attn_jvp_block_lists(A, s["B"], s["H"], s["Lq"], s["Lk"], A + STEP, A + 2 * STEP, None) == 2
+        assert aj.attn_jvp_block_lists(A, s["B"], s["H"], s["Lq"], s["Lk"], A + STEP, A + 2 * STEP, None, None) == 2
 
 
 def test_selection_refuses(aj):
@@ -63,9 +63,11 @@ def test_selection_refuses(aj):
     assert select(aj, mask=A + 64) == 7 and select(aj, tiles=A + 3 * STEP) == 7
     assert select(aj, n=aj.attn_jvp_block_select_workspace_bytes(**BASE) - 1) == 12
     lists = aj.attn_jvp_block_lists
-    assert lists(None, 1, 2, 300, 500, A, A + STEP, None) == 1
-    assert lists(A, 1, 2, 300, 500, A + 1, A + STEP, None) == 4
-    assert lists(A, 1, 2, 300, 500, A, A + STEP, None) == 7
+    assert lists(None, 1, 2, 300, 500, A, A + STEP, None, None) == 1
+    assert lists(A, 1, 2, 300, 500, A + 1, A + STEP, None, None) == 4
+    assert lists(A, 1, 2, 300, 500, A, A + STEP, None, None) == 7
+    assert lists(A, 1, 2, 300, 500, A + STEP, A + 2 * STEP, A + 3 * STEP + 2, None) == 4
+    assert lists(A, 1, 2, 300, 500, A + STEP, A + 2 * STEP, A + 2 * STEP, None) == 7
 
 
 def test_forward_refuses(aj):
@@ -74,6 +76,7 @@ def test_forward_refuses(aj):
     assert fwd(aj, flags=8) == 5
     assert fwd(aj, scale=float("nan")) == 6
     assert fwd(aj, k=A + STEP + 8) == 4 and fwd(aj, lse=A + 10 * STEP + 4) == 4
+    assert fwd(aj, order=A + 6 * STEP + 2) == 4 and fwd(aj, order=A + 8 * STEP) == 7 and bwd(aj, order=A + 9 * STEP) == 7
     assert fwd(aj, o=A) == 7 and fwd(aj, to=A + 6 * STEP) == 7 and fwd(aj, mu=A + 8 * STEP) == 7
 
 
@@ -92,13 +95,14 @@ def test_good_arguments_stop_at_the_device(aj):
     assert select(aj) in (8, 9) and fwd(aj) in (8, 9) and bwd(aj) in (8, 9)
     assert fwd(aj, flags=2, tq=None, tk=None, tv=None, to=None) in (8, 9)
     assert fwd(aj, flags=1, tk=None, tv=None, mu=A + 11 * STEP) in (8, 9)
-    assert aj.attn_jvp_block_lists(A, 1, 2, 300, 500, A + STEP, A + 2 * STEP, None) in (8, 9)
+    assert aj.attn_jvp_block_lists(A, 1, 2, 300, 500, A + STEP, A + 2 * STEP, None, None) in (8, 9)
 
 
 def test_workspace_sizes(aj):
-    # means of 3 query and 4 key blocks; lists of 4 key blocks over 3 query blocks, their lengths, counters, 384 padded rows
+    # means of 3 query and 4 key blocks; lists of 4 key blocks over 3 query blocks, their lengths and order, counters, 384 padded
+    # rows
     assert aj.attn_jvp_block_select_workspace_bytes(**BASE) == 2 * 64 * 8 * (3 + 4)
-    assert aj.attn_jvp_sparse_bwd_workspace_bytes(**BASE) == 256 + 256 + 256 + 2 * 384 * 8
+    assert aj.attn_jvp_sparse_bwd_workspace_bytes(**BASE) == 256 + 256 + 256 + 256 + 2 * 384 * 8
 
 
 def test_python_layer_refuses_cpu_tensors(aj):
