@@ -893,9 +893,9 @@ int block_select(const void* q, const void* k, int B, int H, int Lq, int Lk, int
     const int n_q = n_blocks(Lq), n_k = n_blocks(Lk);
     double* qm = static_cast<double*>(workspace);
     double* kmt = qm + (size_t)B * H * D * n_q;
-    const unsigned cols = (unsigned)((H * D + 255) / 256);
-    attn_jvp::block_mean_kernel<<<dim3(cols, n_q + n_k, B), 256, 0, stream>>>(static_cast<const uint4*>(q), static_cast<const uint4*>(k), qm, kmt,
-                                                                             Lq, Lk, H, D, n_q, n_k);
+    const long long items = (long long)((H * D + 8 * attn_jvp::kPoolCols - 1) / (8 * attn_jvp::kPoolCols)) * (n_q + n_k) * B, slots = (long long)attn_jvp::kPoolCtas * kSms;
+    attn_jvp::block_mean_kernel<<<(unsigned)(items < slots ? items : slots), attn_jvp::kPoolRows * attn_jvp::kPoolCols, 0, stream>>>(static_cast<const uint4*>(q), static_cast<const uint4*>(k), qm, kmt,
+                                                                                           Lq, Lk, H, D, n_q, n_k, (int)items);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail("block mean kernel launch", e);
     // eight rows of scores per CTA where they fit into its shared memory, else four
