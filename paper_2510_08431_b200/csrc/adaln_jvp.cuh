@@ -179,6 +179,26 @@ struct RowShape {
     bool active;          // this thread has channels (below C)
 };
 
+// Sums of N values over a warp's lanes, N = 2, 4 or 8: while a lane holds more than one value it hands half of them to its
+// partner and takes the other half over, so that N values cost N - 1 + log2(32 / N) shuffles instead of 5 N.  Afterwards v[0]
+// of lane l is the sum of value l / (32 / N).
+template <int N>
+__device__ __forceinline__ void join_lanes(float (&v)[N]) {
+    const int lane = threadIdx.x & 31;
+    int m = 16;
+#pragma unroll
+    for (int n = N / 2; n >= 1; n /= 2, m /= 2) {
+        const bool upper = (lane & m) != 0;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float give = upper ? v[i] : v[i + n], keep = upper ? v[i + n] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, m);
+        }
+    }
+#pragma unroll
+    for (; m >= 1; m /= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], m);
+}
+
 // One block-wide reduction for kRows rows.  `red`: 2 x kRows x 32 float4 of shared memory used in turn (`turn` flips per
 // call: one barrier per call suffices, since a buffer is written again only after the next call's barrier, which every
 // thread reaches after its reads).  Channels that a thread does not have (behind C) hold zeros.
@@ -277,11 +297,12 @@ __host__ __device__ constexpr int adaln_slot_bytes(bool x_fp32, bool has_h, int 
 }
 
 // kMode: 0 forward, 1 forward with tangents, 2 backward.  kThreads: the most threads a CTA is launched with; kCtas: how
-// many of those an SM should hold.
-template <typename TX, int kMode, int kRows, int kStages, int kThreads, int kCtas>
+// many of those an SM should hold.  kPipe: a row's sums are formed while the row before it is finished (for calls with a norm
+// and without a post norm): the wait for one row's chain of shuffles is filled with the other row's arithmetic.
+template <typename TX, int kMode, int kRows, int kStages, int kThreads, int kCtas, bool kPipe = false>
 __global__ void __launch_bounds__(kThreads, kCtas) adaln_kernel(const AdalnParams p) {
     extern __shared__ __align__(16) uint8_t adaln_smem[];
-    constexpr int kRed = 2 * kRows * 32;
+    constexpr int kRed = 2 * kRows * 32 + (kPipe ? 16 : 0);     // (kPipe: pivots behind the sums)
     __shared__ float4 red[kRed];
     constexpr bool kJvp = kMode == 1, kBwd = kMode == 2;
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5, n_warps = blockDim.x >> 5;
@@ -352,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) adaln_kernel(const AdalnParam
         if (slot_ahead == ring_end) slot_ahead = smem;
     };
 #pragma unroll
-    for (int s = 0; s < kStages - 1; ++s) fetch();
+    for (int s = 0; s < kStages - (kPipe ? 2 : 1); ++s) fetch();
 
     pair_t gate[4], mul[4], shift[4], tgate[4], tmul[4], tshift[4];
     zero4(gate); zero4(mul); zero4(shift); zero4(tgate); zero4(tmul); zero4(tshift);
@@ -386,6 +407,134 @@ __global__ void __launch_bounds__(kThreads, kCtas) adaln_kernel(const AdalnParam
     uint32_t slot = smem;
     long long at = first + c;
     __syncthreads();                                             // (the zeros in `red`)
+    if constexpr (kPipe) {
+        static_assert(kRows == 1 && (kJvp || kBwd), "one row at a time, two sums and a companion's two");
+        // The norm of x' alone (no post norm), of row r + 1 while row r is finished: the sums of r + 1 over this warp and those of
+        // r over the warps go through the same five levels of shuffles, and the barrier between them is that of the row.
+        float* pivots = reinterpret_cast<float*>(red + 64);
+        const float inv_first = 1.0f / static_cast<float>(min(256, p.C));
+        const float n_theirs = lane < n_warps ? static_cast<float>(min(256, p.C - lane * 256)) : 0.0f;
+        const float inv_theirs = lane < n_warps ? 1.0f / n_theirs : 0.0f;
+        // x' and its companion (tx', or dy w (1 + scale)) of a row from the ring
+        auto row_of = [&](uint32_t s, pair_t (&x)[4], pair_t (&x2)[4]) {
+            load_slot<TX>(s + at_x, lane, x);
+            pair_t h[4];
+            if (kJvp) load_slot<TX>(s + at_x2, lane, x2);
+            if (has_h) {
+                load_slot<__nv_bfloat16>(s + at_h, lane, h);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[i] = fma2(gate[i], h[i], x[i]);
+                    if (kJvp) x2[i] = fma2(tgate[i], h[i], x2[i]);
+                }
+                if (kJvp) {
+                    load_slot<__nv_bfloat16>(s + at_h2, lane, h);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x2[i] = fma2(gate[i], h[i], x2[i]);
+                }
+            }
+            if (kBwd) {
+                if (has_dy) load_slot<__nv_bfloat16>(s + at_h2, lane, x2); else zero4(x2);
+            }
+        };
+        uint32_t before = ring_end - row_bytes;                  // the slot of row r; `slot`: that of row r + 1
+        for (int row = row0 - 1; row < row1; ++row) {
+            float v[8], mean = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+            if (row + 1 < row1) {
+                __syncwarp();                                    // (the slot that is filled now was read by the whole warp)
+                fetch();
+                cp_async_wait<kStages - 2>();
+                __syncwarp();
+                pair_t x[4], t2[4], d[4];
+                row_of(slot, x, t2);
+                if (kBwd) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) t2[i] = mul2(t2[i], mul[i]);
+                }
+                mean = __shfl_sync(0xffffffffu, sum2(add2(add2(x[0], x[1]), add2(x[2], x[3]))), 0) * 0.125f;
+                const pair_t minus = twice(active ? -mean : 0.0f);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d[i] = add2(x[i], minus);
+                v[0] = sum2(add2(add2(d[0], d[1]), add2(d[2], d[3])));
+                v[1] = sum2(add2(fma2(d[1], d[1], mul2(d[0], d[0])), fma2(d[3], d[3], mul2(d[2], d[2]))));
+                v[2] = sum2(add2(add2(t2[0], t2[1]), add2(t2[2], t2[3])));
+                v[3] = sum2(add2(fma2(d[1], t2[1], mul2(d[0], t2[0])), fma2(d[3], t2[3], mul2(d[2], t2[2]))));
+            }
+            float mean0 = 0.0f;
+            if (row >= row0) {
+                // lane w: warp w's sums of row r, about that warp's mean and then about the first warp's
+                const float4* buf = red + (turn ^ 1) * 32;
+                const float* piv = pivots + (turn ^ 1) * 32;
+                const float4 e = buf[lane];
+                const float d = e.x * inv_theirs;
+                mean0 = fmaf(buf[0].x, inv_first, piv[0]);
+                const float d2 = piv[lane] + d - mean0;
+                v[4] = n_theirs * d2;
+                v[5] = fmaf(v[4], d2, fmaf(-d, e.x, e.y));
+                v[6] = e.z;
+                v[7] = fmaf(d2, e.z, fmaf(-d, e.z, e.w));
+            }
+            join_lanes(v);
+            if ((lane & 3) == 0 && lane < 16) reinterpret_cast<float*>(red + turn * 32 + warp)[lane >> 2] = v[0];
+            if (lane == 0) pivots[turn * 32 + warp] = mean;
+            turn ^= 1;
+            if (row >= row0) {
+                const float s = __shfl_sync(0xffffffffu, v[0], 16), sq = __shfl_sync(0xffffffffu, v[0], 20);
+                const float T = __shfl_sync(0xffffffffu, v[0], 24), Q = __shfl_sync(0xffffffffu, v[0], 28);
+                const bool layer = p.norm == kAdalnLayer;
+                const float d = s * shape.inv_c, mu = mean0 + d, m2 = fmaxf(fmaf(-d, s, sq), 0.0f), q = fmaf(-d, T, Q);
+                const float r = rsqrtf((layer ? m2 * shape.inv_c : fmaf(mu, mu, m2 * shape.inv_c)) + p.eps);
+                const pair_t rr = twice(r), minus_q = twice(-r * shape.inv_c * (layer ? q : fmaf(mu, T, q)));
+                const pair_t minus_mean = twice(layer && active ? -mu : 0.0f), minus_tbar = twice(layer && active ? -T * shape.inv_c : 0.0f);
+                pair_t x[4], x2[4];
+                row_of(before, x, x2);
+                if (kJvp) {
+                    if (has_h && active) {
+                        store8(static_cast<TX*>(p.xn) + at, x, p.wide);
+                        store8(static_cast<TX*>(p.txn) + at, x2, p.wide);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const pair_t n = mul2(add2(x[i], minus_mean), rr);
+                        const pair_t tn = mul2(rr, fma2(n, minus_q, add2(x2[i], minus_tbar)));
+                        x[i] = fma2(n, mul[i], shift[i]);
+                        x2[i] = fma2(tn, mul[i], fma2(n, tmul[i], tshift[i]));
+                    }
+                    if (active) {
+                        store8(p.y + at, x);
+                        store8(p.ty + at, x2);
+                    }
+                } else {
+                    pair_t g[4], h[4];
+                    if (has_dxn) load_slot<TX>(before + at_x2, lane, g); else zero4(g);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const pair_t n = mul2(add2(x[i], minus_mean), rr);
+                        sum_dy[i] = add2(sum_dy[i], x2[i]);
+                        sum_dyn[i] = fma2(x2[i], n, sum_dyn[i]);
+                        g[i] = fma2(rr, fma2(n, minus_q, fma2(x2[i], mul[i], minus_tbar)), g[i]);
+                    }
+                    if (active) store8(static_cast<TX*>(p.dx) + at, g, p.wide);
+                    if (has_h) {
+                        load_slot<__nv_bfloat16>(before + at_h, lane, h);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            sum_dhn[i] = fma2(g[i], h[i], sum_dhn[i]);
+                            g[i] = mul2(g[i], gate[i]);
+                        }
+                        if (active) store8(p.dh + at, g);
+                    }
+                }
+                at += p.C;
+            }
+            __syncthreads();
+            before = slot;
+            slot += row_bytes;
+            if (slot == ring_end) slot = smem;
+        }
+    } else
     for (int row = row0; row < row1; row += kRows, at += static_cast<long long>(kRows) * p.C) {
         __syncwarp();                                            // (the slot that is filled now was read by the whole warp)
         fetch();

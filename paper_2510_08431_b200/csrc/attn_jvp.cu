@@ -47,7 +47,7 @@ struct DeviceState {
     std::atomic<int> dyn_smem_sparse[2][3];       // ... of the kernels that walk lists of key blocks
     std::atomic<bool> sparse_bwd_ready[2][2];     // launch attribute of sparse_bwd_kernel<D><pass> is set
     std::atomic<bool> topk_ready[2];              // ... of block_topk_kernel<8>, <4>
-    std::atomic<bool> adaln_ready[2][3][3];       // launch attribute of adaln_kernel<x fp32><mode><wide> is set
+    std::atomic<bool> adaln_ready[2][3][2][3];    // launch attribute of adaln_kernel<x fp32><mode><a row ahead><width> is set
     std::atomic<void*> static_scratch{nullptr};   // device address of the built-in scratch array
 };
 DeviceState g_dev[kMaxDevices];
@@ -673,16 +673,17 @@ bool adaln_shape_ok(int B, int L, int C) {
     return (long double)B * L * C * 4 < 9.0e18L && (long double)B * L < 2.0e9L;
 }
 
-template <typename TX, int MODE, int CLASS>
+template <typename TX, int MODE, int CLASS, bool PIPE = false>
 int adaln_launch(const AdalnParams& p, const AdalnGrid& g, int B, cudaStream_t stream, DeviceState& st) {
     constexpr bool fp32 = sizeof(TX) == 4;
     using Plan = AdalnPlan<MODE, fp32, CLASS>;
-    auto kern = attn_jvp::adaln_kernel<TX, MODE, Plan::rows, Plan::stages, Plan::threads, Plan::ctas>;
-    const int smem = Plan::stages * Plan::rows * attn_jvp::adaln_slot_bytes(fp32, p.h != nullptr, MODE) * g.threads;
+    constexpr int rows = PIPE ? 1 : Plan::rows, stages = PIPE ? (fp32 ? 3 : 4) : Plan::stages;    // (PIPE: two of them are in use)
+    auto kern = attn_jvp::adaln_kernel<TX, MODE, rows, stages, Plan::threads, Plan::ctas, PIPE>;
+    const int smem = stages * rows * attn_jvp::adaln_slot_bytes(fp32, p.h != nullptr, MODE) * g.threads;
     // once per kernel and device: the most this instantiation can ask for (threads that race here set the same value)
-    std::atomic<bool>& ready = st.adaln_ready[fp32][MODE][CLASS];
+    std::atomic<bool>& ready = st.adaln_ready[fp32][MODE][PIPE][CLASS];
     if (!ready.load(std::memory_order_acquire)) {
-        constexpr int most = Plan::stages * Plan::rows * attn_jvp::adaln_slot_bytes(fp32, true, MODE) * Plan::threads;
+        constexpr int most = stages * rows * attn_jvp::adaln_slot_bytes(fp32, true, MODE) * Plan::threads;
         static_assert(most * Plan::ctas <= 220 * 1024, "ring does not fit into shared memory");
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
         if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute(MaxDynamicSharedMemorySize)", e);
@@ -696,6 +697,16 @@ int adaln_launch(const AdalnParams& p, const AdalnGrid& g, int B, cudaStream_t s
 template <int MODE>
 int adaln_dispatch(const AdalnParams& p, const AdalnGrid& g, int B, bool x_fp32, cudaStream_t stream, DeviceState& st) {
     const int cls = g.threads <= 256 ? 0 : g.threads <= 640 ? 1 : 2;
+    if constexpr (MODE != 0) {
+        // With a row ahead (one row at a time, no post norm to wait for): above 2048 channels, where two rows at a time do not
+        // fit the registers (16000 rows of 5120: gradients 213 -> 184 us, with an fp32 stream 262 -> 239; tangents 226 -> 219,
+        // 378 -> 355), and below for a bf16 stream and long runs of rows (40000 rows of 1536: tangents 181 -> 158, gradients
+        // 167 -> 149); an fp32 stream is 0 to 3 % slower there, and runs of under some twenty rows 0 to 10 %.
+        if (p.norm != ATTN_JVP_NORM_NONE && p.post == ATTN_JVP_NORM_NONE) {
+            if (cls == 1) return x_fp32 ? adaln_launch<float, MODE, 1, true>(p, g, B, stream, st) : adaln_launch<__nv_bfloat16, MODE, 1, true>(p, g, B, stream, st);
+            if (cls == 0 && !x_fp32 && g.rows_per_cta >= 24) return adaln_launch<__nv_bfloat16, MODE, 0, true>(p, g, B, stream, st);
+        }
+    }
     if (x_fp32)
         return cls == 0 ? adaln_launch<float, MODE, 0>(p, g, B, stream, st) : cls == 1 ? adaln_launch<float, MODE, 1>(p, g, B, stream, st)
                                                                           : adaln_launch<float, MODE, 2>(p, g, B, stream, st);

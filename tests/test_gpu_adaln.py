@@ -154,6 +154,24 @@ def test_gradients(aj, B, L, C, xt, norm, post):
     grad_checks(aj, a, d, norm, post, g)
 
 
+@pytest.mark.parametrize("B,L,C,xt", [(1, 7301, 1536, torch.bfloat16), (2, 9001, 520, torch.bfloat16), (1, 57001, 64, torch.bfloat16),
+                                      (1, 7200, 2048, torch.bfloat16), (1, 150, 5120, torch.bfloat16), (3, 50, 2056, torch.float32),
+                                      (1, 1, 4096, torch.float32)])
+@pytest.mark.parametrize("norm,has_h", [("layer", True), ("rms", True), ("layer", False)])
+def test_long_runs_without_a_post_norm(aj, B, L, C, xt, norm, has_h):
+    """The rows of a CTA overlap here (a row's sums are formed while the row before is finished), in every combination."""
+    a, t, d = make(B, L, C, xt, has_h=has_h)
+    x, y, tx, ty = aj.adaln_jvp(**a, norm=norm, eps=1e-6, **t)
+    (rx, ry), (rtx, rty) = reference(a, norm, None, 1e-6, t=t)
+    for n, g, r in (("x'", x, rx), ("y", y, ry), ("tx'", tx, rtx), ("ty", ty, rty)):
+        close(n, g, r)
+    for dx_new, dy in ((d["dx_new"], d["dy"]), (None, d["dy"]), (d["dx_new"], None)):
+        g = aj.adaln_backward(dx_new, dy, **a, norm=norm, eps=1e-6)
+        grad_checks(aj, a, dict(dx_new=dx_new, dy=dy), norm, None, g)
+    for u, v in zip(aj.adaln_backward(d["dx_new"], d["dy"], **a, norm=norm), aj.adaln_backward(d["dx_new"], d["dy"], **a, norm=norm)):
+        assert u is v or torch.equal(u, v)
+
+
 @pytest.mark.parametrize("mods", [(), ("scale",), ("gate", "shift"), ("shift",)])
 @pytest.mark.parametrize("norm,post,has_h", [("layer", None, False), ("rms", None, False), (None, "rms", True), (None, None, True),
                                              ("layer", None, True)])
@@ -220,6 +238,8 @@ def test_rows_whose_mean_is_far_from_zero(aj, C):
     _, y, _, _ = aj.adaln_jvp(x, norm="layer", eps=1e-6)
     ref = adaln_ref.normed(x.double(), "layer", 1e-6)
     assert (y.double() - ref).abs().max() <= 2.0 ** -8 * ref.abs().max() + 20 * 4096 * 2.0 ** -24
+    _, y, _, ty = aj.adaln_jvp(x, norm="layer", eps=1e-6, tx=torch.zeros_like(x))
+    assert (y.double() - ref).abs().max() <= 2.0 ** -8 * ref.abs().max() + 20 * 4096 * 2.0 ** -24 and not ty.any()
 
 
 def test_constant_and_zero_rows(aj):
