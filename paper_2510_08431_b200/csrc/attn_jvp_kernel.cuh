@@ -555,6 +555,9 @@ __host__ __device__ constexpr int score_buffers(int D, int mode) {
 // taken as 0, all of its P~ are 0, and the epilogue's 1 / l as 0.  Each role reads the length and the first entry of its next
 // item's list while it works on the current one (the loads would cost some 800 cycles each at every hand-over).  Items are
 // not streamed into each other: tried, with short lists filled up to one tile per score buffer, 2 to 10 % slower.
+// 12 heads of 32760 tokens at D = 128, 32 of 256 blocks kept: 686 us in a short run (1200 TFLOP/s), 750 in a long
+// one (1000 W, about 1.45 GHz); tangents at 2 x 16 heads of 4096 tokens, 8 of 32 blocks: 162 us; tangents with a constant context at
+// D = 64, 24 heads of 4100 queries, up to 30 of 63 blocks: 156 us.
 template <int D, int MODE, bool kSplit, int kGroups, bool kPair, bool kSparse = false>
 __global__ void __launch_bounds__(num_threads(kGroups), 1)
 attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
