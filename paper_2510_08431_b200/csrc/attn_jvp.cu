@@ -1046,8 +1046,8 @@ template <int D>
 int sparse_bwd_run(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo,
                    attn_jvp::SparseBwdPrep prep, const attn_jvp::SparseBwdArgs& dkv, const attn_jvp::SparseBwdArgs& dq, cudaStream_t stream,
                    DeviceState& st) {
-    const long long threads = (long long)prep.B * prep.n_q * kSelBlock * prep.H * (D / 8);
-    prep.row_blocks = (int)((threads + 255) / 256);
+    const long long rows = (long long)prep.B * prep.n_q * kSelBlock * prep.H;
+    prep.row_blocks = (int)((rows + attn_jvp::kPrepRows<D> - 1) / attn_jvp::kPrepRows<D>);
     prep.zero_blocks = (dkv.n_items + dq.n_items + 7) / 8;
     attn_jvp::sparse_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + prep.zero_blocks) + order_windows(dkv.n_items), 256, 0, stream>>>(prep);
     const cudaError_t e = cudaGetLastError();

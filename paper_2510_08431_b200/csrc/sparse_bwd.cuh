@@ -24,8 +24,8 @@
 // with the last value MMAs of the one before, and all that an item boundary costs is the hand-over of the accumulators
 // (with one CTA per item a boundary cost about 15 thousand cycles at D = 128, as much as six tiles).
 // Bound by the tensor pipe (active 76 % in kDkv, 70 % in kDq) in short runs and by power in long ones.  12 heads of 32760 tokens at
-// D = 128, 32 of 256 blocks kept: preparation 54, kDkv 1173, kDq 918 us in a short run; D = 64, 12 heads of 4000, lists of
-// eight blocks: 7, 40, 32 us.
+// D = 128, 32 of 256 blocks kept: preparation 46, kDkv 1156, kDq 903 us in a short run; D = 64, 12 heads of 4000, lists of
+// eight blocks: 6, 40, 32 us.
 #pragma once
 
 #include "attn_jvp_kernel.cuh"
@@ -85,6 +85,9 @@ struct SparseBwdPrep {
     int* counters;
     int B, H, Lq, Lk, n_q, n_k, row_blocks, zero_blocks;
 };
+constexpr int kPrepEach = 2;                 // rows per thread, their loads in flight together
+template <int D>
+constexpr unsigned kPrepRows = kPrepEach * 256 / (D / 8);        // ... per CTA
 template <int D>
 __global__ void __launch_bounds__(256)
 sparse_bwd_prep_kernel(const SparseBwdPrep p) {
@@ -114,37 +117,47 @@ sparse_bwd_prep_kernel(const SparseBwdPrep p) {
         return;
     }
     if (blockIdx.x == 0 && threadIdx.x < 2) p.counters[threadIdx.x] = 0;
-    const int padded = p.n_q * kBwdBlock;
-    const long long n = static_cast<long long>(p.B) * padded * p.H;
-    const long long r = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) / kLanes;
-    const int sub = threadIdx.x % kLanes;
-    // (row order [B][padded][H], that of the tensors)
-    const long long bl = min(r, n - 1) / p.H;
-    const int h = static_cast<int>(min(r, n - 1) - bl * p.H);
-    const int b = static_cast<int>(bl / padded), l = static_cast<int>(bl - static_cast<long long>(b) * padded);
-    float sum = 0.0f;
-    if (l < p.Lq) {
-        const long long at = ((static_cast<long long>(b) * p.Lq + l) * p.H + h) * kLanes + sub;
-        const uint4 x = __ldg(p.o + at), y = __ldg(p.d_o + at);
-        const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+    // (row order [B][padded][H], that of the tensors; their number fits 32 bits)
+    const unsigned padded = p.n_q * kBwdBlock, n = static_cast<unsigned>(p.B) * padded * p.H;
+    const unsigned r0 = blockIdx.x * kPrepRows<D> + threadIdx.x / kLanes, sub = threadIdx.x % kLanes;
+    constexpr unsigned kStep = 256 / kLanes;
+    uint4 x[kPrepEach], y[kPrepEach];
+    unsigned b[kPrepEach], l[kPrepEach], h[kPrepEach];
+#pragma unroll
+    for (int u = 0; u < kPrepEach; ++u) {
+        const unsigned r = min(r0 + u * kStep, n - 1), bl = r / p.H;
+        h[u] = r - bl * p.H;
+        b[u] = bl / padded;
+        l[u] = bl - b[u] * padded;
+        x[u] = y[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (l[u] < static_cast<unsigned>(p.Lq)) {
+            const long long at = ((static_cast<long long>(b[u]) * p.Lq + l[u]) * p.H + h[u]) * kLanes + sub;
+            x[u] = __ldg(p.o + at);
+            y[u] = __ldg(p.d_o + at);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kPrepEach; ++u) {
+        const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w}, ys[4] = {y[u].x, y[u].y, y[u].z, y[u].w};
+        float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             sum = fmaf(__uint_as_float(xs[i] << 16), __uint_as_float(ys[i] << 16), sum);
             sum = fmaf(__uint_as_float(xs[i] & 0xFFFF0000u), __uint_as_float(ys[i] & 0xFFFF0000u), sum);
         }
-    }
 #pragma unroll
-    for (int m = kLanes / 2; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-    if (sub == 0 && r < n) {
-        const long long bh = static_cast<long long>(b) * p.H + h;
-        float ls = INFINITY;
-        if (l < p.Lq) {
-            ls = p.lse[bh * p.Lq + l] * 1.4426950408889634f;
-            if (ls == -INFINITY) ls = INFINITY;
+        for (int m = kLanes / 2; m >= 1; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+        if (sub == 0 && r0 + u * kStep < n) {
+            const long long bh = static_cast<long long>(b[u]) * p.H + h[u];
+            float ls = INFINITY;
+            if (l[u] < static_cast<unsigned>(p.Lq)) {
+                ls = p.lse[bh * p.Lq + l[u]] * 1.4426950408889634f;
+                if (ls == -INFINITY) ls = INFINITY;
+            }
+            float* out = p.rows + 2 * bh * padded + (l[u] / kBwdBlock) * (2 * kBwdBlock) + l[u] % kBwdBlock;
+            out[0] = ls;
+            out[kBwdBlock] = sum;
         }
-        float* out = p.rows + 2 * bh * padded + (l / kBwdBlock) * (2 * kBwdBlock) + l % kBwdBlock;
-        out[0] = ls;
-        out[kBwdBlock] = sum;
     }
 }
 
