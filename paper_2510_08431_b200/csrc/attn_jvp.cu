@@ -17,7 +17,7 @@
 
 namespace {
 
-using attn_jvp::KernelArgs;
+using attn_jvp::ListKernelArgs;
 
 constexpr int kVersion = 100;   // 0.1.0
 constexpr int kMaxDevices = 64;
@@ -185,7 +185,7 @@ bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
 }
 
 template <int D, int MODE, bool SPLIT, int GROUPS, bool PAIR = false, bool SPARSE = false>
-int launch(const CUtensorMap* maps, const KernelArgs& ka, dim3 grid, cudaStream_t stream, DeviceState& st) {
+int launch(const CUtensorMap* maps, const ListKernelArgs& ka, dim3 grid, cudaStream_t stream, DeviceState& st) {
     auto kern = attn_jvp::attn_jvp_fwd_kernel<D, MODE, SPLIT, GROUPS, PAIR, SPARSE>;
     using Plan = attn_jvp::SmemPlan<D, MODE, GROUPS, PAIR, SPLIT>;
     std::atomic<int>& slot = SPARSE ? st.dyn_smem_sparse[D == 128][MODE]
@@ -339,7 +339,7 @@ int run(const void* q, const void* k, const void* v, const void* tq, const void*
     // K once more with boxes of half a key tile (the CTA-pair kernel splits the operand of tQ K^T by rows)
     if (int rc = make_map(&maps[8], k, B, Lk, H, D, attn_jvp::kBlockN / 2)) return rc;
 
-    KernelArgs ka;
+    ListKernelArgs ka = {};
     ka.o = reinterpret_cast<__nv_bfloat16*>(o);
     ka.to = reinterpret_cast<__nv_bfloat16*>(to);
     ka.lse = lse;
@@ -359,8 +359,6 @@ int run(const void* q, const void* k, const void* v, const void* tq, const void*
     ka.splits = eff_splits;
     ka.tiles_per_split = tiles_per_split;
     ka.part_o = ka.part_to = ka.part_lse = ka.part_mu = nullptr;
-    ka.list = ka.tiles = nullptr;
-    ka.list_stride = 0;
     if (split) {
         char* w = static_cast<char*>(workspace);
         ka.part_o = reinterpret_cast<float*>(w);
@@ -975,7 +973,7 @@ int sparse_fwd(const void* q, const void* k, const void* v, const void* tq, cons
     if (int rc = make_map(&maps[6], o, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
     maps[7] = maps[6];
     if (!fwd_only) if (int rc = make_map(&maps[7], to, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
-    KernelArgs ka = {};
+    ListKernelArgs ka = {};
     ka.o = static_cast<__nv_bfloat16*>(o);
     ka.to = static_cast<__nv_bfloat16*>(to);
     ka.lse = lse;
@@ -991,10 +989,7 @@ int sparse_fwd(const void* q, const void* k, const void* v, const void* tq, cons
     ka.splits = 1;
     ka.n_q_tiles = n_blocks(Lq);
     ka.n_items = ka.n_q_tiles * H * B;
-    ka.list = index;
-    ka.tiles = tiles;
-    ka.order = order;
-    ka.list_stride = n_blocks(Lk);
+    ka.lists = {index, tiles, order, n_blocks(Lk)};
     const dim3 grid((unsigned)(ka.n_items < st.sm_count ? ka.n_items : st.sm_count), 1, 1);
     // softmax groups as softmax_groups_for() chooses them for long items
     if (D == 64) {

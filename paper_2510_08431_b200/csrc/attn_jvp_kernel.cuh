@@ -37,6 +37,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace attn_jvp {
 
 constexpr int kBlockM = 128;        // query rows per CTA (B_r)
@@ -122,13 +124,27 @@ struct KernelArgs {
     int B;
     int n_q_tiles;      // 128-row query tiles per (batch, head)
     int n_items;        // work items = n_q_tiles * H * B * splits; the grid's CTAs share them round-robin
-    // attention over selected key blocks (kSparse): per work item the ascending list of its 128-key blocks and its length
-    // in 64-key tiles (a last block of at most 64 keys is one tile)
-    const int* list;    // [B][H][n_q_tiles][list_stride]
+};
+// Attention over selected key blocks (kSparse): per work item the ascending list of its 128-key blocks and its length in
+// 64-key tiles (a last block of at most 64 keys is one tile).
+struct KeyLists {
+    const int* list;    // [B][H][n_q_tiles][stride]
     const int* tiles;   // [B][H][n_q_tiles]
     const int* order;   // the lists in the order of their work (block_order()); null: as they lie
-    int list_stride;
+    int stride;
 };
+// Which form of the kernel has the lists among its parameters.  The list form needs them; in the dense forms they change nothing
+// but how the compiler allocates and schedules, and there they are left out where that costs time: the tangent-free CTA pair
+// spills 52 / 396 bytes (stores / loads) with them and 24 / 136 without (cross-attention, 40 heads of 32760 queries and 512 keys:
+// 645 against 622 us; full JVP at D = 64, image length: 566 against 559).  Forward only is faster with them (image length, D = 128:
+// 268 against 284 us; D = 64: 308 against 332).
+struct ListKernelArgs : KernelArgs {
+    KeyLists lists;
+};
+template <int MODE, bool kSparse>
+using KernelArgsOf = std::conditional_t<kSparse || MODE == kModeFwdOnly, ListKernelArgs, KernelArgs>;
+__device__ __forceinline__ KeyLists lists_of(const KernelArgs&) { return {}; }
+__device__ __forceinline__ KeyLists lists_of(const ListKernelArgs& a) { return a.lists; }
 
 // Shared-memory plan of a kernel variant.
 //   One Q/tQ buffer (full JVP at D = 128, and every CTA-pair variant): Q, tQ resident, ring slots of one primal +
@@ -564,7 +580,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_tq,
                     const __grid_constant__ CUtensorMap tm_tk, const __grid_constant__ CUtensorMap tm_tv,
                     const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ CUtensorMap tm_to,
-                    const __grid_constant__ CUtensorMap tm_k32, const KernelArgs args) {
+                    const __grid_constant__ CUtensorMap tm_k32, const KernelArgsOf<MODE, kSparse> args) {
     static_assert(!kPair || (D == 128 && !kSplit), "the CTA-pair variant exists at D = 128, without key chunks");
     static_assert(!kSparse || (!kPair && !kSplit), "key block lists: one CTA per query tile, no key chunks");
     using Plan = SmemPlan<D, MODE, kGroups, kPair, kSplit>;
@@ -621,6 +637,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const bool lead_cta = cta_rank == 0u;
     const int first_item = kPair ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
     const int item_stride = kPair ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
+    const KeyLists lists = lists_of(args);
     struct Item { int q0, h, b, split, tile0, n_kv; int n_real, first; const int* list; };
     // Work item number -> (query tile, head, batch [, chunk]).  The roles walk their items with a fixed stride, so
     // after the first item the three indices are advanced by the stride's own decomposition (carry by compare and
@@ -634,13 +651,13 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const int item = first_item + round * item_stride;
         if (item >= args.n_items) return args.n_items;
         const bool back = (round & 1) != 0 && (round + 1) * item_stride <= args.n_items;
-        return min(max(__ldg(args.order + (back ? round * item_stride + item_stride - 1 - first_item : item)), 0), args.n_items - 1);
+        return min(max(__ldg(lists.order + (back ? round * item_stride + item_stride - 1 - first_item : item)), 0), args.n_items - 1);
     };
     // the length of a list and its first entry
     auto read_list = [&](Walk& k, int row) {
         const bool exists = row < args.n_items;
-        k.tiles64 = exists ? __ldg(args.tiles + row) : 0;
-        k.first = exists ? __ldg(args.list + static_cast<size_t>(row) * args.list_stride) : 0;
+        k.tiles64 = exists ? __ldg(lists.tiles + row) : 0;
+        k.first = exists ? __ldg(lists.list + static_cast<size_t>(row) * lists.stride) : 0;
     };
     auto walk_init = [&](int item) -> Walk {
         Walk k{};
@@ -652,7 +669,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     };
     const Walk walk_stride = walk_init(item_stride);
     auto walk_first = [&]() -> Walk {
-        const bool ordered = kSparse && args.order != nullptr;
+        const bool ordered = kSparse && lists.order != nullptr;
         const int row = ordered ? ordered_list(0) : first_item;
         Walk k = walk_init(row);
         if (kSparse) read_list(k, row);
@@ -661,7 +678,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     };
     // to item number `item`, item_stride items on
     auto walk_step = [&](Walk& k, int item) {
-        if (kSparse && args.order != nullptr) {
+        if (kSparse && lists.order != nullptr) {
             const int row = k.after, round = k.round + 1;
             k = walk_init(min(row, args.n_items - 1));
             read_list(k, row);
@@ -688,8 +705,8 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         w.n_real = w.first = 0;
         if (kSparse) {
             const int row = (k.z * args.H + k.h) * args.n_q_tiles + k.qt;
-            const int tiles64 = min(k.tiles64, 2 * args.list_stride);
-            w.list = args.list + static_cast<size_t>(row) * args.list_stride;
+            const int tiles64 = min(k.tiles64, 2 * lists.stride);
+            w.list = lists.list + static_cast<size_t>(row) * lists.stride;
             w.first = k.first;
             w.n_real = kBN == kBlockN ? tiles64 : (tiles64 + 1) / 2;
             w.n_kv = max(1, w.n_real);
@@ -699,7 +716,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     // first key of tile j of an item (a tile that only fills up: behind the last key, where TMA fills in zeros)
     auto key_of = [&](const Item& w, int j) -> int {
         if (!kSparse) return (w.tile0 + j) * kBN;
-        if (j >= w.n_real) return args.list_stride * kBlockM;
+        if (j >= w.n_real) return lists.stride * kBlockM;
         const int e = kBN == kBlockN ? j >> 1 : j;
         const int block = e == 0 ? w.first : __ldg(w.list + e);
         return block * kBlockM + (kBN == kBlockN ? (j & 1) * kBlockN : 0);
