@@ -164,23 +164,28 @@ sparse_bwd_prep_kernel(const SparseBwdPrep p) {
 // 2^x of two values on the FMA pipe, for kernels whose pace the special-function unit sets (8 cycles per warp instruction):
 // x = n + f with n the nearest integer (added and taken off again as 1.5 * 2^23 + n), 2^f by a polynomial on [-1/2, 1/2]
 // whose coefficients minimise the largest relative error with p(0) = 1 (2.9e-6 in fp32; P is rounded to bf16 for the value
-// products, an error of 3.9e-3, and sums of P take the error on average), and n added to the exponent field.  x below
-// -127 is taken as -127, where p(0) = 1 makes the result exactly +0; x must not exceed 127.
+// products, an error of 3.9e-3, and sums of P take the error on average), times 2^n.  x below -127 is taken as -127, where the
+// factor is exactly +0; a NaN stays one (hence a maximum that hands NaN on, and a product instead of an addition to the exponent
+// field, which would make a number of it); x must not exceed 127.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 __device__ __forceinline__ void exp2_poly_pair(uint64_t x, float& p0, float& p1) {
     float x0, x1;
     unpack_f32x2(x, x0, x1);
-    x = pack_f32x2(fmaxf(x0, -127.0f), fmaxf(x1, -127.0f));
+    x = pack_f32x2(max_nan(x0, -127.0f), max_nan(x1, -127.0f));
     const uint64_t t = add_f32x2(x, pack_f32x2(12582912.0f, 12582912.0f));
     const uint64_t f = add_f32x2(x, fma_f32x2(t, pack_f32x2(-1.0f, -1.0f), pack_f32x2(12582912.0f, 12582912.0f)));
     uint64_t y = fma_f32x2(f, pack_f32x2(0x1.3a02ccp-7f, 0x1.3a02ccp-7f), pack_f32x2(0x1.c9fc46p-5f, 0x1.c9fc46p-5f));
     y = fma_f32x2(f, y, pack_f32x2(0x1.ec037ap-3f, 0x1.ec037ap-3f));
     y = fma_f32x2(f, y, pack_f32x2(0x1.62e12cp-1f, 0x1.62e12cp-1f));
     y = fma_f32x2(f, y, pack_f32x2(1.0f, 1.0f));
-    float t0, t1, y0, y1;
+    float t0, t1;
     unpack_f32x2(t, t0, t1);
-    unpack_f32x2(y, y0, y1);
-    p0 = __int_as_float(__float_as_int(y0) + (__float_as_int(t0) << 23));
-    p1 = __int_as_float(__float_as_int(y1) + (__float_as_int(t1) << 23));
+    const uint64_t two_n = pack_f32x2(__int_as_float((__float_as_int(t0) << 23) + 0x3F800000), __int_as_float((__float_as_int(t1) << 23) + 0x3F800000));
+    unpack_f32x2(mul_f32x2(y, two_n), p0, p1);
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"

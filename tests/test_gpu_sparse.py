@@ -321,6 +321,25 @@ def test_nothing_is_read_where_nothing_is_kept(aj, D):
     assert not got["dk"][:, 256:384].any() and not got["dv"][:, 256:384].any()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_nan_in_one_query_reaches_its_gradients(aj, D):
+    """P of a query with a NaN is NaN for every key it keeps, whichever row of its block it is: dQ of the row, dK and dV of its
+    key blocks show it, and nothing else does."""
+    B, H, Lq, Lk = 1, 1, 300, 400
+    mask = torch.tensor([[[[1, 0, 1, 1], [0, 1, 0, 1], [1, 1, 1, 1]]]], dtype=torch.bool, device="cuda")
+    sel = aj.block_selection(mask, Lq, Lk)
+    for row in [128 + r for r in range(20)] + [128 + 126, 128 + 127]:
+        x = inputs(B, H, Lq, Lk, D)
+        x["q"][0, row, 0, 3] = float("nan")
+        o, _, lse = aj.sparse_attention_jvp(x["q"], x["k"], x["v"], sel, fwd_only=True)
+        dq, dk, dv = aj.sparse_attention_backward(x["d_o"], x["q"], x["k"], x["v"], o, lse, sel)
+        no_timeout(aj)
+        kept = mask[0, 0, 1].repeat_interleave(128)[:Lk]
+        assert dq[0, row].isnan().all() and dq.isnan().sum() == D, row
+        for n, g in (("dk", dk), ("dv", dv)):
+            assert g[0, kept].isnan().all() and g[0, ~kept].isfinite().all(), (n, row)
+
+
 def test_outputs_between_sectors_and_given_buffers(aj):
     """Gradients 16 bytes off a 32-byte boundary, outputs and workspaces of the caller: the same bits."""
     B, H, Lq, Lk, D = 1, 3, 300, 450, 64
