@@ -341,7 +341,8 @@ int attn_jvp_adaln_bwd(const attn_jvp_adaln_t* in, const void* dx_new, const voi
  * tensors; results are defined for lists that one of the two calls wrote.
  *
  * attn_jvp_block_select -- keeps, for every query block, the min(topk, n_k) key blocks with the largest
- * mean(q over the block) . mean(k over the block), formed in 64 bits, ties going to the lower key block.
+ * mean(q over the block) . mean(k over the block), formed in 64 bits, ties going to the lower key block.  Infinities and NaN
+ * follow IEEE arithmetic, and a score that is NaN counts as larger than any other (equal to another NaN).
  *   workspace  device, 16-byte aligned, attn_jvp_block_select_workspace_bytes(...) bytes.
  * attn_jvp_block_lists -- index, tiles and order (NULL: not wanted) of a mask that the caller made.  (Rows of
  * attn_jvp_block_select are of one length and need no order.)

@@ -7,7 +7,9 @@
 // going to the lower key block.  One wrong comparison exchanges 128 keys of 128 queries, so the order has to be that of
 // the scores themselves: means and dot products are formed in 64 bits, where the sum of 128 bf16 values is exact unless
 // their exponents lie more than 38 apart.  (In 32 bits neighbours around the topk-th place, about a hundredth of a
-// deviation apart, would change places a few times per call of a long video.)  The arithmetic is cheap all the same:
+// deviation apart, would change places a few times per call of a long video.)  Infinities and NaN go through means and
+// scores by the rules of IEEE arithmetic, and a score that is NaN counts as the largest: a block that holds one is kept, and the
+// NaN shows in the result, instead of dropping out of it.  The arithmetic is cheap all the same:
 // tokens / 128 means per head, 0.17 G multiply-adds for 12 heads of 32760 tokens, while reading q and k once bounds the
 // whole selection (201 MB there, 31 us).
 #pragma once
@@ -23,8 +25,11 @@ constexpr int kPoolCols = 16;        // 16-byte pieces (8 channels) of a row it 
 
 // A bf16 value's bits (the upper half of `u`) as the upper word of a double, without a conversion to fp64 (a quarter-rate
 // instruction): sign, exponent and mantissa land in place with the exponent field taken as it is, which scales every finite
-// value, subnormal ones included, by exactly 2^-896.
+// value, subnormal ones included, by exactly 2^-896.  (An infinity or NaN comes out as a finite number, see not_finite().)
 __device__ __forceinline__ double scaled_bf16(int u) { return __hiloint2double((u >> 3) & 0x8FFFE000, 0); }
+// Bit 15 or 31 is set if the lower or upper of two bf16 values is an infinity or NaN (other bits: anything): an exponent
+// field of ones carries into the sign's place.
+__device__ __forceinline__ uint32_t not_finite(uint32_t two) { return (two & 0x7FFF7FFFu) + 0x00800080u; }
 
 // Block means of q and k in one launch.  q, k: [B][L][H * D] bf16.  qm: [B * H][n_q][D] fp64, kmt: [B * H][D][n_k] fp64 (a
 // channel's values of all key blocks side by side, as the scores read them).
@@ -67,6 +72,7 @@ block_mean_kernel(const uint4* __restrict__ q, const uint4* __restrict__ k, doub
     for (int item = blockIdx.x; item < n_items; item += gridDim.x, turn ^= 1) {
         const Work next = work(n_items - item > static_cast<int>(gridDim.x) ? item + gridDim.x : n_items);
         double s[8];
+        uint32_t bad = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] = 0.0;
 #pragma unroll
@@ -78,7 +84,12 @@ block_mean_kernel(const uint4* __restrict__ q, const uint4* __restrict__ k, doub
             for (int i = 0; i < 4; ++i) {
                 s[2 * i] += scaled_bf16(static_cast<int>(u[i] << 16));
                 s[2 * i + 1] += scaled_bf16(static_cast<int>(u[i]));
+                bad |= not_finite(u[i]);
             }
+        }
+        if (bad & 0x80008000u) {                                 // (rare: the channel's sum is then taken again below)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = __longlong_as_double(0x7FF8000000000000ll);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) part[turn][group][i * kPoolCols + piece] = s[i];
@@ -92,7 +103,15 @@ block_mean_kernel(const uint4* __restrict__ q, const uint4* __restrict__ k, doub
 #pragma unroll
             for (int g = 0; g < kPoolRows; ++g) sum += part[turn][g][at];
             // (every term is a multiple of 2^-1029, far above the last place of a subnormal double: nothing is lost down there)
-            const double mean = sum * 0x1p896 / static_cast<double>(w.rows);
+            double mean = sum * 0x1p896 / static_cast<double>(w.rows);
+            if (isnan(sum)) {                                    // an infinity or NaN near this channel: unscaled, in IEEE arithmetic
+                const long long token = static_cast<long long>(w.b) * (w.keys ? Lk : Lq) + w.block * kSelBlock;
+                const unsigned short* x = reinterpret_cast<const unsigned short*>(w.keys ? k : q) + token * H * D + channel;
+                mean = 0.0;
+#pragma unroll 1
+                for (int r = 0; r < w.rows; ++r) mean += static_cast<double>(__uint_as_float(static_cast<uint32_t>(x[static_cast<long long>(r) * H * D]) << 16));
+                mean /= static_cast<double>(w.rows);
+            }
             const int h = channel / D, d = channel - h * D;
             const long long bh = static_cast<long long>(w.b) * H + h;
             if (w.keys) kmt[(bh * D + d) * n_k + w.block] = mean;
@@ -102,8 +121,9 @@ block_mean_kernel(const uint4* __restrict__ q, const uint4* __restrict__ k, doub
     }
 }
 
-// 64-bit keys whose unsigned order is the order of the doubles.
+// 64-bit keys whose unsigned order is the order of the doubles, with every NaN above the rest.
 __device__ __forceinline__ unsigned long long ordered_key(double v) {
+    if (isnan(v)) return ~0ull;
     const long long b = __double_as_longlong(v + 0.0);           // (-0 becomes +0: equal scores have equal keys)
     return b < 0 ? ~static_cast<unsigned long long>(b) : static_cast<unsigned long long>(b) | 0x8000000000000000ull;
 }
@@ -215,7 +235,7 @@ block_topk_kernel(const double* __restrict__ qm, const double* __restrict__ kmt,
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const int j = lane + 32 * u;
-                own[u] = j < n_k ? row_keys[j] : 0ull;           // (0 is below every key of a finite score)
+                own[u] = j < n_k ? row_keys[j] : 0ull;           // (0 is below every key of a score)
                 if (j < n_k) { all_or |= own[u]; all_and &= own[u]; }
             }
             for (int m = 16; m >= 1; m >>= 1) {

@@ -59,7 +59,7 @@ class BlockSelection(NamedTuple):
 
 def block_select(q, k, topk, workspace=None) -> BlockSelection:
     """For every (batch, head, block of 128 queries) the ``topk`` key blocks whose mean key has the largest dot product with
-    the block's mean query (64-bit arithmetic, ties to the lower block; all of them where there are fewer).
+    the block's mean query (64-bit arithmetic, ties to the lower block, NaN above everything; all of them where there are fewer).
 
     q: [B][Lq][H][D], k: [B][Lk][H][D], contiguous CUDA bf16, D = 64 or 128.  ``workspace``: a CUDA uint8 tensor of at least
     attn_jvp_block_select_workspace_bytes(B, H, Lq, Lk, D)."""

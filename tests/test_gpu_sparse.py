@@ -225,6 +225,41 @@ def test_selection_of_tiny_and_huge_values(aj):
         assert torch.equal(aj.block_select(qq, kk, 4).mask, R.top_mask(qq, kk, 4))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n_k", [6, 300])
+@pytest.mark.parametrize("bad", ["nan", "inf", "-inf", "both", "nan_and_inf", "query", "all_queries"])
+def test_selection_with_infinities_and_nan(aj, D, n_k, bad):
+    """They follow IEEE arithmetic through means and scores, and NaN scores come first, ties to the lower block, as a stable
+    descending sort has them (the reference sorts on the CPU, which orders NaN by value and not by sign)."""
+    B, H, Lq, Lk = 2, 2, 400, n_k * 128 - 50
+    x = inputs(B, H, Lq, Lk, D)
+    q, k = x["q"], x["k"]
+    inf, nan = float("inf"), float("nan")
+    if bad == "nan":
+        k[0, 128 * 4 + 77, 1, 5] = nan
+        k[1, 128 * 2, 0, D - 1] = -nan
+    elif bad == "inf":
+        k[0, 130, 0, 9] = inf
+        k[1, Lk - 1, 1, 0] = inf
+    elif bad == "-inf":
+        k[:, 128 * 3 + 127, :, D // 2] = -inf
+    elif bad == "both":
+        k[0, 128, 1, 1], k[0, 255, 1, 1] = inf, -inf          # one channel's mean is NaN
+        k[1, 128, 1, 1], k[1, 300, 1, 2] = inf, -inf          # two blocks, each infinite
+    elif bad == "nan_and_inf":
+        k[:, 10, :, 3], k[:, 140, :, 3], k[:, 500, :, 7] = nan, inf, nan
+    elif bad == "query":
+        q[0, 129, 0, 2], q[1, 399, 1, 8] = nan, inf
+    else:
+        q[:, :, :, 4] = inf
+        k[:, 128:256, :, 4] = 0.0                             # 0 times infinity
+    for topk in (1, 2, 5):
+        sel = aj.block_select(q, k, topk)
+        assert torch.equal(sel.mask.cpu(), R.top_mask(q.cpu(), k.cpu(), topk)), topk
+        assert (sel.mask.sum(-1) == topk).all()
+        lists(sel)
+
+
 def test_select_attend_and_train_together(aj):
     """The path as it is used: selection, forward, gradients; two passes give the same bits."""
     B, H, Lq, Lk, D = 1, 4, 2100, 2500, 128
