@@ -121,11 +121,12 @@ block_mean_kernel(const uint4* __restrict__ q, const uint4* __restrict__ k, doub
     }
 }
 
-// 64-bit keys whose unsigned order is the order of the doubles, with every NaN above the rest.
+// 64-bit keys whose unsigned order is the order of the doubles, with every NaN above the rest.  (NaN is told by its bits: an fp64
+// comparison and its branch per score made the top-k 25 % slower, 16.7 -> 21 us for 4 heads of 148 x 148 blocks.)
 __device__ __forceinline__ unsigned long long ordered_key(double v) {
-    if (isnan(v)) return ~0ull;
     const long long b = __double_as_longlong(v + 0.0);           // (-0 becomes +0: equal scores have equal keys)
-    return b < 0 ? ~static_cast<unsigned long long>(b) : static_cast<unsigned long long>(b) | 0x8000000000000000ull;
+    const unsigned long long u = static_cast<unsigned long long>(b), key = b < 0 ? ~u : u | 0x8000000000000000ull;
+    return (u & 0x7FFFFFFFFFFFFFFFull) > 0x7FF0000000000000ull ? ~0ull : key;
 }
 
 // Writes one row of a selection: mask bytes (optional), the ascending list and its length in 64-token tiles (a last
