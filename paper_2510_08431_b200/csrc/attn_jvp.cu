@@ -144,11 +144,21 @@ int current_device(int* dev_out, DeviceState** st_out) {
     return 0;
 }
 
-// The pinned status word a kernel writes its timeout code to; allocated on the first call that may allocate.
+// What cudaHostAlloc is not allowed while a stream is being captured (in the default, global capture mode), this thread may do
+// meanwhile: the allocation has no part in the captured work.
+struct RelaxedCapture {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    RelaxedCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+    ~RelaxedCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+};
+
+// The pinned status word a kernel writes its timeout code to; allocated on the first call that may allocate, which may be one
+// that is captured into a graph.
 int ensure_status_word(DeviceState& st) {
     if (st.host_status.load(std::memory_order_acquire)) return 0;
     std::lock_guard<std::mutex> guard(st.lock);
     if (st.host_status.load(std::memory_order_relaxed)) return 0;
+    const RelaxedCapture relaxed;
     int* hp = nullptr;
     cudaError_t e = cudaHostAlloc((void**)&hp, sizeof(int), cudaHostAllocMapped);
     if (e != cudaSuccess) return cuda_fail("cudaHostAlloc(status word)", e);
