@@ -6,6 +6,7 @@
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -72,17 +73,16 @@ at::Tensor scratch(PyObject* o, const at::Tensor& on, size_t need) {
 }
 int size32(int64_t v) { return v > 0x7fffffff ? 0x7fffffff : static_cast<int>(v); }      // (sizes that large are refused by the library)
 
-// What every function does around its body: exceptions become Python's, and nothing gets past this point.
+// What every function does around its body: exceptions become Python's (torch's own those that it raises for them, as
+// torch.OutOfMemoryError), and nothing gets past this point.
 template <typename F>
 PyObject* guarded(F&& body) {
     try {
         return body();
     } catch (const Refused& e) {
         PyErr_SetString(PyExc_ValueError, e.what());
-    } catch (const c10::Error& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
-    } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        torch::translate_exception_to_python(std::current_exception());
     }
     return nullptr;
 }
