@@ -136,7 +136,7 @@ def host():
         try:
             from . import _host
         except ImportError as e:
-            raise RuntimeError("_host.so is missing or does not load: build it with `python -m paper_2510_08431_b200.build` "
+            raise RuntimeError(f"_host.so is missing or does not load ({e}): build it with `python -m paper_2510_08431_b200.build` "
                                "(there is no fallback path)") from e
         names = ("adaln_fwd", "adaln_bwd", "adaln_bwd_workspace_bytes", "block_select", "block_select_workspace_bytes",
                  "block_lists", "sparse_fwd", "sparse_bwd", "sparse_bwd_workspace_bytes")

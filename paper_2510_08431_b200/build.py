@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import shutil
 import subprocess
+import warnings
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -15,6 +16,7 @@ DEPS = [SRC, os.path.join(PKG, "csrc", "attn_jvp_kernel.cuh"), os.path.join(PKG,
 LIB = os.path.join(PKG, "libattn_jvp.so")
 HOST_SRC = os.path.join(PKG, "csrc", "host_binding.cpp")
 HOST_LIB = os.path.join(PKG, "_host.so")
+HOST_STAMP = HOST_LIB + ".stamp"         # what the host binding was built against
 
 
 def _nvcc() -> str:
@@ -32,10 +34,24 @@ def is_stale() -> bool:
     return _older(LIB, DEPS)
 
 
+def _host_stamp() -> str:
+    import sys
+
+    import torch
+    return f"torch {torch.__version__}, {sys.implementation.cache_tag}"
+
+
+def host_is_stale() -> bool:
+    """The host binding is missing, older than its sources, or of another torch or Python (whose module would not load)."""
+    if _older(HOST_LIB, [HOST_SRC, os.path.join(ROOT, "include", "attn_jvp.h")]) or not os.path.exists(HOST_STAMP):
+        return True
+    with open(HOST_STAMP) as f:
+        return f.read() != _host_stamp()
+
+
 def build_host(force: bool = False) -> str:
-    """Compiles the host binding (a CPython module against the installed torch) if it is missing or older than its sources."""
-    deps = [HOST_SRC, os.path.join(ROOT, "include", "attn_jvp.h")]
-    if not force and not _older(HOST_LIB, deps):
+    """Compiles the host binding (a CPython module against the installed torch) if it is stale."""
+    if not force and not host_is_stale():
         return HOST_LIB
     import sysconfig
 
@@ -52,14 +68,27 @@ def build_host(force: bool = False) -> str:
     if res.returncode != 0:
         raise RuntimeError("g++ failed:\n" + res.stdout + res.stderr)
     os.replace(tmp, HOST_LIB)
+    with open(tmp, "w") as f:
+        f.write(_host_stamp())
+    os.replace(tmp, HOST_STAMP)
     return HOST_LIB
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compiles the library and the host binding where they are missing or older than their sources; returns the library's path."""
-    build_host(force)
-    if not force and not is_stale():
-        return LIB
+    """Compiles the library where it is missing or older than its sources, and after it the host binding; returns the library's path.
+
+    The library needs nvcc alone.  The host binding needs torch's and Python's C++ headers; where it cannot be built, that is a
+    warning here, the C ABI and the calls that go through ctypes work, and those that need the binding raise."""
+    if force or is_stale():
+        _build_library(verbose)
+    try:
+        build_host(force)
+    except (RuntimeError, OSError) as e:
+        warnings.warn(f"the host binding is not built, adaln_*, block_sele* and sparse_attention_* will not work: {e}", RuntimeWarning)
+    return LIB
+
+
+def _build_library(verbose: bool) -> None:
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
            "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-o", tmp, SRC, "-lcudart"]
@@ -73,7 +102,6 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     os.replace(tmp, LIB)
     if verbose:
         print(res.stderr)
-    return LIB
 
 
 if __name__ == "__main__":
