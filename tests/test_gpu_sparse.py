@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2510_08431_b200 import synth
+from tests import sparse_differences as F
 from tests import sparse_ref as R
 
 pytestmark = pytest.mark.gpu
@@ -301,6 +302,23 @@ def test_gradients_against_differences(aj):
         want = (loss(e, n, d) - loss(-e, n, d)) / (2 * e)
         got = (grad.double()[0, :, 0] * d).sum()
         assert abs(got - want) <= (ref["d" + n][1][0, :, 0] * d.abs()).sum() + 1e-6 * abs(want)
+
+
+@pytest.mark.parametrize("D,scale", [(64, None), (128, None), (64, -0.2)])
+def test_gradients_along_their_own_directions(aj, D, scale):
+    """<gradient, direction> = central difference of the 64-bit loss, with a tolerance that a wrong gradient exceeds
+    (tests/sparse_differences.py; tests/test_sparse_differences.py shows which mistakes it finds)."""
+    B, H, Lq, Lk = 2, 2, 150, 300
+    x = inputs(B, H, Lq, Lk, D)
+    mask = make_mask("all", B, H, 2, 3)
+    mask[:, :, 0, 1] = False
+    mask[0, 1, 1, 2] = False
+    sel = aj.block_selection(mask, Lq, Lk)
+    o, _, lse = aj.sparse_attention_jvp(x["q"], x["k"], x["v"], sel, fwd_only=True, scale=scale)
+    grads = aj.sparse_attention_backward(x["d_o"], x["q"], x["k"], x["v"], o, lse, sel, scale=scale)
+    no_timeout(aj)
+    rows = F.compare(dict(zip("qkv", grads)), x, mask, D ** -0.5 if scale is None else scale)
+    assert F.passes(rows) == {"q", "k", "v"}, rows
 
 
 def test_rows_behind_the_last_are_left_alone(aj):
