@@ -17,8 +17,9 @@
  * Conventions common to every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller.  The
  *     library neither frees nor retains them and allocates no device memory;
- *     the split-KV and the host-buffer entry points need a (caller-provided)
- *     device workspace, all others need none.
+ *     the entry points with a `workspace` argument (split-KV, host buffers,
+ *     attn_jvp_adaln_bwd, attn_jvp_block_select, attn_jvp_sparse_bwd) need a
+ *     (caller-provided) device workspace, all others need none.
  *   - q, tq, o, to : bf16, layout [B][Lq][H][D] contiguous ("BLHD").
  *     k, v, tk, tv : bf16, layout [B][Lk][H][D] contiguous.
  *     lse          : fp32, layout [B][H][Lq], natural log of the scaled scores.

@@ -14,9 +14,10 @@
 // Hence two fp32 values per instruction (packed fp32x2 arithmetic), kRows rows at a time where one row's chain would not
 // be covered by other CTAs (their shuffles interleave and share the barrier) or one row's sums beside the row before (kPipe),
 // and only what a sum needs is held across it: everything else is read from shared memory again.
-// Measured, inputs in HBM: forward at 32760 x 5120 bf16 213 us (6.3 TB/s, 98 % of a copy's rate), forward and gradients 561 us
-// (4.8 TB/s), tangents at 2 x 4096 x 2048 with an fp32 stream 78 us (5.1 TB/s), with a post norm at 30021 x 1536 bf16 148 us
-// (5.0 TB/s).
+// Measured, inputs in HBM, launch after launch on the GPU alone: forward at 32760 x 5120 bf16 212 us (6.3 TB/s, 98 % of a copy's
+// rate; a single call behind other work, which leaves L2 full of lines to write back, 229 to 239), forward and gradients 556 us
+// (4.8 TB/s; 604 to 633), tangents at 2 x 4096 x 2048 with an fp32 stream 77 us (5.2 TB/s), with a post norm at 3 x 10007 x 1536 bf16
+// 147 us (5.0 TB/s).  Widths between 2048 and 5120 and above 5120 channels are slower: see the launch code's comments.
 // One CTA works down a range of rows, thread t owns channels 8 t .. 8 t + 7 (16-byte accesses) and keeps that batch's
 // modulation of its channels in registers, so HBM sees each row once and the modulation about never.  Rows come in
 // through cp.async into a slot of shared memory that only the issuing warp reads back: the ring needs no block-wide

@@ -650,6 +650,9 @@ constexpr int kSms = 148;            // grids and workspaces are laid out for a 
 // budgeted for.  Two rows at a time pay where a row's chain of shuffles is long (tangents: two norms and their companions)
 // and the registers allow (147 against 160 us on 3 x 10007 rows of 1536 with a post norm, gradients 25 against 27 us on
 // 514 rows); at 5120 channels the second row of the backward pass spills (585 against 408 us).
+// CLASS 2 is the weak one: 1024 threads leave 64 registers each, and the tangent and gradient kernels spill (388 to 472 and 212 to 228
+// bytes of stores).  100 M elements in bf16 / with an fp32 stream, TB/s of forward, tangents, gradients: 5120 channels 6.2, 6.1, 5.7 /
+// 5.4, 5.6, 6.5; 6144 channels 5.5, 4.0, 2.6 / 6.4, 4.8, 3.3; 8192 channels 5.9, 4.4, 2.9 / 5.7, 4.7, 3.4.
 template <int MODE, bool FP32, int CLASS> struct AdalnPlan;
 template <bool F> struct AdalnPlan<0, F, 0> { static constexpr int rows = 1, stages = 4, threads = 256, ctas = 3; };
 template <bool F> struct AdalnPlan<0, F, 1> { static constexpr int rows = 1, stages = 4, threads = 640, ctas = 1; };
@@ -659,9 +662,15 @@ template <bool F> struct AdalnPlan<2, F, 0> { static constexpr int rows = 2, sta
 template <bool F> struct AdalnPlan<2, F, 1> { static constexpr int rows = 1, stages = 3, threads = 640, ctas = 1; };
 template <int M, bool F> struct AdalnPlan<M, F, 2> { static constexpr int rows = 1, stages = 2, threads = 1024, ctas = 1; };
 
-// Rows per CTA and CTAs per batch: as many CTAs as fit at once, each with the same number of rows (but for the last of
+// Rows per CTA and CTAs per batch: about as many CTAs as fit at once, each with the same number of rows (but for the last of
 // a batch).  More, shorter CTAs spread better, but each pays for its modulation rows and for filling its ring (measured:
-// twice as many cost 6-12 % at 2048 channels).
+// twice as many cost 6-12 % at 2048 channels).  The rows per CTA are those of all batches together, rounded up, and a batch is
+// then cut on its own, so that a few CTAs more than fit can come out where the batches do not share the slots evenly, and
+// these run after all others: 3 x 10920 x 5120 has 150 CTAs on 148 SMs and takes 251 / 476 / 408 us (forward, tangents, gradients, bf16)
+// where 1 x 32760 x 5120, the same bytes, takes 212 / 442 / 343; 3 x 10007 x 1536 with tangents has 297 on 296.
+// Above 2048 channels (256 threads) an SM holds one CTA whatever the width, and between 2048 and 5120 channels that is fewer warps
+// than the bandwidth wants (100 M elements in bf16, TB/s of forward, tangents, gradients: 2048 channels 5.5, 5.9, 5.9; 2560: 4.5, 5.5, 4.2;
+// 4096: 5.9, 6.4, 5.5; 5120: 6.2, 6.1, 5.7).
 struct AdalnGrid { int threads, rows_per_cta, chunks; };
 AdalnGrid adaln_grid(int mode, long long B, int L, int C) {
     AdalnGrid g;
@@ -858,7 +867,7 @@ int sparse_shape(int B, int H, int Lq, int Lk, int D) {
     if (B < 1 || H < 1 || Lq < 1 || Lk < 1) return ATTN_JVP_ERR_SHAPE;
     if (D != 64 && D != 128) return ATTN_JVP_ERR_UNSUPPORTED_D;
     if (n_blocks(Lq) > kSelMaxBlocks || n_blocks(Lk) > kSelMaxBlocks || B > 65535) return ATTN_JVP_ERR_SHAPE;
-    // work items and rows of lists are counted in ints, 2048 blocks of 256 threads read an item's rows at the most
+    // work items, rows of lists and padded rows of queries (128 to a block) are counted in 32 bits
     const long long most = n_blocks(Lq) > n_blocks(Lk) ? n_blocks(Lq) : n_blocks(Lk);
     if ((long double)B * H * most > 1.0e7L) return ATTN_JVP_ERR_SHAPE;
     return 0;

@@ -5,8 +5,9 @@ The paper restructures every network layer so that one call can carry primals al
 pairs, selected by a ``withT`` keyword (Appendix C.2, "Network Restructuring"); all layers use PyTorch's
 forward-mode operator for the JVP branch except the attention core, which calls the fused kernel
 (Appendix C.1).  Here the attention core for [B][L][H][D] bf16 tensors and the norms around it run in the CUDA library
-in both modes; the plain calls of the layers below the dense core are differentiable (once).  Their forward and backward
-passes can be captured into a CUDA graph; as with any layer, no autograd graph made outside the capture may then be alive
+in both modes; the plain calls of the layers below the dense core are differentiable (once).  Calls with ``withT`` and the
+dense core's plain call are not: their results carry no autograd graph, also where the arguments require grad.
+All passes can be captured into a CUDA graph; as with any layer, no autograd graph made outside the capture may then be alive
 for the same leaf tensors (the layers themselves keep none).
 """
 from __future__ import annotations
@@ -116,7 +117,7 @@ class AdaLNJVP(torch.nn.Module):
 
     ``forward(x, h, gate, scale, shift)`` returns (x', y); h and the modulation may be None.  ``forward(..., withT=True)``
     takes x and h as (primal, tangent) pairs and gate, scale, shift as pairs or as plain tensors (constant), and returns the
-    pairs (x', tx') and (y, ty).  ``affine`` / ``post_affine`` give the norms learnt fp32 weights (constants of the tangents:
+    pairs (x', tx') and (y, ty), without an autograd graph.  ``affine`` / ``post_affine`` give the norms learnt fp32 weights (constants of the tangents:
     the JVP runs on the frozen network).
     """
 
@@ -165,7 +166,7 @@ class SparseAttentionCoreJVP(torch.nn.Module):
     whose mean key fits its mean query best, or to those of a ``selection`` that the caller passes.
 
     Plain calls are differentiable (the selection is a constant); ``withT=True`` takes and returns pairs as
-    ``AttentionCoreJVP`` does.  The selection, log-sum-exp and (``keep_mu``) its tangent of the last call are kept in
+    ``AttentionCoreJVP`` does, without an autograd graph.  The selection, log-sum-exp and (``keep_mu``) its tangent of the last call are kept in
     ``last_selection``, ``last_lse`` and ``last_mu``.
     """
 
