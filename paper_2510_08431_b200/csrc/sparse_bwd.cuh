@@ -187,6 +187,11 @@ __device__ __forceinline__ void exp2_poly_pair(uint64_t x, float& p0, float& p1)
     const uint64_t two_n = pack_f32x2(__int_as_float((__float_as_int(t0) << 23) + 0x3F800000), __int_as_float((__float_as_int(t1) << 23) + 0x3F800000));
     unpack_f32x2(mul_f32x2(y, two_n), p0, p1);
 }
+// A number read from a list as an index below n.  The lists, the order and the counter lie in memory that a caller can have
+// shared between two calls at once by mistake: results are then undefined, addresses formed from them are not.  (Coordinates of
+// tensor maps need no such care: the copy fills in zeros outside the tensor.)
+__host__ __device__ constexpr int index_below(int v, int n) { return static_cast<unsigned>(v) < static_cast<unsigned>(n) ? v : n - 1; }
+static_assert(index_below(-1, 3) == 2 && index_below(2, 3) == 2 && index_below(3, 3) == 2 && index_below(0x7fffffff, 1) == 0, "inside");
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
@@ -321,8 +326,8 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
             // the next item that keeps anything, from place `at` of the order on; -1: none.  n: its streaming blocks
             auto next_item = [&](int at, int& n) -> int {
                 for (;; at = static_cast<int>(gridDim.x) + atomicAdd(args.counter, 1)) {
-                    if (at >= args.n_items) return -1;
-                    const int item = args.order == nullptr ? at : min(max(__ldg(args.order + at), 0), args.n_items - 1);
+                    if (static_cast<unsigned>(at) >= static_cast<unsigned>(args.n_items)) return -1;
+                    const int item = args.order == nullptr ? at : index_below(__ldg(args.order + at), args.n_items);
                     n = min((__ldg(args.tiles + item) + 1) >> 1, args.list_stride);
                     if (n > 0) return item;
                 }
@@ -347,7 +352,7 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
                 const float* rows = args.rows + static_cast<long long>(bh) * args.n_q * (2 * kBwdBlock);
                 int next = -1;
                 for (int j = 0; j < n; ++j, ++T) {
-                    const int row0 = __ldg(list + j) * kBwdBlock;
+                    const int block = __ldg(list + j), row0 = block * kBwdBlock;
                     if (j == 0) {
                         if (it > 0) ok = mbar_wait(smem_u32(&bar_x1_free), (it - 1) & 1, abort_state);
                         if (!ok) break;
@@ -374,7 +379,7 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
                         }
                         const uint32_t rb = smem_u32(&bar_rows_full[T & 1]);
                         mbar_arrive_expect_tx(rb, Plan::kRowsBytes);
-                        bulk_load(smem + Plan::kRowsOff + (T & 1) * Plan::kRowsBytes, rows + 2 * row0, Plan::kRowsBytes, rb);
+                        bulk_load(smem + Plan::kRowsOff + (T & 1) * Plan::kRowsBytes, rows + index_below(block, args.n_q) * (2 * kBwdBlock), Plan::kRowsBytes, rb);
                     }
                     if (++s1 == kBwdY1) { s1 = 0; ph1 ^= 1u; }
                     if (++s2 == kBwdY2) { s2 = 0; ph2 ^= 1u; }
