@@ -383,6 +383,86 @@ int attn_jvp_sparse_bwd(const void* d_o, const void* q, const void* k, const voi
                         void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Rotary positions.  attn_jvp_rotary_table -- for n positions, the entries (m cos, m sin) of all pairs of channels.  A position has
+ * `axes` coordinates (one for text; frame, row and column for video); axis a turns dims[a] channels, dims[a] / 2 pairs, and the
+ * pairs of the axes follow each other.  The angle of pair i of axis a is
+ *     position_a . theta(i),   theta(i) = base_a^(-2 i / dims[a])
+ * and `scaling` stretches an axis by its `factor` s > 0, for sequences longer than those of training:
+ *     ATTN_JVP_ROTARY_LINEAR  theta / s                       ATTN_JVP_ROTARY_NTK  base s^(d / (d - 2)) in place of base (d = dims[a] > 2)
+ *     ATTN_JVP_ROTARY_YARN    theta (1 - g) / s + theta g with g = clamp((turns - 1) / 31, 0, 1), turns = original_length theta / (2 pi):
+ *                             slow pairs are stretched, fast ones kept (Peng et al. 2023); m = 0.1 log(s) + 1, s that of the first axis.
+ * m = 1 but for YARN.
+ *   positions  device, [n][axes] contiguous, int32, int64 or fp32 (pos_type: ATTN_JVP_INT32, _INT64, _FP32)
+ *   dims, base, factor   HOST arrays of `axes` values, read before the call returns.  dims even; at most 8 axes and 128 pairs.
+ *   table      output, device, fp32 [n][sum(dims) / 2][2] contiguous, 16-byte aligned.
+ * Angles are formed in 64 bits: entries are right to fp32 rounding (some 2^-23 of m) at any position below 2^31.
+ */
+#define ATTN_JVP_INT32 2
+#define ATTN_JVP_INT64 3
+#define ATTN_JVP_ROTARY_PLAIN 0
+#define ATTN_JVP_ROTARY_LINEAR 1
+#define ATTN_JVP_ROTARY_NTK 2
+#define ATTN_JVP_ROTARY_YARN 3
+int attn_jvp_rotary_table(const void* positions, int pos_type, long long n, int axes, const int* dims, const double* base,
+                          int scaling, const double* factor, double original_length, float* table, void* cuda_stream);
+
+/*
+ * The step between the projections and the attention core: the heads of queries and keys normalised, each with its own weights,
+ * and rotated, both in one launch.  Per token and head, x in R^D, with the token's row of a rotary table of R / 2 pairs:
+ *     u = weight . norm(x) + bias,   y = u with its first R channels turned by pairs:
+ *     (y_a, y_c) = (u_a cos - u_c sin, u_c cos + u_a sin),  (a, c) = (2 i, 2 i + 1) for ATTN_JVP_ROTARY_INTERLEAVED, (i, i + R / 2) for _HALF
+ * norm as above (over the head's D channels).  The JVP mode needs the step with tangents (weights and table are constants), the student step the
+ * gradients.
+ *   q, k       device, bf16 [B][L][H][D] and [B][L][Hk][D] with strides of batch, token and head in elements (multiples of 8; a head's
+ *              channels are contiguous): slices of a fused projection need no copy.  k may be NULL (Hk = 0): queries alone.
+ *   tq, tk     their tangents, with strides of their own; read by attn_jvp_qk_rotary_fwd when it has outputs for them
+ *   q_weight, k_weight, q_bias, k_bias   device, fp32 [D], or NULL: 1 and 0
+ *   table      device, fp32 [table_rows][R / 2][2] for each batch, `table_batch` rows apart (0: one table for all), 16-byte aligned
+ *   index      device, int32, the table row of token l of batch b at index[b index_batch + l], or NULL: row l.  An index outside
+ *              the table is taken as its nearest row.
+ *   D is 64 or 128, R a multiple of 8 up to D.  eps >= 0.  B L (H + Hk) below 2 * 10^9.
+ * Tensors are 16-byte aligned.  Arithmetic is fp32 from bf16 inputs to one rounding of each output; sums do not change from run to run.
+ */
+#define ATTN_JVP_ROTARY_INTERLEAVED 0
+#define ATTN_JVP_ROTARY_HALF 1
+typedef struct attn_jvp_qk_rotary {
+    const void* q;
+    const void* k;
+    const void* tq;
+    const void* tk;
+    const float* q_weight;
+    const float* k_weight;
+    const float* q_bias;
+    const float* k_bias;
+    const float* table;
+    const int* index;
+    long long q_stride[3], k_stride[3], tq_stride[3], tk_stride[3];      /* batch, token, head */
+    long long table_rows, table_batch, index_batch;
+    int B, L, H, Hk, D, R;
+    int norm, layout;
+    float eps;
+} attn_jvp_qk_rotary_t;
+
+/*
+ * attn_jvp_qk_rotary_fwd -- y of queries and keys, and with tangents ty.
+ *   q_new, k_new   outputs, bf16 contiguous; k_new NULL exactly when k is.     tq_new, tk_new   both NULL (no tangents), or given as q_new, k_new are
+ * Outputs must not overlap inputs.  Asynchronous on `cuda_stream`; returns 0 or an ATTN_JVP_ERR_* code.
+ */
+int attn_jvp_qk_rotary_fwd(const attn_jvp_qk_rotary_t* in, void* q_new, void* k_new, void* tq_new, void* tk_new, void* cuda_stream);
+
+/*
+ * attn_jvp_qk_rotary_bwd -- gradients of attn_jvp_qk_rotary_fwd (tangent fields of `in` are ignored).
+ *   dq_new, dk_new   gradients of y, bf16 contiguous; dk_new NULL exactly when k is.
+ *   dq, dk           outputs, bf16 contiguous.      dq_weight, dk_weight, dq_bias, dk_bias   outputs, fp32 [D], each optional (NULL; those of k where it is NULL)
+ *   workspace        device, 16-byte aligned, attn_jvp_qk_rotary_bwd_workspace_bytes(...) bytes (the blocks' sums, joined in a fixed order); may be NULL
+ *                    where no gradient of a weight or bias is wanted.  Calls that share one must be ordered on the GPU.
+ */
+size_t attn_jvp_qk_rotary_bwd_workspace_bytes(int B, int L, int H, int Hk, int D);
+int attn_jvp_qk_rotary_bwd(const attn_jvp_qk_rotary_t* in, const void* dq_new, const void* dk_new, void* dq, void* dk,
+                           float* dq_weight, float* dk_weight, float* dq_bias, float* dk_bias, void* workspace,
+                           size_t workspace_bytes, void* cuda_stream);
+
+/*
  * Self-test of the failure path (no counterpart in the paper): enqueues a one-warp kernel that waits on a
  * barrier nothing ever signals.  The wait expires after its time limit (about 2 s), the kernel ends normally,
  * and attn_jvp_device_status() then reports ATTN_JVP_ERR_DEVICE_TIMEOUT, exactly as it would for a stalled

@@ -25,7 +25,8 @@ EXPORTS = ("attn_jvp_fwd", "attn_jvp_fwd_stream", "attn_jvp_fwd_mu", "attn_jvp_s
            "attn_jvp_suggest_splits", "attn_jvp_fwd_splitkv", "attn_jvp_fwd_splitkv_static", "attn_jvp_host_workspace_bytes",
            "attn_jvp_fwd_host", "attn_jvp_qknorm_fwd", "attn_jvp_adaln_fwd", "attn_jvp_adaln_bwd_workspace_bytes",
            "attn_jvp_adaln_bwd", "attn_jvp_block_select_workspace_bytes", "attn_jvp_block_select", "attn_jvp_block_lists",
-           "attn_jvp_sparse_fwd", "attn_jvp_sparse_bwd_workspace_bytes", "attn_jvp_sparse_bwd", "attn_jvp_set_tuning", "attn_jvp_debug_timeout_info", "attn_jvp_selftest_bounded_wait", "attn_jvp_set_stream", "attn_jvp_device_status", "attn_jvp_strerror",
+           "attn_jvp_sparse_fwd", "attn_jvp_sparse_bwd_workspace_bytes", "attn_jvp_sparse_bwd", "attn_jvp_rotary_table",
+           "attn_jvp_qk_rotary_fwd", "attn_jvp_qk_rotary_bwd_workspace_bytes", "attn_jvp_qk_rotary_bwd", "attn_jvp_set_tuning", "attn_jvp_debug_timeout_info", "attn_jvp_selftest_bounded_wait", "attn_jvp_set_stream", "attn_jvp_device_status", "attn_jvp_strerror",
            "attn_jvp_version")
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libattn_jvp.so")
@@ -93,6 +94,14 @@ def load():
             lib.attn_jvp_sparse_bwd_workspace_bytes.restype = ctypes.c_size_t
             lib.attn_jvp_sparse_bwd.argtypes = [vp] * 13 + [ci] * 5 + [cf, vp, ctypes.c_size_t, vp]
             lib.attn_jvp_sparse_bwd.restype = ci
+            lib.attn_jvp_rotary_table.argtypes = [vp, ci, ctypes.c_longlong, ci, vp, vp, ci, vp, ctypes.c_double, vp, vp]
+            lib.attn_jvp_rotary_table.restype = ci
+            lib.attn_jvp_qk_rotary_fwd.argtypes = [vp] * 6
+            lib.attn_jvp_qk_rotary_fwd.restype = ci
+            lib.attn_jvp_qk_rotary_bwd_workspace_bytes.argtypes = [ci] * 5
+            lib.attn_jvp_qk_rotary_bwd_workspace_bytes.restype = ctypes.c_size_t
+            lib.attn_jvp_qk_rotary_bwd.argtypes = [vp] * 10 + [ctypes.c_size_t, vp]
+            lib.attn_jvp_qk_rotary_bwd.restype = ci
             lib.attn_jvp_selftest_bounded_wait.argtypes = [vp]
             lib.attn_jvp_selftest_bounded_wait.restype = ci
             lib.attn_jvp_set_tuning.argtypes = [ci, ci]
@@ -139,7 +148,8 @@ def host():
             raise RuntimeError(f"_host.so is missing or does not load ({e}): build it with `python -m paper_2510_08431_b200.build` "
                                "(there is no fallback path)") from e
         names = ("adaln_fwd", "adaln_bwd", "adaln_bwd_workspace_bytes", "block_select", "block_select_workspace_bytes",
-                 "block_lists", "sparse_fwd", "sparse_bwd", "sparse_bwd_workspace_bytes")
+                 "block_lists", "sparse_fwd", "sparse_bwd", "sparse_bwd_workspace_bytes", "rotary_table", "qk_rotary_fwd",
+                 "qk_rotary_bwd", "qk_rotary_bwd_workspace_bytes")
         _host.bind(*(ctypes.cast(getattr(lib, "attn_jvp_" + n), ctypes.c_void_p).value for n in names))
         _host_module = _host
     return _host_module

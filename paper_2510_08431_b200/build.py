@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "attn_jvp.cu")
 DEPS = [SRC, os.path.join(PKG, "csrc", "attn_jvp_kernel.cuh"), os.path.join(PKG, "csrc", "qknorm_jvp.cuh"),
         os.path.join(PKG, "csrc", "adaln_jvp.cuh"), os.path.join(PKG, "csrc", "block_select.cuh"),
-        os.path.join(PKG, "csrc", "sparse_bwd.cuh"),
+        os.path.join(PKG, "csrc", "sparse_bwd.cuh"), os.path.join(PKG, "csrc", "rotary.cuh"),
         os.path.join(ROOT, "include", "attn_jvp.h")]
 LIB = os.path.join(PKG, "libattn_jvp.so")
 HOST_SRC = os.path.join(PKG, "csrc", "host_binding.cpp")
@@ -84,7 +84,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     try:
         build_host(force)
     except (RuntimeError, OSError) as e:
-        warnings.warn(f"the host binding is not built, adaln_*, block_sele* and sparse_attention_* will not work: {e}", RuntimeWarning)
+        warnings.warn(f"the host binding is not built, adaln_*, block_sele*, sparse_attention_* and *rotary* will not work: {e}", RuntimeWarning)
     return LIB
 
 

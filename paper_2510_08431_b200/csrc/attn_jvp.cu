@@ -13,6 +13,7 @@
 #include "attn_jvp_kernel.cuh"
 #include "block_select.cuh"
 #include "qknorm_jvp.cuh"
+#include "rotary.cuh"
 #include "sparse_bwd.cuh"
 
 namespace {
@@ -1143,6 +1144,230 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
                     : sparse_bwd_run<64>(mq, mk, mv, mdo, prep, dkv, dqa, stream, st);
 }
 
+// ---------------------------------------------------------------------------------------------
+// Rotary positions (rotary.cuh)
+// ---------------------------------------------------------------------------------------------
+int rotary_table(const void* positions, int pos_type, long long n, int axes, const int* dims, const double* base, int scaling,
+                 const double* factor, double original_length, float* table, cudaStream_t stream) {
+    if (n < 1 || n > (1LL << 40) || axes < 1 || axes > attn_jvp::kRotaryMaxAxes) return ATTN_JVP_ERR_SHAPE;
+    if (!positions || !dims || !base || !factor || !table) return ATTN_JVP_ERR_NULL;
+    if (pos_type != ATTN_JVP_INT32 && pos_type != ATTN_JVP_INT64 && pos_type != ATTN_JVP_FP32) return ATTN_JVP_ERR_FLAGS;
+    if (scaling < ATTN_JVP_ROTARY_PLAIN || scaling > ATTN_JVP_ROTARY_YARN) return ATTN_JVP_ERR_FLAGS;
+    attn_jvp::RotaryTableParams p;
+    constexpr double kTwoPi = 6.283185307179586476925286766559;
+    p.pairs = 0;
+    for (int a = 0; a < axes; ++a) {
+        const int d = dims[a];
+        if (d < 2 || d % 2 != 0 || p.pairs + d / 2 > attn_jvp::kRotaryMaxPairs) return ATTN_JVP_ERR_SHAPE;
+        double b = base[a];
+        const double s = factor[a];
+        if (!std::isfinite(b) || !(b > 0.0) || !std::isfinite(s) || !(s > 0.0)) return ATTN_JVP_ERR_SCALE;
+        if (scaling == ATTN_JVP_ROTARY_NTK) {
+            if (d == 2) return ATTN_JVP_ERR_SHAPE;
+            b *= std::pow(s, (double)d / (d - 2));
+        }
+        if (scaling == ATTN_JVP_ROTARY_YARN && !(std::isfinite(original_length) && original_length > 0.0)) return ATTN_JVP_ERR_SCALE;
+        for (int i = 0; i < d / 2; ++i, ++p.pairs) {
+            double theta = std::pow(b, -2.0 * i / d);
+            if (scaling == ATTN_JVP_ROTARY_LINEAR) theta /= s;
+            if (scaling == ATTN_JVP_ROTARY_YARN) {
+                const double g = std::fmin(1.0, std::fmax(0.0, (original_length * theta / kTwoPi - 1.0) / 31.0));
+                theta = theta * (1.0 - g) / s + theta * g;
+            }
+            p.turns[p.pairs] = theta / kTwoPi;
+            p.axis[p.pairs] = (unsigned char)a;
+        }
+    }
+    const size_t pos_bytes = pos_type == ATTN_JVP_INT64 ? 8 : 4;
+    const Span ins[] = {{positions, (size_t)n * axes * pos_bytes, (int)pos_bytes}};
+    const Span outs[] = {{table, (size_t)n * p.pairs * 8, 16}};
+    if (int rc = check_spans(ins, 1, outs, 1)) return rc;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    p.positions = positions;
+    p.table = reinterpret_cast<float2*>(table);
+    p.n = n;
+    p.axes = axes;
+    p.size = scaling == ATTN_JVP_ROTARY_YARN ? (float)(0.1 * std::log(factor[0]) + 1.0) : 1.0f;
+    const int rows = attn_jvp::kTableThreads / p.pairs, threads = rows * p.pairs;
+    const long long want = (n + rows - 1) / rows;
+    const unsigned grid = (unsigned)(want < 8LL * kSms ? want : 8LL * kSms);
+    if (pos_type == ATTN_JVP_INT32) attn_jvp::rotary_table_kernel<int><<<grid, threads, 0, stream>>>(p);
+    else if (pos_type == ATTN_JVP_INT64) attn_jvp::rotary_table_kernel<long long><<<grid, threads, 0, stream>>>(p);
+    else attn_jvp::rotary_table_kernel<float><<<grid, threads, 0, stream>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? 0 : cuda_fail("rotary table kernel launch", e);
+}
+
+bool rotary_shape_ok(int B, int L, int H, int Hk, int D) {
+    if (B < 1 || L < 1 || H < 1 || Hk < 0 || (D != 64 && D != 128)) return false;
+    return (long double)B * L * ((long double)H + Hk) < 2.0e9L;
+}
+
+// How the heads are dealt out.  A group of lanes takes as many heads of a token as leave four units of work or so for every group that fits on the
+// GPU (with few tokens, few heads each), and the blocks are shared between queries and keys by their heads.
+void rotary_grid(int mode, long long tokens, int H, int Hk, int D, attn_jvp::RotaryTensor* q, attn_jvp::RotaryTensor* k) {
+    const int rows = attn_jvp::rotary_rows(mode), groups = attn_jvp::kRotaryThreads / (D / 8);
+    const long long slots = (long long)kSms * 4, most = slots * groups;       // blocks, groups that fit at once
+    for (auto* t : {q, k}) {
+        t->H = t == q ? H : Hk;
+        t->blocks = 0;
+        if (t->H == 0) continue;
+        int heads = (t->H + rows - 1) / rows * rows;
+        while (heads > rows && tokens * ((H + Hk + heads - 1) / heads) < 4 * most) heads = (heads / 2 + rows - 1) / rows * rows;
+        t->heads = heads;
+        t->chunks = (t->H + heads - 1) / heads;
+        const long long want = (tokens * t->chunks + groups - 1) / groups;
+        long long share = (slots * t->H + (H + Hk) - 1) / (H + Hk);
+        t->blocks = (unsigned)(want < share ? want : share);
+    }
+}
+
+using attn_jvp::RotaryParams;
+template <int MODE>
+int rotary_launch(const RotaryParams& p, int D, bool half, cudaStream_t stream) {
+    const unsigned grid = p.q.blocks + p.k.blocks;
+    if (D == 128) {
+        if (half) attn_jvp::qk_rotary_kernel<128, MODE, true><<<grid, attn_jvp::kRotaryThreads, 0, stream>>>(p);
+        else attn_jvp::qk_rotary_kernel<128, MODE, false><<<grid, attn_jvp::kRotaryThreads, 0, stream>>>(p);
+    } else {
+        if (half) attn_jvp::qk_rotary_kernel<64, MODE, true><<<grid, attn_jvp::kRotaryThreads, 0, stream>>>(p);
+        else attn_jvp::qk_rotary_kernel<64, MODE, false><<<grid, attn_jvp::kRotaryThreads, 0, stream>>>(p);
+    }
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? 0 : cuda_fail("rotary kernel launch", e);
+}
+
+// Strides of batch, token and head of a strided tensor (0 along an axis of one), the bytes it spans, and whether they are in order.
+bool head_strides(const long long* in, int B, int L, int H, int D, long long* out, size_t* bytes) {
+    const int n[3] = {B, L, H};
+    size_t last = 0;
+    for (int i = 0; i < 3; ++i) {
+        out[i] = n[i] > 1 ? in[i] : 0;
+        if (out[i] < 0 || out[i] > (1LL << 40) || out[i] % 8 != 0) return false;
+        last += (size_t)(n[i] - 1) * (size_t)out[i];
+    }
+    *bytes = (last + D) * 2;
+    return true;
+}
+
+// What the two directions share: checks, and the kernel's parameters but for its outputs.  spans: q, k, tq, tk, weights, biases, table, index.
+constexpr int kRotaryIns = 10;
+int rotary_common(const attn_jvp_qk_rotary_t* in, bool tangents, RotaryParams& p, Span* spans) {
+    if (!in) return ATTN_JVP_ERR_NULL;
+    if (in->D != 64 && in->D != 128) return ATTN_JVP_ERR_UNSUPPORTED_D;
+    if (!rotary_shape_ok(in->B, in->L, in->H, in->Hk, in->D)) return ATTN_JVP_ERR_SHAPE;
+    if (in->R < 8 || in->R > in->D || in->R % 8 != 0 || in->table_rows < 1 || in->table_batch < 0 || in->index_batch < 0) return ATTN_JVP_ERR_SHAPE;
+    if (in->table_rows > (1LL << 40) || in->table_batch > (1LL << 40) || in->index_batch > (1LL << 40)) return ATTN_JVP_ERR_SHAPE;
+    if (!in->index && in->table_rows < in->L) return ATTN_JVP_ERR_SHAPE;
+    if (in->norm < 0 || in->norm > ATTN_JVP_NORM_RMS || in->layout < 0 || in->layout > ATTN_JVP_ROTARY_HALF) return ATTN_JVP_ERR_FLAGS;
+    if (!std::isfinite(in->eps) || in->eps < 0.0f) return ATTN_JVP_ERR_SCALE;
+    if (!in->q || !in->table || (in->k != nullptr) != (in->Hk > 0)) return ATTN_JVP_ERR_NULL;
+    if (tangents && (!in->tq || (in->k && !in->tk))) return ATTN_JVP_ERR_NULL;
+    p = RotaryParams{};
+    size_t bytes[4] = {};
+    long long s[4][3] = {};
+    if (!head_strides(in->q_stride, in->B, in->L, in->H, in->D, s[0], &bytes[0])) return ATTN_JVP_ERR_SHAPE;
+    if (in->k && !head_strides(in->k_stride, in->B, in->L, in->Hk, in->D, s[1], &bytes[1])) return ATTN_JVP_ERR_SHAPE;
+    if (tangents && !head_strides(in->tq_stride, in->B, in->L, in->H, in->D, s[2], &bytes[2])) return ATTN_JVP_ERR_SHAPE;
+    if (tangents && in->k && !head_strides(in->tk_stride, in->B, in->L, in->Hk, in->D, s[3], &bytes[3])) return ATTN_JVP_ERR_SHAPE;
+    auto fill = [&](attn_jvp::RotaryTensor& t, const void* x, const void* tx, const float* w, const float* b, const long long* xs, const long long* ts) {
+        t.x = static_cast<const __nv_bfloat16*>(x);
+        t.t = static_cast<const __nv_bfloat16*>(tx);
+        t.w = w;
+        t.b = b;
+        t.x_b = xs[0]; t.x_l = xs[1]; t.x_h = xs[2];
+        t.t_b = ts[0]; t.t_l = ts[1]; t.t_h = ts[2];
+    };
+    fill(p.q, in->q, tangents ? in->tq : nullptr, in->q_weight, in->q_bias, s[0], s[2]);
+    if (in->k) fill(p.k, in->k, tangents ? in->tk : nullptr, in->k_weight, in->k_bias, s[1], s[3]);
+    p.table = reinterpret_cast<const float2*>(in->table);
+    p.index = in->index;
+    p.table_batch = in->B > 1 ? in->table_batch : 0;
+    p.index_batch = in->B > 1 ? in->index_batch : 0;
+    p.table_rows = in->table_rows;
+    p.tokens = (long long)in->B * in->L;
+    p.L = in->L;
+    p.R = in->R;
+    p.norm = in->norm;
+    p.eps = in->eps;
+    const size_t wb = (size_t)in->D * 4;
+    const size_t table_bytes = ((size_t)(in->B - 1) * p.table_batch + in->table_rows) * in->R * 4;
+    const Span all[kRotaryIns] = {{p.q.x, bytes[0], 16}, {p.k.x, bytes[1], 16}, {p.q.t, bytes[2], 16}, {p.k.t, bytes[3], 16}, {p.q.w, wb, 4}, {p.k.w, wb, 4},
+                                  {p.q.b, wb, 4}, {p.k.b, wb, 4}, {p.table, table_bytes, 16},
+                                  {p.index, ((size_t)(in->B - 1) * p.index_batch + in->L) * 4, 4}};
+    for (int i = 0; i < kRotaryIns; ++i) spans[i] = all[i];
+    return 0;
+}
+
+int rotary_fwd(const attn_jvp_qk_rotary_t* in, void* q_new, void* k_new, void* tq_new, void* tk_new, cudaStream_t stream) {
+    RotaryParams p;
+    Span ins[kRotaryIns];
+    const bool jvp = tq_new || tk_new;
+    if (int rc = rotary_common(in, jvp, p, ins)) return rc;
+    if (!q_new || (k_new != nullptr) != (in->k != nullptr)) return ATTN_JVP_ERR_NULL;
+    if (jvp && (!tq_new || (tk_new != nullptr) != (in->k != nullptr))) return ATTN_JVP_ERR_NULL;
+    const size_t row = (size_t)in->B * in->L * in->D * 2, qb = row * in->H, kb = row * in->Hk;
+    const Span outs[] = {{q_new, qb, 16}, {k_new, kb, 16}, {tq_new, qb, 16}, {tk_new, kb, 16}};
+    if (int rc = check_spans(ins, kRotaryIns, outs, 4)) return rc;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    p.q.y = static_cast<__nv_bfloat16*>(q_new);
+    p.k.y = static_cast<__nv_bfloat16*>(k_new);
+    p.q.ty = static_cast<__nv_bfloat16*>(tq_new);
+    p.k.ty = static_cast<__nv_bfloat16*>(tk_new);
+    rotary_grid(jvp ? attn_jvp::kRotaryJvp : attn_jvp::kRotaryFwd, p.tokens, in->H, in->Hk, in->D, &p.q, &p.k);
+    const bool half = in->layout == ATTN_JVP_ROTARY_HALF;
+    return jvp ? rotary_launch<attn_jvp::kRotaryJvp>(p, in->D, half, stream) : rotary_launch<attn_jvp::kRotaryFwd>(p, in->D, half, stream);
+}
+
+size_t rotary_workspace(int B, int L, int H, int Hk, int D) {
+    attn_jvp::RotaryTensor q, k;
+    rotary_grid(attn_jvp::kRotaryBwd, (long long)B * L, H, Hk, D, &q, &k);
+    return (size_t)(q.blocks + k.blocks) * 2 * D * sizeof(float);
+}
+
+int rotary_bwd(const attn_jvp_qk_rotary_t* in, const void* dq_new, const void* dk_new, void* dq, void* dk, float* dq_weight, float* dk_weight,
+               float* dq_bias, float* dk_bias, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+    RotaryParams p;
+    Span ins[kRotaryIns + 2];
+    if (int rc = rotary_common(in, false, p, ins)) return rc;
+    if (!dq_new || !dq || (dk_new != nullptr) != (in->k != nullptr) || (dk != nullptr) != (in->k != nullptr)) return ATTN_JVP_ERR_NULL;
+    if (!in->k && (dk_weight || dk_bias)) return ATTN_JVP_ERR_NULL;
+    const bool sums = dq_weight || dk_weight || dq_bias || dk_bias;
+    if (sums && !workspace) return ATTN_JVP_ERR_NULL;
+    const size_t row = (size_t)in->B * in->L * in->D * 2, qb = row * in->H, kb = row * in->Hk, wb = (size_t)in->D * 4;
+    const size_t need = sums ? rotary_workspace(in->B, in->L, in->H, in->Hk, in->D) : 0;
+    if (sums && workspace_bytes < need) return ATTN_JVP_ERR_WORKSPACE;
+    ins[kRotaryIns] = {dq_new, qb, 16};
+    ins[kRotaryIns + 1] = {dk_new, kb, 16};
+    const Span outs[] = {{dq, qb, 16}, {dk, kb, 16}, {dq_weight, wb, 4}, {dk_weight, wb, 4}, {dq_bias, wb, 4}, {dk_bias, wb, 4},
+                         {sums ? workspace : nullptr, need, 16}};
+    if (int rc = check_spans(ins, kRotaryIns + 2, outs, 7)) return rc;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    const long long D = in->D;
+    for (auto* t : {&p.q, &p.k}) {
+        const long long H = t == &p.q ? in->H : in->Hk;
+        t->t = static_cast<const __nv_bfloat16*>(t == &p.q ? dq_new : dk_new);
+        t->y = static_cast<__nv_bfloat16*>(t == &p.q ? dq : dk);
+        t->t_b = in->L * H * D;
+        t->t_l = H * D;
+        t->t_h = D;
+    }
+    p.part = sums ? static_cast<float*>(workspace) : nullptr;
+    rotary_grid(attn_jvp::kRotaryBwd, p.tokens, in->H, in->Hk, in->D, &p.q, &p.k);
+    if (int rc = rotary_launch<attn_jvp::kRotaryBwd>(p, in->D, in->layout == ATTN_JVP_ROTARY_HALF, stream)) return rc;
+    if (!sums) return 0;
+    const attn_jvp::RotaryJoin j = {p.part, {dq_weight, dq_bias, dk_weight, dk_bias}, {p.q.blocks, p.k.blocks}, in->D};
+    attn_jvp::qk_rotary_join_kernel<<<dim3((unsigned)in->D / 32, in->k ? 4 : 2), 32 * attn_jvp::kRotaryJoinRows, 0, stream>>>(j);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? 0 : cuda_fail("rotary join kernel launch", e);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1334,6 +1559,26 @@ int attn_jvp_sparse_bwd(const void* d_o, const void* q, const void* k, const voi
                         const unsigned char* mask, const int* index, const int* tiles, const int* order, void* dq, void* dk, void* dv,
                         int B, int H, int Lq, int Lk, int D, float scale, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     return sparse_bwd(d_o, q, k, v, o, lse, mask, index, tiles, order, dq, dk, dv, B, H, Lq, Lk, D, scale, workspace, workspace_bytes,
+                      static_cast<cudaStream_t>(cuda_stream));
+}
+
+int attn_jvp_rotary_table(const void* positions, int pos_type, long long n, int axes, const int* dims, const double* base,
+                          int scaling, const double* factor, double original_length, float* table, void* cuda_stream) {
+    return rotary_table(positions, pos_type, n, axes, dims, base, scaling, factor, original_length, table, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int attn_jvp_qk_rotary_fwd(const attn_jvp_qk_rotary_t* in, void* q_new, void* k_new, void* tq_new, void* tk_new, void* cuda_stream) {
+    return rotary_fwd(in, q_new, k_new, tq_new, tk_new, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t attn_jvp_qk_rotary_bwd_workspace_bytes(int B, int L, int H, int Hk, int D) {
+    return rotary_shape_ok(B, L, H, Hk, D) ? rotary_workspace(B, L, H, Hk, D) : 0;
+}
+
+int attn_jvp_qk_rotary_bwd(const attn_jvp_qk_rotary_t* in, const void* dq_new, const void* dk_new, void* dq, void* dk,
+                           float* dq_weight, float* dk_weight, float* dq_bias, float* dk_bias, void* workspace,
+                           size_t workspace_bytes, void* cuda_stream) {
+    return rotary_bwd(in, dq_new, dk_new, dq, dk, dq_weight, dk_weight, dq_bias, dk_bias, workspace, workspace_bytes,
                       static_cast<cudaStream_t>(cuda_stream));
 }
 

@@ -13,6 +13,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <stdexcept>
+#include <vector>
 
 #include "attn_jvp.h"
 
@@ -27,6 +28,10 @@ decltype(&attn_jvp_block_lists) f_block_lists = nullptr;
 decltype(&attn_jvp_sparse_fwd) f_sparse_fwd = nullptr;
 decltype(&attn_jvp_sparse_bwd) f_sparse_bwd = nullptr;
 decltype(&attn_jvp_sparse_bwd_workspace_bytes) f_sparse_bwd_bytes = nullptr;
+decltype(&attn_jvp_rotary_table) f_rotary_table = nullptr;
+decltype(&attn_jvp_qk_rotary_fwd) f_qk_rotary_fwd = nullptr;
+decltype(&attn_jvp_qk_rotary_bwd) f_qk_rotary_bwd = nullptr;
+decltype(&attn_jvp_qk_rotary_bwd_workspace_bytes) f_qk_rotary_bwd_bytes = nullptr;
 
 // An argument that does not fit: becomes a ValueError.
 struct Refused : std::runtime_error { using std::runtime_error::runtime_error; };
@@ -363,11 +368,166 @@ PyObject* sparse_bwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
     });
 }
 
+// ---- rotary positions ----
+// The numbers of a sequence (a tuple or list), one per axis.
+int numbers(PyObject* o, const char* name, double* out, int most) {
+    if (!PyTuple_Check(o) && !PyList_Check(o)) refuse("%s must be a tuple or list", name);
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+    if (n < 1 || n > most) refuse("%s must have 1 to %d entries", name, most);
+    for (Py_ssize_t i = 0; i < n; ++i) out[i] = number(PySequence_Fast_GET_ITEM(o, i), name);
+    return static_cast<int>(n);
+}
+
+// positions, dims, base, scaling, factor, original_length -> (rc, table)
+PyObject* rotary_table(PyObject*, PyObject* const* p, Py_ssize_t n) {
+    if (!count(n, 6, "rotary_table")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        constexpr int kMost = 8;
+        at::Tensor pos = required(p[0], "positions");
+        double d[kMost], base[kMost], factor[kMost];
+        int dims[kMost], channels = 0;
+        const int axes = numbers(p[1], "dims", d, kMost);
+        if (numbers(p[2], "base", base, kMost) != axes || numbers(p[4], "factor", factor, kMost) != axes) refuse("base and factor must have an entry for each of the %d axes", axes);
+        for (int a = 0; a < axes; ++a) {
+            if (!(d[a] >= 2 && d[a] <= 1024) || d[a] != std::floor(d[a])) refuse("dims must be even numbers of channels");
+            channels += dims[a] = static_cast<int>(d[a]);
+        }
+        const auto type = pos.scalar_type();
+        if (!pos.is_cuda() || !pos.is_contiguous() || (type != at::kInt && type != at::kLong && type != at::kFloat)) refuse("positions must be a contiguous CUDA tensor of int32, int64 or fp32");
+        std::vector<int64_t> shape(pos.sizes().begin(), pos.sizes().end());
+        if (axes > 1) {
+            if (shape.empty() || shape.back() != axes) refuse("positions must have shape [...][%d], one coordinate per axis", axes);
+            shape.pop_back();
+        }
+        shape.push_back(channels / 2);
+        shape.push_back(2);
+        at::Tensor table = like(pos, shape, at::kFloat);
+        const int scaling = whole(p[3], "scaling"), kind = type == at::kInt ? ATTN_JVP_INT32 : type == at::kLong ? ATTN_JVP_INT64 : ATTN_JVP_FP32;
+        const double original = p[5] == Py_None ? 0.0 : number(p[5], "original_length");
+        const c10::cuda::CUDAGuard guard(pos.device());
+        const int rc = unlocked([&] { return f_rotary_table(ptr(pos), kind, pos.numel() / axes, axes, dims, base, scaling, factor, original, ptr<float>(table),
+                                       c10::cuda::getCurrentCUDAStream(pos.device().index()).stream()); });
+        return result(rc, {table});
+    });
+}
+
+// Strides of batch, token and head of a tensor whose heads are contiguous.
+void heads_of(const at::Tensor& t, const char* name, at::IntArrayRef shape, const at::Device& device, long long* stride) {
+    if (t.device() != device || t.scalar_type() != at::kBFloat16 || t.sizes() != shape || t.stride(3) != 1)
+        refuse("%s must be a bf16 tensor on %s of the shape that the other arguments give, with contiguous heads", name, device.str().c_str());
+    for (int i = 0; i < 3; ++i) {
+        stride[i] = t.stride(i);
+        if (t.size(i) > 1 && stride[i] % 8 != 0) refuse("%s: strides must be multiples of 8 elements", name);
+    }
+}
+
+// args: q, k, table, index, norm, layout, eps, q_weight, k_weight, q_bias, k_bias
+struct Rotary {
+    at::Tensor q, k, table, index, w[4];
+    attn_jvp_qk_rotary_t a = {};
+    explicit Rotary(PyObject* const* p) : q(required(p[0], "q")), k(tensor(p[1], "k")), table(required(p[2], "table")), index(tensor(p[3], "index")) {
+        if (!q.is_cuda() || q.dim() != 4 || q.numel() == 0) refuse("q must be a CUDA tensor [B][L][H][D] that is not empty");
+        const at::Device dev = q.device();
+        heads_of(q, "q", q.sizes(), dev, a.q_stride);
+        if (k.defined()) {
+            if (k.dim() != 4 || k.numel() == 0) refuse("k must have shape [B][L][Hk][D] and not be empty");
+            heads_of(k, "k", {q.size(0), q.size(1), k.size(2), q.size(3)}, dev, a.k_stride);
+        }
+        a.B = size32(q.size(0));
+        a.L = size32(q.size(1));
+        a.H = size32(q.size(2));
+        a.Hk = k.defined() ? size32(k.size(2)) : 0;
+        a.D = size32(q.size(3));
+        const int64_t td = table.dim();
+        if (table.device() != dev || table.scalar_type() != at::kFloat || !table.is_contiguous() || (td != 3 && td != 4) || table.size(td - 1) != 2 ||
+            (td == 4 && table.size(0) != q.size(0)))
+            refuse("table must be a contiguous fp32 tensor [rows][R / 2][2] or [B][rows][R / 2][2] on %s", dev.str().c_str());
+        a.R = size32(2 * table.size(td - 2));
+        a.table_rows = table.size(td - 3);
+        a.table_batch = td == 4 ? a.table_rows : 0;
+        if (index.defined()) {
+            const int64_t id = index.dim();
+            if (index.device() != dev || index.scalar_type() != at::kInt || !index.is_contiguous() || (id != 1 && id != 2) || index.size(id - 1) != q.size(1) ||
+                (id == 2 && index.size(0) != q.size(0)))
+                refuse("index must be a contiguous int32 tensor [L] or [B][L] on %s", dev.str().c_str());
+            a.index_batch = id == 2 ? q.size(1) : 0;
+        } else if (a.table_rows < a.L) {
+            refuse("the table has %lld rows for %d tokens", a.table_rows, a.L);
+        }
+        a.norm = whole(p[4], "norm");
+        a.layout = whole(p[5], "layout");
+        a.eps = static_cast<float>(number(p[6], "eps"));
+        static const char* const names[4] = {"q_weight", "k_weight", "q_bias", "k_bias"};
+        for (int i = 0; i < 4; ++i) {
+            w[i] = tensor(p[7 + i], names[i]);
+            if (!w[i].defined()) continue;
+            if (i % 2 == 1 && !k.defined()) refuse("%s acts on k, which is None", names[i]);
+            expect(w[i], names[i], at::kFloat, {q.size(3)}, dev);
+        }
+        a.q = ptr(q);
+        a.k = ptr(k);
+        a.q_weight = ptr<float>(w[0]);
+        a.k_weight = ptr<float>(w[1]);
+        a.q_bias = ptr<float>(w[2]);
+        a.k_bias = ptr<float>(w[3]);
+        a.table = ptr<float>(table);
+        a.index = ptr<int>(index);
+    }
+    at::Tensor out(const at::Tensor& t) const { return t.defined() ? like(t, t.sizes(), at::kBFloat16) : at::Tensor(); }
+    cudaStream_t stream() const { return c10::cuda::getCurrentCUDAStream(q.device().index()).stream(); }
+};
+
+// ... , tq, tk -> (rc, q', k', tq', tk')
+PyObject* qk_rotary_fwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
+    if (!count(n, 13, "qk_rotary_fwd")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Rotary c(p);
+        at::Tensor tq = tensor(p[11], "tq"), tk = tensor(p[12], "tk"), q = c.out(c.q), k = c.out(c.k), tqn, tkn;
+        if (tq.defined() || tk.defined()) {
+            if (!tq.defined() || tk.defined() != c.k.defined()) refuse("with tangents tq is required, and tk exactly where k is given");
+            heads_of(tq, "tq", c.q.sizes(), c.q.device(), c.a.tq_stride);
+            if (tk.defined()) heads_of(tk, "tk", c.k.sizes(), c.q.device(), c.a.tk_stride);
+            c.a.tq = ptr(tq);
+            c.a.tk = ptr(tk);
+            tqn = c.out(c.q);
+            tkn = c.out(c.k);
+        }
+        const c10::cuda::CUDAGuard guard(c.q.device());
+        const int rc = unlocked([&] { return f_qk_rotary_fwd(&c.a, ptr(q), ptr(k), ptr(tqn), ptr(tkn), c.stream()); });
+        return result(rc, {q, k, tqn, tkn});
+    });
+}
+
+// dq_new, dk_new, (the eleven of Rotary), workspace -> (rc, dq, dk, dq_weight, dk_weight, dq_bias, dk_bias)
+PyObject* qk_rotary_bwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
+    if (!count(n, 14, "qk_rotary_bwd")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        at::Tensor dqn = required(p[0], "dq_new"), dkn = tensor(p[1], "dk_new");
+        Rotary c(p + 2);
+        if (dkn.defined() != c.k.defined()) refuse("dk_new is required exactly where k is given");
+        expect(dqn, "dq_new", at::kBFloat16, c.q.sizes(), c.q.device());
+        if (dkn.defined()) expect(dkn, "dk_new", at::kBFloat16, c.k.sizes(), c.q.device());
+        at::Tensor dq = c.out(c.q), dk = c.out(c.k), d[4], ws;
+        bool sums = false;
+        for (int i = 0; i < 4; ++i) if (c.w[i].defined()) {
+            d[i] = like(c.q, {c.q.size(3)}, at::kFloat);
+            sums = true;
+        }
+        if (sums) ws = scratch(p[13], c.q, f_qk_rotary_bwd_bytes(c.a.B, c.a.L, c.a.H, c.a.Hk, c.a.D));
+        const c10::cuda::CUDAGuard guard(c.q.device());
+        const int rc = unlocked([&] { return f_qk_rotary_bwd(&c.a, ptr(dqn), ptr(dkn), ptr(dq), ptr(dk), ptr<float>(d[0]), ptr<float>(d[1]), ptr<float>(d[2]), ptr<float>(d[3]), ptr(ws),
+                                       ws.defined() ? ws.nbytes() : 0, c.stream()); });
+        return result(rc, {dq, dk, d[0], d[1], d[2], d[3]});
+    });
+}
+
 // The library's functions, by address and in this order.
 PyObject* bind(PyObject*, PyObject* const* p, Py_ssize_t n) {
     void** slots[] = {reinterpret_cast<void**>(&f_adaln_fwd), reinterpret_cast<void**>(&f_adaln_bwd), reinterpret_cast<void**>(&f_adaln_bwd_bytes),
                       reinterpret_cast<void**>(&f_block_select), reinterpret_cast<void**>(&f_block_select_bytes), reinterpret_cast<void**>(&f_block_lists),
-                      reinterpret_cast<void**>(&f_sparse_fwd), reinterpret_cast<void**>(&f_sparse_bwd), reinterpret_cast<void**>(&f_sparse_bwd_bytes)};
+                      reinterpret_cast<void**>(&f_sparse_fwd), reinterpret_cast<void**>(&f_sparse_bwd), reinterpret_cast<void**>(&f_sparse_bwd_bytes),
+                      reinterpret_cast<void**>(&f_rotary_table), reinterpret_cast<void**>(&f_qk_rotary_fwd), reinterpret_cast<void**>(&f_qk_rotary_bwd),
+                      reinterpret_cast<void**>(&f_qk_rotary_bwd_bytes)};
     constexpr Py_ssize_t slots_n = sizeof slots / sizeof slots[0];
     if (!count(n, slots_n, "bind")) return nullptr;
     for (Py_ssize_t i = 0; i < slots_n; ++i) {
@@ -383,7 +543,8 @@ PyObject* bind(PyObject*, PyObject* const* p, Py_ssize_t n) {
 
 #define HOST_FN(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HOST_FN(bind), HOST_FN(adaln_fwd), HOST_FN(adaln_bwd), HOST_FN(block_select), HOST_FN(block_lists),
-                         HOST_FN(sparse_fwd), HOST_FN(sparse_bwd), {nullptr, nullptr, 0, nullptr}};
+                         HOST_FN(sparse_fwd), HOST_FN(sparse_bwd), HOST_FN(rotary_table), HOST_FN(qk_rotary_fwd),
+                         HOST_FN(qk_rotary_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", "Tensor checks and calls into the C ABI.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -18,6 +18,7 @@ import torch
 
 from . import adaln as _adaln
 from . import attn_jvp as _binding
+from . import rotary as _rotary
 from . import sparse as _sparse
 
 TensorWithT = Tuple[torch.Tensor, torch.Tensor]   # (primal, tangent)
@@ -142,6 +143,55 @@ class AdaLNJVP(torch.nn.Module):
         xn, y, txn, ty = _adaln.adaln_jvp(x, h, gate, scale, shift, w, wp, **kinds, tx=tx.detach(),
                                           th=None if th is None else th.detach(), tgate=tgate, tscale=tscale, tshift=tshift)
         return (xn, txn), (y, ty)
+
+
+class _QKRotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, table, index, q_weight, k_weight, q_bias, k_bias, kinds):
+        ctx.kinds = kinds
+        ctx.save_for_backward(q, k, table, index, q_weight, k_weight, q_bias, k_bias)
+        qn, kn, _, _ = _rotary.qk_rotary_jvp(q, k, table, index, q_weight=q_weight, k_weight=k_weight, q_bias=q_bias, k_bias=k_bias, **kinds)
+        return qn if k is None else (qn, kn)
+
+    @staticmethod
+    def backward(ctx, dqn, dkn=None):
+        q, k, table, index, q_weight, k_weight, q_bias, k_bias = ctx.saved_tensors
+        g = _rotary.qk_rotary_backward(dqn.contiguous(), None if k is None else dkn.contiguous(), q, k, table, index, q_weight=q_weight,
+                                       k_weight=k_weight, q_bias=q_bias, k_bias=k_bias, **ctx.kinds)
+        g = _first_order(g, dqn, dkn, *ctx.saved_tensors)
+        return g[0], g[1], None, None, g[2], g[3], g[4], g[5], None
+
+
+class QKRotaryJVP(torch.nn.Module):
+    """The heads of queries and keys normalised and rotated (``qk_rotary_jvp``), with an optional tangent channel and, without
+    it, autograd.
+
+    ``forward(q, k, table)`` returns (q', k'), with k = None (queries alone) q'; q and k may be slices of a fused projection.
+    ``table``: a ``rotary_table``, read by a token's place or by ``index``; a constant.  ``withT=True`` takes and returns pairs, without an autograd graph.
+    ``affine`` / ``bias`` give each norm a learnt fp32 weight / bias over the head's channels (constants of the tangents); ``keys=False``: no k, and none for it.
+    """
+
+    def __init__(self, head_dim: int, norm: Optional[str] = "rms", layout: str = "interleaved", eps: float = 1e-6, affine: bool = True,
+                 bias: bool = False, keys: bool = True):
+        super().__init__()
+        self.kinds = dict(norm=norm, layout=layout, eps=eps)
+        self.q_weight = torch.nn.Parameter(torch.ones(head_dim)) if affine else None
+        self.k_weight = torch.nn.Parameter(torch.ones(head_dim)) if affine and keys else None
+        self.q_bias = torch.nn.Parameter(torch.zeros(head_dim)) if bias else None
+        self.k_bias = torch.nn.Parameter(torch.zeros(head_dim)) if bias and keys else None
+
+    def forward(self, q, k, table, index=None, withT: bool = False):
+        kp = k if not withT else _pair(k)[0]
+        kw, kb = (None, None) if kp is None else (self.k_weight, self.k_bias)
+        if not withT:
+            return _QKRotary.apply(q, k, table, index, self.q_weight, kw, self.q_bias, kb, self.kinds)
+        (q, tq), (k, tk) = _pair(q), _pair(k)
+        if tq is None or (k is not None and tk is None):
+            raise ValueError("withT: q and k must carry tangents")
+        w = [None if t is None else t.detach() for t in (self.q_weight, kw, self.q_bias, kb)]
+        qn, kn, tqn, tkn = _rotary.qk_rotary_jvp(q.detach(), None if k is None else k.detach(), table, index, q_weight=w[0], k_weight=w[1], q_bias=w[2],
+                                                 k_bias=w[3], **self.kinds, tq=tq.detach(), tk=None if tk is None else tk.detach())
+        return (qn, tqn) if k is None else ((qn, tqn), (kn, tkn))
 
 
 class _SparseAttention(torch.autograd.Function):
