@@ -18,8 +18,9 @@
  *   - All tensor pointers are DEVICE pointers owned by the caller.  The
  *     library neither frees nor retains them and allocates no device memory;
  *     the entry points with a `workspace` argument (split-KV, host buffers,
- *     attn_jvp_adaln_bwd, attn_jvp_block_select, attn_jvp_sparse_bwd) need a
- *     (caller-provided) device workspace, all others need none.
+ *     attn_jvp_adaln_bwd, attn_jvp_block_select, attn_jvp_sparse_bwd,
+ *     attn_jvp_attention_bwd, attn_jvp_qk_rotary_bwd) need a (caller-provided)
+ *     device workspace, all others need none.
  *   - q, tq, o, to : bf16, layout [B][Lq][H][D] contiguous ("BLHD").
  *     k, v, tk, tv : bf16, layout [B][Lk][H][D] contiguous.
  *     lse          : fp32, layout [B][H][Lq], natural log of the scaled scores.
@@ -381,6 +382,48 @@ int attn_jvp_sparse_bwd(const void* d_o, const void* q, const void* k, const voi
                         void* dq, void* dk, void* dv,
                         int B, int H, int Lq, int Lk, int D, float scale,
                         void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Dense attention with a causal mask, key lengths, key heads that query heads share, and strided inputs: forward (with or without
+ * tangents) and gradients.
+ *   q          device, bf16 [B][Lq][H][D];  k, v   bf16 [B][Lk][Hk][D], H a multiple of Hk: query head h reads key head h / (H / Hk).  Strides of
+ *              batch, token and head in elements, multiples of 8 and at least D (the channels of a head are contiguous): slices of a fused projection need no copy.
+ *   tq, tk, tv tangents, contiguous; read by attn_jvp_attention_fwd only, as its flags say.
+ *   k_lengths  device, int32 [B]: batch b has the first min(max(k_lengths[b], 0), Lk) keys, and what lies behind them (NaN included) has no
+ *              influence; or NULL: all have Lk.
+ *   causal     0, or 1: query i sees the keys j <= i + Lk - Lq (the ends are aligned, whatever the lengths).
+ * A query that sees no key has O = tO = 0, LSE = -inf, mu = 0 and no gradient; so has a key that nothing sees.  Sequences and sizes as for the
+ * block-sparse calls below 786432 tokens; tensors 16-byte aligned.
+ *
+ * attn_jvp_attention_fwd -- o, to, lse, mu (optional) and flags as attn_jvp_fwd_mu; o and to contiguous.
+ */
+typedef struct attn_jvp_attention {
+    const void* q;
+    const void* k;
+    const void* v;
+    const void* tq;
+    const void* tk;
+    const void* tv;
+    const int* k_lengths;
+    long long q_stride[3], k_stride[3], v_stride[3];     /* batch, token, head */
+    int B, H, Hk, Lq, Lk, D;
+    int causal;
+    float scale;
+} attn_jvp_attention_t;
+int attn_jvp_attention_fwd(const attn_jvp_attention_t* in, void* o, void* to, float* lse, float* mu, unsigned flags, void* cuda_stream);
+
+/*
+ * attn_jvp_attention_bwd -- gradients of O = softmax(s Q K^T) V (the probabilities are recomputed from LSE):
+ *     dS = P (dO V^T - rowsum(dO . O)),  dQ = s dS K,  dK = s dS^T Q,  dV = P^T dO,  dK and dV summed over the query heads that share theirs.
+ *   d_o, o     bf16 [B][Lq][H][D] contiguous: the gradient of O and the forward's O;  lse: the forward's LSE.
+ *   dq, dk, dv outputs, bf16 contiguous, shapes of q, k, v; every element is written.
+ *   workspace  device, 256-byte aligned, attn_jvp_attention_bwd_workspace_bytes(...) bytes (two words per query, the last block of every batch's
+ *              keys, and partial sums where there are few blocks).  Calls that share one must be ordered on the GPU.
+ * P and dS are rounded to bf16 as MMA operands, sums are fp32; no atomics: results do not change from run to run.
+ */
+size_t attn_jvp_attention_bwd_workspace_bytes(int B, int H, int Hk, int Lq, int Lk, int D);
+int attn_jvp_attention_bwd(const attn_jvp_attention_t* in, const void* d_o, const void* o, const float* lse, void* dq, void* dk, void* dv,
+                           void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
  * Rotary positions.  attn_jvp_rotary_table -- for n positions, the entries (m cos, m sin) of all pairs of channels.  A position has

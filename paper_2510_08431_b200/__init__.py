@@ -3,6 +3,8 @@ from . import synth  # noqa: F401
 from .adaln import (  # noqa: F401
     AdaLNArgs, AdaLNGrads, adaln_backward, adaln_jvp, attn_jvp_adaln_bwd, attn_jvp_adaln_bwd_workspace_bytes,
     attn_jvp_adaln_fwd)
+from .dense import (  # noqa: F401
+    AttentionArgs, attention_backward, attn_jvp_attention_bwd, attn_jvp_attention_bwd_workspace_bytes, attn_jvp_attention_fwd)
 from .layers import AdaLNJVP, AttentionCoreJVP, QKRotaryJVP, SparseAttentionCoreJVP, TensorWithT  # noqa: F401
 from .rotary import (  # noqa: F401
     QKRotaryArgs, QKRotaryGrads, attn_jvp_qk_rotary_bwd, attn_jvp_qk_rotary_bwd_workspace_bytes, attn_jvp_qk_rotary_fwd,

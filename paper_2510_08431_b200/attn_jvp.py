@@ -25,7 +25,8 @@ EXPORTS = ("attn_jvp_fwd", "attn_jvp_fwd_stream", "attn_jvp_fwd_mu", "attn_jvp_s
            "attn_jvp_suggest_splits", "attn_jvp_fwd_splitkv", "attn_jvp_fwd_splitkv_static", "attn_jvp_host_workspace_bytes",
            "attn_jvp_fwd_host", "attn_jvp_qknorm_fwd", "attn_jvp_adaln_fwd", "attn_jvp_adaln_bwd_workspace_bytes",
            "attn_jvp_adaln_bwd", "attn_jvp_block_select_workspace_bytes", "attn_jvp_block_select", "attn_jvp_block_lists",
-           "attn_jvp_sparse_fwd", "attn_jvp_sparse_bwd_workspace_bytes", "attn_jvp_sparse_bwd", "attn_jvp_rotary_table",
+           "attn_jvp_sparse_fwd", "attn_jvp_sparse_bwd_workspace_bytes", "attn_jvp_sparse_bwd", "attn_jvp_attention_fwd",
+           "attn_jvp_attention_bwd_workspace_bytes", "attn_jvp_attention_bwd", "attn_jvp_rotary_table",
            "attn_jvp_qk_rotary_fwd", "attn_jvp_qk_rotary_bwd_workspace_bytes", "attn_jvp_qk_rotary_bwd", "attn_jvp_set_tuning", "attn_jvp_debug_timeout_info", "attn_jvp_selftest_bounded_wait", "attn_jvp_set_stream", "attn_jvp_device_status", "attn_jvp_strerror",
            "attn_jvp_version")
 
@@ -94,6 +95,12 @@ def load():
             lib.attn_jvp_sparse_bwd_workspace_bytes.restype = ctypes.c_size_t
             lib.attn_jvp_sparse_bwd.argtypes = [vp] * 13 + [ci] * 5 + [cf, vp, ctypes.c_size_t, vp]
             lib.attn_jvp_sparse_bwd.restype = ci
+            lib.attn_jvp_attention_fwd.argtypes = [vp] * 5 + [cu, vp]
+            lib.attn_jvp_attention_fwd.restype = ci
+            lib.attn_jvp_attention_bwd_workspace_bytes.argtypes = [ci] * 6
+            lib.attn_jvp_attention_bwd_workspace_bytes.restype = ctypes.c_size_t
+            lib.attn_jvp_attention_bwd.argtypes = [vp] * 8 + [ctypes.c_size_t, vp]
+            lib.attn_jvp_attention_bwd.restype = ci
             lib.attn_jvp_rotary_table.argtypes = [vp, ci, ctypes.c_longlong, ci, vp, vp, ci, vp, ctypes.c_double, vp, vp]
             lib.attn_jvp_rotary_table.restype = ci
             lib.attn_jvp_qk_rotary_fwd.argtypes = [vp] * 6
@@ -148,7 +155,8 @@ def host():
             raise RuntimeError(f"_host.so is missing or does not load ({e}): build it with `python -m paper_2510_08431_b200.build` "
                                "(there is no fallback path)") from e
         names = ("adaln_fwd", "adaln_bwd", "adaln_bwd_workspace_bytes", "block_select", "block_select_workspace_bytes",
-                 "block_lists", "sparse_fwd", "sparse_bwd", "sparse_bwd_workspace_bytes", "rotary_table", "qk_rotary_fwd",
+                 "block_lists", "sparse_fwd", "sparse_bwd", "sparse_bwd_workspace_bytes", "attention_fwd",
+                 "attention_bwd", "attention_bwd_workspace_bytes", "rotary_table", "qk_rotary_fwd",
                  "qk_rotary_bwd", "qk_rotary_bwd_workspace_bytes")
         _host.bind(*(ctypes.cast(getattr(lib, "attn_jvp_" + n), ctypes.c_void_p).value for n in names))
         _host_module = _host
@@ -275,7 +283,7 @@ def _check(t, name, shape):
 
 
 def attention_jvp(q, k, v, tq=None, tk=None, tv=None, scale=None, fwd_only=False, out=None,
-                  return_mu=False, splits=1, workspace=None):
+                  return_mu=False, splits=1, workspace=None, causal=False, k_lengths=None):
     """O, tO, LSE of Algorithm 2 for [B][L][H][D] bf16 CUDA tensors, on torch's current stream.
 
     ``tk is None and tv is None`` selects the tangent-free K/V path (cross-attention on a constant
@@ -285,8 +293,20 @@ def attention_jvp(q, k, v, tq=None, tk=None, tv=None, scale=None, fwd_only=False
     second kernel (for few queries and many keys), ``splits=0`` lets the library choose
     (``attn_jvp_suggest_splits``); ``workspace`` may supply its scratch (a CUDA uint8
     tensor of at least attn_jvp_splitkv_workspace_bytes), else it is allocated here with torch.
+    ``causal``: query i sees the keys j <= i + Lk - Lq.  ``k_lengths`` (CUDA int32 [B]): the keys of each batch, what lies behind
+    them has no influence.  k and v may have fewer heads than q, each shared by as many query heads in a row, and q, k, v may be strided (slices of a fused
+    projection: heads contiguous, strides multiples of 8; tangents stay contiguous).  Rows that see no key: o = to = 0, lse = -inf.  None of
+    these four goes with ``splits`` > 1.
     Returns (o, to, lse) or (o, to, lse, mu).
     """
+    if causal or k_lengths is not None or q.shape[2:] != k.shape[2:] or not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
+        if splits > 1 or workspace is not None:
+            raise ValueError("chunks of keys (splits > 1) go without masks, lengths, shared heads and strided inputs")
+        rc, o, to, lse, mu = host().attention_fwd(q, k, v, scale, bool(causal), k_lengths, tq, tk, tv, bool(fwd_only), bool(return_mu),
+                                                  *(out or (None, None, None)))
+        if rc:
+            _raise(rc)
+        return (o, to, lse, mu) if return_mu else (o, to, lse)
     B, Lq, H, D = q.shape
     Lk = k.shape[1]
     _check(q, "q", (B, Lq, H, D)); _check(k, "k", (B, Lk, H, D)); _check(v, "v", (B, Lk, H, D))

@@ -46,7 +46,8 @@ struct DeviceState {
     std::atomic<int> dyn_smem[2][3][2][2];        // dynamic shared memory per kernel instantiation, 0 = not set up
     std::atomic<int> dyn_smem_pair[3][2];         // ... of the CTA-pair kernels
     std::atomic<int> dyn_smem_sparse[2][3];       // ... of the kernels that walk lists of key blocks
-    std::atomic<bool> sparse_bwd_ready[2][2];     // launch attribute of sparse_bwd_kernel<D><pass> is set
+    std::atomic<int> dyn_smem_masked[2][3];       // ... of the kernels with a mask
+    std::atomic<bool> sparse_bwd_ready[2][2][2];  // launch attribute of sparse_bwd_kernel<D><pass><dense> is set
     std::atomic<bool> topk_ready[2];              // ... of block_topk_kernel<8>, <4>
     std::atomic<bool> adaln_ready[2][3][2][3];    // launch attribute of adaln_kernel<x fp32><mode><a row ahead><width> is set
     std::atomic<void*> static_scratch{nullptr};   // device address of the built-in scratch array
@@ -174,9 +175,11 @@ int ensure_status_word(DeviceState& st) {
 
 // bf16 [B][L][H][D] tensor seen as a rank-4 map {D, H, L, B}; one box = 64 columns x `rows` rows
 // of one head, laid out in shared memory with the 128-byte swizzle the MMA descriptors expect.
-int make_map(CUtensorMap* map, const void* base, int B, int L, int H, int D, int rows) {
+// `stride`: of batch, token and head in elements where the tensor is not contiguous (0 along an axis of one).
+int make_map(CUtensorMap* map, const void* base, int B, int L, int H, int D, int rows, const long long* stride = nullptr) {
     const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)H, (cuuint64_t)L, (cuuint64_t)B};
-    const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)H * D * 2, (cuuint64_t)L * H * D * 2};
+    cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)H * D * 2, (cuuint64_t)L * H * D * 2};
+    for (int i = 0; i < 3; ++i) if (stride && stride[2 - i]) strides[i] = (cuuint64_t)stride[2 - i] * 2;
     const cuuint32_t box[4] = {64, 1, (cuuint32_t)rows, 1};
     const cuuint32_t estr[4] = {1, 1, 1, 1};
     CUresult r = g_encode_tiled.load(std::memory_order_acquire)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box,
@@ -195,11 +198,12 @@ bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
     return a0 < b0 + nb && b0 < a0 + na;
 }
 
-template <int D, int MODE, bool SPLIT, int GROUPS, bool PAIR = false, bool SPARSE = false>
-int launch(const CUtensorMap* maps, const ListKernelArgs& ka, dim3 grid, cudaStream_t stream, DeviceState& st) {
-    auto kern = attn_jvp::attn_jvp_fwd_kernel<D, MODE, SPLIT, GROUPS, PAIR, SPARSE>;
+// HostArgs: ListKernelArgs, or MaskKernelArgs (MASKED)
+template <int D, int MODE, bool SPLIT, int GROUPS, bool PAIR = false, bool SPARSE = false, bool MASKED = false, typename HostArgs>
+int launch(const CUtensorMap* maps, const HostArgs& ka, dim3 grid, cudaStream_t stream, DeviceState& st) {
+    auto kern = attn_jvp::attn_jvp_fwd_kernel<D, MODE, SPLIT, GROUPS, PAIR, SPARSE, MASKED>;
     using Plan = attn_jvp::SmemPlan<D, MODE, GROUPS, PAIR, SPLIT>;
-    std::atomic<int>& slot = SPARSE ? st.dyn_smem_sparse[D == 128][MODE]
+    std::atomic<int>& slot = MASKED ? st.dyn_smem_masked[D == 128][MODE] : SPARSE ? st.dyn_smem_sparse[D == 128][MODE]
                              : PAIR ? st.dyn_smem_pair[MODE][GROUPS - 1] : st.dyn_smem[D == 128][MODE][SPLIT][GROUPS - 1];
     int smem = slot.load(std::memory_order_acquire);
     if (smem == 0) {
@@ -1041,20 +1045,20 @@ SparseBwdLayout sparse_bwd_layout(int B, int H, int Lq, int Lk) {
     return l;
 }
 
-template <int D, bool DKV>
+template <int D, bool DKV, bool DENSE = false>
 int launch_sparse_bwd(const CUtensorMap& x1, const CUtensorMap& x2, const CUtensorMap& y1, const CUtensorMap& y2,
-                      const attn_jvp::SparseBwdArgs& a, cudaStream_t stream, DeviceState& st) {
-    auto kern = attn_jvp::sparse_bwd_kernel<D, DKV>;
+                      const attn_jvp::BwdArgsOf<DENSE>& a, int n_items, cudaStream_t stream, DeviceState& st) {
+    auto kern = attn_jvp::sparse_bwd_kernel<D, DKV, DENSE>;
     constexpr int smem = attn_jvp::SparseBwdPlan<D>::kDynBytes;
-    std::atomic<bool>& ready = st.sparse_bwd_ready[D == 128][DKV];
+    std::atomic<bool>& ready = st.sparse_bwd_ready[D == 128][DKV][DENSE];
     if (!ready.load(std::memory_order_acquire)) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute(MaxDynamicSharedMemorySize)", e);
         ready.store(true, std::memory_order_release);
     }
-    kern<<<(unsigned)(a.n_items < st.sm_count ? a.n_items : st.sm_count), attn_jvp::kBwdThreads, smem, stream>>>(x1, x2, y1, y2, a);
+    kern<<<(unsigned)(n_items < st.sm_count ? n_items : st.sm_count), attn_jvp::kBwdThreads, smem, stream>>>(x1, x2, y1, y2, a);
     const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? 0 : cuda_fail("sparse backward kernel launch", e);
+    return e == cudaSuccess ? 0 : cuda_fail("attention backward kernel launch", e);
 }
 
 template <int D>
@@ -1067,8 +1071,8 @@ int sparse_bwd_run(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorM
     attn_jvp::sparse_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + prep.zero_blocks) + order_windows(dkv.n_items), 256, 0, stream>>>(prep);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail("sparse backward preparation launch", e);
-    if (int rc = launch_sparse_bwd<D, true>(mk, mv, mq, mdo, dkv, stream, st)) return rc;
-    return launch_sparse_bwd<D, false>(mq, mdo, mk, mv, dq, stream, st);
+    if (int rc = launch_sparse_bwd<D, true>(mk, mv, mq, mdo, dkv, dkv.n_items, stream, st)) return rc;
+    return launch_sparse_bwd<D, false>(mq, mdo, mk, mv, dq, dq.n_items, stream, st);
 }
 
 int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse,
@@ -1142,6 +1146,246 @@ int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, con
                                     dkv.out2, dkv.out1, dkv.counter, B, H, Lq, Lk, n_q, n_k, 0, 0};
     return D == 128 ? sparse_bwd_run<128>(mq, mk, mv, mdo, prep, dkv, dqa, stream, st)
                     : sparse_bwd_run<64>(mq, mk, mv, mdo, prep, dkv, dqa, stream, st);
+}
+
+// Strides of batch, token and head of a strided tensor (0 along an axis of one), the bytes it spans, and whether they are in order.
+bool head_strides(const long long* in, int B, int L, int H, int D, long long* out, size_t* bytes) {
+    const int n[3] = {B, L, H};
+    size_t last = 0;
+    for (int i = 0; i < 3; ++i) {
+        out[i] = n[i] > 1 ? in[i] : 0;
+        if (out[i] < 0 || out[i] > (1LL << 40) || out[i] % 8 != 0) return false;
+        last += (size_t)(n[i] - 1) * (size_t)out[i];
+    }
+    *bytes = (last + D) * 2;
+    return true;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Attention with a causal mask, key lengths, shared key heads and strided inputs (the masked form of the forward kernel, the dense form of sparse_bwd.cuh)
+// ---------------------------------------------------------------------------------------------
+// Checks and strides of what both directions read.
+struct AttentionInputs { long long q[3], k[3], v[3]; size_t q_bytes, k_bytes, v_bytes; };
+int attention_common(const attn_jvp_attention_t* in, AttentionInputs& x) {
+    if (!in) return ATTN_JVP_ERR_NULL;
+    if (int rc = sparse_shape(in->B, in->H, in->Lq, in->Lk, in->D)) return rc;
+    if (in->Hk < 1 || in->H % in->Hk != 0) return ATTN_JVP_ERR_SHAPE;
+    if (!in->q || !in->k || !in->v) return ATTN_JVP_ERR_NULL;
+    if (!std::isfinite(in->scale)) return ATTN_JVP_ERR_SCALE;
+    if (in->causal != 0 && in->causal != 1) return ATTN_JVP_ERR_FLAGS;
+    if (!head_strides(in->q_stride, in->B, in->Lq, in->H, in->D, x.q, &x.q_bytes)) return ATTN_JVP_ERR_SHAPE;
+    if (!head_strides(in->k_stride, in->B, in->Lk, in->Hk, in->D, x.k, &x.k_bytes)) return ATTN_JVP_ERR_SHAPE;
+    if (!head_strides(in->v_stride, in->B, in->Lk, in->Hk, in->D, x.v, &x.v_bytes)) return ATTN_JVP_ERR_SHAPE;
+    // (a tensor map takes no stride of 0 along an axis that has more than one entry)
+    for (const long long* st : {x.q, x.k, x.v}) {
+        const int n[3] = {in->B, st == x.q ? in->Lq : in->Lk, st == x.q ? in->H : in->Hk};
+        for (int i = 0; i < 3; ++i) if (n[i] > 1 && st[i] < in->D) return ATTN_JVP_ERR_SHAPE;
+    }
+    return 0;
+}
+
+int attention_fwd(const attn_jvp_attention_t* in, void* o, void* to, float* lse, float* mu, unsigned flags, cudaStream_t stream) {
+    if (flags & ~(ATTN_JVP_KV_TANGENT_FREE | ATTN_JVP_FWD_ONLY)) return ATTN_JVP_ERR_FLAGS;
+    AttentionInputs x;
+    if (int rc = attention_common(in, x)) return rc;
+    const bool fwd_only = (flags & ATTN_JVP_FWD_ONLY) != 0;
+    const int mode = fwd_only ? attn_jvp::kModeFwdOnly
+                              : (flags & ATTN_JVP_KV_TANGENT_FREE) ? attn_jvp::kModeKvTangentFree : attn_jvp::kModeJvp;
+    const bool jvp_kv = mode == attn_jvp::kModeJvp;
+    if (!o || !lse || (!fwd_only && (!in->tq || !to)) || (jvp_kv && (!in->tk || !in->tv))) return ATTN_JVP_ERR_NULL;
+    const int B = in->B, H = in->H, Hk = in->Hk, Lq = in->Lq, Lk = in->Lk, D = in->D;
+    const size_t row = (size_t)B * D * 2, nq = row * H * Lq, nk = row * Hk * Lk, nl = (size_t)B * H * Lq * 4;
+    const Span ins[] = {{in->q, x.q_bytes, 16}, {in->k, x.k_bytes, 16}, {in->v, x.v_bytes, 16}, {fwd_only ? nullptr : in->tq, nq, 16},
+                        {jvp_kv ? in->tk : nullptr, nk, 16}, {jvp_kv ? in->tv : nullptr, nk, 16}, {in->k_lengths, (size_t)B * 4, 4}};
+    const Span outs[] = {{o, nq, 16}, {fwd_only ? nullptr : to, nq, 16}, {lse, nl, 16}, {mu, nl, 16}};
+    if (int rc = check_spans(ins, 7, outs, 4)) return rc;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    DeviceState& st = *stp;
+    if (int rc = get_encode_fn()) return rc;
+    if (int rc = ensure_status_word(st)) return rc;
+
+    const int key_tile = attn_jvp::key_tile(D, mode, false, false);
+    CUtensorMap maps[9];                                 // (maps that the mode does not read are copies)
+    if (int rc = make_map(&maps[0], in->q, B, Lq, H, D, attn_jvp::kBlockM, x.q)) return rc;
+    if (int rc = make_map(&maps[1], in->k, B, Lk, Hk, D, key_tile, x.k)) return rc;
+    if (int rc = make_map(&maps[2], in->v, B, Lk, Hk, D, key_tile, x.v)) return rc;
+    maps[3] = maps[0];
+    maps[4] = maps[5] = maps[8] = maps[1];
+    if (!fwd_only) if (int rc = make_map(&maps[3], in->tq, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
+    if (jvp_kv) {
+        if (int rc = make_map(&maps[4], in->tk, B, Lk, Hk, D, key_tile)) return rc;
+        if (int rc = make_map(&maps[5], in->tv, B, Lk, Hk, D, key_tile)) return rc;
+    }
+    if (int rc = make_map(&maps[6], o, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
+    maps[7] = maps[6];
+    if (!fwd_only) if (int rc = make_map(&maps[7], to, B, Lq, H, D, attn_jvp::kBlockM)) return rc;
+    attn_jvp::MaskKernelArgs ka = {};
+    ka.o = static_cast<__nv_bfloat16*>(o);
+    ka.to = static_cast<__nv_bfloat16*>(to);
+    ka.lse = lse;
+    ka.mu = mu;
+    ka.host_status = st.host_status_dev.load(std::memory_order_acquire);
+    ka.B = B;
+    ka.H = H;
+    ka.Lq = Lq;
+    ka.Lk = Lk;
+    ka.n_kv_tiles = (Lk + key_tile - 1) / key_tile;
+    ka.scale = in->scale;
+    ka.scale_log2 = (in->scale == 0.0f) ? 0x1p-100f : in->scale * 1.4426950408889634f;     // (see run())
+    ka.splits = 1;
+    ka.n_q_tiles = n_blocks(Lq);
+    ka.n_items = ka.n_q_tiles * H * B;
+    ka.mask = {in->k_lengths, in->causal, Lk - Lq, H / Hk};
+    // one CTA per item where items are long or of unlike length (the hardware balances them), else persistent ones, as in run()
+    const bool persistent = !in->causal && (Lk + attn_jvp::kBlockN - 1) / attn_jvp::kBlockN <= kPersistentMaxTiles;
+    const dim3 grid((unsigned)(persistent && ka.n_items > st.sm_count ? st.sm_count : ka.n_items), 1, 1);
+    // softmax groups as softmax_groups_for() chooses them for long items
+    if (D == 64) {
+        switch (mode) {
+            case attn_jvp::kModeJvp: return launch<64, attn_jvp::kModeJvp, false, 2, false, false, true>(maps, ka, grid, stream, st);
+            case attn_jvp::kModeKvTangentFree: return launch<64, attn_jvp::kModeKvTangentFree, false, 2, false, false, true>(maps, ka, grid, stream, st);
+            default: return launch<64, attn_jvp::kModeFwdOnly, false, 2, false, false, true>(maps, ka, grid, stream, st);
+        }
+    }
+    switch (mode) {
+        case attn_jvp::kModeJvp: return launch<128, attn_jvp::kModeJvp, false, 1, false, false, true>(maps, ka, grid, stream, st);
+        case attn_jvp::kModeKvTangentFree: return launch<128, attn_jvp::kModeKvTangentFree, false, 1, false, false, true>(maps, ka, grid, stream, st);
+        default: return launch<128, attn_jvp::kModeFwdOnly, false, 2, false, false, true>(maps, ka, grid, stream, st);
+    }
+}
+
+// Parts that the tiles of each item are cut into: one where the items alone keep the SMs busy.  A part costs about a tile to start, and two accumulators'
+// bytes each way (in tiles of about 1.2 us at D = 128) and another launch to join; the SMs draw parts until none is left.
+int dense_splits(long long items, int tiles, int D, bool dkv) {
+    double best = 0.0;
+    int splits = 1;
+    for (int s = 1; s <= 16 && (s == 1 || tiles / s >= 2); ++s) {
+        const double rounds = (double)((items * s + kSms - 1) / kSms);
+        const double join = s == 1 ? 0.0 : 3.0 + items * s * (dkv ? 2.0 : 1.0) * 128 * D * 4 * 2 / 5.0e6 / 1.2 / (D / 128.0);
+        const double cost = rounds * ((double)tiles / s + 1.0) + join;
+        if (s == 1 || cost < best) { best = cost; splits = s; }
+    }
+    return splits;
+}
+struct DenseBwdLayout { size_t counters, rows, tail_k, tail_v, part, total; int dkv_splits, dq_splits; };
+DenseBwdLayout dense_bwd_layout(int B, int H, int Hk, int Lq, int Lk, int D) {
+    auto pad = [](size_t n) { return (n + 255) & ~(size_t)255; };
+    const size_t n_q = n_blocks(Lq), n_k = n_blocks(Lk);
+    DenseBwdLayout l;
+    l.dkv_splits = dense_splits((long long)B * Hk * n_k, (int)n_q * (H / Hk), D, true);
+    l.dq_splits = dense_splits((long long)B * H * n_q, (int)n_k, D, false);
+    const size_t dkv = l.dkv_splits > 1 ? (size_t)l.dkv_splits * B * Hk * n_k * kSelBlock * 2 * D * 4 : 0;
+    const size_t dq = l.dq_splits > 1 ? (size_t)l.dq_splits * B * H * n_q * kSelBlock * D * 4 : 0;
+    l.counters = 0;
+    l.rows = 256;
+    l.tail_k = l.rows + pad((size_t)B * H * n_q * kSelBlock * 2 * sizeof(float));
+    l.tail_v = l.tail_k + pad((size_t)B * Hk * kSelBlock * D * 2);
+    l.part = l.tail_v + pad((size_t)B * Hk * kSelBlock * D * 2);
+    l.total = l.part + (dkv > dq ? dkv : dq);            // (the passes run one after the other)
+    return l;
+}
+
+template <int D>
+int dense_bwd_run(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo, attn_jvp::DenseBwdPrep& prep,
+                  cudaStream_t stream, DeviceState& st) {
+    const attn_jvp::DenseBwdArgs &dkv = prep.dkv, &dq = prep.dq;
+    const long long rows = (long long)prep.B * prep.n_q * kSelBlock * prep.H;
+    prep.row_blocks = (int)((rows + attn_jvp::kPrepRows<D> - 1) / attn_jvp::kPrepRows<D>);
+    prep.zero_blocks = dkv.mask.lengths || dkv.mask.causal ? (dkv.n_items + dq.n_items + 7) / 8 : 0;       // (without a mask every item has tiles)
+    const int tails = dkv.mask.lengths ? prep.B * dkv.H : 0;
+    attn_jvp::dense_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + prep.zero_blocks + tails), 256, 0, stream>>>(prep);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return cuda_fail("attention backward preparation launch", e);
+    if (int rc = launch_sparse_bwd<D, true, true>(mk, mv, mq, mdo, dkv, dkv.n_items * dkv.splits, stream, st)) return rc;
+    if (dkv.splits > 1) attn_jvp::dense_join_kernel<D, true><<<(unsigned)dkv.n_items * (kSelBlock * 2 * D / 2048), 256, 0, stream>>>(dkv);
+    if (int rc = launch_sparse_bwd<D, false, true>(mq, mdo, mk, mv, dq, dq.n_items * dq.splits, stream, st)) return rc;
+    if (dq.splits > 1) attn_jvp::dense_join_kernel<D, false><<<(unsigned)dq.n_items * (kSelBlock * D / 2048), 256, 0, stream>>>(dq);
+    e = cudaGetLastError();
+    return e == cudaSuccess ? 0 : cuda_fail("attention backward join launch", e);
+}
+
+int attention_bwd(const attn_jvp_attention_t* in, const void* d_o, const void* o, const float* lse, void* dq, void* dk, void* dv, void* workspace,
+                  size_t workspace_bytes, cudaStream_t stream) {
+    AttentionInputs x;
+    if (int rc = attention_common(in, x)) return rc;
+    if (!d_o || !o || !lse || !dq || !dk || !dv || !workspace) return ATTN_JVP_ERR_NULL;
+    const int B = in->B, H = in->H, Hk = in->Hk, Lq = in->Lq, Lk = in->Lk, D = in->D;
+    const size_t row = (size_t)B * D * 2, nq = row * H * Lq, nk = row * Hk * Lk;
+    const DenseBwdLayout lay = dense_bwd_layout(B, H, Hk, Lq, Lk, D);
+    const Span ins[] = {{d_o, nq, 16}, {in->q, x.q_bytes, 16}, {in->k, x.k_bytes, 16}, {in->v, x.v_bytes, 16}, {o, nq, 16},
+                        {lse, (size_t)B * H * Lq * 4, 4}, {in->k_lengths, (size_t)B * 4, 4}};
+    const Span outs[] = {{dq, nq, 16}, {dk, nk, 16}, {dv, nk, 16}, {workspace, lay.total, 256}};
+    if (workspace_bytes < lay.total) return ATTN_JVP_ERR_WORKSPACE;
+    if (int rc = check_spans(ins, 7, outs, 4)) return rc;
+    int dev = 0;
+    DeviceState* stp = nullptr;
+    if (int rc = current_device(&dev, &stp)) return rc;
+    DeviceState& st = *stp;
+    if (int rc = get_encode_fn()) return rc;
+    if (int rc = ensure_status_word(st)) return rc;
+    CUtensorMap mq, mk, mv, mdo;
+    if (int rc = make_map(&mq, in->q, B, Lq, H, D, kSelBlock, x.q)) return rc;
+    if (int rc = make_map(&mk, in->k, B, Lk, Hk, D, kSelBlock, x.k)) return rc;
+    if (int rc = make_map(&mv, in->v, B, Lk, Hk, D, kSelBlock, x.v)) return rc;
+    if (int rc = make_map(&mdo, d_o, B, Lq, H, D, kSelBlock)) return rc;
+
+    char* w = static_cast<char*>(workspace);
+    const int n_q = n_blocks(Lq), n_k = n_blocks(Lk);
+    attn_jvp::DenseBwdPrep p = {};
+    attn_jvp::DenseBwdArgs a = {};
+    a.rows = reinterpret_cast<float*>(w + lay.rows);
+    a.host_status = st.host_status_dev.load(std::memory_order_acquire);
+    a.n_q = n_q;
+    a.n_k = n_k;
+    a.Lq = Lq;
+    a.Lk = Lk;
+    a.scale = in->scale;
+    a.scale_log2 = in->scale * 1.4426950408889634f;
+    a.wide_out = (((uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv) & 31u) == 0;
+    a.mask = {in->k_lengths, in->causal, Lk - Lq, H / Hk};
+    a.part = reinterpret_cast<float*>(w + lay.part);
+    a.tail1 = mk;
+    a.tail2 = mv;
+    p.tail_k = reinterpret_cast<__nv_bfloat16*>(w + lay.tail_k);
+    p.tail_v = reinterpret_cast<__nv_bfloat16*>(w + lay.tail_v);
+    if (in->k_lengths) {
+        if (int rc = make_map(&a.tail1, p.tail_k, B, kSelBlock, Hk, D, kSelBlock)) return rc;
+        if (int rc = make_map(&a.tail2, p.tail_v, B, kSelBlock, Hk, D, kSelBlock)) return rc;
+    }
+    p.counters = reinterpret_cast<int*>(w + lay.counters);
+    p.dkv = p.dq = a;
+    p.dkv.counter = p.counters;
+    p.dkv.H = Hk;
+    p.dkv.n_items_per_head = n_k;
+    p.dkv.n_items = B * Hk * n_k;
+    p.dkv.L_own = Lk;
+    p.dkv.L_other = Lq;
+    p.dkv.out1 = static_cast<__nv_bfloat16*>(dv);
+    p.dkv.out2 = static_cast<__nv_bfloat16*>(dk);
+    p.dkv.splits = lay.dkv_splits;
+    p.dq.counter = p.counters + 1;
+    p.dq.H = H;
+    p.dq.n_items_per_head = n_q;
+    p.dq.n_items = B * H * n_q;
+    p.dq.L_own = Lq;
+    p.dq.L_other = Lk;
+    p.dq.out1 = static_cast<__nv_bfloat16*>(dq);
+    p.dq.splits = lay.dq_splits;
+    p.o = static_cast<const uint4*>(o);
+    p.d_o = static_cast<const uint4*>(d_o);
+    p.lse = lse;
+    p.rows = reinterpret_cast<float*>(w + lay.rows);
+    p.k = static_cast<const __nv_bfloat16*>(in->k);
+    p.v = static_cast<const __nv_bfloat16*>(in->v);
+    p.k_b = x.k[0]; p.k_l = x.k[1]; p.k_h = x.k[2];
+    p.v_b = x.v[0]; p.v_l = x.v[1]; p.v_h = x.v[2];
+    p.B = B;
+    p.H = H;
+    p.Lq = Lq;
+    p.n_q = n_q;
+    return D == 128 ? dense_bwd_run<128>(mq, mk, mv, mdo, p, stream, st) : dense_bwd_run<64>(mq, mk, mv, mdo, p, stream, st);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1237,19 +1481,6 @@ int rotary_launch(const RotaryParams& p, int D, bool half, cudaStream_t stream) 
     }
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? 0 : cuda_fail("rotary kernel launch", e);
-}
-
-// Strides of batch, token and head of a strided tensor (0 along an axis of one), the bytes it spans, and whether they are in order.
-bool head_strides(const long long* in, int B, int L, int H, int D, long long* out, size_t* bytes) {
-    const int n[3] = {B, L, H};
-    size_t last = 0;
-    for (int i = 0; i < 3; ++i) {
-        out[i] = n[i] > 1 ? in[i] : 0;
-        if (out[i] < 0 || out[i] > (1LL << 40) || out[i] % 8 != 0) return false;
-        last += (size_t)(n[i] - 1) * (size_t)out[i];
-    }
-    *bytes = (last + D) * 2;
-    return true;
 }
 
 // What the two directions share: checks, and the kernel's parameters but for its outputs.  spans: q, k, tq, tk, weights, biases, table, index.
@@ -1560,6 +1791,20 @@ int attn_jvp_sparse_bwd(const void* d_o, const void* q, const void* k, const voi
                         int B, int H, int Lq, int Lk, int D, float scale, void* workspace, size_t workspace_bytes, void* cuda_stream) {
     return sparse_bwd(d_o, q, k, v, o, lse, mask, index, tiles, order, dq, dk, dv, B, H, Lq, Lk, D, scale, workspace, workspace_bytes,
                       static_cast<cudaStream_t>(cuda_stream));
+}
+
+int attn_jvp_attention_fwd(const attn_jvp_attention_t* in, void* o, void* to, float* lse, float* mu, unsigned flags, void* cuda_stream) {
+    return attention_fwd(in, o, to, lse, mu, flags, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t attn_jvp_attention_bwd_workspace_bytes(int B, int H, int Hk, int Lq, int Lk, int D) {
+    if (sparse_shape(B, H, Lq, Lk, D) || Hk < 1 || H % Hk != 0) return 0;
+    return dense_bwd_layout(B, H, Hk, Lq, Lk, D).total;
+}
+
+int attn_jvp_attention_bwd(const attn_jvp_attention_t* in, const void* d_o, const void* o, const float* lse, void* dq, void* dk, void* dv,
+                           void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    return attention_bwd(in, d_o, o, lse, dq, dk, dv, workspace, workspace_bytes, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int attn_jvp_rotary_table(const void* positions, int pos_type, long long n, int axes, const int* dims, const double* base,

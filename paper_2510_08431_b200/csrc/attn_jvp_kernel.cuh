@@ -141,10 +141,21 @@ struct KeyLists {
 struct ListKernelArgs : KernelArgs {
     KeyLists lists;
 };
-template <int MODE, bool kSparse>
-using KernelArgsOf = std::conditional_t<kSparse || MODE == kModeFwdOnly, ListKernelArgs, KernelArgs>;
+// Which keys a query sees (kMasked), and which head's.
+struct KeyMask {
+    const int* lengths;   // [B] keys of each batch, or null: all of Lk
+    int causal, offset;   // causal: query i sees the keys j <= i + offset
+    int group;            // query heads that share a key head
+};
+struct MaskKernelArgs : KernelArgs {
+    KeyMask mask;
+};
+template <int MODE, bool kSparse, bool kMasked>
+using KernelArgsOf = std::conditional_t<kMasked, MaskKernelArgs, std::conditional_t<kSparse || MODE == kModeFwdOnly, ListKernelArgs, KernelArgs>>;
 __device__ __forceinline__ KeyLists lists_of(const KernelArgs&) { return {}; }
 __device__ __forceinline__ KeyLists lists_of(const ListKernelArgs& a) { return a.lists; }
+__device__ __forceinline__ KeyMask mask_of(const KernelArgs&) { return {}; }
+__device__ __forceinline__ KeyMask mask_of(const MaskKernelArgs& a) { return a.mask; }
 
 // Shared-memory plan of a kernel variant.
 //   One Q/tQ buffer (full JVP at D = 128, and every CTA-pair variant): Q, tQ resident, ring slots of one primal +
@@ -574,15 +585,22 @@ __host__ __device__ constexpr int score_buffers(int D, int mode) {
 // 12 heads of 32760 tokens at D = 128, 32 of 256 blocks kept: 686 us in a short run (1200 TFLOP/s), 750 in a long
 // one (1000 W, about 1.45 GHz); tangents at 2 x 16 heads of 4096 tokens, 8 of 32 blocks: 162 us; tangents with a constant context at
 // D = 64, 24 heads of 4100 queries, up to 30 of 63 blocks: 156 us.
-template <int D, int MODE, bool kSplit, int kGroups, bool kPair, bool kSparse = false>
+//
+// kMasked: a causal mask, a length of every batch's keys, and key heads that several query heads share.  An item's tiles are those that
+// its last row sees; which of a tile's keys a row sees is a number per row (`valid`), and what it does not see is replaced, not multiplied
+// away: -inf for scores, 0 for tangent scores.  What lies in memory behind a batch's length may be anything: the MMA warp writes zeros over those
+// rows of the one V tile that holds the end (0 times NaN would be NaN).  Under a causal mask a head's long items come first.
+template <int D, int MODE, bool kSplit, int kGroups, bool kPair, bool kSparse = false, bool kMasked = false>
 __global__ void __launch_bounds__(num_threads(kGroups), 1)
 attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_tq,
                     const __grid_constant__ CUtensorMap tm_tk, const __grid_constant__ CUtensorMap tm_tv,
                     const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ CUtensorMap tm_to,
-                    const __grid_constant__ CUtensorMap tm_k32, const KernelArgsOf<MODE, kSparse> args) {
+                    const __grid_constant__ CUtensorMap tm_k32, const KernelArgsOf<MODE, kSparse, kMasked> args) {
     static_assert(!kPair || (D == 128 && !kSplit), "the CTA-pair variant exists at D = 128, without key chunks");
-    static_assert(!kSparse || (!kPair && !kSplit), "key block lists: one CTA per query tile, no key chunks");
+    static_assert(!(kSparse || kMasked) || (!kPair && !kSplit), "key block lists and masks: one CTA per query tile, no key chunks");
+    static_assert(!kSparse || !kMasked, "lists or masks");
+    constexpr bool kRagged = kSparse || kMasked;             // items have their own numbers of key tiles, possibly none
     using Plan = SmemPlan<D, MODE, kGroups, kPair, kSplit>;
     constexpr int kBN = Plan::kBN;                           // keys per tile
     constexpr bool kDoubleQ = Plan::kDoubleQ;
@@ -638,7 +656,8 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const int first_item = kPair ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
     const int item_stride = kPair ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
     const KeyLists lists = lists_of(args);
-    struct Item { int q0, h, b, split, tile0, n_kv; int n_real, first; const int* list; };
+    const KeyMask mask = mask_of(args);
+    struct Item { int q0, h, b, split, tile0, n_kv; int n_real, first; const int* list; int len, hk; };
     // Work item number -> (query tile, head, batch [, chunk]).  The roles walk their items with a fixed stride, so
     // after the first item the three indices are advanced by the stride's own decomposition (carry by compare and
     // subtract) instead of being divided out again: the divisions would sit on the critical path of every item
@@ -646,7 +665,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     // kSparse: item number i is list number i, or with an order its entry at place i, where every other round of the CTAs runs
     // backwards through the sorted lists, so that each CTA gets its share of long and short ones.  `after`: the list of the
     // item behind this one.
-    struct Walk { int qt, h, z; int tiles64, first, round, after; };
+    struct Walk { int qt, h, z; int tiles64, first, round, after; int len; };
     auto ordered_list = [&](int round) -> int {
         const int item = first_item + round * item_stride;
         if (item >= args.n_items) return args.n_items;
@@ -658,6 +677,10 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const bool exists = row < args.n_items;
         k.tiles64 = exists ? __ldg(lists.tiles + row) : 0;
         k.first = exists ? __ldg(lists.list + static_cast<size_t>(row) * lists.stride) : 0;
+    };
+    // kMasked: the keys of the walk's batch (read an item ahead, as the lists are)
+    auto read_length = [&](Walk& k) {
+        k.len = mask.lengths == nullptr ? args.Lk : min(max(__ldg(mask.lengths + min(k.z, args.B - 1)), 0), args.Lk);
     };
     auto walk_init = [&](int item) -> Walk {
         Walk k{};
@@ -673,6 +696,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const int row = ordered ? ordered_list(0) : first_item;
         Walk k = walk_init(row);
         if (kSparse) read_list(k, row);
+        if (kMasked) read_length(k);
         if (ordered) k.after = ordered_list(1);
         return k;
     };
@@ -692,6 +716,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (k.h >= args.H) { k.h -= args.H; ++k.z; }
         k.z += walk_stride.z;
         if (kSparse) read_list(k, item);
+        if (kMasked) read_length(k);
     };
     auto item_of = [&](const Walk& k) -> Item {
         Item w;
@@ -711,10 +736,20 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             w.n_real = kBN == kBlockN ? tiles64 : (tiles64 + 1) / 2;
             w.n_kv = max(1, w.n_real);
         }
+        w.len = w.hk = 0;
+        if (kMasked) {
+            if (mask.causal) w.q0 = (args.n_q_tiles - 1 - k.qt) * kBlockM;
+            w.len = k.len;
+            w.hk = k.h / mask.group;
+            const int seen = mask.causal ? min(k.len, max(0, min(w.q0 + kBlockM, args.Lq) + mask.offset)) : k.len;    // by the last row
+            w.n_real = (seen + kBN - 1) / kBN;
+            w.n_kv = max(1, w.n_real);
+        }
         return w;
     };
     // first key of tile j of an item (a tile that only fills up: behind the last key, where TMA fills in zeros)
     auto key_of = [&](const Item& w, int j) -> int {
+        if (kMasked) return (j < w.n_real ? j : args.n_kv_tiles) * kBN;
         if (!kSparse) return (w.tile0 + j) * kBN;
         if (j >= w.n_real) return lists.stride * kBlockM;
         const int e = kBN == kBlockN ? j >> 1 : j;
@@ -726,7 +761,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     // CTA's items form one stream.  The score MMAs of an item's leading tiles are issued in the last bursts of the
     // item before (its Q, tQ are resident by then), and the ring carries their K tiles in that order, so that an
     // item boundary costs the MMA warp and the producer nothing.
-    const bool stream_items = kDoubleQ && !kSplit && !kSparse && args.n_kv_tiles >= kBufs;
+    const bool stream_items = kDoubleQ && !kSplit && !kRagged && args.n_kv_tiles >= kBufs;
     // Score buffer and barrier phase of a key tile, g % kBufs and (g / kBufs) & 1, carried along tile by tile (a
     // division by three per use would sit on the MMA warp's critical chain of dependent instructions).
     struct BufPos { int buf; uint32_t phase; };
@@ -920,9 +955,9 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 // per 64-column half: [K_half (8 KB)][tK_half (8 KB)] so that [K ; tK] is one N = 128 operand
 #pragma unroll
                 for (int hf = 0; hf < kHalves; ++hf) {
-                    tma_load_4d(dst + hf * kKHalfStride, &tm_k, bar, hf * 64, w.h, row0, w.b);
+                    tma_load_4d(dst + hf * kKHalfStride, &tm_k, bar, hf * 64, kMasked ? w.hk : w.h, row0, w.b);
                     if (kHasTKV)
-                        tma_load_4d(dst + hf * kKHalfStride + Plan::kKvHalfBytes, &tm_tk, bar, hf * 64, w.h, row0, w.b);
+                        tma_load_4d(dst + hf * kKHalfStride + Plan::kKvHalfBytes, &tm_tk, bar, hf * 64, kMasked ? w.hk : w.h, row0, w.b);
                 }
                 return true;
             };
@@ -951,9 +986,9 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 // [V_half0][V_half1][tV_half0][tV_half1]: consecutive 64-wide N atoms of [V | tV]
 #pragma unroll
                 for (int hf = 0; hf < kHalves; ++hf) {
-                    tma_load_4d(dst + hf * Plan::kKvHalfBytes, &tm_v, bar, hf * 64, w.h, row0, w.b);
+                    tma_load_4d(dst + hf * Plan::kKvHalfBytes, &tm_v, bar, hf * 64, kMasked ? w.hk : w.h, row0, w.b);
                     if (kHasTKV)
-                        tma_load_4d(dst + (kHalves + hf) * Plan::kKvHalfBytes, &tm_tv, bar, hf * 64, w.h, row0, w.b);
+                        tma_load_4d(dst + (kHalves + hf) * Plan::kKvHalfBytes, &tm_tv, bar, hf * 64, kMasked ? w.hk : w.h, row0, w.b);
                 }
                 return true;
             };
@@ -1339,6 +1374,18 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     if (leader) TRACE(29, g0 + j);   // MMA: burst of tile j begins (loop top)
                     tc_fence_after();
                     if (leader) TRACE(30, g0 + j);   // MMA: after the tensor-core fence
+                    if (kMasked && w.len < args.Lk && j < w.n_real && w.len - j * kBN < kBN) {
+                        // the batch's keys end inside this tile: whatever the rows behind them hold, P~ is 0 there, and so must V be
+                        constexpr int kPieces = (kHasTKV ? 2 : 1) * kHalves;
+                        const int from = w.len - j * kBN;
+                        const uint32_t tile = smem_ring + pos_v.slot * Plan::kSlotBytes;
+                        for (int i = lane; i < (kBN - from) * 8; i += 32) {
+#pragma unroll
+                            for (int h = 0; h < kPieces; ++h) st_shared_v4(tile + h * Plan::kKvHalfBytes + from * 128 + i * 16, 0u, 0u, 0u, 0u);
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
                     issue_values_p(j, g0 + j, bp.buf);
                     issue_values_h(j, g0 + j, bp.buf, pos_v.slot);
                     if (has_k) issue_scores_a(g0 + j + kBufs, bp.buf);    // tile j + kBufs reuses tile j's buffer
@@ -1487,8 +1534,9 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #endif
 
                 // keys past Lk (zero-filled by TMA) must not enter the softmax
-                const int valid = !kSparse ? args.Lk - (w.tile0 + j) * kBN
-                                           : (j + 1 < w.n_real ? kBN : (j + 1 == w.n_real ? last_valid : 0));
+                const int valid = kMasked ? (j < w.n_real ? (mask.causal ? min(w.len, w.q0 + row + 1 + mask.offset) : w.len) - j * kBN : 0)
+                                  : !kSparse ? args.Lk - (w.tile0 + j) * kBN
+                                             : (j + 1 < w.n_real ? kBN : (j + 1 == w.n_real ? last_valid : 0));
                 if (valid < kBN) {
                     const uint32_t masked = neg_scale ? 0x7F800000u : 0xFF800000u;   // -inf after scaling
 #pragma unroll
@@ -1509,7 +1557,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 float mx = neg_scale ? fminf(fminf(mx4[0], mx4[1]), fminf(mx4[2], mx4[3]))
                                      : fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3]));
                 mx *= c1;
-                if (kSparse && j == 0 && valid <= 0) mx = 0.0f;       // (a finite reference for rows without any key)
+                if (kRagged && j == 0 && valid <= 0) mx = 0.0f;       // (a finite reference for rows without any key)
 
                 if (kGroups == 2) {
                     // The decision of tile g - 1 (the other group's) comes first, also across items: the exchange
@@ -1540,7 +1588,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     float sm4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int c = 0; c < kBN; ++c) sm4[c & 3] += __uint_as_float(tv[c]);
-                    const int n_valid = valid < kBN ? (kSparse ? max(1, valid) : valid) : kBN;
+                    const int n_valid = valid < kBN ? (kRagged ? max(1, valid) : valid) : kBN;
                     return sc * ((sm4[0] + sm4[1]) + (sm4[2] + sm4[3])) / static_cast<float>(n_valid);
                 };
                 if (kHasTQ && kGroups == 1) tc_wait_ld();      // tS is in registers
@@ -1548,6 +1596,10 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     // (a row without any key has H~ = 0 whatever its query holds: NaN times the zero-filled keys is NaN)
 #pragma unroll
                     for (int c = 0; c < kBN; ++c) tv[c] = 0u;
+                }
+                if (kMasked && kHasTQ && valid < kBN) {
+#pragma unroll
+                    for (int c = 0; c < kBN; ++c) if (c >= valid) tv[c] = 0u;
                 }
                 if (kHasTQ && j == 0) ts_shift = centre_of_first_tile();
 
@@ -1669,7 +1721,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 const bool has_next = n_items - item > item_stride;
                 const int next_start = (ring_slot + 2 * (n_kv % kSlots) + (it > 0 ? kRingStage : 0)) % kSlots;
                 int lead = n_kv;                                  // key tiles of the next item
-                if (kSparse && has_next) lead = item_of(wk_next).n_kv;
+                if (kRagged && has_next) lead = item_of(wk_next).n_kv;
                 stage_slot_o = has_next ? (next_start + min(kBufs, lead)) % kSlots : next_start;
                 ring_slot = next_start;
             }
@@ -1741,7 +1793,7 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const float l_tot = l_run, r_tot = r_run;
             const int qi = w.q0 + row;
             const bool in_range = qi < args.Lq;
-            const float inv_l = (kSparse && l_tot == 0.0f) ? 0.0f : 1.0f / l_tot;
+            const float inv_l = (kRagged && l_tot == 0.0f) ? 0.0f : 1.0f / l_tot;
             const float mu = r_tot * inv_l;
             const int b = w.b, h = w.h, split = w.split;
             const size_t row_off = ((static_cast<size_t>(b) * args.Lq + (in_range ? qi : 0)) * args.H + h) * D;

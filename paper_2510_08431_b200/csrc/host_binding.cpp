@@ -28,6 +28,9 @@ decltype(&attn_jvp_block_lists) f_block_lists = nullptr;
 decltype(&attn_jvp_sparse_fwd) f_sparse_fwd = nullptr;
 decltype(&attn_jvp_sparse_bwd) f_sparse_bwd = nullptr;
 decltype(&attn_jvp_sparse_bwd_workspace_bytes) f_sparse_bwd_bytes = nullptr;
+decltype(&attn_jvp_attention_fwd) f_attention_fwd = nullptr;
+decltype(&attn_jvp_attention_bwd) f_attention_bwd = nullptr;
+decltype(&attn_jvp_attention_bwd_workspace_bytes) f_attention_bwd_bytes = nullptr;
 decltype(&attn_jvp_rotary_table) f_rotary_table = nullptr;
 decltype(&attn_jvp_qk_rotary_fwd) f_qk_rotary_fwd = nullptr;
 decltype(&attn_jvp_qk_rotary_bwd) f_qk_rotary_bwd = nullptr;
@@ -368,6 +371,100 @@ PyObject* sparse_bwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
     });
 }
 
+// Strides of batch, token and head of a tensor whose heads are contiguous.
+void heads_of(const at::Tensor& t, const char* name, at::IntArrayRef shape, const at::Device& device, long long* stride) {
+    if (t.device() != device || t.scalar_type() != at::kBFloat16 || t.sizes() != shape || t.stride(3) != 1)
+        refuse("%s must be a bf16 tensor on %s of the shape that the other arguments give, with contiguous heads", name, device.str().c_str());
+    for (int i = 0; i < 3; ++i) {
+        stride[i] = t.stride(i);
+        if (t.size(i) > 1 && stride[i] % 8 != 0) refuse("%s: strides must be multiples of 8 elements", name);
+    }
+}
+
+// ---- dense attention with masks, shared heads and strides ----
+// args: q, k, v, scale (None: 1/sqrt D), causal, k_lengths
+struct Attention {
+    at::Tensor q, k, v, lengths;
+    attn_jvp_attention_t a = {};
+    explicit Attention(PyObject* const* p) : q(required(p[0], "q")), k(required(p[1], "k")), v(required(p[2], "v")), lengths(tensor(p[5], "k_lengths")) {
+        if (!q.is_cuda() || q.dim() != 4 || k.dim() != 4) refuse("q and k must be CUDA tensors [B][L][H][D]");
+        const at::Device dev = q.device();
+        heads_of(q, "q", q.sizes(), dev, a.q_stride);
+        heads_of(k, "k", {q.size(0), k.size(1), k.size(2), q.size(3)}, dev, a.k_stride);
+        heads_of(v, "v", k.sizes(), dev, a.v_stride);
+        if (k.size(2) == 0 || q.size(2) % k.size(2) != 0) refuse("%lld query heads cannot share %lld key heads evenly", (long long)q.size(2), (long long)k.size(2));
+        if (lengths.defined()) expect(lengths, "k_lengths", at::kInt, {q.size(0)}, dev);
+        a.q = ptr(q);
+        a.k = ptr(k);
+        a.v = ptr(v);
+        a.k_lengths = ptr<int>(lengths);
+        a.B = size32(q.size(0));
+        a.Lq = size32(q.size(1));
+        a.H = size32(q.size(2));
+        a.D = size32(q.size(3));
+        a.Lk = size32(k.size(1));
+        a.Hk = size32(k.size(2));
+        a.scale = p[3] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(a.D))) : static_cast<float>(number(p[3], "scale"));
+        a.causal = p[4] == Py_True;
+    }
+    cudaStream_t stream() const { return c10::cuda::getCurrentCUDAStream(q.device().index()).stream(); }
+};
+
+// ... , tq, tk, tv, fwd_only, return_mu, o, to, lse (outputs, or None) -> (rc, o, to, lse, mu)
+PyObject* attention_fwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
+    if (!count(n, 14, "attention_fwd")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        Attention c(p);
+        p += 6;
+        const at::Device dev = c.q.device();
+        const bool fwd_only = p[3] == Py_True;
+        unsigned flags = ATTN_JVP_FWD_ONLY;
+        at::Tensor tq, tk, tv;
+        if (!fwd_only) {
+            tq = required(p[0], "tq");
+            tk = tensor(p[1], "tk");
+            tv = tensor(p[2], "tv");
+            expect(tq, "tq", at::kBFloat16, c.q.sizes(), dev);
+            if (tk.defined() != tv.defined()) refuse("tk and tv must both be given or both be None");
+            flags = tk.defined() ? 0u : ATTN_JVP_KV_TANGENT_FREE;
+            if (tk.defined()) {
+                expect(tk, "tk", at::kBFloat16, c.k.sizes(), dev);
+                expect(tv, "tv", at::kBFloat16, c.k.sizes(), dev);
+            }
+            c.a.tq = ptr(tq);
+            c.a.tk = ptr(tk);
+            c.a.tv = ptr(tv);
+        }
+        const int64_t rows[3] = {c.q.size(0), c.q.size(2), c.q.size(1)};
+        at::Tensor o = tensor(p[5], "o"), to = fwd_only ? at::Tensor() : tensor(p[6], "to"), lse = tensor(p[7], "lse"), mu;
+        if (o.defined()) expect(o, "o", at::kBFloat16, c.q.sizes(), dev); else o = same(c.q);
+        if (to.defined()) expect(to, "to", at::kBFloat16, c.q.sizes(), dev); else if (!fwd_only) to = same(c.q);
+        if (lse.defined()) expect(lse, "lse", at::kFloat, rows, dev); else lse = like(c.q, rows, at::kFloat);
+        if (p[4] == Py_True) mu = like(c.q, rows, at::kFloat);
+        const c10::cuda::CUDAGuard guard(dev);
+        const int rc = unlocked([&] { return f_attention_fwd(&c.a, ptr(o), ptr(to), ptr<float>(lse), ptr<float>(mu), flags, c.stream()); });
+        return result(rc, {o, to, lse, mu});
+    });
+}
+
+// d_o, (the six of Attention), o, lse, workspace -> (rc, dq, dk, dv)
+PyObject* attention_bwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
+    if (!count(n, 10, "attention_bwd")) return nullptr;
+    return guarded([&]() -> PyObject* {
+        at::Tensor d_o = required(p[0], "d_o"), o = required(p[7], "o"), lse = required(p[8], "lse");
+        Attention c(p + 1);
+        const at::Device dev = c.q.device();
+        expect(d_o, "d_o", at::kBFloat16, c.q.sizes(), dev);
+        expect(o, "o", at::kBFloat16, c.q.sizes(), dev);
+        expect(lse, "lse", at::kFloat, {c.q.size(0), c.q.size(2), c.q.size(1)}, dev);
+        at::Tensor ws = scratch(p[9], c.q, f_attention_bwd_bytes(c.a.B, c.a.H, c.a.Hk, c.a.Lq, c.a.Lk, c.a.D));
+        at::Tensor dq = same(c.q), dk = same(c.k), dv = same(c.k);
+        const c10::cuda::CUDAGuard guard(dev);
+        const int rc = unlocked([&] { return f_attention_bwd(&c.a, ptr(d_o), ptr(o), ptr<float>(lse), ptr(dq), ptr(dk), ptr(dv), ptr(ws), ws.nbytes(), c.stream()); });
+        return result(rc, {dq, dk, dv});
+    });
+}
+
 // ---- rotary positions ----
 // The numbers of a sequence (a tuple or list), one per axis.
 int numbers(PyObject* o, const char* name, double* out, int most) {
@@ -409,16 +506,6 @@ PyObject* rotary_table(PyObject*, PyObject* const* p, Py_ssize_t n) {
                                        c10::cuda::getCurrentCUDAStream(pos.device().index()).stream()); });
         return result(rc, {table});
     });
-}
-
-// Strides of batch, token and head of a tensor whose heads are contiguous.
-void heads_of(const at::Tensor& t, const char* name, at::IntArrayRef shape, const at::Device& device, long long* stride) {
-    if (t.device() != device || t.scalar_type() != at::kBFloat16 || t.sizes() != shape || t.stride(3) != 1)
-        refuse("%s must be a bf16 tensor on %s of the shape that the other arguments give, with contiguous heads", name, device.str().c_str());
-    for (int i = 0; i < 3; ++i) {
-        stride[i] = t.stride(i);
-        if (t.size(i) > 1 && stride[i] % 8 != 0) refuse("%s: strides must be multiples of 8 elements", name);
-    }
 }
 
 // args: q, k, table, index, norm, layout, eps, q_weight, k_weight, q_bias, k_bias
@@ -526,6 +613,7 @@ PyObject* bind(PyObject*, PyObject* const* p, Py_ssize_t n) {
     void** slots[] = {reinterpret_cast<void**>(&f_adaln_fwd), reinterpret_cast<void**>(&f_adaln_bwd), reinterpret_cast<void**>(&f_adaln_bwd_bytes),
                       reinterpret_cast<void**>(&f_block_select), reinterpret_cast<void**>(&f_block_select_bytes), reinterpret_cast<void**>(&f_block_lists),
                       reinterpret_cast<void**>(&f_sparse_fwd), reinterpret_cast<void**>(&f_sparse_bwd), reinterpret_cast<void**>(&f_sparse_bwd_bytes),
+                      reinterpret_cast<void**>(&f_attention_fwd), reinterpret_cast<void**>(&f_attention_bwd), reinterpret_cast<void**>(&f_attention_bwd_bytes),
                       reinterpret_cast<void**>(&f_rotary_table), reinterpret_cast<void**>(&f_qk_rotary_fwd), reinterpret_cast<void**>(&f_qk_rotary_bwd),
                       reinterpret_cast<void**>(&f_qk_rotary_bwd_bytes)};
     constexpr Py_ssize_t slots_n = sizeof slots / sizeof slots[0];
@@ -543,7 +631,7 @@ PyObject* bind(PyObject*, PyObject* const* p, Py_ssize_t n) {
 
 #define HOST_FN(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HOST_FN(bind), HOST_FN(adaln_fwd), HOST_FN(adaln_bwd), HOST_FN(block_select), HOST_FN(block_lists),
-                         HOST_FN(sparse_fwd), HOST_FN(sparse_bwd), HOST_FN(rotary_table), HOST_FN(qk_rotary_fwd),
+                         HOST_FN(sparse_fwd), HOST_FN(sparse_bwd), HOST_FN(attention_fwd), HOST_FN(attention_bwd), HOST_FN(rotary_table), HOST_FN(qk_rotary_fwd),
                          HOST_FN(qk_rotary_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", "Tensor checks and calls into the C ABI.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 

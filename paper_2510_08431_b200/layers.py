@@ -5,8 +5,8 @@ The paper restructures every network layer so that one call can carry primals al
 pairs, selected by a ``withT`` keyword (Appendix C.2, "Network Restructuring"); all layers use PyTorch's
 forward-mode operator for the JVP branch except the attention core, which calls the fused kernel
 (Appendix C.1).  Here the attention core for [B][L][H][D] bf16 tensors and the norms around it run in the CUDA library
-in both modes; the plain calls of the layers below the dense core are differentiable (once).  Calls with ``withT`` and the
-dense core's plain call are not: their results carry no autograd graph, also where the arguments require grad.
+in both modes; plain calls are differentiable (once).  Calls with ``withT`` are not: their results carry no autograd graph, also
+where the arguments require grad.
 All passes can be captured into a CUDA graph; as with any layer, no autograd graph made outside the capture may then be alive
 for the same leaf tensors (the layers themselves keep none).
 """
@@ -18,55 +18,11 @@ import torch
 
 from . import adaln as _adaln
 from . import attn_jvp as _binding
+from . import dense as _dense
 from . import rotary as _rotary
 from . import sparse as _sparse
 
 TensorWithT = Tuple[torch.Tensor, torch.Tensor]   # (primal, tangent)
-
-
-class AttentionCoreJVP(torch.nn.Module):
-    """softmax(s q k^T) v with an optional tangent channel.
-
-    ``forward(q, k, v)`` returns O.  ``forward(q, k, v, withT=True)`` takes q as a (primal, tangent) pair and
-    k, v either as pairs (self-attention: their tangents matter) or as plain tensors (cross-attention on a
-    context that does not depend on the differentiated input, so tK = tV = 0), and returns (O, tO).
-    The log-sum-exp of the last call is kept in ``self.last_lse`` (and mu, the tangent of the LSE, in
-    ``self.last_mu`` when ``keep_mu`` is set).
-    """
-
-    def __init__(self, scale: Optional[float] = None, keep_mu: bool = False):
-        super().__init__()
-        self.scale = scale
-        self.keep_mu = keep_mu
-        self.last_lse = None
-        self.last_mu = None
-
-    def forward(self, q, k, v, withT: bool = False):
-        if withT:
-            return self._forward_jvp(q, k, v)
-        return self._forward(q, k, v)
-
-    def _forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
-        o, _, lse = _binding.attention_jvp(q, k, v, scale=self.scale, fwd_only=True)
-        self.last_lse, self.last_mu = lse, None
-        return o
-
-    def _forward_jvp(self, q: TensorWithT, k: Union[TensorWithT, torch.Tensor],
-                     v: Union[TensorWithT, torch.Tensor]) -> TensorWithT:
-        qp, qt = q
-        k_pair, v_pair = isinstance(k, (tuple, list)), isinstance(v, (tuple, list))
-        if k_pair != v_pair:
-            raise ValueError("k and v must both carry tangents (self-attention) or both be constant (context)")
-        if k_pair:
-            (kp, kt), (vp, vt) = k, v
-        else:
-            kp, kt, vp, vt = k, None, v, None
-        res = _binding.attention_jvp(qp, kp, vp, qt.detach(), None if kt is None else kt.detach(),
-                                     None if vt is None else vt.detach(), scale=self.scale,
-                                     return_mu=self.keep_mu)
-        self.last_lse = res[2]
-        self.last_mu = res[3] if self.keep_mu else None
-        return res[0], res[1]
 
 
 def _pair(v):
@@ -91,6 +47,70 @@ def _first_order(grads, *inputs):
     if not torch.is_grad_enabled():
         return grads
     return tuple(None if g is None else _FirstOrder.apply(g, *inputs) for g in grads)
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, scale, causal, k_lengths):
+        o, _, lse = _binding.attention_jvp(q, k, v, scale=scale, fwd_only=True, causal=causal, k_lengths=k_lengths)
+        ctx.scale, ctx.causal = scale, causal
+        ctx.save_for_backward(q, k, v, o, lse, k_lengths)           # (lengths that are written to meanwhile are an error)
+        ctx.mark_non_differentiable(lse)
+        return o, lse
+
+    @staticmethod
+    def backward(ctx, d_o, _):
+        q, k, v, o, lse, k_lengths = ctx.saved_tensors
+        grads = _dense.attention_backward(d_o.contiguous(), q, k, v, o, lse, scale=ctx.scale, causal=ctx.causal, k_lengths=k_lengths)
+        return (*_first_order(grads, d_o, q, k, v), None, None, None)
+
+
+class AttentionCoreJVP(torch.nn.Module):
+    """softmax(s q k^T) v with an optional tangent channel.
+
+    ``forward(q, k, v)`` returns O.  ``forward(q, k, v, withT=True)`` takes q as a (primal, tangent) pair and
+    k, v either as pairs (self-attention: their tangents matter) or as plain tensors (cross-attention on a
+    context that does not depend on the differentiated input, so tK = tV = 0), and returns (O, tO).
+    Plain calls are differentiable (``attention_backward``).  ``causal``: query i sees the keys j <= i + Lk - Lq; ``k_lengths`` (int32 [B]): how
+    many keys each batch has; k and v may have fewer heads than q, and q, k, v may be slices of a fused projection: as in ``attention_jvp``.
+    The log-sum-exp of the last call is kept in ``self.last_lse`` (and mu, the tangent of the LSE, in
+    ``self.last_mu`` when ``keep_mu`` is set).
+    """
+
+    def __init__(self, scale: Optional[float] = None, keep_mu: bool = False, causal: bool = False):
+        super().__init__()
+        self.scale = scale
+        self.causal = causal
+        self.keep_mu = keep_mu
+        self.last_lse = None
+        self.last_mu = None
+
+    def forward(self, q, k, v, withT: bool = False, k_lengths=None):
+        if withT:
+            return self._forward_jvp(q, k, v, k_lengths)
+        return self._forward(q, k, v, k_lengths)
+
+    def _forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_lengths) -> torch.Tensor:
+        o, lse = _Attention.apply(q, k, v, self.scale, self.causal, k_lengths)
+        self.last_lse, self.last_mu = lse, None
+        return o
+
+    def _forward_jvp(self, q: TensorWithT, k: Union[TensorWithT, torch.Tensor],
+                     v: Union[TensorWithT, torch.Tensor], k_lengths) -> TensorWithT:
+        qp, qt = q
+        k_pair, v_pair = isinstance(k, (tuple, list)), isinstance(v, (tuple, list))
+        if k_pair != v_pair:
+            raise ValueError("k and v must both carry tangents (self-attention) or both be constant (context)")
+        if k_pair:
+            (kp, kt), (vp, vt) = k, v
+        else:
+            kp, kt, vp, vt = k, None, v, None
+        res = _binding.attention_jvp(qp, kp, vp, qt.detach(), None if kt is None else kt.detach(),
+                                     None if vt is None else vt.detach(), scale=self.scale,
+                                     return_mu=self.keep_mu, causal=self.causal, k_lengths=k_lengths)
+        self.last_lse = res[2]
+        self.last_mu = res[3] if self.keep_mu else None
+        return res[0], res[1]
 
 
 class _AdaLN(torch.autograd.Function):
