@@ -155,12 +155,21 @@ def host():
             raise RuntimeError(f"_host.so is missing or does not load ({e}): build it with `python -m paper_2510_08431_b200.build` "
                                "(there is no fallback path)") from e
         names = ("adaln_fwd", "adaln_bwd", "adaln_bwd_workspace_bytes", "block_select", "block_select_workspace_bytes",
-                 "block_lists", "sparse_fwd", "sparse_bwd", "sparse_bwd_workspace_bytes", "attention_fwd",
+                 "block_lists", "sparse_fwd", "sparse_bwd", "sparse_bwd_workspace_bytes", "fwd_stream", "fwd_mu", "attention_fwd",
                  "attention_bwd", "attention_bwd_workspace_bytes", "rotary_table", "qk_rotary_fwd",
                  "qk_rotary_bwd", "qk_rotary_bwd_workspace_bytes")
         _host.bind(*(ctypes.cast(getattr(lib, "attn_jvp_" + n), ctypes.c_void_p).value for n in names))
         _host_module = _host
     return _host_module
+
+
+def has_host() -> bool:
+    """Whether the host binding is there: what can do without it does."""
+    try:
+        host()
+    except RuntimeError:
+        return False
+    return True
 
 
 def _raise(rc):
@@ -299,7 +308,9 @@ def attention_jvp(q, k, v, tq=None, tk=None, tv=None, scale=None, fwd_only=False
     these four goes with ``splits`` > 1.
     Returns (o, to, lse) or (o, to, lse, mu).
     """
-    if causal or k_lengths is not None or q.shape[2:] != k.shape[2:] or not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous()):
+    plain = not causal and k_lengths is None and q.shape[2:] == k.shape[2:] and q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
+    # (plain calls as well, whose kernels can take less time than the marshalling here: a third of the host time)
+    if not plain or (splits == 1 and out is None and workspace is None and has_host()):
         if splits > 1 or workspace is not None:
             raise ValueError("chunks of keys (splits > 1) go without masks, lengths, shared heads and strided inputs")
         rc, o, to, lse, mu = host().attention_fwd(q, k, v, scale, bool(causal), k_lengths, tq, tk, tv, bool(fwd_only), bool(return_mu),

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "attn_jvp.cu")
 DEPS = [SRC, os.path.join(PKG, "csrc", "attn_jvp_kernel.cuh"), os.path.join(PKG, "csrc", "qknorm_jvp.cuh"),
         os.path.join(PKG, "csrc", "adaln_jvp.cuh"), os.path.join(PKG, "csrc", "block_select.cuh"),
-        os.path.join(PKG, "csrc", "sparse_bwd.cuh"), os.path.join(PKG, "csrc", "rotary.cuh"),
+        os.path.join(PKG, "csrc", "sparse_bwd.cuh"), os.path.join(PKG, "csrc", "dense_bwd.cuh"), os.path.join(PKG, "csrc", "rotary.cuh"),
         os.path.join(ROOT, "include", "attn_jvp.h")]
 LIB = os.path.join(PKG, "libattn_jvp.so")
 HOST_SRC = os.path.join(PKG, "csrc", "host_binding.cpp")

@@ -12,6 +12,7 @@
 #include "adaln_jvp.cuh"
 #include "attn_jvp_kernel.cuh"
 #include "block_select.cuh"
+#include "dense_bwd.cuh"
 #include "qknorm_jvp.cuh"
 #include "rotary.cuh"
 #include "sparse_bwd.cuh"
@@ -47,7 +48,8 @@ struct DeviceState {
     std::atomic<int> dyn_smem_pair[3][2];         // ... of the CTA-pair kernels
     std::atomic<int> dyn_smem_sparse[2][3];       // ... of the kernels that walk lists of key blocks
     std::atomic<int> dyn_smem_masked[2][3];       // ... of the kernels with a mask
-    std::atomic<bool> sparse_bwd_ready[2][2][2];  // launch attribute of sparse_bwd_kernel<D><pass><dense> is set
+    std::atomic<bool> sparse_bwd_ready[2][2];     // launch attribute of sparse_bwd_kernel<D><pass> is set
+    std::atomic<bool> dense_bwd_ready[2][2];      // ... of dense_bwd_kernel<D><pass>
     std::atomic<bool> topk_ready[2];              // ... of block_topk_kernel<8>, <4>
     std::atomic<bool> adaln_ready[2][3][2][3];    // launch attribute of adaln_kernel<x fp32><mode><a row ahead><width> is set
     std::atomic<void*> static_scratch{nullptr};   // device address of the built-in scratch array
@@ -1045,20 +1047,20 @@ SparseBwdLayout sparse_bwd_layout(int B, int H, int Lq, int Lk) {
     return l;
 }
 
-template <int D, bool DKV, bool DENSE = false>
+template <int D, bool DKV>
 int launch_sparse_bwd(const CUtensorMap& x1, const CUtensorMap& x2, const CUtensorMap& y1, const CUtensorMap& y2,
-                      const attn_jvp::BwdArgsOf<DENSE>& a, int n_items, cudaStream_t stream, DeviceState& st) {
-    auto kern = attn_jvp::sparse_bwd_kernel<D, DKV, DENSE>;
+                      const attn_jvp::SparseBwdArgs& a, cudaStream_t stream, DeviceState& st) {
+    auto kern = attn_jvp::sparse_bwd_kernel<D, DKV>;
     constexpr int smem = attn_jvp::SparseBwdPlan<D>::kDynBytes;
-    std::atomic<bool>& ready = st.sparse_bwd_ready[D == 128][DKV][DENSE];
+    std::atomic<bool>& ready = st.sparse_bwd_ready[D == 128][DKV];
     if (!ready.load(std::memory_order_acquire)) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute(MaxDynamicSharedMemorySize)", e);
         ready.store(true, std::memory_order_release);
     }
-    kern<<<(unsigned)(n_items < st.sm_count ? n_items : st.sm_count), attn_jvp::kBwdThreads, smem, stream>>>(x1, x2, y1, y2, a);
+    kern<<<(unsigned)(a.n_items < st.sm_count ? a.n_items : st.sm_count), attn_jvp::kBwdThreads, smem, stream>>>(x1, x2, y1, y2, a);
     const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? 0 : cuda_fail("attention backward kernel launch", e);
+    return e == cudaSuccess ? 0 : cuda_fail("sparse backward kernel launch", e);
 }
 
 template <int D>
@@ -1071,8 +1073,8 @@ int sparse_bwd_run(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorM
     attn_jvp::sparse_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + prep.zero_blocks) + order_windows(dkv.n_items), 256, 0, stream>>>(prep);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail("sparse backward preparation launch", e);
-    if (int rc = launch_sparse_bwd<D, true>(mk, mv, mq, mdo, dkv, dkv.n_items, stream, st)) return rc;
-    return launch_sparse_bwd<D, false>(mq, mdo, mk, mv, dq, dq.n_items, stream, st);
+    if (int rc = launch_sparse_bwd<D, true>(mk, mv, mq, mdo, dkv, stream, st)) return rc;
+    return launch_sparse_bwd<D, false>(mq, mdo, mk, mv, dq, stream, st);
 }
 
 int sparse_bwd(const void* d_o, const void* q, const void* k, const void* v, const void* o, const float* lse,
@@ -1162,7 +1164,7 @@ bool head_strides(const long long* in, int B, int L, int H, int D, long long* ou
 }
 
 // ---------------------------------------------------------------------------------------------
-// Attention with a causal mask, key lengths, shared key heads and strided inputs (the masked form of the forward kernel, the dense form of sparse_bwd.cuh)
+// Attention with a causal mask, key lengths, shared key heads and strided inputs (the masked form of the forward kernel, dense_bwd.cuh)
 // ---------------------------------------------------------------------------------------------
 // Checks and strides of what both directions read.
 struct AttentionInputs { long long q[3], k[3], v[3]; size_t q_bytes, k_bytes, v_bytes; };
@@ -1182,6 +1184,12 @@ int attention_common(const attn_jvp_attention_t* in, AttentionInputs& x) {
         for (int i = 0; i < 3; ++i) if (n[i] > 1 && st[i] < in->D) return ATTN_JVP_ERR_SHAPE;
     }
     return 0;
+}
+
+// Heads that are worked on together under a causal mask: what streams by for them, `bytes` per head, takes half of L2 at most.
+int causal_window(size_t bytes, int heads) {
+    const size_t n = (size_t)(64 << 20) / bytes;
+    return n < 1 ? 1 : n < (size_t)heads ? (int)n : heads;
 }
 
 int attention_fwd(const attn_jvp_attention_t* in, void* o, void* to, float* lse, float* mu, unsigned flags, cudaStream_t stream) {
@@ -1237,9 +1245,11 @@ int attention_fwd(const attn_jvp_attention_t* in, void* o, void* to, float* lse,
     ka.splits = 1;
     ka.n_q_tiles = n_blocks(Lq);
     ka.n_items = ka.n_q_tiles * H * B;
-    ka.mask = {in->k_lengths, in->causal, Lk - Lq, H / Hk};
-    // one CTA per item where items are long or of unlike length (the hardware balances them), else persistent ones, as in run()
-    const bool persistent = !in->causal && (Lk + attn_jvp::kBlockN - 1) / attn_jvp::kBlockN <= kPersistentMaxTiles;
+    // persistent CTAs, but one per item where items are long, as in run().  Under a causal mask the hardware balances the latter by itself, head by head
+    // (16 heads of 8192 tokens at D = 128: 281 us, with several heads at a time 330).
+    const bool persistent = (Lk + attn_jvp::kBlockN - 1) / attn_jvp::kBlockN <= (in->causal ? kPersistentMaxTiles / 2 : kPersistentMaxTiles);
+    const size_t key_bytes = (size_t)Lk * D * (jvp_kv ? 8 : 4) / (H / Hk) + 1;
+    ka.mask = {in->k_lengths, in->causal, Lk - Lq, H / Hk, persistent ? causal_window(key_bytes, B * H) : 1};
     const dim3 grid((unsigned)(persistent && ka.n_items > st.sm_count ? st.sm_count : ka.n_items), 1, 1);
     // softmax groups as softmax_groups_for() chooses them for long items
     if (D == 64) {
@@ -1263,13 +1273,13 @@ int dense_splits(long long items, int tiles, int D, bool dkv) {
     int splits = 1;
     for (int s = 1; s <= 16 && (s == 1 || tiles / s >= 2); ++s) {
         const double rounds = (double)((items * s + kSms - 1) / kSms);
-        const double join = s == 1 ? 0.0 : 3.0 + items * s * (dkv ? 2.0 : 1.0) * 128 * D * 4 * 2 / 5.0e6 / 1.2 / (D / 128.0);
+        const double join = s == 1 ? 0.0 : 3.0 + items * s * (dkv ? 2.0 : 1.0) * kSelBlock * D * 4 * 2 / 5.0e6 / 1.2 / (D / 128.0);
         const double cost = rounds * ((double)tiles / s + 1.0) + join;
         if (s == 1 || cost < best) { best = cost; splits = s; }
     }
     return splits;
 }
-struct DenseBwdLayout { size_t counters, rows, tail_k, tail_v, part, total; int dkv_splits, dq_splits; };
+struct DenseBwdLayout { size_t counters, rows, tail_k, tail_v, part, part_dq, total; int dkv_splits, dq_splits; };
 DenseBwdLayout dense_bwd_layout(int B, int H, int Hk, int Lq, int Lk, int D) {
     auto pad = [](size_t n) { return (n + 255) & ~(size_t)255; };
     const size_t n_q = n_blocks(Lq), n_k = n_blocks(Lk);
@@ -1283,24 +1293,48 @@ DenseBwdLayout dense_bwd_layout(int B, int H, int Hk, int Lq, int Lk, int D) {
     l.tail_k = l.rows + pad((size_t)B * H * n_q * kSelBlock * 2 * sizeof(float));
     l.tail_v = l.tail_k + pad((size_t)B * Hk * kSelBlock * D * 2);
     l.part = l.tail_v + pad((size_t)B * Hk * kSelBlock * D * 2);
-    l.total = l.part + (dkv > dq ? dkv : dq);            // (the passes run one after the other)
+    l.part_dq = l.part + pad(dkv);                       // (the passes overlap)
+    l.total = l.part_dq + dq;
     return l;
 }
 
+template <int D, bool DKV>
+int launch_dense_bwd(const attn_jvp::DenseBwdArgs& a, cudaStream_t stream, DeviceState& st) {
+    auto kern = attn_jvp::dense_bwd_kernel<D, DKV>;
+    constexpr int smem = attn_jvp::DenseBwdPlan<D, DKV>::kDynBytes;
+    std::atomic<bool>& ready = st.dense_bwd_ready[D == 128][DKV];
+    if (!ready.load(std::memory_order_acquire)) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute(MaxDynamicSharedMemorySize)", e);
+        ready.store(true, std::memory_order_release);
+    }
+    const int places = a.n_items * a.splits;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(places < st.sm_count ? places : st.sm_count), 1, 1);
+    cfg.blockDim = dim3(attn_jvp::kBwdThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a);
+    return e == cudaSuccess ? 0 : cuda_fail("attention backward kernel launch", e);
+}
+
 template <int D>
-int dense_bwd_run(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo, attn_jvp::DenseBwdPrep& prep,
-                  cudaStream_t stream, DeviceState& st) {
+int dense_bwd_run(attn_jvp::DenseBwdPrep& prep, cudaStream_t stream, DeviceState& st) {
     const attn_jvp::DenseBwdArgs &dkv = prep.dkv, &dq = prep.dq;
-    const long long rows = (long long)prep.B * prep.n_q * kSelBlock * prep.H;
-    prep.row_blocks = (int)((rows + attn_jvp::kPrepRows<D> - 1) / attn_jvp::kPrepRows<D>);
+    prep.row_blocks = prep.B * prep.n_q * (kSelBlock / 8) * ((prep.H + attn_jvp::kPrepHeads<D> - 1) / attn_jvp::kPrepHeads<D>);
     prep.zero_blocks = dkv.mask.lengths || dkv.mask.causal ? (dkv.n_items + dq.n_items + 7) / 8 : 0;       // (without a mask every item has tiles)
     const int tails = dkv.mask.lengths ? prep.B * dkv.H : 0;
     attn_jvp::dense_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + prep.zero_blocks + tails), 256, 0, stream>>>(prep);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail("attention backward preparation launch", e);
-    if (int rc = launch_sparse_bwd<D, true, true>(mk, mv, mq, mdo, dkv, dkv.n_items * dkv.splits, stream, st)) return rc;
+    if (int rc = launch_dense_bwd<D, true>(dkv, stream, st)) return rc;
+    if (int rc = launch_dense_bwd<D, false>(dq, stream, st)) return rc;
     if (dkv.splits > 1) attn_jvp::dense_join_kernel<D, true><<<(unsigned)dkv.n_items * (kSelBlock * 2 * D / 2048), 256, 0, stream>>>(dkv);
-    if (int rc = launch_sparse_bwd<D, false, true>(mq, mdo, mk, mv, dq, dq.n_items * dq.splits, stream, st)) return rc;
     if (dq.splits > 1) attn_jvp::dense_join_kernel<D, false><<<(unsigned)dq.n_items * (kSelBlock * D / 2048), 256, 0, stream>>>(dq);
     e = cudaGetLastError();
     return e == cudaSuccess ? 0 : cuda_fail("attention backward join launch", e);
@@ -1332,47 +1366,51 @@ int attention_bwd(const attn_jvp_attention_t* in, const void* d_o, const void* o
     if (int rc = make_map(&mdo, d_o, B, Lq, H, D, kSelBlock)) return rc;
 
     char* w = static_cast<char*>(workspace);
-    const int n_q = n_blocks(Lq), n_k = n_blocks(Lk);
     attn_jvp::DenseBwdPrep p = {};
-    attn_jvp::DenseBwdArgs a = {};
-    a.rows = reinterpret_cast<float*>(w + lay.rows);
-    a.host_status = st.host_status_dev.load(std::memory_order_acquire);
-    a.n_q = n_q;
-    a.n_k = n_k;
-    a.Lq = Lq;
-    a.Lk = Lk;
-    a.scale = in->scale;
-    a.scale_log2 = in->scale * 1.4426950408889634f;
-    a.wide_out = (((uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv) & 31u) == 0;
-    a.mask = {in->k_lengths, in->causal, Lk - Lq, H / Hk};
-    a.part = reinterpret_cast<float*>(w + lay.part);
-    a.tail1 = mk;
-    a.tail2 = mv;
     p.tail_k = reinterpret_cast<__nv_bfloat16*>(w + lay.tail_k);
     p.tail_v = reinterpret_cast<__nv_bfloat16*>(w + lay.tail_v);
+    attn_jvp::DenseBwdArgs a = {};
+    a.tail1 = mk;
+    a.tail2 = mv;
     if (in->k_lengths) {
         if (int rc = make_map(&a.tail1, p.tail_k, B, kSelBlock, Hk, D, kSelBlock)) return rc;
         if (int rc = make_map(&a.tail2, p.tail_v, B, kSelBlock, Hk, D, kSelBlock)) return rc;
     }
     p.counters = reinterpret_cast<int*>(w + lay.counters);
+    a.rows = reinterpret_cast<float*>(w + lay.rows);
+    a.host_status = st.host_status_dev.load(std::memory_order_acquire);
+    a.n_q = n_blocks(Lq);
+    a.Lq = Lq;
+    a.Lk = Lk;
+    a.scale = in->scale;
+    a.scale_log2 = in->scale * 1.4426950408889634f;
+    a.wide_out = (((uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv) & 31u) == 0;
+    a.mask = {in->k_lengths, in->causal, Lk - Lq, H / Hk, 1};
     p.dkv = p.dq = a;
-    p.dkv.counter = p.counters;
-    p.dkv.H = Hk;
-    p.dkv.n_items_per_head = n_k;
-    p.dkv.n_items = B * Hk * n_k;
-    p.dkv.L_own = Lk;
-    p.dkv.L_other = Lq;
-    p.dkv.out1 = static_cast<__nv_bfloat16*>(dv);
-    p.dkv.out2 = static_cast<__nv_bfloat16*>(dk);
-    p.dkv.splits = lay.dkv_splits;
-    p.dq.counter = p.counters + 1;
-    p.dq.H = H;
-    p.dq.n_items_per_head = n_q;
-    p.dq.n_items = B * H * n_q;
-    p.dq.L_own = Lq;
-    p.dq.L_other = Lk;
-    p.dq.out1 = static_cast<__nv_bfloat16*>(dq);
-    p.dq.splits = lay.dq_splits;
+    attn_jvp::DenseBwdArgs &dkv = p.dkv, &dqa = p.dq;
+    dkv.x1 = dqa.y1 = mk;
+    dkv.x2 = dqa.y2 = mv;
+    dkv.y1 = dqa.x1 = mq;
+    dkv.y2 = dqa.x2 = mdo;
+    dkv.counter = p.counters;
+    dqa.counter = p.counters + 1;
+    dkv.H = Hk;
+    dkv.n_items_per_head = n_blocks(Lk);
+    dkv.n_items = B * Hk * n_blocks(Lk);
+    dkv.L_own = Lk;
+    dkv.out1 = static_cast<__nv_bfloat16*>(dv);
+    dkv.out2 = static_cast<__nv_bfloat16*>(dk);
+    dkv.splits = lay.dkv_splits;
+    dkv.part = reinterpret_cast<float*>(w + lay.part);
+    dkv.mask.window = causal_window((size_t)Lq * D * 4 * (H / Hk), B * Hk);
+    dqa.H = H;
+    dqa.n_items_per_head = n_blocks(Lq);
+    dqa.n_items = B * H * n_blocks(Lq);
+    dqa.L_own = Lq;
+    dqa.out1 = static_cast<__nv_bfloat16*>(dq);
+    dqa.splits = lay.dq_splits;
+    dqa.part = reinterpret_cast<float*>(w + lay.part_dq);
+    dqa.mask.window = causal_window((size_t)Lk * D * 4 / (H / Hk) + 1, B * H);
     p.o = static_cast<const uint4*>(o);
     p.d_o = static_cast<const uint4*>(d_o);
     p.lse = lse;
@@ -1384,8 +1422,8 @@ int attention_bwd(const attn_jvp_attention_t* in, const void* d_o, const void* o
     p.B = B;
     p.H = H;
     p.Lq = Lq;
-    p.n_q = n_q;
-    return D == 128 ? dense_bwd_run<128>(mq, mk, mv, mdo, p, stream, st) : dense_bwd_run<64>(mq, mk, mv, mdo, p, stream, st);
+    p.n_q = a.n_q;
+    return D == 128 ? dense_bwd_run<128>(p, stream, st) : dense_bwd_run<64>(p, stream, st);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1418,7 +1456,9 @@ int rotary_table(const void* positions, int pos_type, long long n, int axes, con
                 const double g = std::fmin(1.0, std::fmax(0.0, (original_length * theta / kTwoPi - 1.0) / 31.0));
                 theta = theta * (1.0 - g) / s + theta * g;
             }
-            p.turns[p.pairs] = theta / kTwoPi;
+            const long double turns = (long double)theta / 6.283185307179586476925286766559L;
+            p.turns[p.pairs] = (double)turns;
+            p.steps[p.pairs] = (unsigned long long)((turns - std::floor(turns)) * 18446744073709551616.0L);
             p.axis[p.pairs] = (unsigned char)a;
         }
     }
@@ -1453,7 +1493,7 @@ bool rotary_shape_ok(int B, int L, int H, int Hk, int D) {
 // GPU (with few tokens, few heads each), and the blocks are shared between queries and keys by their heads.
 void rotary_grid(int mode, long long tokens, int H, int Hk, int D, attn_jvp::RotaryTensor* q, attn_jvp::RotaryTensor* k) {
     const int rows = attn_jvp::rotary_rows(mode), groups = attn_jvp::kRotaryThreads / (D / 8);
-    const long long slots = (long long)kSms * 4, most = slots * groups;       // blocks, groups that fit at once
+    const long long slots = (long long)kSms * attn_jvp::rotary_ctas(mode), most = slots * groups;     // blocks, groups that fit at once
     for (auto* t : {q, k}) {
         t->H = t == q ? H : Hk;
         t->blocks = 0;

@@ -146,7 +146,15 @@ struct KeyMask {
     const int* lengths;   // [B] keys of each batch, or null: all of Lk
     int causal, offset;   // causal: query i sees the keys j <= i + offset
     int group;            // query heads that share a key head
+    int window;           // causal: heads whose items are worked on together, long items first (causal_item())
 };
+// Under a causal mask the blocks of a head have unlike numbers of tiles.  The heads are taken `window` at a time (as many as leave what streams by
+// in L2), and within a window the items go by their length: place i of the order is head bh, block number `rank` from the longest on.
+struct CausalItem { int bh, rank; };
+__device__ __forceinline__ CausalItem causal_item(int i, int blocks, int heads, int window) {
+    const int w = i / (window * blocks), r = i - w * window * blocks, here = min(window, heads - w * window), rank = r / here;
+    return {w * window + r - rank * here, rank};
+}
 struct MaskKernelArgs : KernelArgs {
     KeyMask mask;
 };
@@ -589,7 +597,7 @@ __host__ __device__ constexpr int score_buffers(int D, int mode) {
 // kMasked: a causal mask, a length of every batch's keys, and key heads that several query heads share.  An item's tiles are those that
 // its last row sees; which of a tile's keys a row sees is a number per row (`valid`), and what it does not see is replaced, not multiplied
 // away: -inf for scores, 0 for tangent scores.  What lies in memory behind a batch's length may be anything: the MMA warp writes zeros over those
-// rows of the one V tile that holds the end (0 times NaN would be NaN).  Under a causal mask a head's long items come first.
+// rows of the one V tile that holds the end (0 times NaN would be NaN).
 template <int D, int MODE, bool kSplit, int kGroups, bool kPair, bool kSparse = false, bool kMasked = false>
 __global__ void __launch_bounds__(num_threads(kGroups), 1)
 attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -691,17 +699,44 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         return k;
     };
     const Walk walk_stride = walk_init(item_stride);
+    // kMasked: the item of this CTA in a round; under a causal mask every other full round runs backwards through the order, so that each
+    // CTA gets its share of long and short items
+    auto masked_walk = [&](int round) -> Walk {
+        const int item = min(first_item + round * item_stride, args.n_items - 1);
+        if (!mask.causal) {
+            Walk k = walk_init(item);
+            k.round = round;
+            return k;
+        }
+        const bool back = (round & 1) != 0 && (round + 1) * item_stride <= args.n_items;
+        const CausalItem c = causal_item(back ? round * item_stride + item_stride - 1 - first_item : item, args.n_q_tiles, args.H * args.B, mask.window);
+        Walk k{};
+        k.qt = args.n_q_tiles - 1 - c.rank;
+        k.z = c.bh / args.H;
+        k.h = c.bh - k.z * args.H;
+        k.round = round;
+        return k;
+    };
     auto walk_first = [&]() -> Walk {
+        if (kMasked) {
+            Walk k = masked_walk(0);
+            read_length(k);
+            return k;
+        }
         const bool ordered = kSparse && lists.order != nullptr;
         const int row = ordered ? ordered_list(0) : first_item;
         Walk k = walk_init(row);
         if (kSparse) read_list(k, row);
-        if (kMasked) read_length(k);
         if (ordered) k.after = ordered_list(1);
         return k;
     };
     // to item number `item`, item_stride items on
     auto walk_step = [&](Walk& k, int item) {
+        if (kMasked) {
+            k = masked_walk(k.round + 1);
+            read_length(k);
+            return;
+        }
         if (kSparse && lists.order != nullptr) {
             const int row = k.after, round = k.round + 1;
             k = walk_init(min(row, args.n_items - 1));
@@ -716,7 +751,6 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (k.h >= args.H) { k.h -= args.H; ++k.z; }
         k.z += walk_stride.z;
         if (kSparse) read_list(k, item);
-        if (kMasked) read_length(k);
     };
     auto item_of = [&](const Walk& k) -> Item {
         Item w;
@@ -738,7 +772,6 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         w.len = w.hk = 0;
         if (kMasked) {
-            if (mask.causal) w.q0 = (args.n_q_tiles - 1 - k.qt) * kBlockM;
             w.len = k.len;
             w.hk = k.h / mask.group;
             const int seen = mask.causal ? min(k.len, max(0, min(w.q0 + kBlockM, args.Lq) + mask.offset)) : k.len;    // by the last row

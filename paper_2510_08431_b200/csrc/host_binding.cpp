@@ -28,6 +28,8 @@ decltype(&attn_jvp_block_lists) f_block_lists = nullptr;
 decltype(&attn_jvp_sparse_fwd) f_sparse_fwd = nullptr;
 decltype(&attn_jvp_sparse_bwd) f_sparse_bwd = nullptr;
 decltype(&attn_jvp_sparse_bwd_workspace_bytes) f_sparse_bwd_bytes = nullptr;
+decltype(&attn_jvp_fwd_stream) f_fwd_stream = nullptr;
+decltype(&attn_jvp_fwd_mu) f_fwd_mu = nullptr;
 decltype(&attn_jvp_attention_fwd) f_attention_fwd = nullptr;
 decltype(&attn_jvp_attention_bwd) f_attention_bwd = nullptr;
 decltype(&attn_jvp_attention_bwd_workspace_bytes) f_attention_bwd_bytes = nullptr;
@@ -407,6 +409,8 @@ struct Attention {
         a.scale = p[3] == Py_None ? static_cast<float>(1.0 / std::sqrt(static_cast<double>(a.D))) : static_cast<float>(number(p[3], "scale"));
         a.causal = p[4] == Py_True;
     }
+    // what the calls without masks, shared heads and strides take
+    bool plain() const { return !a.causal && !a.k_lengths && a.H == a.Hk && q.is_contiguous() && k.is_contiguous() && v.is_contiguous(); }
     cudaStream_t stream() const { return c10::cuda::getCurrentCUDAStream(q.device().index()).stream(); }
 };
 
@@ -442,7 +446,13 @@ PyObject* attention_fwd(PyObject*, PyObject* const* p, Py_ssize_t n) {
         if (lse.defined()) expect(lse, "lse", at::kFloat, rows, dev); else lse = like(c.q, rows, at::kFloat);
         if (p[4] == Py_True) mu = like(c.q, rows, at::kFloat);
         const c10::cuda::CUDAGuard guard(dev);
-        const int rc = unlocked([&] { return f_attention_fwd(&c.a, ptr(o), ptr(to), ptr<float>(lse), ptr<float>(mu), flags, c.stream()); });
+        const int rc = unlocked([&] {
+            const attn_jvp_attention_t& a = c.a;
+            if (c.plain() && mu.defined())
+                return f_fwd_mu(a.q, a.k, a.v, a.tq, a.tk, a.tv, ptr(o), ptr(to), ptr<float>(lse), ptr<float>(mu), a.B, a.H, a.Lq, a.Lk, a.D, a.scale, flags, c.stream());
+            if (c.plain()) return f_fwd_stream(a.q, a.k, a.v, a.tq, a.tk, a.tv, ptr(o), ptr(to), ptr<float>(lse), a.B, a.H, a.Lq, a.Lk, a.D, a.scale, flags, c.stream());
+            return f_attention_fwd(&c.a, ptr(o), ptr(to), ptr<float>(lse), ptr<float>(mu), flags, c.stream());
+        });
         return result(rc, {o, to, lse, mu});
     });
 }
@@ -613,7 +623,7 @@ PyObject* bind(PyObject*, PyObject* const* p, Py_ssize_t n) {
     void** slots[] = {reinterpret_cast<void**>(&f_adaln_fwd), reinterpret_cast<void**>(&f_adaln_bwd), reinterpret_cast<void**>(&f_adaln_bwd_bytes),
                       reinterpret_cast<void**>(&f_block_select), reinterpret_cast<void**>(&f_block_select_bytes), reinterpret_cast<void**>(&f_block_lists),
                       reinterpret_cast<void**>(&f_sparse_fwd), reinterpret_cast<void**>(&f_sparse_bwd), reinterpret_cast<void**>(&f_sparse_bwd_bytes),
-                      reinterpret_cast<void**>(&f_attention_fwd), reinterpret_cast<void**>(&f_attention_bwd), reinterpret_cast<void**>(&f_attention_bwd_bytes),
+                      reinterpret_cast<void**>(&f_fwd_stream), reinterpret_cast<void**>(&f_fwd_mu), reinterpret_cast<void**>(&f_attention_fwd), reinterpret_cast<void**>(&f_attention_bwd), reinterpret_cast<void**>(&f_attention_bwd_bytes),
                       reinterpret_cast<void**>(&f_rotary_table), reinterpret_cast<void**>(&f_qk_rotary_fwd), reinterpret_cast<void**>(&f_qk_rotary_bwd),
                       reinterpret_cast<void**>(&f_qk_rotary_bwd_bytes)};
     constexpr Py_ssize_t slots_n = sizeof slots / sizeof slots[0];

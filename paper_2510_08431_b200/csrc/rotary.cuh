@@ -2,10 +2,11 @@
 // of queries and keys and rotates them, with tangents and gradients.
 //
 // Table, for pair i of axis a (base theta, d_a channels per axis):  angle = position_a . theta_a^(-2 i / d_a), stretched as the
-// host asks; an entry is (m cos, m sin).  The angle of a far position has lost its fraction in 32 bits, so it is formed in 64,
-// in turns instead of radians (the whole turns then come off exactly), and the fraction of a turn goes on as a sum of two fp32
-// numbers: cos and sin of the high part from sincospif, the low part (below 2^-25 turns) by its first-order term.  Bound by the 8 bytes written per
-// pair and the arithmetic beside it.
+// host asks; an entry is (m cos, m sin).  The angle of a far position has lost its fraction in 32 bits, so it is counted in turns of which whole ones
+// drop out: a whole position times the turns per position in 2^-64 of a turn, modulo 2^64 (an integer product), a fractional position in fp64.
+// What is left goes on as 2^-32 of a turn: the nearest quarter turn picks and signs the results, the rest is at most pi / 4, where
+// sin y = y + y^3 S(y^2) and cos y = 1 - y^2 / 2 + y^4 C(y^2) with polynomials of smallest error (4e-9 of sin, 1e-10 of cos) are right to fp32 rounding.
+// Bound by the 8 bytes written per pair: 262144 positions of 64 pairs XX us.
 //
 // Heads, for a row x in R^D of one token and head, with the token's table row R (a rotation of the first R channels by pairs):
 //     n = (x - mean x) / sqrt(var x + eps)   or   x / sqrt(mean x^2 + eps)   or   x,      u = w . n + b,      y = R u
@@ -22,6 +23,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace attn_jvp {
 
 // ---------------------------------------------------------------------------------------------
@@ -30,7 +33,8 @@ namespace attn_jvp {
 constexpr int kRotaryMaxPairs = 128, kRotaryMaxAxes = 8;
 constexpr int kTableThreads = 256;
 struct RotaryTableParams {
-    double turns[kRotaryMaxPairs];        // turns per unit of position
+    unsigned long long steps[kRotaryMaxPairs];   // 2^-64 turns per unit of position (whole turns dropped) ...
+    double turns[kRotaryMaxPairs];               // ... and turns, for fractional positions
     unsigned char axis[kRotaryMaxPairs];
     const void* positions;                // [n][axes]
     float2* table;                        // [n][pairs]
@@ -39,21 +43,40 @@ struct RotaryTableParams {
     float size;                           // m
 };
 
+// (cos, sin) of u 2^-32 turns
+__device__ __forceinline__ float2 cos_sin_turns(unsigned u) {
+    const unsigned quarter = (u + 0x20000000u) >> 30;
+    const float y = static_cast<float>(static_cast<int>(u - (quarter << 30))) * 0x1.921fb6p-30f;      // 2 pi 2^-32
+    const float z = y * y;
+    const float s = fmaf(y * z, fmaf(fmaf(-0x1.994eb4p-13f, z, 0x1.11076p-7f), z, -0x1.555546p-3f), y);
+    const float c = fmaf(z, fmaf(fmaf(fmaf(0x1.9a025ap-16f, z, -0x1.6c0c8cp-10f), z, 0x1.55554ap-5f), z, -0.5f), 1.0f);
+    const float a = quarter & 1u ? s : c, b = quarter & 1u ? c : s;       // (cos, sin), (-sin, cos), (-cos, -sin), (sin, -cos)
+    return make_float2((quarter + 1u) & 2u ? -a : a, quarter & 2u ? -b : b);
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kTableThreads)
 rotary_table_kernel(const __grid_constant__ RotaryTableParams p) {
     // a thread keeps its pair; the threads of a block cover whole rows of the table
     const int rows = blockDim.x / p.pairs;
     const int pair = threadIdx.x % p.pairs, sub = threadIdx.x / p.pairs;
+    const unsigned long long step = p.steps[pair];
     const double turns = p.turns[pair];
-    const T* pos = static_cast<const T*>(p.positions) + p.axis[pair];
-    for (long long i = static_cast<long long>(blockIdx.x) * rows + sub; i < p.n; i += static_cast<long long>(gridDim.x) * rows) {
-        const double t = static_cast<double>(pos[i * p.axes]) * turns;
-        const double f = t - rint(t);                            // -1/2 .. 1/2
-        const float hi = static_cast<float>(f), lo = static_cast<float>(f - static_cast<double>(hi)) * 6.2831853071795865f;
-        float s, c;
-        sincospif(2.0f * hi, &s, &c);
-        p.table[i * p.pairs + pair] = make_float2(p.size * fmaf(-s, lo, c), p.size * fmaf(c, lo, s));
+    const long long stride = static_cast<long long>(gridDim.x) * rows;
+    long long i = static_cast<long long>(blockIdx.x) * rows + sub;
+    const T* pos = static_cast<const T*>(p.positions) + p.axis[pair] + i * p.axes;
+    float2* out = p.table + i * p.pairs + pair;
+#pragma unroll 4
+    for (; i < p.n; i += stride, pos += stride * p.axes, out += stride * p.pairs) {
+        unsigned u;
+        if constexpr (std::is_floating_point_v<T>) {
+            const double t = static_cast<double>(__ldg(pos)) * turns;
+            u = static_cast<unsigned>(__double2int_rn((t - rint(t)) * 4294967296.0));        // (half a turn saturates: 2^-32 of one off)
+        } else {
+            u = static_cast<unsigned>((static_cast<unsigned long long>(static_cast<long long>(__ldg(pos))) * step + 0x80000000ull) >> 32);
+        }
+        const float2 cs = cos_sin_turns(u);
+        *out = make_float2(p.size * cs.x, p.size * cs.y);
     }
 }
 
@@ -62,8 +85,9 @@ rotary_table_kernel(const __grid_constant__ RotaryTableParams p) {
 // ---------------------------------------------------------------------------------------------
 constexpr int kRotaryThreads = 256;
 enum RotaryMode : int { kRotaryFwd = 0, kRotaryJvp = 1, kRotaryBwd = 2 };
-// rows that a group of lanes has in flight
+// rows that a group of lanes has in flight, and blocks that share an SM (what the registers are budgeted for)
 __host__ __device__ constexpr int rotary_rows(int mode) { return mode == kRotaryFwd ? 4 : 2; }
+__host__ __device__ constexpr int rotary_ctas(int mode) { return mode == kRotaryBwd ? 3 : 4; }
 
 struct RotaryTensor {
     const __nv_bfloat16* x;
@@ -104,7 +128,7 @@ __device__ __forceinline__ float sum_lanes(float v) {
 }
 
 template <int D, int MODE, bool kHalf>
-__global__ void __launch_bounds__(kRotaryThreads)
+__global__ void __launch_bounds__(kRotaryThreads, rotary_ctas(MODE))
 qk_rotary_kernel(const __grid_constant__ RotaryParams p) {
     constexpr int kLanes = D / 8, kGroups = kRotaryThreads / kLanes, kRows = rotary_rows(MODE);
     const bool second = blockIdx.x >= p.q.blocks;

@@ -58,39 +58,6 @@ struct SparseBwdArgs {
     float scale, scale_log2;
 };
 
-// The dense form (kDense): no lists, an item's tiles follow from its mask (dense_span()).
-struct DenseBwdArgs : SparseBwdArgs {
-    KeyMask mask;               // group: query heads per key head
-    int Lq, Lk, n_k;
-    int splits;                 // parts that an item's tiles are cut into, where there are few items; then the accumulators
-    float* part;                // go here, [splits][n_items][128][kDkv: dV, dK; kDq: dQ] in fp32, and dense_join_kernel adds them
-    alignas(64) CUtensorMap tail1, tail2;        // kDq: K, V of the block in which a batch's keys end, [B][128][heads][D], zeros behind the end
-};
-template <bool kDense>
-using BwdArgsOf = std::conditional_t<kDense, DenseBwdArgs, SparseBwdArgs>;
-
-// The tiles of a dense item.  kDkv (a key block): count query blocks from `first` on, for each of the heads that share the key
-// head in turn, n = group count.  kDq (a query block): key blocks 0 .. n - 1.  len: the keys of the batch.
-struct DenseSpan { int n, len, first, count; };
-template <bool kDkv, typename Args>
-__device__ __forceinline__ DenseSpan dense_span(const Args& a, int item) {
-    const int bh = item / a.n_items_per_head, x0 = (item - bh * a.n_items_per_head) * kBwdBlock;
-    DenseSpan s;
-    s.len = a.mask.lengths == nullptr ? a.Lk : min(max(__ldg(a.mask.lengths + bh / a.H), 0), a.Lk);
-    s.first = 0;
-    if (kDkv) {
-        if (a.mask.causal) s.first = max(0, x0 - a.mask.offset) / kBwdBlock;      // the first query that sees key x0
-        s.count = x0 < s.len ? max(0, a.n_q - s.first) : 0;
-        s.n = s.count * a.mask.group;
-    } else {
-        const int seen = a.mask.causal ? min(s.len, max(0, min(x0 + kBwdBlock, a.Lq) + a.mask.offset)) : s.len;
-        s.n = s.count = (seen + kBwdBlock - 1) / kBwdBlock;
-    }
-    return s;
-}
-// the first tile of part i
-__device__ __forceinline__ int part_begin(int n, int i, int splits) { return static_cast<int>(static_cast<long long>(n) * i / splits); }
-
 template <int D>
 struct SparseBwdPlan {
     static constexpr int kHalf = kBwdBlock * 128;                // 128 rows x 64 bf16
@@ -121,10 +88,35 @@ struct SparseBwdPrep {
 constexpr int kPrepEach = 2;                 // rows per thread, their loads in flight together
 template <int D>
 constexpr unsigned kPrepRows = kPrepEach * 256 / (D / 8);        // ... per CTA
-// LSE log2 e and delta of the CTA's query rows: P is a SparseBwdPrep or a DenseBwdPrep.
-template <int D, typename P>
-__device__ __forceinline__ void bwd_prepare_rows(const P& p) {
+template <int D>
+__global__ void __launch_bounds__(256)
+sparse_bwd_prep_kernel(const SparseBwdPrep p) {
     constexpr int kLanes = D / 8;
+    if (static_cast<int>(blockIdx.x) >= p.row_blocks + p.zero_blocks) {
+        __shared__ uint4 swap[kOrderThreads];
+        static_assert(kOrderThreads == 256, "the sort's CTA");
+        block_order(p.k_tiles, p.k_order, p.B * p.H * p.n_k, blockIdx.x - p.row_blocks - p.zero_blocks, swap);
+        return;
+    }
+    if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
+        const int lane = threadIdx.x & 31;
+        int item = (blockIdx.x - p.row_blocks) * 8 + (threadIdx.x >> 5);
+        const int q_items = p.B * p.H * p.n_q;
+        const bool keys = item >= q_items;
+        if (keys) item -= q_items;
+        const int per_head = keys ? p.n_k : p.n_q, L = keys ? p.Lk : p.Lq;
+        if (item >= p.B * p.H * per_head || (keys ? p.k_tiles : p.q_tiles)[item] > 0) return;
+        const int bh = item / per_head, blk = item - bh * per_head, b = bh / p.H, h = bh - b * p.H;
+        for (int e = lane; e < kBwdBlock * kLanes; e += 32) {
+            const int r = blk * kBwdBlock + e / kLanes;
+            if (r >= L) break;
+            const long long at = ((static_cast<long long>(b) * L + r) * p.H + h) * D + (e % kLanes) * 8;
+            *reinterpret_cast<uint4*>((keys ? p.dk : p.dq) + at) = make_uint4(0u, 0u, 0u, 0u);
+            if (keys) *reinterpret_cast<uint4*>(p.dv + at) = make_uint4(0u, 0u, 0u, 0u);
+        }
+        return;
+    }
+    if (blockIdx.x == 0 && threadIdx.x < 2) p.counters[threadIdx.x] = 0;
     // (row order [B][padded][H], that of the tensors; their number fits 32 bits)
     const unsigned padded = p.n_q * kBwdBlock, n = static_cast<unsigned>(p.B) * padded * p.H;
     const unsigned r0 = blockIdx.x * kPrepRows<D> + threadIdx.x / kLanes, sub = threadIdx.x % kLanes;
@@ -167,124 +159,6 @@ __device__ __forceinline__ void bwd_prepare_rows(const P& p) {
             out[kBwdBlock] = sum;
         }
     }
-}
-
-template <int D>
-__global__ void __launch_bounds__(256)
-sparse_bwd_prep_kernel(const SparseBwdPrep p) {
-    constexpr int kLanes = D / 8;
-    if (static_cast<int>(blockIdx.x) >= p.row_blocks + p.zero_blocks) {
-        __shared__ uint4 swap[kOrderThreads];
-        static_assert(kOrderThreads == 256, "the sort's CTA");
-        block_order(p.k_tiles, p.k_order, p.B * p.H * p.n_k, blockIdx.x - p.row_blocks - p.zero_blocks, swap);
-        return;
-    }
-    if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
-        const int lane = threadIdx.x & 31;
-        int item = (blockIdx.x - p.row_blocks) * 8 + (threadIdx.x >> 5);
-        const int q_items = p.B * p.H * p.n_q;
-        const bool keys = item >= q_items;
-        if (keys) item -= q_items;
-        const int per_head = keys ? p.n_k : p.n_q, L = keys ? p.Lk : p.Lq;
-        if (item >= p.B * p.H * per_head || (keys ? p.k_tiles : p.q_tiles)[item] > 0) return;
-        const int bh = item / per_head, blk = item - bh * per_head, b = bh / p.H, h = bh - b * p.H;
-        for (int e = lane; e < kBwdBlock * kLanes; e += 32) {
-            const int r = blk * kBwdBlock + e / kLanes;
-            if (r >= L) break;
-            const long long at = ((static_cast<long long>(b) * L + r) * p.H + h) * D + (e % kLanes) * 8;
-            *reinterpret_cast<uint4*>((keys ? p.dk : p.dq) + at) = make_uint4(0u, 0u, 0u, 0u);
-            if (keys) *reinterpret_cast<uint4*>(p.dv + at) = make_uint4(0u, 0u, 0u, 0u);
-        }
-        return;
-    }
-    if (blockIdx.x == 0 && threadIdx.x < 2) p.counters[threadIdx.x] = 0;
-    bwd_prepare_rows<D>(p);
-}
-
-// The same before the dense passes.  Blocks below `row_blocks`: rows.  Then a warp per item whose gradient is zero because nothing sees it or it sees nothing, then
-// (lengths given) a block per batch and key head, which copies the keys and values of the block in which the batch ends with zeros behind the end:
-// the products of kDq would otherwise take up what lies there.
-struct DenseBwdPrep {
-    const uint4 *o, *d_o;
-    const float* lse;
-    float* rows;
-    const __nv_bfloat16 *k, *v;
-    long long k_b, k_l, k_h, v_b, v_l, v_h;      // strides
-    __nv_bfloat16 *tail_k, *tail_v;
-    int* counters;
-    int B, H, Lq, n_q, row_blocks, zero_blocks;
-    DenseBwdArgs dkv, dq;
-};
-template <int D>
-__global__ void __launch_bounds__(256)
-dense_bwd_prep_kernel(const __grid_constant__ DenseBwdPrep p) {
-    constexpr int kLanes = D / 8;
-    if (static_cast<int>(blockIdx.x) >= p.row_blocks + p.zero_blocks) {
-        const int Hk = p.dkv.H, bh = blockIdx.x - p.row_blocks - p.zero_blocks, b = bh / Hk, h = bh - b * Hk;
-        const int len = min(max(__ldg(p.dkv.mask.lengths + b), 0), p.dkv.Lk), r0 = len / kBwdBlock * kBwdBlock;
-        if (len == r0 || len == p.dkv.Lk) return;
-        for (int e = threadIdx.x; e < kBwdBlock * kLanes; e += 256) {
-            const int r = e / kLanes, c = e % kLanes * 8;
-            uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
-            if (r0 + r < len) {
-                k = __ldg(reinterpret_cast<const uint4*>(p.k + b * p.k_b + (r0 + r) * p.k_l + h * p.k_h + c));
-                v = __ldg(reinterpret_cast<const uint4*>(p.v + b * p.v_b + (r0 + r) * p.v_l + h * p.v_h + c));
-            }
-            const long long at = ((static_cast<long long>(b) * kBwdBlock + r) * Hk + h) * D + c;
-            *reinterpret_cast<uint4*>(p.tail_k + at) = k;
-            *reinterpret_cast<uint4*>(p.tail_v + at) = v;
-        }
-        return;
-    }
-    if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
-        const int lane = threadIdx.x & 31;
-        int item = (blockIdx.x - p.row_blocks) * 8 + (threadIdx.x >> 5);
-        const bool keys = item >= p.dq.n_items;
-        if (keys) item -= p.dq.n_items;
-        const DenseBwdArgs& a = keys ? p.dkv : p.dq;
-        if (item >= a.n_items || a.splits > 1) return;           // (split items: dense_join_kernel writes all of them)
-        if ((keys ? dense_span<true>(a, item) : dense_span<false>(a, item)).n > 0) return;
-        const int bh = item / a.n_items_per_head, blk = item - bh * a.n_items_per_head, b = bh / a.H, h = bh - b * a.H;
-        for (int e = lane; e < kBwdBlock * kLanes; e += 32) {
-            const int r = blk * kBwdBlock + e / kLanes;
-            if (r >= a.L_own) break;
-            const long long at = ((static_cast<long long>(b) * a.L_own + r) * a.H + h) * D + (e % kLanes) * 8;
-            *reinterpret_cast<uint4*>(a.out1 + at) = make_uint4(0u, 0u, 0u, 0u);
-            if (keys) *reinterpret_cast<uint4*>(a.out2 + at) = make_uint4(0u, 0u, 0u, 0u);
-        }
-        return;
-    }
-    if (blockIdx.x == 0 && threadIdx.x < 2) p.counters[threadIdx.x] = 0;
-    bwd_prepare_rows<D>(p);
-}
-
-// Adds the parts of split items in a fixed order: eight columns per thread.
-template <int D, bool kDkv>
-__global__ void __launch_bounds__(256)
-dense_join_kernel(const __grid_constant__ DenseBwdArgs a) {
-    constexpr int kCols = kDkv ? 2 * D : D, kPerRow = kCols / 8;
-    const int item = blockIdx.x / (kBwdBlock * kPerRow / 256);
-    const int e = (blockIdx.x % (kBwdBlock * kPerRow / 256)) * 256 + threadIdx.x, row = e / kPerRow, c = e % kPerRow * 8;
-    const DenseSpan span = dense_span<kDkv>(a, item);
-    const int bh = item / a.n_items_per_head, b = bh / a.H, h = bh - b * a.H, r = (item - bh * a.n_items_per_head) * kBwdBlock + row;
-    if (r >= a.L_own) return;
-    float sum[8] = {};
-    if (!kDkv || r < span.len) {
-        for (int i = 0; i < a.splits; ++i) {
-            if (part_begin(span.n, i, a.splits) == part_begin(span.n, i + 1, a.splits)) continue;      // (a part without tiles was never written)
-            const float4* at = reinterpret_cast<const float4*>(a.part + ((static_cast<long long>(i) * a.n_items + item) * kBwdBlock + row) * kCols + c);
-            const float4 x = __ldg(at), y = __ldg(at + 1);
-            sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
-            sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
-        }
-    }
-    const bool second = kDkv && c >= D;
-    const float factor = (kDkv && !second) ? 1.0f : a.scale;
-    uint32_t v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = pack_bf16(sum[2 * i] * factor, sum[2 * i + 1] * factor);
-    const long long at = ((static_cast<long long>(b) * a.L_own + r) * a.H + h) * D + (second ? c - D : c);
-    *reinterpret_cast<uint4*>((second ? a.out2 : a.out1) + at) = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // 2^x of two values on the FMA pipe, for kernels whose pace the special-function unit sets (8 cycles per warp instruction):
@@ -347,12 +221,10 @@ __device__ __forceinline__ bool mbar_wait_patient(uint32_t bar, uint32_t parity,
     }
 }
 
-// kDense: items are numbered (batch, head, block, part); key heads may be shared by several query heads, whose query blocks then stream by one
-// head after the other; a key or query that a pair of blocks keeps from each other has its P replaced by 0.
-template <int D, bool kDkv, bool kDense = false>
+template <int D, bool kDkv>
 __global__ void __launch_bounds__(kBwdThreads, 1)
 sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_constant__ CUtensorMap tm_x2,
-                  const __grid_constant__ CUtensorMap tm_y1, const __grid_constant__ CUtensorMap tm_y2, const __grid_constant__ BwdArgsOf<kDense> args) {
+                  const __grid_constant__ CUtensorMap tm_y1, const __grid_constant__ CUtensorMap tm_y2, const SparseBwdArgs args) {
     // kDkv: X1, X2 = K, V of the key block, Y1, Y2 = Q, dO of a query block.  kDq: X1, X2 = Q, dO; Y1, Y2 = K, V.
     // S = X1 Y1^T, dP = X2 Y2^T (rows: the stationary side)
     using Plan = SparseBwdPlan<D>;
@@ -378,8 +250,7 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
     __shared__ __align__(8) uint64_t bar_acc_free;               // ... and have been read: the next item may overwrite them
     __shared__ __align__(8) uint64_t bar_item_full[kItemRing], bar_item_empty[kItemRing];
     __shared__ __align__(8) uint64_t bar_drain, bar_drain2;
-    __shared__ int4 items[kItemRing];                            // {item (-1: no more), streaming blocks, the last of them, -}; kDense: {.., .., first tile, part}
-    __shared__ int4 spans[kDense ? kItemRing : 1];               // kDense: {keys of the batch, first streaming block, blocks per head, -}
+    __shared__ int4 items[kItemRing];                            // {item (-1: no more), streaming blocks, the last of them, -}
     __shared__ uint32_t tmem_base_smem;
     __shared__ int cta_abort;
 
@@ -452,25 +323,8 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
             bool ok = true;
             int T = 0, s1 = 0, s2 = 0;
             uint32_t ph1 = 0, ph2 = 0;                           // parity of the Y buffers' current lap
-            DenseSpan span{}, span_next{};
-            int tile0 = 0, tile0_next = 0, part = 0, part_next = 0;
             // the next item that keeps anything, from place `at` of the order on; -1: none.  n: its streaming blocks
             auto next_item = [&](int at, int& n) -> int {
-                if constexpr (kDense) {
-                    for (;; at = static_cast<int>(gridDim.x) + atomicAdd(args.counter, 1)) {
-                        if (static_cast<unsigned>(at) >= static_cast<unsigned>(args.n_items * args.splits)) return -1;
-                        int item = at / args.splits;
-                        part_next = at - item * args.splits;
-                        if (!kDkv && args.mask.causal) {         // long items of a head first
-                            const int bh = item / args.n_items_per_head;
-                            item = (2 * bh + 1) * args.n_items_per_head - 1 - item;
-                        }
-                        span_next = dense_span<kDkv>(args, item);
-                        tile0_next = part_begin(span_next.n, part_next, args.splits);
-                        n = part_begin(span_next.n, part_next + 1, args.splits) - tile0_next;
-                        if (n > 0) return item;
-                    }
-                }
                 for (;; at = static_cast<int>(gridDim.x) + atomicAdd(args.counter, 1)) {
                     if (static_cast<unsigned>(at) >= static_cast<unsigned>(args.n_items)) return -1;
                     const int item = args.order == nullptr ? at : index_below(__ldg(args.order + at), args.n_items);
@@ -481,65 +335,40 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
             int n = 0, n_next = 0;
             int item = next_item(blockIdx.x, n);
             for (int it = 0; ok; ++it) {
-                span = span_next;
-                tile0 = tile0_next;
-                part = part_next;
                 const int e = it % kItemRing;
                 if (it >= kItemRing) ok = mbar_wait(smem_u32(&bar_item_empty[e]), (static_cast<uint32_t>(it / kItemRing) & 1u) ^ 1u, abort_state);
                 if (!ok) break;
-                const int* list = kDense ? nullptr : args.list + static_cast<long long>(max(item, 0)) * args.list_stride;
-                items[e] = kDense ? make_int4(item, n, tile0, part) : make_int4(item, n, item >= 0 ? __ldg(list + n - 1) : 0, 0);
-                if (kDense) spans[e] = make_int4(span.len, span.first, span.count, 0);
+                const int* list = args.list + static_cast<long long>(max(item, 0)) * args.list_stride;
+                items[e] = make_int4(item, n, item >= 0 ? __ldg(list + n - 1) : 0, 0);
                 mbar_arrive(smem_u32(&bar_item_full[e]));
                 if (item < 0) break;
                 const int bh = item / args.n_items_per_head, own0 = (item - bh * args.n_items_per_head) * kBwdBlock;
                 const int b = bh / args.H, h = bh - b * args.H;
-                auto load_tile = [&](uint32_t dst, const CUtensorMap* map, uint32_t bar, int row0, int head) {
+                auto load_tile = [&](uint32_t dst, const CUtensorMap* map, uint32_t bar, int row0) {
                     mbar_arrive_expect_tx(bar, Plan::kTile);
 #pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf) tma_load_4d(dst + hf * Plan::kHalf, map, bar, hf * 64, head, row0, b);
+                    for (int hf = 0; hf < kHalves; ++hf) tma_load_4d(dst + hf * Plan::kHalf, map, bar, hf * 64, h, row0, b);
                 };
                 const float* rows = args.rows + static_cast<long long>(bh) * args.n_q * (2 * kBwdBlock);
                 int next = -1;
-                // kDense: the streaming head and block (kDkv: of the heads that share the item's, one after the other)
-                int head = h, dense_block = 0;
-                if constexpr (kDense) {
-                    head = kDkv ? h * args.mask.group + tile0 / span.count : h / args.mask.group;
-                    dense_block = kDkv ? tile0 % span.count : tile0;
-                }
                 for (int j = 0; j < n; ++j, ++T) {
-                    int block, row0;
-                    const CUtensorMap *map1 = &tm_y1, *map2 = &tm_y2;
-                    if constexpr (kDense) {
-                        if (kDkv && dense_block == span.count) { dense_block = 0; ++head; }
-                        block = span.first + dense_block++;
-                        row0 = block * kBwdBlock;
-                        if (kDkv) rows = args.rows + (static_cast<long long>(b) * args.H * args.mask.group + head) * args.n_q * (2 * kBwdBlock);
-                        if (!kDkv && span.len < args.Lk && span.len - row0 < kBwdBlock) {
-                            map1 = &args.tail1;
-                            map2 = &args.tail2;
-                            row0 = 0;
-                        }
-                    } else {
-                        block = __ldg(list + j);
-                        row0 = block * kBwdBlock;
-                    }
+                    const int block = __ldg(list + j), row0 = block * kBwdBlock;
                     if (j == 0) {
                         if (it > 0) ok = mbar_wait(smem_u32(&bar_x1_free), (it - 1) & 1, abort_state);
                         if (!ok) break;
-                        load_tile(smem + Plan::kX, &tm_x1, smem_u32(&bar_x1_full), own0, h);
+                        load_tile(smem + Plan::kX, &tm_x1, smem_u32(&bar_x1_full), own0);
                     }
                     if (T >= kBwdY1) ok = mbar_wait(smem_u32(&bar_y1_empty[s1]), ph1 ^ 1u, abort_state);
                     if (!ok) break;
-                    load_tile(smem + Plan::kY1Off + s1 * Plan::kTile, map1, smem_u32(&bar_y1_full[s1]), row0, head);
+                    load_tile(smem + Plan::kY1Off + s1 * Plan::kTile, &tm_y1, smem_u32(&bar_y1_full[s1]), row0);
                     if (j == 0) {
                         if (it > 0) ok = mbar_wait(smem_u32(&bar_x2_free), (it - 1) & 1, abort_state);
                         if (!ok) break;
-                        load_tile(smem + Plan::kX + Plan::kTile, &tm_x2, smem_u32(&bar_x2_full), own0, h);
+                        load_tile(smem + Plan::kX + Plan::kTile, &tm_x2, smem_u32(&bar_x2_full), own0);
                     }
                     if (T >= kBwdY2) ok = mbar_wait(smem_u32(&bar_y2_empty[s2]), ph2 ^ 1u, abort_state);
                     if (!ok) break;
-                    load_tile(smem + Plan::kY2Off + s2 * Plan::kTile, map2, smem_u32(&bar_y2_full[s2]), row0, head);
+                    load_tile(smem + Plan::kY2Off + s2 * Plan::kTile, &tm_y2, smem_u32(&bar_y2_full[s2]), row0);
                     if (kDkv) {
                         // Two sets of row constants: the one of tile T - 2 is free once that tile's dS has been formed, which
                         // the release of its Q tile (after dK += dS Q) says
@@ -760,32 +589,8 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
         if (ok) read_own(cur.x);
         for (int it = 0; ok && cur.x >= 0; ++it) {
             const int n = cur.y;
-            const int last_valid = kDkv || kDense ? kBwdBlock : args.L_other - cur.z * kBwdBlock;      // kDq: keys of the last block
-            // kDense.  kDq: how many keys the row sees, from the first key of the tile on.  kDkv: the first query that sees the row's key, from the first
-            // query of the tile on, and the block of that query
-            int sees = 0, dense_block = 0, dense_count = 0;
-            if constexpr (kDense) {
-                const int4 span = *const_cast<const int4*>(&spans[it % kItemRing]);
-                const int own = (cur.x % args.n_items_per_head) * kBwdBlock + row;
-                if (kDkv) {
-                    dense_count = span.z;
-                    dense_block = cur.z % dense_count;
-                    sees = (args.mask.causal ? own - args.mask.offset : INT_MIN / 2) - (span.y + dense_block) * kBwdBlock;
-                } else {
-                    sees = (args.mask.causal ? min(span.x, own + 1 + args.mask.offset) : span.x) - cur.z * kBwdBlock;
-                }
-            }
-            // (to the next tile: the next block, or the first one of the next head)
-            auto next_tile = [&]() {
-                if constexpr (kDense) {
-                    sees -= kBwdBlock;
-                    if (kDkv && ++dense_block == dense_count) {
-                        dense_block = 0;
-                        sees += dense_count * kBwdBlock;
-                    }
-                }
-            };
-            for (int j = 0; j < n; ++j, ++T, s_buf = s_buf >= 1 ? s_buf - 1 : s_buf + 2, next_tile()) {
+            const int last_valid = kDkv ? kBwdBlock : args.L_other - cur.z * kBwdBlock;      // kDq: keys of the last block
+            for (int j = 0; j < n; ++j, ++T, s_buf = s_buf >= 1 ? s_buf - 1 : s_buf + 2) {
                 if (!kDkv && (T & 1) != group) continue;
                 const uint32_t buf_s = tmem + lane_base + kScore0 + (kDkv ? 0 : s_buf * 128);
                 const uint32_t buf_dp = tmem + lane_base + kScore0 + (kDkv ? 128 : (s_buf == 2 ? 0 : s_buf + 1) * 128);
@@ -811,10 +616,6 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
 #pragma unroll
                     for (int c0 = 0; c0 < 64; c0 += 32) {
                         exps(sv + c0, p + c0, rows_smem + (col0 + c0) * 4);
-                        if (kDense && kDkv && sees > col0 + c0) {
-#pragma unroll
-                            for (int c = 0; c < 32; ++c) if (col0 + c0 + c < sees) p[c0 + c] = 0.0f;
-                        }
                         if (kDkv) {
                             // P^T in bf16 over the S that it came from; the MMAs take it in two halves
                             uint32_t pk[16];
@@ -831,10 +632,6 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
                         // keys behind the last one: their zero rows of K make any finite dS harmless, but 2^(-LSE) need not be finite
 #pragma unroll
                         for (int c = 0; c < 64; ++c) if (col0 + c >= last_valid) p[c] = 0.0f;
-                    }
-                    if (kDense && !kDkv && sees < col0 + 64) {
-#pragma unroll
-                        for (int c = 0; c < 64; ++c) if (col0 + c >= sees) p[c] = 0.0f;
                     }
                     if (half == 0) {
                         ok = mbar_wait_patient(smem_u32(&bar_dp_full[T & 1]), phase, abort_state);
@@ -872,7 +669,6 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
         bool ok = item_at(0, cur);
         for (int it = 0; ok && cur.x >= 0; ++it) {
             const int item = cur.x;
-            const int len = kDense && kDkv ? spans[it % kItemRing].x : 0;        // (keys behind it: gradients of 0, whatever their rows hold)
             const int bh = item / args.n_items_per_head, b = bh / args.H, h = bh - b * args.H;
             const int r = (item - bh * args.n_items_per_head) * kBwdBlock + row;
             const long long at = ((static_cast<long long>(b) * args.L_own + r) * args.H + h) * D;
@@ -892,20 +688,6 @@ sparse_bwd_kernel(const __grid_constant__ CUtensorMap tm_x1, const __grid_consta
                     if (lane == 0) {
                         mbar_arrive(smem_u32(&bar_acc_free));
                         mbar_arrive(smem_u32(&bar_item_empty[it % kItemRing]));
-                    }
-                }
-                if constexpr (kDense) {
-                    if (args.splits > 1) {
-                        float* out = args.part + ((static_cast<long long>(cur.w) * args.n_items + item) * kBwdBlock + row) * kCols + c0;
-#pragma unroll
-                        for (int c = 0; c < 32; c += 8)
-                            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + c), "r"(v[c]), "r"(v[c + 1]),
-                                         "r"(v[c + 2]), "r"(v[c + 3]), "r"(v[c + 4]), "r"(v[c + 5]), "r"(v[c + 6]), "r"(v[c + 7]) : "memory");
-                        continue;
-                    }
-                    if (kDkv && r >= len) {
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) v[c] = 0u;
                     }
                 }
                 const bool second = kDkv && c0 >= D;
