@@ -25,6 +25,8 @@
 
 #include <type_traits>
 
+#include "attn_jvp_kernel.cuh"
+
 namespace attn_jvp {
 
 // ---------------------------------------------------------------------------------------------
@@ -85,9 +87,12 @@ rotary_table_kernel(const __grid_constant__ RotaryTableParams p) {
 // ---------------------------------------------------------------------------------------------
 constexpr int kRotaryThreads = 256;
 enum RotaryMode : int { kRotaryFwd = 0, kRotaryJvp = 1, kRotaryBwd = 2 };
-// rows that a group of lanes has in flight, and blocks that share an SM (what the registers are budgeted for)
-__host__ __device__ constexpr int rotary_rows(int mode) { return mode == kRotaryFwd ? 4 : 2; }
-__host__ __device__ constexpr int rotary_ctas(int mode) { return mode == kRotaryBwd ? 3 : 4; }
+// Rows that a group of lanes works on at a time, blocks that share an SM (what the registers are budgeted for), and whether the next rows are loaded beside these.
+// 40 + 40 heads of 32760 tokens: forward 230 us with four rows, 221 with two and the next two ahead; tangents 471 us with two rows at four blocks, 422 with four
+// at two, 480 with two and two ahead; gradients 398, 348, 361.
+__host__ __device__ constexpr int rotary_rows(int mode) { return mode == kRotaryFwd ? 2 : 4; }
+__host__ __device__ constexpr int rotary_ctas(int mode) { return mode == kRotaryFwd ? 4 : 2; }
+__host__ __device__ constexpr bool rotary_ahead(int mode) { return mode == kRotaryFwd; }
 
 struct RotaryTensor {
     const __nv_bfloat16* x;
@@ -113,13 +118,6 @@ struct RotaryParams {
     float* part;                          // backward: [blocks][2][D], sums of dw and db; null: not wanted
 };
 
-__device__ __forceinline__ void unpack8(const uint32_t (&v)[4], float (&f)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(v[i] << 16);                  // bf16 -> fp32 is a shift
-        f[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
-    }
-}
 template <int kLanes>
 __device__ __forceinline__ float sum_lanes(float v) {
 #pragma unroll
@@ -131,18 +129,24 @@ template <int D, int MODE, bool kHalf>
 __global__ void __launch_bounds__(kRotaryThreads, rotary_ctas(MODE))
 qk_rotary_kernel(const __grid_constant__ RotaryParams p) {
     constexpr int kLanes = D / 8, kGroups = kRotaryThreads / kLanes, kRows = rotary_rows(MODE);
+    constexpr bool kAhead = rotary_ahead(MODE);
     const bool second = blockIdx.x >= p.q.blocks;
     const RotaryTensor& T = second ? p.k : p.q;
     const unsigned block = second ? blockIdx.x - p.q.blocks : blockIdx.x;
     const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
     const bool turned = lane < p.R / 8;
-    // the lane's channels: o1 .. o1 + 3 and o2 .. o2 + 3; pairs (o1 + i, o2 + i), or (2 i, 2 i + 1) of the eight
+    // The lane's channels: o1 .. o1 + 3 and o2 .. o2 + 3.  In registers the four pairs' first channels come first, then the four second ones (half: as they lie;
+    // interleaved: from words that hold a pair each), two to a 64-bit register: the packed instructions below then do the same for either layout.
     int o1 = 8 * lane, o2 = o1 + 4;
     if (kHalf && turned) {
         o1 = 4 * lane;
         o2 = p.R / 2 + 4 * lane;
     }
-    auto channel = [&](int i) { return i < 4 ? o1 + i : o2 + i - 4; };
+    auto channel = [&](int i) {                                  // of place i in registers
+        if (kHalf) return i < 4 ? o1 + i : o2 + i - 4;
+        return o1 + 2 * (i % 4) + i / 4;
+    };
+    using Row = uint64_t[4];
     auto load8 = [&](const __nv_bfloat16* at, uint32_t (&v)[4]) {
         if (kHalf) {
             const uint2 a = __ldg(reinterpret_cast<const uint2*>(at + o1)), c = __ldg(reinterpret_cast<const uint2*>(at + o2));
@@ -152,13 +156,22 @@ qk_rotary_kernel(const __grid_constant__ RotaryParams p) {
             v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
         }
     };
-    auto store8 = [&](__nv_bfloat16* at, const float (&f)[8]) {
-        uint32_t v[4];
+    auto unpack8 = [&](const uint32_t (&v)[4], Row& f) {         // (bf16 -> fp32 is a shift)
+        auto lo = [&](int i) { return __uint_as_float(v[i] << 16); };
+        auto hi = [&](int i) { return __uint_as_float(v[i] & 0xFFFF0000u); };
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-            v[i] = *reinterpret_cast<const uint32_t*>(&h);
+            if (kHalf) f[i] = pack_f32x2(lo(i), hi(i));
+            else f[i] = i < 2 ? pack_f32x2(lo(2 * i), lo(2 * i + 1)) : pack_f32x2(hi(2 * i - 4), hi(2 * i - 3));
         }
+    };
+    auto store8 = [&](__nv_bfloat16* at, const Row& f) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) unpack_f32x2(f[i], x[2 * i], x[2 * i + 1]);
+        uint32_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = kHalf ? pack_bf16(x[2 * i], x[2 * i + 1]) : pack_bf16(x[i], x[i + 4]);
         if (kHalf) {
             *reinterpret_cast<uint2*>(at + o1) = make_uint2(v[0], v[1]);
             *reinterpret_cast<uint2*>(at + o2) = make_uint2(v[2], v[3]);
@@ -166,24 +179,29 @@ qk_rotary_kernel(const __grid_constant__ RotaryParams p) {
             *reinterpret_cast<uint4*>(at + o1) = make_uint4(v[0], v[1], v[2], v[3]);
         }
     };
-    // a rotation (back = false) or its transpose of the lane's four pairs
-    auto turn = [&](float (&f)[8], const float (&cs)[8], bool back) {
+    // the four pairs rotated, with sines (forward) or their negatives (back) and the other sign in `neg`
+    auto turn = [&](Row& f, const uint64_t (&co)[2], const uint64_t (&si)[2], const uint64_t (&neg)[2]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int a = kHalf ? i : 2 * i, c = kHalf ? i + 4 : 2 * i + 1;
-            const float co = cs[2 * i], si = back ? -cs[2 * i + 1] : cs[2 * i + 1];
-            const float x = f[a], y = f[c];
-            f[a] = x * co - y * si;
-            f[c] = y * co + x * si;
+        for (int i = 0; i < 2; ++i) {
+            const uint64_t x = f[i], y = f[i + 2];
+            f[i] = fma_f32x2(y, neg[i], mul_f32x2(x, co[i]));
+            f[i + 2] = fma_f32x2(x, si[i], mul_f32x2(y, co[i]));
         }
     };
-    float w[8], bias[8];
+    auto sum2 = [](uint64_t a, uint64_t b) {
+        float x, y;
+        unpack_f32x2(add_f32x2(a, b), x, y);
+        return x + y;
+    };
+    auto twice = [](float v) { return pack_f32x2(v, v); };
+    Row w, bias;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        w[i] = T.w ? __ldg(T.w + channel(i)) : 1.0f;
-        bias[i] = (MODE != kRotaryBwd && T.b) ? __ldg(T.b + channel(i)) : 0.0f;
+    for (int i = 0; i < 4; ++i) {
+        const int c0 = channel(2 * i), c1 = channel(2 * i + 1);
+        w[i] = T.w ? pack_f32x2(__ldg(T.w + c0), __ldg(T.w + c1)) : twice(1.0f);
+        bias[i] = (MODE != kRotaryBwd && T.b) ? pack_f32x2(__ldg(T.b + c0), __ldg(T.b + c1)) : 0ull;
     }
-    float dw[8] = {}, db[8] = {};
+    Row dw = {}, db = {};
 
     const unsigned units = static_cast<unsigned>(p.tokens) * T.chunks, stride = T.blocks * kGroups;
     // The bounds of both loops are the same for the whole block (the shuffles need whole warps); what lies behind the last unit or
@@ -193,96 +211,106 @@ qk_rotary_kernel(const __grid_constant__ RotaryParams p) {
         const unsigned unit = exists ? base + group : units - 1;
         const unsigned token = unit / T.chunks, chunk = unit - token * T.chunks;
         const unsigned b = token / p.L, l = token - b * p.L;
-        float cs[8];
+        uint64_t co[2] = {twice(1.0f), twice(1.0f)}, si[2] = {0ull, 0ull}, neg[2];
         if (turned) {
             long long row = l;
             if (p.index) row = __ldg(p.index + b * p.index_batch + l);
             row = row < 0 ? 0 : row >= p.table_rows ? p.table_rows - 1 : row;          // (an index from anywhere reads inside the table)
             const float4* at = reinterpret_cast<const float4*>(p.table + (b * p.table_batch + row) * (p.R / 2) + 4 * lane);
-            const float4 c0 = __ldg(at), c1 = __ldg(at + 1);
-            cs[0] = c0.x; cs[1] = c0.y; cs[2] = c0.z; cs[3] = c0.w;
-            cs[4] = c1.x; cs[5] = c1.y; cs[6] = c1.z; cs[7] = c1.w;
-        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) cs[i] = i & 1 ? 0.0f : 1.0f;
+            for (int i = 0; i < 2; ++i) {
+                const float4 c = __ldg(at + i);
+                co[i] = pack_f32x2(c.x, c.z);
+                si[i] = MODE == kRotaryBwd ? pack_f32x2(-c.y, -c.w) : pack_f32x2(c.y, c.w);
+            }
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) neg[i] = mul_f32x2(si[i], twice(-1.0f));
         const __nv_bfloat16* x = T.x + b * T.x_b + l * T.x_l;
         const __nv_bfloat16* t = MODE == kRotaryFwd ? nullptr : T.t + b * T.t_b + l * T.t_l;
         const long long out = static_cast<long long>(token) * T.H * D;
-        for (int h0 = 0; h0 < T.heads; h0 += kRows) {
-            const int first = static_cast<int>(chunk) * T.heads + h0;
-            uint32_t xr[kRows][4], tr[kRows][4];
+        uint32_t xr[kRows][4], tr[kRows][4], x_next[kRows][4], t_next[kRows][4];
+        auto load_rows = [&](int first, uint32_t (&xs)[kRows][4], uint32_t (&ts)[kRows][4]) {
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
                 const int h = min(first + r, T.H - 1);
-                load8(x + h * T.x_h, xr[r]);
-                if (MODE != kRotaryFwd) load8(t + h * T.t_h, tr[r]);
+                load8(x + h * T.x_h, xs[r]);
+                if (MODE != kRotaryFwd) load8(t + h * T.t_h, ts[r]);
+            }
+        };
+        if (kAhead) load_rows(static_cast<int>(chunk) * T.heads, x_next, t_next);
+        for (int h0 = 0; h0 < T.heads; h0 += kRows) {
+            const int first = static_cast<int>(chunk) * T.heads + h0;
+            if (kAhead) {
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        xr[r][i] = x_next[r][i];
+                        if (MODE != kRotaryFwd) tr[r][i] = t_next[r][i];
+                    }
+                }
+                if (h0 + kRows < T.heads) load_rows(first + kRows, x_next, t_next);
+            } else {
+                load_rows(first, xr, tr);
             }
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
                 const int h = first + r;
                 const bool real = exists && h0 + r < T.heads && h < T.H;
-                float v[8], g[8];
+                Row v, g, du;
                 unpack8(xr[r], v);
                 if (MODE != kRotaryFwd) unpack8(tr[r], g);
-                float du[8];
                 if (MODE == kRotaryBwd) {
-                    turn(g, cs, true);
+                    turn(g, co, si, neg);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                    for (int i = 0; i < 4; ++i) {
                         du[i] = g[i];
-                        g[i] *= w[i];
+                        g[i] = mul_f32x2(g[i], w[i]);
                     }
                 }
                 if (p.norm != 0) {
                     constexpr float kInv = 1.0f / D;
-                    float mean = 0.0f, gmean = 0.0f;
                     if (p.norm == 1) {                           // layer: centred first
-                        float s = 0.0f, sg = 0.0f;
+                        const uint64_t mean = twice(sum_lanes<kLanes>(sum2(add_f32x2(v[0], v[1]), add_f32x2(v[2], v[3]))) * -kInv);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            s += v[i];
-                            if (MODE != kRotaryFwd) sg += g[i];
-                        }
-                        mean = sum_lanes<kLanes>(s) * kInv;
-                        if (MODE != kRotaryFwd) gmean = sum_lanes<kLanes>(sg) * kInv;
-                    }
-                    float ss = 0.0f, sg = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        v[i] -= mean;
-                        ss = fmaf(v[i], v[i], ss);
+                        for (int i = 0; i < 4; ++i) v[i] = add_f32x2(v[i], mean);
                         if (MODE != kRotaryFwd) {
-                            g[i] -= gmean;
-                            sg = fmaf(v[i], g[i], sg);
+                            const uint64_t gmean = twice(sum_lanes<kLanes>(sum2(add_f32x2(g[0], g[1]), add_f32x2(g[2], g[3]))) * -kInv);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) g[i] = add_f32x2(g[i], gmean);
                         }
                     }
+                    const float ss = sum2(fma_f32x2(v[1], v[1], mul_f32x2(v[0], v[0])), fma_f32x2(v[3], v[3], mul_f32x2(v[2], v[2])));
                     const float rn = rsqrtf(fmaf(sum_lanes<kLanes>(ss), kInv, p.eps));
-                    const float m = MODE == kRotaryFwd ? 0.0f : sum_lanes<kLanes>(sg) * kInv * rn;       // mean(n . g)
+                    const uint64_t rn2 = twice(rn);
+                    if (MODE != kRotaryFwd) {
+                        const float sg = sum2(fma_f32x2(v[1], g[1], mul_f32x2(v[0], g[0])), fma_f32x2(v[3], g[3], mul_f32x2(v[2], g[2])));
+                        const uint64_t m = twice(sum_lanes<kLanes>(sg) * -kInv * rn * rn);       // -mean(n . g) in units of v
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        v[i] *= rn;
-                        if (MODE != kRotaryFwd) g[i] = rn * fmaf(-v[i], m, g[i]);
+                        for (int i = 0; i < 4; ++i) g[i] = mul_f32x2(fma_f32x2(v[i], m, g[i]), rn2);
                     }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = mul_f32x2(v[i], rn2);
                 }
                 const long long at = out + static_cast<long long>(h) * D;
                 if (MODE == kRotaryBwd) {
                     if (real) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            dw[i] = fmaf(du[i], v[i], dw[i]);
-                            db[i] += du[i];
+                        for (int i = 0; i < 4; ++i) {
+                            dw[i] = fma_f32x2(du[i], v[i], dw[i]);
+                            db[i] = add_f32x2(db[i], du[i]);
                         }
                         store8(T.y + at, g);
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        v[i] = fmaf(w[i], v[i], bias[i]);
-                        if (MODE == kRotaryJvp) g[i] *= w[i];
+                    for (int i = 0; i < 4; ++i) {
+                        v[i] = fma_f32x2(w[i], v[i], bias[i]);
+                        if (MODE == kRotaryJvp) g[i] = mul_f32x2(g[i], w[i]);
                     }
-                    turn(v, cs, false);
-                    if (MODE == kRotaryJvp) turn(g, cs, false);
+                    turn(v, co, si, neg);
+                    if (MODE == kRotaryJvp) turn(g, co, si, neg);
                     if (real) {
                         store8(T.y + at, v);
                         if (MODE == kRotaryJvp) store8(T.ty + at, g);
@@ -295,9 +323,9 @@ qk_rotary_kernel(const __grid_constant__ RotaryParams p) {
         // the block's groups in a fixed order
         __shared__ float sums[kGroups][2][D];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            sums[group][0][channel(i)] = dw[i];
-            sums[group][1][channel(i)] = db[i];
+        for (int i = 0; i < 4; ++i) {
+            unpack_f32x2(dw[i], sums[group][0][channel(2 * i)], sums[group][0][channel(2 * i + 1)]);
+            unpack_f32x2(db[i], sums[group][1][channel(2 * i)], sums[group][1][channel(2 * i + 1)]);
         }
         __syncthreads();
         for (int c = threadIdx.x; c < 2 * D; c += kRotaryThreads) {
