@@ -1326,7 +1326,7 @@ int launch_dense_bwd(const attn_jvp::DenseBwdArgs& a, cudaStream_t stream, Devic
 template <int D>
 int dense_bwd_run(attn_jvp::DenseBwdPrep& prep, cudaStream_t stream, DeviceState& st) {
     const attn_jvp::DenseBwdArgs &dkv = prep.dkv, &dq = prep.dq;
-    prep.row_blocks = prep.B * prep.n_q * (kSelBlock / 8) * ((prep.H + attn_jvp::kPrepHeads<D> - 1) / attn_jvp::kPrepHeads<D>);
+    prep.row_blocks = prep.B * prep.n_q * (kSelBlock / 8 / attn_jvp::kPrepTurns) * ((prep.H + attn_jvp::kPrepHeads<D> - 1) / attn_jvp::kPrepHeads<D>);
     prep.zero_blocks = dkv.mask.lengths || dkv.mask.causal ? (dkv.n_items + dq.n_items + 7) / 8 : 0;       // (without a mask every item has tiles)
     const int tails = dkv.mask.lengths ? prep.B * dkv.H : 0;
     attn_jvp::dense_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + prep.zero_blocks + tails), 256, 0, stream>>>(prep);

@@ -699,21 +699,37 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         return k;
     };
     const Walk walk_stride = walk_init(item_stride);
+    // kMasked: a batch without keys has no items (at most 32 batches; of more, an item that sees nothing still runs through one tile of zeros).  The
+    // two warps that have no role write its outputs.
+    uint32_t with_keys = 0u;
+    int batches = args.B;
+    const bool skips = kMasked && mask.lengths != nullptr && args.B <= 32;
+    if (skips) {
+        with_keys = __ballot_sync(0xffffffffu, lane < args.B && __ldg(mask.lengths + min(lane, args.B - 1)) > 0);
+        batches = __popc(with_keys);
+    }
+    const int n_items = skips ? args.n_q_tiles * args.H * batches : args.n_items;
+    auto batch_at = [&](int place) -> int {
+        if (!skips) return place;
+        uint32_t m = with_keys;
+        for (; place > 0; --place) m &= m - 1u;
+        return max(__ffs(m) - 1, 0);
+    };
     // kMasked: the item of this CTA in a round; under a causal mask every other full round runs backwards through the order, so that each
     // CTA gets its share of long and short items
     auto masked_walk = [&](int round) -> Walk {
-        const int item = min(first_item + round * item_stride, args.n_items - 1);
-        if (!mask.causal) {
-            Walk k = walk_init(item);
-            k.round = round;
-            return k;
-        }
-        const bool back = (round & 1) != 0 && (round + 1) * item_stride <= args.n_items;
-        const CausalItem c = causal_item(back ? round * item_stride + item_stride - 1 - first_item : item, args.n_q_tiles, args.H * args.B, mask.window);
+        const int item = max(min(first_item + round * item_stride, n_items - 1), 0);
         Walk k{};
-        k.qt = args.n_q_tiles - 1 - c.rank;
-        k.z = c.bh / args.H;
-        k.h = c.bh - k.z * args.H;
+        if (mask.causal) {
+            const bool back = (round & 1) != 0 && (round + 1) * item_stride <= n_items;
+            const CausalItem c = causal_item(back ? round * item_stride + item_stride - 1 - first_item : item, args.n_q_tiles, args.H * max(batches, 1), mask.window);
+            k.qt = args.n_q_tiles - 1 - c.rank;
+            k.z = c.bh / args.H;
+            k.h = c.bh - k.z * args.H;
+        } else {
+            k = walk_init(item);
+        }
+        k.z = batch_at(k.z);
         k.round = round;
         return k;
     };
@@ -789,7 +805,6 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const int block = e == 0 ? w.first : __ldg(w.list + e);
         return block * kBlockM + (kBN == kBlockN ? (j & 1) * kBlockN : 0);
     };
-    const int n_items = args.n_items;
     // Two Q/tQ buffers, no key chunks (every item then has the same number of key tiles): the key tiles of all of a
     // CTA's items form one stream.  The score MMAs of an item's leading tiles are issued in the last bursts of the
     // item before (its Q, tQ are resident by then), and the ring carries their K tiles in that order, so that an
@@ -923,6 +938,22 @@ attn_jvp_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     constexpr bool kMoveRegs = kHasTQ || kBN > kBlockN;
     if (warp < kFirstSoftmaxWarp) {
     if (kMoveRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsLightWarps));
+    if (kMasked && skips && (warp == 2 || warp == 3)) {
+        // batches without keys: O = tO = 0, LSE = -inf, mu = 0
+        const int at = static_cast<int>(blockIdx.x) * 64 + static_cast<int>(threadIdx.x) - 64, step = static_cast<int>(gridDim.x) * 64;
+        const long long cells = static_cast<long long>(args.Lq) * args.H * (D / 8), rows = static_cast<long long>(args.Lq) * args.H;
+        for (int b = 0; b < args.B; ++b) {
+            if ((with_keys >> b) & 1u) continue;
+            for (long long i = at; i < cells; i += step) {
+                reinterpret_cast<uint4*>(args.o)[b * cells + i] = make_uint4(0u, 0u, 0u, 0u);
+                if (kHasTQ) reinterpret_cast<uint4*>(args.to)[b * cells + i] = make_uint4(0u, 0u, 0u, 0u);
+            }
+            for (long long i = at; i < rows; i += step) {
+                args.lse[b * rows + i] = -INFINITY;
+                if (args.mu != nullptr) args.mu[b * rows + i] = 0.0f;
+            }
+        }
+    }
     if (warp == kProducerWarp) {
         // =====================================================================================
         // TMA producer.  Per item: Q, tQ (once the previous item's score MMAs are done), then the ring in

@@ -83,6 +83,14 @@ def test_lengths(aj, D, lengths):
         run_all(aj, inputs(3, 2, 1, 300, 300, D), causal, lengths)
 
 
+@pytest.mark.parametrize("B", [31, 32, 33, 40])
+@pytest.mark.parametrize("causal", [False, True])
+def test_many_batches_some_without_keys(aj, B, causal):
+    lengths = [0 if b % 3 == 1 else 1 + (37 * b) % 200 for b in range(B)]
+    run_all(aj, inputs(B, 2, 1, 150, 200, 64), causal, lengths)
+    run_all(aj, inputs(B, 1, 1, 150, 200, 128), causal, [0] * (B - 1) + [130], tangents=False)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_more_items_than_multiprocessors(aj, D):
     for causal in (False, True):
