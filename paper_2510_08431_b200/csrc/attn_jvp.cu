@@ -1311,7 +1311,7 @@ int launch_dense_bwd(const attn_jvp::DenseBwdArgs& a, cudaStream_t stream, Devic
     const int places = a.n_items * a.splits;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(places < st.sm_count ? places : st.sm_count), 1, 1);
-    cfg.blockDim = dim3(attn_jvp::kDenseThreads, 1, 1);
+    cfg.blockDim = dim3(attn_jvp::DenseRoles<D>::kThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];

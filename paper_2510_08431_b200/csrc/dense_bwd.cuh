@@ -24,16 +24,19 @@
 namespace attn_jvp {
 
 constexpr int kDenseBlock = 128;
-// Warps 0..3: MMA issue, loads; then the score warps, four to a scheduler, and the epilogue warps.  The block is launched with 80 registers a thread, 61440 in all.
-constexpr int kDenseScoreWarps = 16, kDenseEpilogueWarps = 4;
-constexpr int kDenseThreads = 32 * (4 + kDenseScoreWarps + kDenseEpilogueWarps);
-#ifndef RL
-#define RL 64
-#define RS 88
-#define RE 64
-#endif
-constexpr int kDenseRegsLight = RL, kDenseRegsScore = RS, kDenseRegsEpilogue = RE;
-static_assert(128 * kDenseRegsLight + 32 * kDenseScoreWarps * kDenseRegsScore + 32 * kDenseEpilogueWarps * kDenseRegsEpilogue <= kDenseThreads * 80, "registers");
+// Warps 0..3: MMA issue and loads; then the score warps, and four epilogue warps.  At D = 64, where the scores set the pace, four score warps to a scheduler, 32 columns
+// of a tile each; at D = 128, where they take issue slots from the warp that feeds the tensor pipe, two, 64 columns each (24 / 6 causal heads of 4001 tokens at
+// D = 64: 413 us against 453; 12 heads of 32760 at D = 128: 18.3 ms with two, 19.1 with four, though four are 4 % faster on items of four tiles).
+// Registers per thread: those of the launch, which setmaxnreg shares out anew.
+template <int D>
+struct DenseRoles {
+    static constexpr int kScoreWarps = D == 64 ? 16 : 8, kEpilogueWarps = 4;
+    static constexpr int kThreads = 32 * (4 + kScoreWarps + kEpilogueWarps);
+    static constexpr int kCols = 512 / kScoreWarps;              // of a tile, per score warp
+    static constexpr int kRegsLaunch = D == 64 ? 80 : 128;
+    static constexpr int kRegsLight = 64, kRegsScore = D == 64 ? 88 : 200, kRegsEpilogue = D == 64 ? 64 : 48;
+    static_assert(128 * kRegsLight + 32 * kScoreWarps * kRegsScore + 32 * kEpilogueWarps * kRegsEpilogue <= kThreads * kRegsLaunch, "registers");
+};
 struct DenseBwdArgs {
     // kDkv: X1, X2 = K, V of the block, Y1, Y2 = Q, dO.  kDq: X1, X2 = Q, dO; Y1, Y2 = K, V.  S = X1 Y1^T, dP = X2 Y2^T (rows: the stationary side); dV += P Y2,
     // dK += dS Y1, dQ += dS Y1.  tail1, tail2: kDq, K and V of the block in which a batch's keys end, [B][128][heads][D], zeros behind the end.
@@ -236,15 +239,18 @@ dense_join_kernel(const __grid_constant__ DenseBwdArgs a) {
 // loads, warps 4..11 work on the scores, warps 12..15 write finished accumulators out.
 // ---------------------------------------------------------------------------------------------
 template <int D, bool kDkv>
-__global__ void __launch_bounds__(kDenseThreads, 1)
+__global__ void __launch_bounds__(DenseRoles<D>::kThreads, 1)
 dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
     using Plan = DenseBwdPlan<D, kDkv>;
+    using Roles = DenseRoles<D>;
+    constexpr int kScoreWarps = Roles::kScoreWarps, kEpilogueWarps = Roles::kEpilogueWarps;
     constexpr bool kThree = !kDkv || D == 64;
     constexpr int kY1 = Plan::kY1, kY2 = Plan::kY2, kRowSets = Plan::kRowSets;
     constexpr int kHalf = kDenseBlock * 128;                     // 128 rows x 64 columns
     constexpr int kAcc2 = D;                                     // kDkv: first column of dK
     constexpr int kScore0 = kDkv ? 2 * D : D;                    // first column of score buffer 0
     static_assert(kScore0 + (kThree ? 3 : 2) * 128 <= kTmemCols, "tensor memory");
+    static_assert(kThree || Roles::kCols == 64, "P in two halves");
     static_assert(Plan::kDynBytes <= 227 * 1024 - 1024, "shared memory");
 
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -256,6 +262,7 @@ dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
     // them, which a single barrier's parity could not tell apart
     __shared__ __align__(8) uint64_t bar_s_full[2], bar_dp_full[2];      // S_T / dP_T complete
     __shared__ __align__(8) uint64_t bar_p_ready[2];             // kDkv: P_T is in tensor memory, all of it; kDq: S_T has been read
+    __shared__ __align__(8) uint64_t bar_p_half[2];              // kDkv, two buffers: the first 32 columns of every score warp's part of P_T are
     __shared__ __align__(8) uint64_t bar_ds_ready[2];            // dS_T is in tensor memory
     __shared__ __align__(8) uint64_t bar_done;                   // the item's accumulators are complete, phase it & 1 ...
     __shared__ __align__(8) uint64_t bar_acc_free;               // ... and have been read: the next item may overwrite them
@@ -292,15 +299,16 @@ dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&bar_s_full[i]), 1);
             mbar_init(smem_u32(&bar_dp_full[i]), 1);
-            mbar_init(smem_u32(&bar_p_ready[i]), kDenseScoreWarps);
-            mbar_init(smem_u32(&bar_ds_ready[i]), kDenseScoreWarps);
+            mbar_init(smem_u32(&bar_p_ready[i]), kScoreWarps);
+            mbar_init(smem_u32(&bar_p_half[i]), kScoreWarps);
+            mbar_init(smem_u32(&bar_ds_ready[i]), kScoreWarps);
         }
         for (int i = 0; i < kItemRing; ++i) {
             mbar_init(smem_u32(&bar_item_full[i]), 1);
-            mbar_init(smem_u32(&bar_item_empty[i]), (kDkv ? 1 : 2) + kDenseScoreWarps + kDenseEpilogueWarps);
+            mbar_init(smem_u32(&bar_item_empty[i]), (kDkv ? 1 : 2) + kScoreWarps + kEpilogueWarps);
         }
         mbar_init(smem_u32(&bar_done), 1);
-        mbar_init(smem_u32(&bar_acc_free), kDenseEpilogueWarps);
+        mbar_init(smem_u32(&bar_acc_free), kEpilogueWarps);
         mbar_init(smem_u32(&bar_drain), 1);
         mbar_init(smem_u32(&bar_drain2), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -331,7 +339,7 @@ dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
         return true;
     };
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDenseRegsLight));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Roles::kRegsLight));
         if (warp == kProducerWarp && lane == 0) {
             // ---- TMA producer and scheduler ----
             prefetch_tensormap(&args.x1);
@@ -442,12 +450,13 @@ dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
 #pragma unroll
                 for (int k = 1; k < D / 16; ++k) mma_ss_if<true, false>(pred, d, make_desc(x_lo + koff(k)), make_desc(y_lo + koff(k)), kIdescS);
             };
-            // accumulator += (bf16 rows x 128 in a score buffer) y; every 32 columns of it are at the start of the 32 fp32 columns that they come from
-            auto values = [&](uint32_t d, uint32_t a, uint32_t y, bool first) {
+            // accumulator += (bf16 rows x 128 in a score buffer) y; a score warp's columns of it are at the start of the fp32 columns that they come from
+            // (`part`: 0 = all of it, 1 / 2 = the first / second 32 columns of each 64)
+            auto values = [&](uint32_t d, uint32_t a, uint32_t y, bool first, int part) {
                 const uint32_t y_lo = make_desc_lo(y, kHalf);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    mma_ts_if<false>(pred, d, a + (k / 2) * 32 + (k % 2) * 8, make_desc(y_lo + k * (2048 >> 4)), kIdescV, (first && k == 0) ? 0u : 1u);
+                    if (part == 0 || (k % 4) / 2 == part - 1) mma_ts_if<false>(pred, d, a + k * 16 / Roles::kCols * Roles::kCols + k * 16 % Roles::kCols / 2, make_desc(y_lo + k * (2048 >> 4)), kIdescV, (first && k == 0) ? 0u : 1u);
             };
             auto wait = [&](uint64_t& bar, uint32_t parity) { return mbar_wait_warp(smem_u32(&bar), parity & 1u, abort_state); };
             auto commit = [&](uint64_t& bar) { tc_commit_if<false>(pred, smem_u32(&bar)); };
@@ -521,8 +530,18 @@ dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
                     return ok;
                 };
                 if (kDkv) {
-                    if (!values_ready(bar_p_ready[v.T & 1])) break;
-                    values(tmem, buf_s(v.T), y2_at(v.T), first);
+                    if (kThree) {
+                        if (!values_ready(bar_p_ready[v.T & 1])) break;
+                        values(tmem, buf_s(v.T), y2_at(v.T), first, 0);
+                    } else {
+                        // (what the next tile's S waits for is the second half alone)
+                        if (!values_ready(bar_p_half[v.T & 1])) break;
+                        values(tmem, buf_s(v.T), y2_at(v.T), first, 1);
+                        ok = wait(bar_p_ready[v.T & 1], v.T >> 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        values(tmem, buf_s(v.T), y2_at(v.T), false, 2);
+                    }
                     commit(bar_y2_empty[v.T % kY2]);
                     // (into the buffer that P has just been read from)
                     if (kThree) issue_dp(dp);
@@ -530,14 +549,14 @@ dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
                     if (ok) ok = wait(bar_ds_ready[v.T & 1], v.T >> 1);
                     if (!ok) break;
                     tc_fence_after();
-                    values(tmem + kAcc2, buf_dp(v.T), y1_at(v.T), first);
+                    values(tmem + kAcc2, buf_dp(v.T), y1_at(v.T), first, 0);
                     commit(bar_y1_empty[v.T % kY1]);
                     if (last) commit(bar_done);
                     if (kThree) issue_s(s);                      // (into the buffer that dS has just been read from)
                     else issue_dp(dp);
                 } else {
                     if (!values_ready(bar_ds_ready[v.T & 1])) break;
-                    values(tmem, buf_dp(v.T), y1_at(v.T), first);
+                    values(tmem, buf_dp(v.T), y1_at(v.T), first, 0);
                     commit(bar_y1_empty[v.T % kY1]);
                     if (last) commit(bar_done);
                     issue_s(s);                                  // (into the buffer that dS has just been read from)
@@ -555,10 +574,11 @@ dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
             }
             __syncwarp();
         }
-    } else if (warp < 4 + kDenseScoreWarps) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kDenseRegsScore));
-        // ---- scores.  Warp w owns rows 32 (w % 4) + lane (its lanes of tensor memory) and 32 columns of every tile. ----
-        const int quarter = warp & 3, col0 = 32 * ((warp - 4) >> 2);
+    } else if (warp < 4 + kScoreWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Roles::kRegsScore));
+        // ---- scores.  Warp w owns rows 32 (w % 4) + lane (its lanes of tensor memory) and kCols columns of every tile. ----
+        constexpr int kCols = Roles::kCols;
+        const int quarter = warp & 3, col0 = kCols * ((warp - 4) >> 2);
         const int row = quarter * 32 + lane;
         const uint32_t lane_base = static_cast<uint32_t>(quarter * 32) << 16;
         const float c1 = args.scale_log2;
@@ -632,39 +652,59 @@ dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
                 if (ok && !kDkv) ok = mbar_wait_patient(smem_u32(&bar_dp_full[T & 1]), phase, abort_state);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t sv[32], dp[32], packed[16];
-                float p[32];
-                TMEM_LD32(buf_s, sv, 0);
-                if (!kDkv) TMEM_LD32(buf_dp, dp, 0);
+                uint32_t sv[kCols], dp[kCols];
+                float p[kCols];
+#pragma unroll
+                for (int c0 = 0; c0 < kCols; c0 += 32) TMEM_LD32(buf_s + c0, sv, c0);
+                if (!kDkv) {
+                    // (all of S first: loads that go to and fro between the buffers cost kDq 15 % at D = 128)
+#pragma unroll
+                    for (int c0 = 0; c0 < kCols; c0 += 32) TMEM_LD32(buf_dp + c0, dp, c0);
+                }
                 tc_wait_ld();
                 if (!kDkv) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&bar_p_ready[T & 1]));
                 }
-                exps(sv, p, lse);
-                // what does not see each other: replaced (a product with 0 would keep an infinity or a NaN)
-                if (kDkv ? sees > col0 : sees < col0 + 32) {
+                // (P^T in bf16 over the S that it came from, dS over dP: in the first half of the warp's columns)
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) if (kDkv ? col0 + c < sees : col0 + c >= sees) p[c] = 0.0f;
+                for (int c0 = 0; c0 < kCols; c0 += 32) {
+                    uint32_t packed[16];
+                    exps(sv + c0, p + c0, lse + c0 / 4);
+                    // what does not see each other: replaced (a product with 0 would keep an infinity or a NaN)
+                    if (kDkv ? sees > col0 + c0 : sees < col0 + c0 + 32) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) if (kDkv ? col0 + c0 + c < sees : col0 + c0 + c >= sees) p[c0 + c] = 0.0f;
+                    }
+                    if (kDkv) {
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) packed[c] = pack_bf16(p[c0 + 2 * c], p[c0 + 2 * c + 1]);
+                        TMEM_ST16(buf_s + c0 / 2, packed, 0);
+                        if (kThree && c0 + 32 < kCols) continue;
+                        tc_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(c0 + 32 < kCols ? &bar_p_half[T & 1] : &bar_p_ready[T & 1]));
+                    } else {
+                        ds_of(dp + c0, p + c0, delta, packed);
+                        TMEM_ST16(buf_dp + c0 / 2, packed, 0);
+                    }
                 }
                 if (kDkv) {
-                    // P^T in bf16 over the S that it came from
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) packed[c] = pack_bf16(p[2 * c], p[2 * c + 1]);
-                    TMEM_ST16(buf_s, packed, 0);
-                    tc_wait_st();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&bar_p_ready[T & 1]));
                     ok = mbar_wait_patient(smem_u32(&bar_dp_full[T & 1]), phase, abort_state);
                     if (!ok) break;
                     tc_fence_after();
-                    TMEM_LD32(buf_dp, dp, 0);
+#pragma unroll
+                    for (int c0 = 0; c0 < kCols; c0 += 32) TMEM_LD32(buf_dp + c0, dp, c0);
                     tc_wait_ld();
+#pragma unroll
+                    for (int c0 = 0; c0 < kCols; c0 += 32) {
+                        uint32_t packed[16];
+                        ds_of(dp + c0, p + c0, delta + c0 / 4, packed);
+                        TMEM_ST16(buf_dp + c0 / 2, packed, 0);
+                    }
                 }
-                ds_of(dp, p, delta, packed);
-                TMEM_ST16(buf_dp, packed, 0);
                 tc_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -684,7 +724,7 @@ dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
             if (ok) read_own(cur.x);
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kDenseRegsEpilogue));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Roles::kRegsEpilogue));
         // ---- accumulators out: thread (warp, lane) owns row 32 (warp % 4) + lane of both ----
         const int row = (warp & 3) * 32 + lane;
         const uint32_t acc = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
