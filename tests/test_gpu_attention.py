@@ -126,6 +126,28 @@ def test_slices_of_one_projection(aj, D):
 
 
 @pytest.mark.parametrize("D", [64, 128])
+def test_heads_before_tokens_and_far_batches(aj, D):
+    """Tensors that lie as [B][H][L][D], and batches more than 2^31 elements apart."""
+    B, H, Hk, L, lengths = 2, 4, 2, 200, [200, 130]
+    x = inputs(B, H, Hk, L, L, D)
+    want = run_all(aj, x, True, lengths, tangents=False)
+    y = dict(x, **{n: x[n].transpose(1, 2).contiguous().transpose(1, 2) for n in "qkv"})
+    assert not y["q"].is_contiguous()
+    for a, b in zip(run_all(aj, y, True, lengths), want):
+        assert torch.equal(a, b)
+    far = (1 << 31) + 64
+    buffer = torch.empty(far + L * (H + 2 * Hk) * D, dtype=torch.bfloat16, device="cuda")
+    at = 0
+    for n in "qkv":
+        h = x[n].shape[2]
+        y[n] = buffer[at:].as_strided(x[n].shape, (far, h * D, D, 1))
+        y[n].copy_(x[n])
+        at += L * h * D
+    for a, b in zip(run_all(aj, y, True, lengths, tangents=False), want):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("causal", [False, True])
 def test_padding_may_hold_anything(aj, D, causal):
     """NaN and infinities behind a batch's keys reach nothing: results are those of zeros there, bit for bit."""

@@ -70,6 +70,16 @@ def test_table_shapes(aj):
             aj.rotary_table(p, 32)
 
 
+def test_table_of_no_position(aj):
+    """A position that is NaN or infinite has entries of NaN and leaves the others alone."""
+    pos = torch.arange(20, device="cuda").float()
+    clean = aj.rotary_table(pos, 16)
+    pos[3], pos[7], pos[11] = float("nan"), float("inf"), -float("inf")
+    got = aj.rotary_table(pos, 16)
+    bad = torch.tensor([3, 7, 11], device="cuda")
+    assert got[bad].isnan().all() and torch.equal(got[[i for i in range(20) if i not in (3, 7, 11)]], clean[[i for i in range(20) if i not in (3, 7, 11)]])
+
+
 # ---- heads ----
 def inputs(B, L, H, Hk, D, Rt, fused, index, batches, affine, bias, seed=0, rows=None):
     g = torch.Generator(device="cuda").manual_seed(seed + 1000 * B + L + H)
@@ -196,6 +206,20 @@ def test_rows_do_not_touch_each_other(aj):
     for a, b in zip(aj.qk_rotary_jvp(x["q"], x["k"], x["table"], index=wild, **kw)[:2],
                     aj.qk_rotary_jvp(x["q"], x["k"], x["table"], index=tame, **kw)[:2]):
         assert torch.equal(a, b)
+
+
+def test_heads_before_tokens(aj):
+    """Tensors that lie as [B][H][L][D]."""
+    x = inputs(2, 77, 5, 3, 64, 64, False, 0, False, True, False)
+    kw = dict(norm="rms", layout="half", q_weight=x["q_weight"], k_weight=x["k_weight"])
+    other = {n: x[n].transpose(1, 2).contiguous().transpose(1, 2) for n in ("q", "k", "tq", "tk")}
+    assert not other["q"].is_contiguous()
+    for a, b in zip(aj.qk_rotary_jvp(x["q"], x["k"], x["table"], **kw, tq=x["tq"], tk=x["tk"]),
+                    aj.qk_rotary_jvp(other["q"], other["k"], x["table"], **kw, tq=other["tq"], tk=other["tk"])):
+        assert torch.equal(a, b)
+    for a, b in zip(aj.qk_rotary_backward(x["dq"], x["dk"], x["q"], x["k"], x["table"], **kw),
+                    aj.qk_rotary_backward(x["dq"], x["dk"], other["q"], other["k"], x["table"], **kw)):
+        assert (a is None and b is None) or torch.equal(a, b)
 
 
 def test_far_strides(aj):
