@@ -11,11 +11,17 @@
 //     kDkv, three:  dV += P_j dO_j, dP_(j+1) = V dO_(j+1)^T   |   dK += dS_j Q_j, S_(j+2) = K Q_(j+2)^T
 //     kDkv, two:    dV += P_j dO_j, S_(j+1)                   |   dK += dS_j Q_j, dP_(j+1)
 //     kDq:          dP_(j+1) as soon as S_j has been read     |   dQ += dS_j K_j, S_(j+2)
-// All eight score warps share a tile, 64 columns each, so that what the next tile needs is handed over early and the MMAs run a tile ahead of them (two groups on alternate
-// tiles, as sparse_bwd.cuh has them in kDq: XX).  kDq takes S and dP together, kDv hands P over before it looks at dP.
+// All score warps share a tile, some columns each, so that what the next tile needs is handed over early and the MMAs run a tile ahead of them.  kDq takes S and
+// dP together, kDkv hands P over before it looks at dP.
 //
 // CTAs are persistent, one per SM, and draw their items (stationary blocks, or parts of their tiles where there are few) from a counter; tiles are
-// numbered T = 0, 1, ... over all items and run on without a break.  XX
+// numbered T = 0, 1, ... over all items and run on without a break.
+//
+// What bounds it.  Of the 14 D operations per pair of a training pass the gradients count 10 D, as five products; they take seven, since dQ runs over keys and
+// dK, dV over queries, so that both passes form S and dP, and adding dQ up by atomics would make it differ from run to run.  At D = 128 a product of a tile is 512 cycles of
+// the tensor pipe: a tile of kDkv takes 3100 to 3300 for its four, with P and dS handed over in two buffers, of kDq 2000 to 2300 for its three; in long runs the
+// power limit takes the rest: 12 heads of 32760 tokens 18.0 ms, 916 TF of what counts, 1280 with what is done twice.  At D = 64 (256 cycles a product) the scores
+// set the pace, an exponential, a difference, a product and two roundings per pair: 2350 and 1980 cycles a tile; 24 / 6 causal heads of 4001 tokens 465 us.
 #pragma once
 
 #include "attn_jvp_kernel.cuh"
@@ -100,7 +106,7 @@ __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepco
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Blocks below `row_blocks`: -LSE log2 e and -delta per query row, padded to whole blocks; rows behind the last query and rows without any key get
-// LSE = +inf, which makes their P exactly 0; a group of D / 8 threads per row reads dO and O once.  Then (lengths or a causal mask given) a warp per
+// -inf, which makes their P exactly 0; a group of D / 8 threads per row reads dO and O once.  Then (lengths or a causal mask given) a warp per
 // item whose gradient is zero because it sees nothing or nothing sees it, and (lengths given) a block per batch and key head, which
 // copies the keys and values of the block in which the batch ends with zeros behind the end: the products of kDq would otherwise take up what lies there.
 // Both passes' counters start at 0.
@@ -235,8 +241,7 @@ dense_join_kernel(const __grid_constant__ DenseBwdArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// The passes.  512 threads, roles and registers as in sparse_bwd.cuh: warp 0 (kDq: and warp 2) issues the MMAs, warp 1 the TMA
-// loads, warps 4..11 work on the scores, warps 12..15 write finished accumulators out.
+// The passes.  Warp 0 (kDq: and warp 2) issues the MMAs, warp 1 the TMA loads; the score and epilogue warps are those of DenseRoles.
 // ---------------------------------------------------------------------------------------------
 template <int D, bool kDkv>
 __global__ void __launch_bounds__(DenseRoles<D>::kThreads, 1)
