@@ -1324,12 +1324,10 @@ int launch_dense_bwd(const attn_jvp::DenseBwdArgs& a, cudaStream_t stream, Devic
 }
 
 template <int D>
-int dense_bwd_run(attn_jvp::DenseBwdPrep& prep, cudaStream_t stream, DeviceState& st) {
-    const attn_jvp::DenseBwdArgs &dkv = prep.dkv, &dq = prep.dq;
+int dense_bwd_run(attn_jvp::DenseBwdPrep& prep, const attn_jvp::DenseBwdArgs& dkv, const attn_jvp::DenseBwdArgs& dq, cudaStream_t stream, DeviceState& st) {
     prep.row_blocks = prep.B * prep.n_q * (kSelBlock / 8 / attn_jvp::kPrepTurns) * ((prep.H + attn_jvp::kPrepHeads<D> - 1) / attn_jvp::kPrepHeads<D>);
-    prep.zero_blocks = dkv.mask.lengths || dkv.mask.causal ? (dkv.n_items + dq.n_items + 7) / 8 : 0;       // (without a mask every item has tiles)
-    const int tails = dkv.mask.lengths ? prep.B * dkv.H : 0;
-    attn_jvp::dense_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + prep.zero_blocks + tails), 256, 0, stream>>>(prep);
+    const int tails = prep.lengths ? prep.B * prep.Hk : 0;
+    attn_jvp::dense_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + tails), 256, 0, stream>>>(prep);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_fail("attention backward preparation launch", e);
     if (int rc = launch_dense_bwd<D, true>(dkv, stream, st)) return rc;
@@ -1386,8 +1384,7 @@ int attention_bwd(const attn_jvp_attention_t* in, const void* d_o, const void* o
     a.scale_log2 = in->scale * 1.4426950408889634f;
     a.wide_out = (((uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv) & 31u) == 0;
     a.mask = {in->k_lengths, in->causal, Lk - Lq, H / Hk, 1};
-    p.dkv = p.dq = a;
-    attn_jvp::DenseBwdArgs &dkv = p.dkv, &dqa = p.dq;
+    attn_jvp::DenseBwdArgs dkv = a, dqa = a;
     dkv.x1 = dqa.y1 = mk;
     dkv.x2 = dqa.y2 = mv;
     dkv.y1 = dqa.x1 = mq;
@@ -1420,10 +1417,13 @@ int attention_bwd(const attn_jvp_attention_t* in, const void* d_o, const void* o
     p.k_b = x.k[0]; p.k_l = x.k[1]; p.k_h = x.k[2];
     p.v_b = x.v[0]; p.v_l = x.v[1]; p.v_h = x.v[2];
     p.B = B;
+    p.lengths = in->k_lengths;
     p.H = H;
+    p.Hk = Hk;
     p.Lq = Lq;
+    p.Lk = Lk;
     p.n_q = a.n_q;
-    return D == 128 ? dense_bwd_run<128>(p, stream, st) : dense_bwd_run<64>(p, stream, st);
+    return D == 128 ? dense_bwd_run<128>(p, dkv, dqa, stream, st) : dense_bwd_run<64>(p, dkv, dqa, stream, st);
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -80,8 +80,8 @@ __device__ __forceinline__ DenseSpan dense_span(const DenseBwdArgs& a, int item)
     }
     return s;
 }
-// the first tile of part i
-__device__ __forceinline__ int part_begin(int n, int i, int splits) { return static_cast<int>(static_cast<long long>(n) * i / splits); }
+// the first tile of part i (n at most 10^7, splits 16)
+__device__ __forceinline__ int part_begin(int n, int i, int splits) { return n * i / splits; }
 
 // Shared memory: the stationary operands, rings of the streaming ones, LSE and delta of kRowSets tiles (kDkv).
 template <int D, bool kDkv>
@@ -106,8 +106,7 @@ __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepco
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Blocks below `row_blocks`: -LSE log2 e and -delta per query row, padded to whole blocks; rows behind the last query and rows without any key get
-// -inf, which makes their P exactly 0; a group of D / 8 threads per row reads dO and O once.  Then (lengths or a causal mask given) a warp per
-// item whose gradient is zero because it sees nothing or nothing sees it, and (lengths given) a block per batch and key head, which
+// -inf, which makes their P exactly 0; a group of D / 8 threads per row reads dO and O once.  Then (lengths given) a block per batch and key head, which
 // copies the keys and values of the block in which the batch ends with zeros behind the end: the products of kDq would otherwise take up what lies there.
 // Both passes' counters start at 0.
 struct DenseBwdPrep {
@@ -118,8 +117,8 @@ struct DenseBwdPrep {
     long long k_b, k_l, k_h, v_b, v_l, v_h;      // strides
     __nv_bfloat16 *tail_k, *tail_v;
     int* counters;
-    int B, H, Lq, n_q, row_blocks, zero_blocks;
-    DenseBwdArgs dkv, dq;
+    const int* lengths;
+    int B, H, Hk, Lq, Lk, n_q, row_blocks;
 };
 // (40 heads of 32760 queries: 108 us = 6.2 TB/s; with blocks of one turn and four heads per thread 136)
 constexpr int kPrepTurns = 8;
@@ -130,10 +129,10 @@ __global__ void __launch_bounds__(256)
 dense_bwd_prep_kernel(const __grid_constant__ DenseBwdPrep p) {
     constexpr int kLanes = D / 8;
     grid_launch_dependents();
-    if (static_cast<int>(blockIdx.x) >= p.row_blocks + p.zero_blocks) {
-        const int Hk = p.dkv.H, bh = blockIdx.x - p.row_blocks - p.zero_blocks, b = bh / Hk, h = bh - b * Hk;
-        const int len = min(max(__ldg(p.dkv.mask.lengths + b), 0), p.dkv.Lk), r0 = len / kDenseBlock * kDenseBlock;
-        if (len == r0 || len == p.dkv.Lk) return;
+    if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
+        const int Hk = p.Hk, bh = blockIdx.x - p.row_blocks, b = bh / Hk, h = bh - b * Hk;
+        const int len = min(max(__ldg(p.lengths + b), 0), p.Lk), r0 = len / kDenseBlock * kDenseBlock;
+        if (len == r0 || len == p.Lk) return;
         for (int e = threadIdx.x; e < kDenseBlock * kLanes; e += 256) {
             const int r = e / kLanes, c = e % kLanes * 8;
             uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
@@ -147,29 +146,11 @@ dense_bwd_prep_kernel(const __grid_constant__ DenseBwdPrep p) {
         }
         return;
     }
-    if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
-        const int lane = threadIdx.x & 31;
-        int item = (blockIdx.x - p.row_blocks) * 8 + (threadIdx.x >> 5);
-        const bool keys = item >= p.dq.n_items;
-        if (keys) item -= p.dq.n_items;
-        const DenseBwdArgs& a = keys ? p.dkv : p.dq;
-        if (item >= a.n_items || a.splits > 1) return;           // (split items: dense_join_kernel writes all of them)
-        if ((keys ? dense_span<true>(a, item) : dense_span<false>(a, item)).n > 0) return;
-        const int bh = item / a.n_items_per_head, blk = item - bh * a.n_items_per_head, b = bh / a.H, h = bh - b * a.H;
-        for (int e = lane; e < kDenseBlock * kLanes; e += 32) {
-            const int r = blk * kDenseBlock + e / kLanes;
-            if (r >= a.L_own) break;
-            const long long at = ((static_cast<long long>(b) * a.L_own + r) * a.H + h) * D + (e % kLanes) * 8;
-            *reinterpret_cast<uint4*>(a.out1 + at) = make_uint4(0u, 0u, 0u, 0u);
-            if (keys) *reinterpret_cast<uint4*>(a.out2 + at) = make_uint4(0u, 0u, 0u, 0u);
-        }
-        return;
-    }
     if (blockIdx.x == 0 && threadIdx.x < 2) p.counters[threadIdx.x] = 0;
     // A CTA takes kPrepTurns times eight queries of kPrepHeads heads (what eight queries write fills sectors of `rows`), each turn's loads beside the sums of the one before.
     const unsigned head_groups = (p.H + kPrepHeads<D> - 1) / kPrepHeads<D>, groups = p.n_q * (kDenseBlock / 8 / kPrepTurns);
     const unsigned bl = blockIdx.x / head_groups, b = bl / groups;
-    if (p.dq.mask.lengths != nullptr && __ldg(p.dq.mask.lengths + b) <= 0) return;        // (no pass looks at a batch without keys)
+    if (p.lengths != nullptr && __ldg(p.lengths + b) <= 0) return;        // (no pass looks at a batch without keys)
     const unsigned group = threadIdx.x / kLanes, sub = threadIdx.x % kLanes;
     const unsigned l0 = (bl - b * groups) * (8 * kPrepTurns) + group % 8, h = (blockIdx.x - bl * head_groups) * kPrepHeads<D> + group / 8;
     const bool mine = h < static_cast<unsigned>(p.H);
@@ -222,11 +203,12 @@ dense_join_kernel(const __grid_constant__ DenseBwdArgs a) {
     const int bh = item / a.n_items_per_head, b = bh / a.H, h = bh - b * a.H, r = (item - bh * a.n_items_per_head) * kRows + row;
     if (r >= a.L_own) return;
     float sum[8] = {};
-    if (!kDkv || r < span.len) {
+    if (span.n > 0 && (!kDkv || r < span.len)) {
+#pragma unroll 4
         for (int i = 0; i < a.splits; ++i) {
-            if (part_begin(span.n, i, a.splits) == part_begin(span.n, i + 1, a.splits)) continue;      // (a part without tiles was never written)
+            const bool there = part_begin(span.n, i, a.splits) < part_begin(span.n, i + 1, a.splits);      // (a part without tiles was never written)
             const float4* at = reinterpret_cast<const float4*>(a.part + ((static_cast<long long>(i) * a.n_items + item) * kRows + row) * kCols + c);
-            const float4 x = __ldg(at), y = __ldg(at + 1);
+            const float4 none = make_float4(0.0f, 0.0f, 0.0f, 0.0f), x = there ? __ldg(at) : none, y = there ? __ldg(at + 1) : none;
             sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
             sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
         }
@@ -241,7 +223,8 @@ dense_join_kernel(const __grid_constant__ DenseBwdArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------
-// The passes.  Warp 0 (kDq: and warp 2) issues the MMAs, warp 1 the TMA loads; the score and epilogue warps are those of DenseRoles.
+// The passes.  Warp 0 (kDq: and warp 2) issues the MMAs, warp 1 the TMA loads, warp 3 writes the zero gradients of items that see nothing or that nothing
+// sees (beside the MMAs: as blocks of the preparation, before them, 3 x 16 heads of 8190 queries with keys 77 / 0 / 512 235 us against 226); the score and epilogue warps are those of DenseRoles.
 // ---------------------------------------------------------------------------------------------
 template <int D, bool kDkv>
 __global__ void __launch_bounds__(DenseRoles<D>::kThreads, 1)
@@ -578,6 +561,18 @@ dense_bwd_kernel(const __grid_constant__ DenseBwdArgs args) {
                 while (!mbar_try_wait(smem_u32(&drain), 0) && globaltimer_ns() - t0 < 100000000ull) {}
             }
             __syncwarp();
+        } else if (warp == 3 && args.splits == 1 && (args.mask.lengths != nullptr || args.mask.causal)) {
+            // ---- items without tiles (split ones: dense_join_kernel writes all of them; without a mask every item has tiles) ----
+            for (int item = blockIdx.x; item < args.n_items; item += gridDim.x) {
+                if (dense_span<kDkv>(args, item).n > 0) continue;
+                const int bh = item / args.n_items_per_head, b = bh / args.H, h = bh - b * args.H, r0 = (item - bh * args.n_items_per_head) * kDenseBlock;
+                const int cells = min(kDenseBlock, args.L_own - r0) * (D / 8);
+                for (int e = lane; e < cells; e += 32) {
+                    const long long at = ((static_cast<long long>(b) * args.L_own + r0 + e / (D / 8)) * args.H + h) * D + e % (D / 8) * 8;
+                    *reinterpret_cast<uint4*>(args.out1 + at) = make_uint4(0u, 0u, 0u, 0u);
+                    if (kDkv) *reinterpret_cast<uint4*>(args.out2 + at) = make_uint4(0u, 0u, 0u, 0u);
+                }
+            }
         }
     } else if (warp < 4 + kScoreWarps) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Roles::kRegsScore));
