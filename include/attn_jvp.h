@@ -14,6 +14,9 @@
  * The paper writes S = Q K^T without a softmax scale; here the constant
  * `scale` multiplies both S and tS and is not differentiated.
  *
+ * The calls next to this one (attn_jvp_attention_*, attn_jvp_sparse_*, attn_jvp_adaln_*, attn_jvp_qk_rotary_* and so on) say at their
+ * declarations where they take more: masks, key lengths, fewer key heads, strides, other tensors.
+ *
  * Conventions common to every entry point
  *   - All tensor pointers are DEVICE pointers owned by the caller.  The
  *     library neither frees nor retains them and allocates no device memory;

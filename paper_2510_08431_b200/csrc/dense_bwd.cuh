@@ -106,7 +106,8 @@ __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepco
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Blocks below `row_blocks`: -LSE log2 e and -delta per query row, padded to whole blocks; rows behind the last query and rows without any key get
-// -inf, which makes their P exactly 0; a group of D / 8 threads per row reads dO and O once.  Then (lengths given) a block per batch and key head, which
+// -inf, which makes their P exactly 0; a group of D / 8 threads per row reads dO and O once (O as the forward
+// rounded it: delta is off by 2^-9 of dO . O in the mean, which shows where dS is a small difference; the exact sum of P dP would be two more products in a pass of its own).  Then (lengths given) a block per batch and key head, which
 // copies the keys and values of the block in which the batch ends with zeros behind the end: the products of kDq would otherwise take up what lies there.
 // Both passes' counters start at 0.
 struct DenseBwdPrep {
