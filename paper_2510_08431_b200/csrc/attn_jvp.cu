@@ -1327,8 +1327,26 @@ template <int D>
 int dense_bwd_run(attn_jvp::DenseBwdPrep& prep, const attn_jvp::DenseBwdArgs& dkv, const attn_jvp::DenseBwdArgs& dq, cudaStream_t stream, DeviceState& st) {
     prep.row_blocks = prep.B * prep.n_q * (kSelBlock / 8 / attn_jvp::kPrepTurns) * ((prep.H + attn_jvp::kPrepHeads<D> - 1) / attn_jvp::kPrepHeads<D>);
     const int tails = prep.lengths ? prep.B * prep.Hk : 0;
-    attn_jvp::dense_bwd_prep_kernel<D><<<(unsigned)(prep.row_blocks + tails), 256, 0, stream>>>(prep);
-    cudaError_t e = cudaGetLastError();
+    // queries that may see few keys: the first ones of a causal mask, all where a batch may be that short
+    const long long few = prep.lengths || prep.Lk <= attn_jvp::kExactKeys ? prep.Lq : prep.causal ? (long long)attn_jvp::kExactKeys - prep.offset : 0;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(prep.row_blocks + tails), 1, 1);
+    cfg.blockDim = dim3(256, 1, 1);
+    cfg.stream = stream;
+    cudaError_t e;
+    if (few > 0) {
+        const int blocks = n_blocks((int)(few < prep.Lq ? few : prep.Lq));
+        const int places = prep.B * prep.H * blocks;
+        attn_jvp::dense_bwd_few_kernel<D><<<(unsigned)(places < 4 * st.sm_count ? places : 4 * st.sm_count), 256, 0, stream>>>(prep, blocks);
+        e = cudaGetLastError();
+        if (e != cudaSuccess) return cuda_fail("attention backward launch for rows of few keys", e);
+        cfg.attrs = attr;                                // (the preparation runs beside it)
+        cfg.numAttrs = 1;
+    }
+    e = cudaLaunchKernelEx(&cfg, attn_jvp::dense_bwd_prep_kernel<D>, prep);
     if (e != cudaSuccess) return cuda_fail("attention backward preparation launch", e);
     if (int rc = launch_dense_bwd<D, true>(dkv, stream, st)) return rc;
     if (int rc = launch_dense_bwd<D, false>(dq, stream, st)) return rc;
@@ -1417,7 +1435,12 @@ int attention_bwd(const attn_jvp_attention_t* in, const void* d_o, const void* o
     p.k_b = x.k[0]; p.k_l = x.k[1]; p.k_h = x.k[2];
     p.v_b = x.v[0]; p.v_l = x.v[1]; p.v_h = x.v[2];
     p.B = B;
+    p.q = static_cast<const __nv_bfloat16*>(in->q);
+    p.q_b = x.q[0]; p.q_l = x.q[1]; p.q_h = x.q[2];
     p.lengths = in->k_lengths;
+    p.causal = in->causal;
+    p.offset = Lk - Lq;
+    p.scale_log2 = a.scale_log2;
     p.H = H;
     p.Hk = Hk;
     p.Lq = Lq;

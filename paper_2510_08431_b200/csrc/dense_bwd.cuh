@@ -106,10 +106,9 @@ __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepco
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // Blocks below `row_blocks`: -LSE log2 e and -delta per query row, padded to whole blocks; rows behind the last query and rows without any key get
-// -inf, which makes their P exactly 0; a group of D / 8 threads per row reads dO and O once (O as the forward
-// rounded it: delta is off by 2^-9 of dO . O in the mean, which shows where dS is a small difference; the exact sum of P dP would be two more products in a pass of its own).  Then (lengths given) a block per batch and key head, which
+// -inf, which makes their P exactly 0; a group of D / 8 threads per row reads dO and O once. Then (lengths given) a block per batch and key head, which
 // copies the keys and values of the block in which the batch ends with zeros behind the end: the products of kDq would otherwise take up what lies there.
-// Both passes' counters start at 0.
+// Both passes' counters start at 0.  (delta of rows that see few keys: below.)
 struct DenseBwdPrep {
     const uint4 *o, *d_o;
     const float* lse;
@@ -118,9 +117,81 @@ struct DenseBwdPrep {
     long long k_b, k_l, k_h, v_b, v_l, v_h;      // strides
     __nv_bfloat16 *tail_k, *tail_v;
     int* counters;
+    const __nv_bfloat16* q;
+    long long q_b, q_l, q_h;
     const int* lengths;
     int B, H, Hk, Lq, Lk, n_q, row_blocks;
+    int causal, offset;
+    float scale_log2;
 };
+// O is what the forward rounded to bf16, which leaves delta off by 2^-9 |dO| |O| / 2 or so. Over many keys |O| is small and this is lost beside the rounding of dS; for rows that
+// see at most kExactKeys it is not (of two keys dQ and dK are 0.0036 off in the 2-norm, of 12 0.0025, of many 0.0024, with the exact delta 0.0024 throughout): there
+// delta = sum_j P_j (dO . v_j) is formed anew, from scores in fp32.  Blocks walk over the query blocks that can have such rows (a causal mask: the first of a head; lengths: any), in a kernel of its
+// own beside the preparation, whose registers it would double.  Costs 1 % where a mask leaves few such rows or none (gradients of 24 / 6 causal heads of 4001 tokens
+// 407 -> 410 us; 3 x 16 heads of 8190 queries, keys 77 / 0 / 512, 218 -> 221), more than the rest where all rows are (2 x 16 heads of 8190 queries and 12 keys: 138 -> 340).
+constexpr int kExactKeys = 12;
+// the keys that query l sees of a batch's `len` where they are few, else 0
+__device__ __forceinline__ int few_keys(const DenseBwdPrep& p, int len, int l) {
+    const int seen = p.causal ? min(len, l + 1 + p.offset) : len;
+    return seen > 0 && seen <= kExactKeys ? seen : 0;
+}
+template <int D>
+__global__ void __launch_bounds__(256)
+dense_bwd_few_kernel(const __grid_constant__ DenseBwdPrep p, int blocks) {
+    constexpr int kLanes = D / 8;
+    grid_launch_dependents();
+    const int sub = threadIdx.x % kLanes;
+    for (int i = blockIdx.x; i < p.B * p.H * blocks; i += gridDim.x) {
+        const int bh = i / blocks, b = bh / p.H, h = bh - b * p.H, hk = h / (p.H / p.Hk);
+        const int len = p.lengths == nullptr ? p.Lk : min(__ldg(p.lengths + b), p.Lk);
+        if (len <= 0 || (!p.causal && len > kExactKeys)) continue;
+        const int l0 = (i - bh * blocks) * kDenseBlock + threadIdx.x / kLanes;
+#pragma unroll 1
+        for (int l = l0; l < l0 + kDenseBlock; l += 256 / kLanes) {
+            const int seen = l < p.Lq ? few_keys(p, len, l) : 0;
+            const int most = __reduce_max_sync(0xffffffffu, seen);   // (the shuffles need whole warps)
+            if (most <= 0) continue;
+            uint4 qv = make_uint4(0u, 0u, 0u, 0u), gv = qv;
+            float ls = -INFINITY;
+            if (seen > 0) {
+                qv = __ldg(reinterpret_cast<const uint4*>(p.q + b * p.q_b + l * p.q_l + h * p.q_h + sub * 8));
+                gv = __ldg(p.d_o + ((static_cast<long long>(b) * p.Lq + l) * p.H + h) * kLanes + sub);
+                ls = __ldg(p.lse + static_cast<long long>(bh) * p.Lq + l) * -1.4426950408889634f;
+                if (ls == INFINITY) ls = -INFINITY;
+            }
+            auto dot = [](const uint4& x, const uint4& y) {
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+                float v = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v = fmaf(__uint_as_float(xs[i] << 16), __uint_as_float(ys[i] << 16), v);
+                    v = fmaf(__uint_as_float(xs[i] & 0xFFFF0000u), __uint_as_float(ys[i] & 0xFFFF0000u), v);
+                }
+#pragma unroll
+                for (int m = kLanes / 2; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+                return v;
+            };
+            float delta = 0.0f;
+            for (int j0 = 0; j0 < most; j0 += 4) {                   // (loads of four keys in flight)
+                uint4 k[4], v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    k[i] = v[i] = make_uint4(0u, 0u, 0u, 0u);
+                    if (j0 + i < seen) {
+                        k[i] = __ldg(reinterpret_cast<const uint4*>(p.k + b * p.k_b + (j0 + i) * p.k_l + hk * p.k_h + sub * 8));
+                        v[i] = __ldg(reinterpret_cast<const uint4*>(p.v + b * p.v_b + (j0 + i) * p.v_l + hk * p.v_h + sub * 8));
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float score = dot(qv, k[i]), dp = dot(gv, v[i]);
+                    if (j0 + i < seen) delta = fmaf(ex2f(fmaf(score, p.scale_log2, ls)), dp, delta);
+                }
+            }
+            if (sub == 0 && seen > 0) p.rows[(static_cast<long long>(bh) * p.n_q + l / kDenseBlock) * (2 * kDenseBlock) + kDenseBlock + l % kDenseBlock] = -delta;
+        }
+    }
+}
 // (40 heads of 32760 queries: 108 us = 6.2 TB/s; with blocks of one turn and four heads per thread 136)
 constexpr int kPrepTurns = 8;
 template <int D>
@@ -133,8 +204,7 @@ dense_bwd_prep_kernel(const __grid_constant__ DenseBwdPrep p) {
     if (static_cast<int>(blockIdx.x) >= p.row_blocks) {
         const int Hk = p.Hk, bh = blockIdx.x - p.row_blocks, b = bh / Hk, h = bh - b * Hk;
         const int len = min(max(__ldg(p.lengths + b), 0), p.Lk), r0 = len / kDenseBlock * kDenseBlock;
-        if (len == r0 || len == p.Lk) return;
-        for (int e = threadIdx.x; e < kDenseBlock * kLanes; e += 256) {
+        for (int e = threadIdx.x; len != r0 && len != p.Lk && e < kDenseBlock * kLanes; e += 256) {
             const int r = e / kLanes, c = e % kLanes * 8;
             uint4 k = make_uint4(0u, 0u, 0u, 0u), v = k;
             if (r0 + r < len) {
@@ -145,13 +215,18 @@ dense_bwd_prep_kernel(const __grid_constant__ DenseBwdPrep p) {
             *reinterpret_cast<uint4*>(p.tail_k + at) = k;
             *reinterpret_cast<uint4*>(p.tail_v + at) = v;
         }
+        grid_dependency_wait();
         return;
     }
     if (blockIdx.x == 0 && threadIdx.x < 2) p.counters[threadIdx.x] = 0;
     // A CTA takes kPrepTurns times eight queries of kPrepHeads heads (what eight queries write fills sectors of `rows`), each turn's loads beside the sums of the one before.
     const unsigned head_groups = (p.H + kPrepHeads<D> - 1) / kPrepHeads<D>, groups = p.n_q * (kDenseBlock / 8 / kPrepTurns);
     const unsigned bl = blockIdx.x / head_groups, b = bl / groups;
-    if (p.lengths != nullptr && __ldg(p.lengths + b) <= 0) return;        // (no pass looks at a batch without keys)
+    const int len = p.lengths == nullptr ? p.Lk : min(__ldg(p.lengths + b), p.Lk);
+    if (len <= 0) {                                              // (no pass looks at a batch without keys)
+        grid_dependency_wait();
+        return;
+    }
     const unsigned group = threadIdx.x / kLanes, sub = threadIdx.x % kLanes;
     const unsigned l0 = (bl - b * groups) * (8 * kPrepTurns) + group % 8, h = (blockIdx.x - bl * head_groups) * kPrepHeads<D> + group / 8;
     const bool mine = h < static_cast<unsigned>(p.H);
@@ -188,9 +263,10 @@ dense_bwd_prep_kernel(const __grid_constant__ DenseBwdPrep p) {
             }
             float* out = p.rows + (bh * p.n_q + l / kDenseBlock) * (2 * kDenseBlock) + l % kDenseBlock;
             out[0] = ls;
-            out[kDenseBlock] = -sum;
+            if (few_keys(p, len, l) == 0 || l >= static_cast<unsigned>(p.Lq)) out[kDenseBlock] = -sum;
         }
     }
+    grid_dependency_wait();                                      // (for dense_bwd_few_kernel, if it was launched: the end of this grid is then the end of both)
 }
 
 // Adds the parts of split items in a fixed order: eight columns per thread.

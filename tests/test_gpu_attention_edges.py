@@ -89,3 +89,22 @@ def test_peaked_rows(aj, D):
     for got, want in ((o, x["v"]), (dv, x["d_o"])):
         assert ((got.double() - want.double()).abs() <= off * want.double().abs() + 1e-6).all()
     assert torch.isfinite(dq).all() and torch.isfinite(dk).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Lq,Lk,causal,lengths", [(600, 2, False, None), (600, 5, False, None), (600, 12, False, None), (600, 300, False, [3, 12]), (64, 64, True, None), (16, 16, True, None),
+                                                  (700, 20, True, None), (40, 60, True, [60, 30])])
+def test_rows_that_see_few_keys(aj, D, Lq, Lk, causal, lengths):
+    """dS and the results are rounded to bf16 once each: relative roundings of 2^-9 / sqrt 3 = 0.0011 times the spread of a mantissa (1 to 2: the steps are 2^-8 of its lower end), 0.0017
+    in the 2-norm, so 0.0024 for both and 0.0029 with a fifth of room; an o that was rounded before it went into delta would add up to 0.0027 in quadrature, 0.0036."""
+    x = inputs(2, 4, 2, Lq, Lk, D)
+    s = D ** -0.5
+    kw = dict(causal=causal, k_lengths=None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda"))
+    o, _, lse = aj.attention_jvp(x["q"], x["k"], x["v"], fwd_only=True, **kw)
+    ref = R.attention(x["q"], x["k"], x["v"], s, causal, lengths, d_o=x["d_o"])
+    grads = aj.attention_backward(x["d_o"], x["q"], x["k"], x["v"], o, lse, **kw)
+    no_timeout(aj)
+    for n, got in zip(("dq", "dk", "dv"), grads):
+        rel = ((got.double() - ref[n][0]).norm() / ref[n][0].norm()).item()
+        assert rel <= 0.0029, f"{n}: {rel:.2g}"
+        R.check(n, got, ref[n])
