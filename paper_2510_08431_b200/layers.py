@@ -30,6 +30,14 @@ def _pair(v):
     return v if isinstance(v, (tuple, list)) else (v, None)
 
 
+def _whole(grad):
+    """An output's gradient as the library takes it, contiguous and 16-byte aligned: autograd may hand over a slice that starts anywhere in another tensor."""
+    if grad is None:
+        return None
+    grad = grad.contiguous()
+    return grad if grad.data_ptr() % 16 == 0 else grad.clone()
+
+
 class _FirstOrder(torch.autograd.Function):
     """A gradient as a function of what it was computed from, whose own gradient does not exist."""
 
@@ -61,7 +69,7 @@ class _Attention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, d_o, _):
         q, k, v, o, lse, k_lengths = ctx.saved_tensors
-        grads = _dense.attention_backward(d_o.contiguous(), q, k, v, o, lse, scale=ctx.scale, causal=ctx.causal, k_lengths=k_lengths)
+        grads = _dense.attention_backward(_whole(d_o), q, k, v, o, lse, scale=ctx.scale, causal=ctx.causal, k_lengths=k_lengths)
         return (*_first_order(grads, d_o, q, k, v), None, None, None)
 
 
@@ -127,8 +135,7 @@ class _AdaLN(torch.autograd.Function):
         x, h, gate, scale, shift, weight, post_weight = ctx.saved_tensors
         if dxn is None and dy is None:
             return (None,) * 8
-        g = _adaln.adaln_backward(None if dxn is None else dxn.contiguous(), None if dy is None else dy.contiguous(), x, h, gate,
-                                  scale, shift, weight, post_weight, **ctx.kinds)
+        g = _adaln.adaln_backward(_whole(dxn), _whole(dy), x, h, gate, scale, shift, weight, post_weight, **ctx.kinds)
         return (*_first_order(g, dxn, dy, *ctx.saved_tensors), None)
 
 
@@ -176,8 +183,8 @@ class _QKRotary(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dqn, dkn=None):
         q, k, table, index, q_weight, k_weight, q_bias, k_bias = ctx.saved_tensors
-        g = _rotary.qk_rotary_backward(dqn.contiguous(), None if k is None else dkn.contiguous(), q, k, table, index, q_weight=q_weight,
-                                       k_weight=k_weight, q_bias=q_bias, k_bias=k_bias, **ctx.kinds)
+        g = _rotary.qk_rotary_backward(_whole(dqn), None if k is None else _whole(dkn), q, k, table, index, q_weight=q_weight, k_weight=k_weight, q_bias=q_bias,
+                                       k_bias=k_bias, **ctx.kinds)
         g = _first_order(g, dqn, dkn, *ctx.saved_tensors)
         return g[0], g[1], None, None, g[2], g[3], g[4], g[5], None
 
@@ -227,7 +234,7 @@ class _SparseAttention(torch.autograd.Function):
     def backward(ctx, d_o, _):
         q, k, v, o, lse, *lists = ctx.saved_tensors
         selection = _sparse.BlockSelection(*lists, *ctx.lengths)
-        grads = _sparse.sparse_attention_backward(d_o.contiguous(), q, k, v, o, lse, selection, scale=ctx.scale)
+        grads = _sparse.sparse_attention_backward(_whole(d_o), q, k, v, o, lse, selection, scale=ctx.scale)
         return (*_first_order(grads, d_o, q, k, v), None, None)
 
 
