@@ -141,6 +141,7 @@ def _ptr(x):
 
 
 _host_module = None
+_no_host = False               # it was looked for and is not there
 
 
 def host():
@@ -149,27 +150,29 @@ def host():
     global _host_module
     if _host_module is None:
         lib = load()
-        try:
-            from . import _host
-        except ImportError as e:
-            raise RuntimeError(f"_host.so is missing or does not load ({e}): build it with `python -m paper_2510_08431_b200.build` "
-                               "(there is no fallback path)") from e
         names = ("adaln_fwd", "adaln_bwd", "adaln_bwd_workspace_bytes", "block_select", "block_select_workspace_bytes",
                  "block_lists", "sparse_fwd", "sparse_bwd", "sparse_bwd_workspace_bytes", "fwd_stream", "fwd_mu", "attention_fwd",
                  "attention_bwd", "attention_bwd_workspace_bytes", "rotary_table", "qk_rotary_fwd",
                  "qk_rotary_bwd", "qk_rotary_bwd_workspace_bytes")
-        _host.bind(*(ctypes.cast(getattr(lib, "attn_jvp_" + n), ctypes.c_void_p).value for n in names))
+        try:
+            from . import _host
+            _host.bind(*(ctypes.cast(getattr(lib, "attn_jvp_" + n), ctypes.c_void_p).value for n in names))
+        except (ImportError, TypeError) as e:                # (TypeError: built from other sources, whose functions are not these)
+            raise RuntimeError(f"_host.so is missing or does not load ({e}): build it with `python -m paper_2510_08431_b200.build` "
+                               "(there is no fallback path)") from e
         _host_module = _host
     return _host_module
 
 
 def has_host() -> bool:
-    """Whether the host binding is there: what can do without it does."""
-    try:
-        host()
-    except RuntimeError:
-        return False
-    return True
+    """Whether the host binding is there: what can do without it does.  Looked for once (an import that fails takes 40 to 60 us)."""
+    global _no_host
+    if _host_module is None and not _no_host:
+        try:
+            host()
+        except RuntimeError:
+            _no_host = True
+    return _host_module is not None
 
 
 def _raise(rc):
