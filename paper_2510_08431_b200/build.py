@@ -84,7 +84,8 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     try:
         build_host(force)
     except (RuntimeError, OSError) as e:
-        warnings.warn(f"the host binding is not built, adaln_*, block_sele*, sparse_attention_* and *rotary* will not work: {e}", RuntimeWarning)
+        warnings.warn("the host binding is not built, adaln_*, block_sele*, sparse_attention_*, *rotary*, attention_backward and attention_jvp with masks, "
+                      f"shared heads or strided inputs will not work: {e}", RuntimeWarning)
     return LIB
 
 
