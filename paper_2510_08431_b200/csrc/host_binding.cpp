@@ -379,7 +379,7 @@ void heads_of(const at::Tensor& t, const char* name, at::IntArrayRef shape, cons
         refuse("%s must be a bf16 tensor on %s of the shape that the other arguments give, with contiguous heads", name, device.str().c_str());
     for (int i = 0; i < 3; ++i) {
         stride[i] = t.stride(i);
-        if (t.size(i) > 1 && stride[i] % 8 != 0) refuse("%s: strides must be multiples of 8 elements", name);
+        if (t.size(i) > 1 && stride[i] % 8 != 0 && !t.is_contiguous()) refuse("%s: strides must be multiples of 8 elements", name);     // (else: a head dimension that the library refuses)
     }
 }
 
@@ -394,7 +394,7 @@ struct Attention {
         heads_of(q, "q", q.sizes(), dev, a.q_stride);
         heads_of(k, "k", {q.size(0), k.size(1), k.size(2), q.size(3)}, dev, a.k_stride);
         heads_of(v, "v", k.sizes(), dev, a.v_stride);
-        if (k.size(2) == 0 || q.size(2) % k.size(2) != 0) refuse("%lld query heads cannot share %lld key heads evenly", (long long)q.size(2), (long long)k.size(2));
+        if (k.size(2) == 0 ? q.size(2) != 0 : q.size(2) % k.size(2) != 0) refuse("%lld query heads cannot share %lld key heads evenly", (long long)q.size(2), (long long)k.size(2));
         if (lengths.defined()) expect(lengths, "k_lengths", at::kInt, {q.size(0)}, dev);
         a.q = ptr(q);
         a.k = ptr(k);
