@@ -422,8 +422,9 @@ int attn_jvp_attention_fwd(const attn_jvp_attention_t* in, void* o, void* to, fl
  *   dq, dk, dv outputs, bf16 contiguous, shapes of q, k, v; every element is written.
  *   workspace  device, 256-byte aligned, attn_jvp_attention_bwd_workspace_bytes(...) bytes (two words per query, the last block of every batch's
  *              keys, and partial sums where there are few blocks).  Calls that share one must be ordered on the GPU.
- * P and dS are rounded to bf16 as MMA operands, sums are fp32; rowsum(dO . O) takes O as given, but is formed anew from Q, K, V and LSE for queries that see
- * at most 12 keys, where O's rounding would show.  No atomics: results do not change from run to run.
+ * P and dS are rounded to bf16 as MMA operands, sums are fp32; rowsum(dO . O) takes O as given, which adds to the errors of dQ and dK where few keys hold a
+ * row's probability, however many it sees: relative to 64 bits 0.0024 in the 2-norm over unit-normal tensors, up to 0.006 with queries of 8 times unit size.  For
+ * queries that see at most 12 keys it is formed anew from Q, K, V and LSE (0.0024).  No atomics: results do not change from run to run.
  */
 size_t attn_jvp_attention_bwd_workspace_bytes(int B, int H, int Hk, int Lq, int Lk, int D);
 int attn_jvp_attention_bwd(const attn_jvp_attention_t* in, const void* d_o, const void* o, const float* lse, void* dq, void* dk, void* dv,

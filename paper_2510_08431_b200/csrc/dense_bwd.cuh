@@ -21,7 +21,7 @@
 // dK, dV over queries, so that both passes form S and dP, and adding dQ up by atomics would make it differ from run to run.  At D = 128 a product of a tile is 512 cycles of
 // the tensor pipe: a tile of kDkv takes 3100 to 3300 for its four, with P and dS handed over in two buffers, of kDq 2000 to 2300 for its three; in long runs the
 // power limit takes the rest: 12 heads of 32760 tokens 18.0 ms, 916 TF of what counts, 1280 with what is done twice.  At D = 64 (256 cycles a product) the scores
-// set the pace, an exponential, a difference, a product and two roundings per pair: 2350 and 1980 cycles a tile; 24 / 6 causal heads of 4001 tokens 465 us.
+// set the pace, an exponential, a difference, a product and two roundings per pair: 2350 and 1980 cycles a tile; 2 x 24 / 6 causal heads of 4001 tokens, keys 4001 and 3277: 410 us.
 #pragma once
 
 #include "attn_jvp_kernel.cuh"
@@ -31,8 +31,8 @@ namespace attn_jvp {
 
 constexpr int kDenseBlock = 128;
 // Warps 0..3: MMA issue and loads; then the score warps, and four epilogue warps.  At D = 64, where the scores set the pace, four score warps to a scheduler, 32 columns
-// of a tile each; at D = 128, where they take issue slots from the warp that feeds the tensor pipe, two, 64 columns each (24 / 6 causal heads of 4001 tokens at
-// D = 64: 413 us against 453; 12 heads of 32760 at D = 128: 18.3 ms with two, 19.1 with four, though four are 4 % faster on items of four tiles).
+// of a tile each; at D = 128, where they take issue slots from the warp that feeds the tensor pipe, two, 64 columns each (D = 64, the causal case above when this
+// was taken: 413 us with four, 453 with two; 12 heads of 32760 at D = 128: 18.3 ms with two, 19.1 with four, though four are 4 % faster on items of four tiles).
 // Registers per thread: those of the launch, which setmaxnreg shares out anew.
 template <int D>
 struct DenseRoles {
@@ -124,11 +124,21 @@ struct DenseBwdPrep {
     int causal, offset;
     float scale_log2;
 };
-// O is what the forward rounded to bf16, which leaves delta off by 2^-9 |dO| |O| / 2 or so. Over many keys |O| is small and this is lost beside the rounding of dS; for rows that
-// see at most kExactKeys it is not (of two keys dQ and dK are 0.0036 off in the 2-norm, of 12 0.0025, of many 0.0024, with the exact delta 0.0024 throughout): there
-// delta = sum_j P_j (dO . v_j) is formed anew, from scores in fp32.  Blocks walk over the query blocks that can have such rows (a causal mask: the first of a head; lengths: any), in a kernel of its
-// own beside the preparation, whose registers it would double.  Costs 1 % where a mask leaves few such rows or none (gradients of 24 / 6 causal heads of 4001 tokens
-// 407 -> 410 us; 3 x 16 heads of 8190 queries, keys 77 / 0 / 512, 218 -> 221), more than the rest where all rows are (2 x 16 heads of 8190 queries and 12 keys: 138 -> 340).
+// O comes in bf16, and its products took the exponentials in bf16: delta is off by some 2^-9 of the root of sum (dO O)^2, which moves dS = P (dP - delta) by P times that.  How much it shows hangs on
+// the size of O beside that of the values, so on how few keys hold a row's probability, not on how many it sees.  Errors of dQ in the 2-norm over unit-normal keys and
+// values (dK alike, dV 0.0024 throughout; with an exact delta 0.0024 throughout, which are the roundings of dS and of the result), D = 64:
+//     queries of      1      2      4      8    times unit size            (mean largest probability over 512 keys: 0.03, 0.14, 0.45, 0.72)
+//       13 keys    0.0026 0.0032 0.0044 0.0057
+//       64         0.0025 0.0028 0.0038 0.0050
+//      512         0.0024 0.0028 0.0037 0.0055
+//     4096         0.0024 0.0026 0.0035 0.0052
+// An exact delta for every row would take S and dP of all its keys before the passes: two more products beside the seven.  An O that is not rounded would not do: the
+// exponentials in bf16 alone leave up to 0.005 at 512 keys and 8 times unit size (modelled, with the forward's reference up to 5 below a row's maximum).
+// Rows that see at most kExactKeys keys always have a large O (of two keys 0.0036, with unit-normal queries) and are cheap to form anew, from fp32 scores:
+// delta = sum_j P_j (dO . v_j).  Blocks walk over the query blocks that can have such rows (a causal mask: the first of a head; lengths: any), in a kernel of its
+// own beside the preparation, whose registers it would double.  Costs 1 % where a mask leaves few such rows or none (gradients of the causal case
+// 407 -> 410 us; 3 x 16 heads of 8190 queries, keys 77 / 0 / 512, 218 -> 221), more than the rest where all rows are (2 x 16 heads of 8190 queries and 12 keys: 138 -> 340,
+// for errors that go from 0.0025 to 0.0024).
 constexpr int kExactKeys = 12;
 // the keys that query l sees of a batch's `len` where they are few, else 0
 __device__ __forceinline__ int few_keys(const DenseBwdPrep& p, int len, int l) {
