@@ -394,7 +394,9 @@ int attn_jvp_sparse_bwd(const void* d_o, const void* q, const void* k, const voi
  *   tq, tk, tv tangents, contiguous; read by attn_jvp_attention_fwd only, as its flags say.
  *   k_lengths  device, int32 [B]: batch b has the first min(max(k_lengths[b], 0), Lk) keys, and what lies behind them (NaN included) has no
  *              influence; or NULL: all have Lk.
- *   causal     0, or 1: query i sees the keys j <= i + Lk - Lq (the ends are aligned, whatever the lengths).
+ *   causal     0, or 1: query i sees the keys j <= i + Lk - Lq (the ends are aligned, whatever the lengths).  Inside the 128 x 128 blocks that it cuts, what it
+ *              hides counts as a product with 0: a NaN or infinity in a hidden value may reach O, tO and dQ, in a hidden key dQ, of the block's queries; one in a
+ *              query or its dO dK and dV of the block's keys.  Other blocks stay as they are.
  * A query that sees no key has O = tO = 0, LSE = -inf, mu = 0 and no gradient; so has a key that nothing sees.  Sequences and sizes as for the
  * block-sparse calls below 786432 tokens; tensors 16-byte aligned.
  *

@@ -305,8 +305,8 @@ def attention_jvp(q, k, v, tq=None, tk=None, tv=None, scale=None, fwd_only=False
     second kernel (for few queries and many keys), ``splits=0`` lets the library choose
     (``attn_jvp_suggest_splits``); ``workspace`` may supply its scratch (a CUDA uint8
     tensor of at least attn_jvp_splitkv_workspace_bytes), else it is allocated here with torch.
-    ``causal``: query i sees the keys j <= i + Lk - Lq.  ``k_lengths`` (CUDA int32 [B]): the keys of each batch, what lies behind
-    them has no influence.  k and v may have fewer heads than q, each shared by as many query heads in a row, and q, k, v may be strided (slices of a fused
+    ``causal``: query i sees the keys j <= i + Lk - Lq; what it hides must be finite (in the 128 x 128 blocks that it cuts it counts as a product
+    with 0).  ``k_lengths`` (CUDA int32 [B]): the keys of each batch, what lies behind them has no influence, NaN included.  k and v may have fewer heads than q, each shared by as many query heads in a row, and q, k, v may be strided (slices of a fused
     projection: heads contiguous, strides multiples of 8; tangents stay contiguous).  Rows that see no key: o = to = 0, lse = -inf.  None of
     these four goes with ``splits`` > 1.
     Returns (o, to, lse) or (o, to, lse, mu).
