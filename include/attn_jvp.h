@@ -441,6 +441,7 @@ int attn_jvp_attention_bwd(const attn_jvp_attention_t* in, const void* d_o, cons
  *     ATTN_JVP_ROTARY_LINEAR  theta / s                       ATTN_JVP_ROTARY_NTK  base s^(d / (d - 2)) in place of base (d = dims[a] > 2)
  *     ATTN_JVP_ROTARY_YARN    theta (1 - g) / s + theta g with g = clamp((turns - 1) / 31, 0, 1), turns = original_length theta / (2 pi):
  *                             slow pairs are stretched, fast ones kept (Peng et al. 2023); m = 0.1 log(s) + 1, s that of the first axis.
+ *                             g ramps over turns, as in the paper; code that ramps over the pair's index i between the two ends gives other angles there.
  * m = 1 but for YARN.
  *   positions  device, [n][axes] contiguous, int32, int64 or fp32 (pos_type: ATTN_JVP_INT32, _INT64, _FP32)
  *   dims, base, factor   HOST arrays of `axes` values, read before the call returns.  dims even; at most 8 axes and 128 pairs.

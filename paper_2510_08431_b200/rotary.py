@@ -72,7 +72,8 @@ def rotary_table(positions, dims, base=10000.0, scaling=None, factor=1.0, origin
     [...], of any shape.  dims: the even number of channels that each axis turns (a number: one axis); the angle of pair i of an axis is position base^(-2 i / d).
     ``base`` and ``factor`` are numbers or one per axis.  ``scaling`` stretches the axes by their factors, for sequences
     beyond those of training: "linear" (angles / factor), "ntk" (base factor^(d / (d - 2))) or "yarn" (slow pairs / factor, fast
-    ones kept, by their turns within ``original_length``; entries times 0.1 log(factor) + 1).
+    ones kept, by their turns within ``original_length``; entries times 0.1 log(factor) + 1).  Between slow and fast the share ramps over the turns, as
+    in the paper; some released models ramp over the pair's index i instead, and their tables differ there.
     """
     dims = _per_axis(dims, 1)
     if scaling not in SCALINGS:
