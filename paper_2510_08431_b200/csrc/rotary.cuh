@@ -5,9 +5,9 @@
 // host asks; an entry is (m cos, m sin).  The angle of a far position has lost its fraction in 32 bits, so it is counted in turns of which whole ones
 // drop out: a whole position times the turns per position in 2^-64 of a turn, modulo 2^64 (an integer product), a fractional position in fp64.
 // What is left goes on as 2^-32 of a turn: the nearest quarter turn picks and signs the results, the rest is at most pi / 4, where
-// sin y = y + y^3 S(y^2) and cos y = 1 - y^2 / 2 + y^4 C(y^2) with polynomials of smallest error (4e-9 of sin, 1e-10 of cos) are right to fp32 rounding.
-// Bound by the 8 bytes written per pair: 262144 positions of 64 pairs
-// (134 MB) 35 us; with the fraction in fp64 and sincospif 86.
+// sin y = y + y^3 S(y^2) and cos y = 1 - y^2 / 2 + y^4 C(y^2) with polynomials of smallest error (as stored in fp32 4.3e-9 of sin, 5e-10 of cos) are right to fp32 rounding.
+// 262144 positions of 64 pairs (134 MB) 35 us; with the fraction in fp64 and sincospif 86.  Bound by the instructions of an entry, mostly integer ones (46 per 32 entries, issue slots 69 % busy, DRAM
+// 26 %); short tables by a thread's first reads of its pair's constants, which the constant cache serves one address at a time (32760 positions of three axes 10.6 to 11.8 us).
 //
 // Heads, for a row x in R^D of one token and head, with the token's table row R (a rotation of the first R channels by pairs):
 //     n = (x - mean x) / sqrt(var x + eps)   or   x / sqrt(mean x^2 + eps)   or   x,      u = w . n + b,      y = R u
