@@ -1245,8 +1245,14 @@ int attention_fwd(const attn_jvp_attention_t* in, void* o, void* to, float* lse,
     ka.splits = 1;
     ka.n_q_tiles = n_blocks(Lq);
     ka.n_items = ka.n_q_tiles * H * B;
-    // persistent CTAs, but one per item where items are long, as in run().  Under a causal mask the hardware balances the latter by itself, head by head
-    // (16 heads of 8192 tokens at D = 128: 281 us, with several heads at a time 330).
+    // Persistent CTAs, but one per item where items are long, as in run(); under a causal mask, whose items are half as long, from half as many keys on: there the
+    // hardware balances the items by itself, head by head.  Persistent / one per item, in us, forward and full tangents (means of two runs, 1 to 10 % apart):
+    //      2048 tokens, 48 heads   D = 64:  66 /  95 and  93 / 124      D = 128:  78 / 104 and  197 /  202
+    //      4096, 32                        131 / 180 and 231 / 244               169 / 179 and  459 /  403
+    //      6000, 24                        206 / 253 and 337 / 352               239 / 256 and  676 /  613
+    //      8192, 16                        256 / 291 and 450 / 415               319 / 314 and  794 /  782
+    //     16384, 12                        670 / 781 and 1178 / 1153             779 / 807 and 2284 / 2185
+    // so that 4096 keys is a middle: the forward alone would stay persistent, tangents at D = 128 would not from 4096 on.
     const bool persistent = (Lk + attn_jvp::kBlockN - 1) / attn_jvp::kBlockN <= (in->causal ? kPersistentMaxTiles / 2 : kPersistentMaxTiles);
     const size_t key_bytes = (size_t)Lk * D * (jvp_kv ? 8 : 4) / (H / Hk) + 1;
     ka.mask = {in->k_lengths, in->causal, Lk - Lq, H / Hk, persistent ? causal_window(key_bytes, B * H) : 1};
