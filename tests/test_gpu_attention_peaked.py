@@ -9,14 +9,14 @@ from tests.test_gpu_attention import aj, inputs, no_timeout  # noqa: F401
 pytestmark = pytest.mark.gpu
 
 
-def gradients(aj, x, factor, causal=False, lengths=None):
+def gradients(aj, x, factor, causal=False, lengths=None, rounded_o=True):
     q = (x["q"].float() * factor).bfloat16()
     s = q.shape[-1] ** -0.5
     kw = dict(causal=causal, k_lengths=None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda"))
     o, _, lse = aj.attention_jvp(q, x["k"], x["v"], fwd_only=True, **kw)
     got = aj.attention_backward(x["d_o"], q, x["k"], x["v"], o, lse, **kw)
     no_timeout(aj)
-    return got, E.gradients(q, x["k"], x["v"], x["d_o"], s, causal, lengths)
+    return got, E.gradients(q, x["k"], x["v"], x["d_o"], s, causal, lengths, rounded_o)
 
 
 @pytest.mark.parametrize("D", [64, 128])
@@ -27,6 +27,14 @@ def test_queries_of_any_size(aj, D, n, factor):
     got, want = gradients(aj, inputs(2, 4, 2, 256, n, D), factor)
     rel = E.check(got, want)
     print("D", D, "keys", n, "factor", factor, {name: round(r, 5) for name, r in rel.items()})
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [2, 5, 12])
+@pytest.mark.parametrize("factor", [1, 2, 4, 8])
+def test_few_keys(aj, D, n, factor):
+    """Rows of at most 12 keys, whose delta is formed anew: the rounding of o adds nothing, whatever the size of the queries."""
+    E.check(*gradients(aj, inputs(2, 4, 2, 256, n, D), factor, rounded_o=False))
 
 
 @pytest.mark.parametrize("D", [64, 128])
